@@ -20,8 +20,6 @@ import math
 import torch
 
 own = False
-if own:
-    from paper_2409_14939_amd import binding as B
 
 DEVICE = "cuda"
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
@@ -237,6 +235,8 @@ def _plain(s):
 
 # ------------------------------------------------------------------ the framework's calls
 def _own(s):
+    from paper_2409_14939_amd import binding as B
+
     c = s["case"]
     kind = c["kind"]
     if kind == "drop":
