@@ -36,6 +36,8 @@ EXPORTS = [
     "fastgl_overlap_workspace_bytes", "fastgl_greedy_reorder",
     "fastgl_edge_workspace_bytes", "fastgl_edge_weight_grad", "fastgl_edge_softmax_fwd", "fastgl_edge_softmax_bwd",
     "fastgl_edge_softmax_long_row", "fastgl_edge_score_fwd", "fastgl_edge_score_bwd",
+    "fastgl_norm_fwd", "fastgl_norm_fwd_e4m3", "fastgl_norm_bwd", "fastgl_norm_bwd_workspace_bytes", "fastgl_dropout",
+    "fastgl_gather_rows_e4m3",
 ]
 MAX_REORDER_BATCHES = 64
 IDMAP_MODES = {"ordered": 0, "fused": 1}
@@ -113,6 +115,14 @@ def lib() -> ctypes.CDLL:
         L.fastgl_edge_softmax_long_row.restype = ctypes.c_int32
         L.fastgl_edge_score_fwd.argtypes = [p, p, i64, i64, i64, p, p, ctypes.c_float, p, p]
         L.fastgl_edge_score_bwd.argtypes = [p, p, i64, i64, i64, p, p, ctypes.c_float, p, p, p, p, p]
+        f32, f64 = ctypes.c_float, ctypes.c_double
+        L.fastgl_norm_fwd.argtypes = [i32, p, p, p, i64, i64, f32, p, f64, p, p, p, p]
+        L.fastgl_norm_fwd_e4m3.argtypes = [i32, p, p, p, i64, i64, f32, p, f64, p, p, p, p, p]
+        L.fastgl_norm_bwd_workspace_bytes.argtypes = [i64, i64]
+        L.fastgl_norm_bwd_workspace_bytes.restype = sz
+        L.fastgl_norm_bwd.argtypes = [i32, p, p, p, p, p, i64, i64, p, f64, p, p, p, p, sz, p]
+        L.fastgl_dropout.argtypes = [i32, p, p, i64, i64, p, f64, p, p]
+        L.fastgl_gather_rows_e4m3.argtypes = [p, p, i64, p, i64, i64, i32, p, p]
         L.fastgl_idmap_table_slots.argtypes = [i64]
         L.fastgl_idmap_table_slots.restype = i64
         L.fastgl_idmap_workspace_bytes.argtypes = [i64, i64]
@@ -384,3 +394,49 @@ def fastgl_edge_score_bwd(indptr, indices, el: torch.Tensor, er: torch.Tensor, s
     None).  grad_er needs a plan built with PLAN_BWD | PLAN_PERM."""
     return _native().edge_score_bwd(indptr, indices, el, er, slope, grad_score, plan, grad_el is None and "el" in want,
                                     grad_er is None and "er" in want, grad_el, grad_er)
+
+
+def fastgl_norm_fwd(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                    rng: Optional[torch.Tensor] = None, p: float = 0.0, want_sum: bool = True, want_rstd: bool = True,
+                    sum_out: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
+                    rstd: Optional[torch.Tensor] = None):
+    """(Y, h, rstd) with h = residual + drop(X), Y = h * rstd * weight.  h is None where it is X itself (neither
+    residual nor dropout).  rng: device int64 [2], seed and offset, read when the kernel runs."""
+    Y, _, h, rstd = _native().norm_fwd(False, X, weight, eps, residual, rng, p, want_sum, want_rstd, sum_out, Y, None, rstd)
+    return Y, h, rstd
+
+
+def fastgl_norm_fwd_e4m3(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                         rng: Optional[torch.Tensor] = None, p: float = 0.0, want_sum: bool = True, want_rstd: bool = True,
+                         sum_out: Optional[torch.Tensor] = None, Q: Optional[torch.Tensor] = None,
+                         scale: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None):
+    """(Q, scale, h, rstd): the rows of fastgl_norm_fwd as torch.float8_e4m3fn with one float32 scale each."""
+    return _native().norm_fwd(True, X, weight, eps, residual, rng, p, want_sum, want_rstd, sum_out, Q, scale, rstd)
+
+
+def fastgl_norm_bwd_workspace_bytes(M: int, F: int) -> int:
+    return int(lib().fastgl_norm_bwd_workspace_bytes(M, F))
+
+
+def fastgl_norm_bwd(S: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, dY: torch.Tensor,
+                    dS: Optional[torch.Tensor] = None, rng: Optional[torch.Tensor] = None, p: float = 0.0,
+                    want=("dX", "dR", "dw"), dX: Optional[torch.Tensor] = None, dR: Optional[torch.Tensor] = None,
+                    dw: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """(dX, dR, dw); parts not named in `want` (and not passed in) are None.  S: what the forward pass returned as h
+    (X where that was None); dS: the gradient that reaches h from elsewhere.  Without dropout dX and dR are the
+    same values, and one tensor unless they were passed in."""
+    return _native().norm_bwd(S, weight, rstd, dY, dS, rng, p, dX is None and "dX" in want, dR is None and "dR" in want,
+                              dw is None and "dw" in want, dX, dR, dw, workspace)
+
+
+def fastgl_dropout(X: torch.Tensor, rng: Optional[torch.Tensor], p: float, residual: Optional[torch.Tensor] = None,
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """[residual +] drop(X).  The gradient of X is the same call on the gradient, without a residual."""
+    return _native().dropout(X, rng, p, residual, out)
+
+
+def fastgl_gather_rows_e4m3(table: torch.Tensor, scale: torch.Tensor, ids: torch.Tensor, dtype: str,
+                            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """scale[ids] * table[ids] as "f32" or "bf16"; table torch.float8_e4m3fn with one float32 scale a row.  An ID
+    outside the table gives a row of NaN."""
+    return _native().gather_rows_e4m3(table, scale, ids, DTYPES[dtype], out)

@@ -1,0 +1,231 @@
+// Dropout from the counter-based generator, with an optional addition (fastgl_norm.h has the formula), and the row
+// gather of tables held in 8 bits.  Both are one pass over memory.
+#include "fastgl_norm.h"
+#include "rows_device.h"
+
+namespace fastgl {
+namespace {
+
+constexpr int kUnits = 4;           // chunks of eight columns a lane of the dropout takes
+constexpr int kWide = 2048;         // chunks a row from which a workgroup's units touch at most two rows
+
+struct DropArgs {
+    const void *X, *R;
+    void *Y;
+    int64_t M;
+    int32_t F, chunks;
+    uint32_t inv;                   // ceil(2^32 / chunks), for rows of fewer than kWide chunks
+    const int64_t *rng;
+    uint32_t threshold;
+    float scale;
+};
+
+// Unit u = (row, chunk) in row-major order; a workgroup has kBlock * kUnits consecutive ones.
+template <bool BF16, bool DROP>
+__global__ __launch_bounds__(kBlock) void k_dropout(DropArgs a)
+{
+    typedef typename Chunk<BF16>::elem T;
+    Philox gen;
+    if constexpr (DROP) gen.load(a.rng);
+    const uint64_t first = (uint64_t)blockIdx.x * (kBlock * kUnits);
+    const int64_t row0 = (int64_t)(first / (uint32_t)a.chunks);
+    const uint32_t c0 = (uint32_t)(first - (uint64_t)row0 * (uint32_t)a.chunks);
+    Chunk<BF16> x[kUnits], r[kUnits];
+    int64_t at[kUnits];
+    uint32_t rows[kUnits], cs[kUnits];
+    int left[kUnits];
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        // c0 + the unit's place: below chunks + kBlock * kUnits, so below kWide chunks the product with `inv` is exact
+        // (3072 * 2048 < 2^32) and beyond them the quotient is 0 or 1; one chunk a row divides by itself
+        const uint32_t u = c0 + (uint32_t)(i * kBlock) + threadIdx.x;
+        const uint32_t q = a.chunks == 1 ? u : a.chunks < kWide ? __umulhi(u, a.inv) : (u >= (uint32_t)a.chunks ? 1u : 0u);
+        const int64_t row = row0 + q;
+        rows[i] = (uint32_t)row;
+        cs[i] = u - q * (uint32_t)a.chunks;
+        const int col = (int)cs[i] * kChunk;
+        at[i] = row * a.F + col;
+        left[i] = row < a.M ? a.F - col : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) x[i].load(static_cast<const T *>(a.X) + at[i], left[i]);
+    if (a.R) {
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) r[i].load(static_cast<const T *>(a.R) + at[i], left[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        float v[8];
+        uint32_t words[4];
+        if constexpr (DROP) gen.words(cs[i], rows[i], words);
+        x[i].get(v);
+        if constexpr (DROP) drop8(v, words, a.threshold, a.scale);
+        if (a.R) {
+            float y[8];
+            r[i].get(y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += y[j];
+        }
+        Chunk<BF16>::store(static_cast<T *>(a.Y) + at[i], v, left[i]);
+    }
+}
+
+// ------------------------------------------------------------------------------------ 8-bit rows
+struct Gather8Args {
+    const uint8_t *table;
+    const float *scale;
+    int64_t table_rows;
+    const int64_t *ids;
+    int64_t n;
+    int32_t F;
+    int32_t slices;                 // of 16 columns a row
+    int32_t lg;                     // 2^lg lanes a row
+    void *out;
+};
+
+// Sixteen columns of one row (rows of 16 and more: the last slice starts 16 before the row's end, and what two
+// slices share is written twice alike; shorter rows: column by column).
+template <bool BF16, bool SHORT>
+__global__ __launch_bounds__(kBlock) void k_gather_e4m3(Gather8Args a)
+{
+    typedef uint32_t bytes16 __attribute__((ext_vector_type(4), aligned(1)));
+    typedef typename Chunk<BF16>::elem T;
+    const int64_t row = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> a.lg;
+    if (row >= a.n) return;
+    const int lanes = 1 << a.lg;
+    const int64_t id = a.ids[row];
+    const bool there = (uint64_t)id < (uint64_t)a.table_rows;
+    const float scale = there ? a.scale[id] : __uint_as_float(0x7FC00000u);
+    const uint8_t *q = a.table + (there ? id : 0) * a.F;
+    T *out = static_cast<T *>(a.out) + row * a.F;
+    if constexpr (SHORT) {
+        for (int c = threadIdx.x & (lanes - 1); c < a.F; c += lanes) {
+            const uint32_t b = there ? q[c] : 0u;
+            const float v = __builtin_amdgcn_cvt_f32_fp8((int)b, 0) * scale;
+            if constexpr (BF16) out[c] = __builtin_bit_cast(uint16_t, (__bf16)v);
+            else out[c] = v;
+        }
+    } else {
+        for (int c = threadIdx.x & (lanes - 1); c < a.slices; c += lanes) {
+            const int col = c * 16 < a.F - 16 ? c * 16 : a.F - 16;
+            bytes16 w = {0u, 0u, 0u, 0u};
+            if (there) w = *reinterpret_cast<const bytes16 *>(q + col);
+            float v[2][8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
+                float *o = v[i / 2] + 4 * (i % 2);
+                o[0] = lo[0] * scale;
+                o[1] = lo[1] * scale;
+                o[2] = hi[0] * scale;
+                o[3] = hi[1] * scale;
+            }
+            Chunk<BF16>::store(out + col, v[0], 8);
+            Chunk<BF16>::store(out + col + 8, v[1], 8);
+        }
+    }
+}
+
+bool misaligned_to(const void *p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
+
+}  // namespace
+}  // namespace fastgl
+
+using namespace fastgl;
+
+extern "C" {
+
+fastgl_status fastgl_dropout(fastgl_dtype dtype, const void *X, const void *R, int64_t M, int64_t F, const int64_t *rng,
+                             double p, void *Y, void *stream)
+{
+    DropArgs a = {};
+    if (dtype != FASTGL_F32 && dtype != FASTGL_BF16) {
+        set_error("bad dtype %d", (int)dtype);
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (M < 0 || F < 1) {
+        set_error("negative size or no columns (M=%lld F=%lld)", (long long)M, (long long)F);
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (M > kMaxIndex || F > (int64_t)1 << 24) {
+        set_error("M must stay below 2^31-1-1024 and F at 2^24 or below");
+        return FASTGL_ERR_UNSUPPORTED;
+    }
+    if (!drop_constants(p, &a.threshold, &a.scale)) {
+        set_error("the dropout probability must be in [0, 1]");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (p > 0.0 && (!rng || misaligned_to(rng, 8))) {
+        set_error("dropout needs rng: two int64 {seed, offset} in device memory, aligned to 8 bytes");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (M == 0) return FASTGL_OK;
+    const uintptr_t el = dtype == FASTGL_BF16 ? 2 : 4;
+    if (!X || !Y) {
+        set_error("X or Y is NULL");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (misaligned_to(X, el) || misaligned_to(R, el) || misaligned_to(Y, el)) {
+        set_error("arrays must be aligned to their element size");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    a.X = X; a.R = R; a.Y = Y;
+    a.M = M; a.F = (int32_t)F;
+    a.chunks = (int32_t)ceil_div(F, kChunk);
+    a.inv = (uint32_t)ceil_div((int64_t)1 << 32, a.chunks > 1 ? a.chunks : 2);
+    a.rng = rng;
+    const int64_t blocks = ceil_div(M * a.chunks, kBlock * kUnits);
+    if (blocks > 0x7FFFFFFFLL) {
+        set_error("dropout too large for one launch");
+        return FASTGL_ERR_UNSUPPORTED;
+    }
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, (hipStream_t)stream, a); };
+    if (dtype == FASTGL_BF16) p > 0.0 ? go(k_dropout<true, true>) : go(k_dropout<true, false>);
+    else p > 0.0 ? go(k_dropout<false, true>) : go(k_dropout<false, false>);
+    FASTGL_LAUNCH_CHECK("fastgl_dropout");
+    return FASTGL_OK;
+}
+
+fastgl_status fastgl_gather_rows_e4m3(const uint8_t *table, const float *scale, int64_t table_rows, const int64_t *ids,
+                                      int64_t n, int64_t F, fastgl_dtype dtype, void *out, void *stream)
+{
+    if (dtype != FASTGL_F32 && dtype != FASTGL_BF16) {
+        set_error("bad dtype %d", (int)dtype);
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (n < 0 || table_rows < 0 || F < 1) {
+        set_error("negative size or no columns (n=%lld table_rows=%lld F=%lld)", (long long)n, (long long)table_rows, (long long)F);
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (n > kMaxIndex || F > (int64_t)1 << 24) {
+        set_error("n must stay below 2^31-1-1024 and F at 2^24 or below");
+        return FASTGL_ERR_UNSUPPORTED;
+    }
+    if (n == 0) return FASTGL_OK;
+    if (!ids || !out || (table_rows > 0 && (!table || !scale))) {
+        set_error("table, scale, ids or out is NULL");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (misaligned_to(scale, 4) || misaligned_to(ids, 8) || misaligned_to(out, dtype == FASTGL_BF16 ? 2 : 4)) {
+        set_error("arrays must be aligned to their element size");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    Gather8Args a = {};
+    a.table = table; a.scale = scale; a.table_rows = table_rows;
+    a.ids = ids; a.n = n; a.F = (int32_t)F; a.out = out;
+    a.slices = (int32_t)ceil_div(F, 16);
+    const int64_t units = F < 16 ? F : a.slices;
+    while (a.lg < 6 && ((int64_t)1 << a.lg) < units) ++a.lg;
+    const int64_t blocks = ceil_div(n << a.lg, kBlock);
+    if (blocks > 0x7FFFFFFFLL) {
+        set_error("gather too large for one launch");
+        return FASTGL_ERR_UNSUPPORTED;
+    }
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, (hipStream_t)stream, a); };
+    if (dtype == FASTGL_BF16) F < 16 ? go(k_gather_e4m3<true, true>) : go(k_gather_e4m3<true, false>);
+    else F < 16 ? go(k_gather_e4m3<false, true>) : go(k_gather_e4m3<false, false>);
+    FASTGL_LAUNCH_CHECK("fastgl_gather_rows_e4m3");
+    return FASTGL_OK;
+}
+
+}  // extern "C"

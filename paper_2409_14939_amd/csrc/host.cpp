@@ -25,6 +25,7 @@
 #include "fastgl_edge.h"
 #include "fastgl_idmap.h"
 #include "fastgl_match.h"
+#include "fastgl_norm.h"
 #include "fastgl_update.h"
 
 namespace {
@@ -58,6 +59,7 @@ const char *dtype_name(at::ScalarType t)
         case at::kFloat: return "torch.float32";
         case at::kBFloat16: return "torch.bfloat16";
         case at::kByte: return "torch.uint8";
+        case at::kFloat8_e4m3fn: return "torch.float8_e4m3fn";
         default: return "the right dtype";
     }
 }
@@ -614,6 +616,148 @@ PyObject *edge_score_bwd(PyObject *const *a)
     return tuple({gl.t, gr.t});
 }
 
+// ------------------------------------------------------------------- norm, dropout, rows in 8 bits
+// The generator's state: int64 [2], or None.
+const int64_t *rng_state(PyObject *o)
+{
+    if (none(o)) return nullptr;
+    const at::Tensor &t = dev(o, at::kLong, "rng");
+    if (!shape1(t, 2)) fail(PyExc_ValueError, "rng must be int64 [2]: seed and offset");
+    return (const int64_t *)t.data_ptr();
+}
+
+// A matrix of the shape and type of `x`, or None.
+const void *like_matrix(PyObject *o, const at::Tensor &x, const char *name)
+{
+    if (none(o)) return nullptr;
+    const at::Tensor &t = dev(o, x.scalar_type(), name);
+    if (!shape2(t, x.size(0), x.size(1))) {
+        PyErr_Format(PyExc_ValueError, "%s must be [%lld, %lld]", name, (long long)x.size(0), (long long)x.size(1));
+        throw Raised{};
+    }
+    return t.data_ptr();
+}
+
+// A matrix of features with exactly two dimensions.
+const at::Tensor &features2(PyObject *o, const char *name)
+{
+    const at::Tensor &x = features(o, name);
+    if (x.dim() != 2) {
+        PyErr_Format(PyExc_ValueError, "%s must have two dimensions", name);
+        throw Raised{};
+    }
+    return x;
+}
+
+const float *vector_f32(PyObject *o, int64_t n, const char *name)
+{
+    const at::Tensor &t = dev(o, at::kFloat, name);
+    if (!shape1(t, n)) {
+        PyErr_Format(PyExc_ValueError, "%s must be [%lld]", name, (long long)n);
+        throw Raised{};
+    }
+    return (const float *)t.data_ptr();
+}
+
+// A result of a given shape: the caller's, checked, or a new one.
+Out out_of(PyObject *o, at::ScalarType type, at::IntArrayRef shape, const at::Tensor &like, const char *name)
+{
+    Out r(o, type, shape, like, name);
+    if (r.t.sizes() != shape) {
+        PyErr_Format(PyExc_ValueError, "%s has the wrong shape", name);
+        throw Raised{};
+    }
+    return r;
+}
+
+double to_double(PyObject *o)
+{
+    PyObject *f = PyNumber_Float(o);
+    if (!f) throw Raised{};
+    const double v = PyFloat_AS_DOUBLE(f);
+    Py_DECREF(f);
+    return v;
+}
+
+// (e4m3, X, w, eps, residual, rng, p, want_sum, want_rstd, sum_out, Y, scale, rstd) -> (Y, scale, sum, rstd)
+PyObject *norm_fwd(PyObject *const *a)
+{
+    const bool e4m3 = truth(a[0]);
+    const at::Tensor &X = features2(a[1], "X");
+    const int64_t M = X.size(0), F = X.size(1);
+    const float *w = vector_f32(a[2], F, "weight");
+    const float eps = to_real(a[3]);
+    const void *R = like_matrix(a[4], X, "residual");
+    const int64_t *rng = rng_state(a[5]);
+    const double p = to_double(a[6]);
+    Out sum, scale, rstd;
+    if (!none(a[9]) || (truth(a[7]) && (R || p != 0.0))) sum = out_of(a[9], X.scalar_type(), {M, F}, X, "sum_out");
+    const Out Y = out_of(a[10], e4m3 ? at::kFloat8_e4m3fn : X.scalar_type(), {M, F}, X, "Y");
+    if (e4m3) scale = out_of(a[11], at::kFloat, {M}, X, "scale");
+    if (!none(a[12]) || truth(a[8])) rstd = out_of(a[12], at::kFloat, {M}, X, "rstd");
+    run([&](void *s) {
+        if (e4m3)
+            return fastgl_norm_fwd_e4m3(feat_dtype(X), X.data_ptr(), R, w, M, F, eps, rng, p, sum.p(), (uint8_t *)Y.p(),
+                                        (float *)scale.p(), (float *)rstd.p(), s);
+        return fastgl_norm_fwd(feat_dtype(X), X.data_ptr(), R, w, M, F, eps, rng, p, sum.p(), Y.p(), (float *)rstd.p(), s);
+    });
+    return tuple({Y.t, scale.t, sum.t, rstd.t});
+}
+
+// (S, w, rstd, dY, dS, rng, p, want_dX, want_dR, want_dw, dX, dR, dw, workspace) -> (dX, dR, dw)
+PyObject *norm_bwd(PyObject *const *a)
+{
+    const at::Tensor &S = features2(a[0], "S");
+    const int64_t M = S.size(0), F = S.size(1);
+    const float *w = vector_f32(a[1], F, "weight"), *rstd = vector_f32(a[2], M, "rstd");
+    if (none(a[3])) fail(PyExc_TypeError, "dY must be a tensor");
+    const void *dY = like_matrix(a[3], S, "dY"), *dS = like_matrix(a[4], S, "dS");
+    const int64_t *rng = rng_state(a[5]);
+    const double p = to_double(a[6]);
+    Out dX, dR, dw;
+    const bool one = p == 0.0 && none(a[10]) && none(a[11]);          // without dropout both are the same gradient
+    if (!none(a[10]) || (truth(a[7]) && !one)) dX = out_of(a[10], S.scalar_type(), {M, F}, S, "dX");
+    if (!none(a[11]) || truth(a[8]) || (truth(a[7]) && one)) dR = out_of(a[11], S.scalar_type(), {M, F}, S, "dR");
+    if (!none(a[12]) || truth(a[9])) dw = out_of(a[12], at::kFloat, {F}, S, "dw");
+    const Scratch ws(a[13], S, [&] { return dw.t.defined() ? fastgl_norm_bwd_workspace_bytes(M, F) : 0; });
+    run([&](void *s) {
+        return fastgl_norm_bwd(feat_dtype(S), S.data_ptr(), w, rstd, dY, dS, M, F, rng, p, dX.p(), dR.p(), (float *)dw.p(),
+                               ws.p(), ws.n(), s);
+    });
+    if (one) return tuple({truth(a[7]) ? dR.t : at::Tensor(), truth(a[8]) ? dR.t : at::Tensor(), dw.t});
+    return tuple({dX.t, dR.t, dw.t});
+}
+
+// (X, rng, p, residual, out) -> out
+PyObject *dropout(PyObject *const *a)
+{
+    const at::Tensor &X = features2(a[0], "X");
+    const int64_t *rng = rng_state(a[1]);
+    const double p = to_double(a[2]);
+    const void *R = like_matrix(a[3], X, "residual");
+    const Out out = out_of(a[4], X.scalar_type(), X.sizes(), X, "out");
+    run([&](void *s) {
+        return fastgl_dropout(feat_dtype(X), X.data_ptr(), R, X.size(0), X.size(1), rng, p, out.p(), s);
+    });
+    return wrap(out.t);
+}
+
+// (table, scale, ids, dtype, out) -> out
+PyObject *gather_rows_e4m3(PyObject *const *a)
+{
+    const at::Tensor &table = dev(a[0], at::kFloat8_e4m3fn, "table"), &ids = dev(a[2], at::kLong, "ids");
+    if (table.dim() != 2 || ids.dim() != 1) fail(PyExc_ValueError, "table must be [rows, F] and ids [n]");
+    const float *scale = vector_f32(a[1], table.size(0), "scale");
+    const auto dt = (fastgl_dtype)integer(a[3]);
+    const int64_t n = ids.size(0), F = table.size(1);
+    const Out out = out_of(a[4], dt == FASTGL_BF16 ? at::kBFloat16 : at::kFloat, {n, F}, table, "out");
+    run([&](void *s) {
+        return fastgl_gather_rows_e4m3((const uint8_t *)table.data_ptr(), scale, table.size(0), (const int64_t *)ids.data_ptr(), n,
+                                       F, dt, out.p(), s);
+    });
+    return wrap(out.t);
+}
+
 // (error class): called once by binding.py
 PyObject *set_error_class(PyObject *const *a)
 {
@@ -628,7 +772,8 @@ PyMethodDef g_methods[] = {
     FN(aggregate, 10), FN(aggregate_static, 7), FN(plan_create_many, 3), FN(gather_rows, 3),
     FN(update_fwd, 5), FN(layer_fwd, 14), FN(update_bwd, 12), FN(idmap, 7), FN(match, 7), FN(assemble_rows, 5),
     FN(overlap_counts, 3), FN(edge_weight_grad, 9), FN(edge_softmax_fwd, 4), FN(edge_softmax_bwd, 5),
-    FN(edge_score_fwd, 6), FN(edge_score_bwd, 11), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
+    FN(edge_score_fwd, 6), FN(edge_score_bwd, 11), FN(norm_fwd, 13), FN(norm_bwd, 14), FN(dropout, 5),
+    FN(gather_rows_e4m3, 5), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
 #undef FN
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host", "Native marshalling of the C ABI's calls.", -1, g_methods,

@@ -1,0 +1,661 @@
+// Root-mean-square norm of rows with the residual's addition and dropout in front of it, and its backward pass
+// (fastgl_norm.h has the formulas).
+//
+// A row is read once: its columns stay in registers between the sum of squares and the result.  A lane holds eight
+// columns at a time (one 16-byte word of bf16, two of fp32, one answer of the generator).  A row has 1 to 64 lanes
+// of a wavefront, NC chunks each, and beyond 1024 columns a workgroup; beyond 8192 it is read twice.  Groups of lanes walk the rows with
+// the grid's stride, so that the weights stay in registers and the backward pass keeps its column sums there.
+#include "fastgl_norm.h"
+#include "rows_device.h"
+
+#include <type_traits>
+
+namespace fastgl {
+namespace {
+
+constexpr int kMaxGroupsOfRows = 2048;    // workgroups of a launch: eight per compute unit
+constexpr int kReduceCols = 16;
+
+struct NormArgs {
+    const void *X, *R;
+    const float *w;
+    int64_t M;
+    int32_t F;
+    float eps, inv_F;
+    const int64_t *rng;
+    uint32_t threshold;
+    float drop_scale;
+    void *sum_out, *Y;
+    float *row_scale, *rstd;
+};
+
+struct NormBwdArgs {
+    const void *S, *dY, *dS;
+    const float *w, *rstd;
+    int64_t M;
+    int32_t F;
+    float inv_F;
+    const int64_t *rng;
+    uint32_t threshold;
+    float drop_scale;
+    void *dX, *dR;
+    float *part;               // [workgroups][F] column sums of dY n, or NULL
+};
+
+struct Plus {
+    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+struct Max {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+
+// Over the 2^LG lanes of a row (LG = 8: the workgroup, through `buf`, two halves in turn so that one barrier is
+// enough); the order of the terms is fixed.
+template <int LG, class OP>
+__device__ __forceinline__ float row_reduce(float v, OP op, float (&buf)[2][4], int &turn)
+{
+    constexpr int IN = LG < 6 ? LG : 6;
+#pragma unroll
+    for (int o = 0; o < IN; ++o) v = op(v, __shfl_xor(v, 1 << o, kWave));
+    if constexpr (LG == 8) {
+        if ((threadIdx.x & (kWave - 1)) == 0) buf[turn][threadIdx.x / kWave] = v;
+        __syncthreads();
+        v = op(op(buf[turn][0], buf[turn][1]), op(buf[turn][2], buf[turn][3]));
+        turn ^= 1;
+    }
+    return v;
+}
+
+// y of eight columns as e4m3.
+__device__ __forceinline__ void store_e4m3(uint8_t *p, const float (&v)[8], int left)
+{
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(1)));
+    int a = 0, b = 0;
+    a = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], a, false);
+    a = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], a, true);
+    b = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], b, false);
+    b = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], b, true);
+    if (left >= 8) {
+        *reinterpret_cast<u32x2 *>(p) = u32x2{(uint32_t)a, (uint32_t)b};
+    } else {
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < left) p[j] = (uint8_t)((uint32_t)(j < 4 ? a : b) >> (8 * (j & 3)));
+    }
+}
+
+template <bool BF16, int LG, int NC, bool DROP, bool E4M3>
+__global__ __launch_bounds__(kBlock) void k_norm(NormArgs a)
+{
+    typedef typename Chunk<BF16>::elem T;
+    constexpr int LANES = 1 << LG, ROWS = kBlock >> LG;
+    __shared__ float buf[2][4];
+    int turn = 0;
+    const int lane = threadIdx.x & (LANES - 1), F = a.F;
+    const T *X = static_cast<const T *>(a.X), *R = static_cast<const T *>(a.R);
+    Philox gen;
+    if constexpr (DROP) gen.load(a.rng);
+    float w[NC][8];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        Chunk<false> q;
+        const int col = (c * LANES + lane) * kChunk;
+        q.load(a.w + col, F - col);
+        q.get(w[c]);
+    }
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + (threadIdx.x >> LG); row < a.M; row += step) {
+        const int64_t at = row * F;
+        Chunk<BF16> x[NC], r[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = (c * LANES + lane) * kChunk;
+            x[c].load(X + at + col, F - col);
+        }
+        if (R) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int col = (c * LANES + lane) * kChunk;
+                r[c].load(R + at + col, F - col);
+            }
+        }
+        float h[NC][8], sq = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = (c * LANES + lane) * kChunk;
+            uint32_t words[4];
+            if constexpr (DROP) gen.words((uint32_t)(col / kChunk), (uint32_t)row, words);
+            x[c].get(h[c]);
+            if constexpr (DROP) drop8(h[c], words, a.threshold, a.drop_scale);
+            if (R) {
+                float v[8];
+                r[c].get(v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[c][j] += v[j];
+            }
+            if (a.sum_out) Chunk<BF16>::store(static_cast<T *>(a.sum_out) + at + col, h[c], F - col);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sq = fmaf(h[c][j], h[c][j], sq);
+        }
+        sq = row_reduce<LG>(sq, Plus(), buf, turn);
+        const float rstd = 1.f / sqrtf(sq * a.inv_F + a.eps);
+        if (a.rstd && lane == 0) a.rstd[row] = rstd;
+        float most = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                h[c][j] = h[c][j] * rstd * w[c][j];
+                if constexpr (E4M3) most = fmaxf(most, fabsf(h[c][j]));
+            }
+        if constexpr (E4M3) {
+            most = row_reduce<LG>(most, Max(), buf, turn);
+            const float scale = fmaxf(most / 448.f, 0x1p-126f), inv = 1.f / scale;
+            if (lane == 0) a.row_scale[row] = scale;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int col = (c * LANES + lane) * kChunk;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[c][j] *= inv;
+                store_e4m3(static_cast<uint8_t *>(a.Y) + at + col, h[c], F - col);
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int col = (c * LANES + lane) * kChunk;
+                Chunk<BF16>::store(static_cast<T *>(a.Y) + at + col, h[c], F - col);
+            }
+        }
+    }
+}
+
+// Rows beyond what registers hold: one workgroup a row, h formed in every pass over it.
+template <bool BF16, bool DROP, bool E4M3>
+__global__ __launch_bounds__(kBlock) void k_norm_wide(NormArgs a)
+{
+    typedef typename Chunk<BF16>::elem T;
+    __shared__ float buf[2][4];
+    int turn = 0;
+    const int F = a.F;
+    const T *X = static_cast<const T *>(a.X), *R = static_cast<const T *>(a.R);
+    Philox gen;
+    if constexpr (DROP) gen.load(a.rng);
+    for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+        const int64_t at = row * F;
+        auto sum = [&](int col, float(&h)[8]) {
+            Chunk<BF16> x;
+            x.load(X + at + col, F - col);
+            x.get(h);
+            if constexpr (DROP) {
+                uint32_t words[4];
+                gen.words((uint32_t)(col / kChunk), (uint32_t)row, words);
+                drop8(h, words, a.threshold, a.drop_scale);
+            }
+            if (R) {
+                float v[8];
+                x.load(R + at + col, F - col);
+                x.get(v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[j] += v[j];
+            }
+        };
+        auto scaled = [&](int col, float rstd, float(&h)[8]) {
+            float w[8];
+            Chunk<false> q;
+            q.load(a.w + col, F - col);
+            q.get(w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[j] = h[j] * rstd * w[j];
+        };
+        float sq = 0.f;
+        for (int col = threadIdx.x * kChunk; col < F; col += kBlock * kChunk) {
+            float h[8];
+            sum(col, h);
+            if (a.sum_out) Chunk<BF16>::store(static_cast<T *>(a.sum_out) + at + col, h, F - col);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sq = fmaf(h[j], h[j], sq);
+        }
+        sq = row_reduce<8>(sq, Plus(), buf, turn);
+        const float rstd = 1.f / sqrtf(sq * a.inv_F + a.eps);
+        if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+        float inv = 1.f;
+        if constexpr (E4M3) {
+            float most = 0.f;
+            for (int col = threadIdx.x * kChunk; col < F; col += kBlock * kChunk) {
+                float h[8];
+                sum(col, h);
+                scaled(col, rstd, h);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(h[j]));
+            }
+            most = row_reduce<8>(most, Max(), buf, turn);
+            const float scale = fmaxf(most / 448.f, 0x1p-126f);
+            inv = 1.f / scale;
+            if (threadIdx.x == 0) a.row_scale[row] = scale;
+        }
+        for (int col = threadIdx.x * kChunk; col < F; col += kBlock * kChunk) {
+            float h[8];
+            sum(col, h);
+            scaled(col, rstd, h);
+            if constexpr (E4M3) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[j] *= inv;
+                store_e4m3(static_cast<uint8_t *>(a.Y) + at + col, h, F - col);
+            } else
+                Chunk<BF16>::store(static_cast<T *>(a.Y) + at + col, h, F - col);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------ backward
+template <bool BF16, int LG, int NC, bool DROP>
+__global__ __launch_bounds__(kBlock) void k_norm_bwd(NormBwdArgs a)
+{
+    typedef typename Chunk<BF16>::elem T;
+    constexpr int LANES = 1 << LG, ROWS = kBlock >> LG;
+    __shared__ float buf[2][4];
+    int turn = 0;
+    const int lane = threadIdx.x & (LANES - 1), F = a.F;
+    const T *S = static_cast<const T *>(a.S), *dY = static_cast<const T *>(a.dY), *dS = static_cast<const T *>(a.dS);
+    Philox gen;
+    if constexpr (DROP) gen.load(a.rng);
+    float w[NC][8], dw[NC][8];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        Chunk<false> q;
+        const int col = (c * LANES + lane) * kChunk;
+        q.load(a.w + col, F - col);
+        q.get(w[c]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[c][j] = 0.f;
+    }
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + (threadIdx.x >> LG); row < a.M; row += step) {
+        const int64_t at = row * F;
+        Chunk<BF16> qs[NC], qy[NC], qd[NC];
+        const float rstd = a.rstd[row];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = (c * LANES + lane) * kChunk;
+            qs[c].load(S + at + col, F - col);
+            qy[c].load(dY + at + col, F - col);
+        }
+        if (dS) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int col = (c * LANES + lane) * kChunk;
+                qd[c].load(dS + at + col, F - col);
+            }
+        }
+        float n[NC][8], t[NC][8], dot = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            qs[c].get(n[c]);
+            qy[c].get(t[c]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                n[c][j] *= rstd;
+                dw[c][j] = fmaf(t[c][j], n[c][j], dw[c][j]);
+                t[c][j] *= w[c][j];
+                dot = fmaf(t[c][j], n[c][j], dot);
+            }
+        }
+        dot = row_reduce<LG>(dot, Plus(), buf, turn) * a.inv_F;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = (c * LANES + lane) * kChunk;
+            float d[8];
+            if (dS) qd[c].get(d);
+            else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[j] = 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d[j] = fmaf(rstd, t[c][j] - n[c][j] * dot, d[j]);
+            if (a.dR) Chunk<BF16>::store(static_cast<T *>(a.dR) + at + col, d, F - col);
+            if (a.dX) {
+                if constexpr (DROP) {
+                    uint32_t words[4];
+                    gen.words((uint32_t)(col / kChunk), (uint32_t)row, words);
+                    drop8(d, words, a.threshold, a.drop_scale);
+                }
+                Chunk<BF16>::store(static_cast<T *>(a.dX) + at + col, d, F - col);
+            }
+        }
+    }
+    if (!a.part) return;
+    // the column sums of the workgroup's groups of lanes, in the order of the groups
+    if constexpr (LG == 8) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = (c * LANES + lane) * kChunk;
+            Chunk<false>::store(a.part + (int64_t)blockIdx.x * F + col, dw[c], F - col);
+        }
+    } else {
+        constexpr int STRIDE = LANES * kChunk + 4;
+        __shared__ float sums[4][STRIDE];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int o = LANES; o < kWave; o <<= 1) dw[c][j] += __shfl_xor(dw[c][j], o, kWave);
+            __syncthreads();
+            if ((threadIdx.x & (kWave - 1)) < LANES)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sums[threadIdx.x / kWave][lane * kChunk + j] = dw[c][j];
+            __syncthreads();
+            for (int i = threadIdx.x; i < LANES * kChunk; i += kBlock) {
+                const int col = c * LANES * kChunk + i;
+                if (col < F) a.part[(int64_t)blockIdx.x * F + col] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+            }
+        }
+    }
+}
+
+// Rows beyond what registers hold.  Column sums: a second kernel over the rows (k_norm_dw_wide).
+template <bool BF16, bool DROP>
+__global__ __launch_bounds__(kBlock) void k_norm_bwd_wide(NormBwdArgs a)
+{
+    typedef typename Chunk<BF16>::elem T;
+    __shared__ float buf[2][4];
+    int turn = 0;
+    const int F = a.F;
+    const T *S = static_cast<const T *>(a.S), *dY = static_cast<const T *>(a.dY), *dS = static_cast<const T *>(a.dS);
+    Philox gen;
+    if constexpr (DROP) gen.load(a.rng);
+    for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+        const int64_t at = row * F;
+        const float rstd = a.rstd[row];
+        auto terms = [&](int col, float(&n)[8], float(&t)[8]) {
+            Chunk<BF16> q;
+            Chunk<false> qw;
+            float w[8];
+            q.load(S + at + col, F - col);
+            q.get(n);
+            q.load(dY + at + col, F - col);
+            q.get(t);
+            qw.load(a.w + col, F - col);
+            qw.get(w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                n[j] *= rstd;
+                t[j] *= w[j];
+            }
+        };
+        float dot = 0.f;
+        for (int col = threadIdx.x * kChunk; col < F; col += kBlock * kChunk) {
+            float n[8], t[8];
+            terms(col, n, t);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) dot = fmaf(t[j], n[j], dot);
+        }
+        dot = row_reduce<8>(dot, Plus(), buf, turn) * a.inv_F;
+        for (int col = threadIdx.x * kChunk; col < F; col += kBlock * kChunk) {
+            float n[8], t[8], d[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            terms(col, n, t);
+            if (dS) {
+                Chunk<BF16> q;
+                q.load(dS + at + col, F - col);
+                q.get(d);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d[j] = fmaf(rstd, t[j] - n[j] * dot, d[j]);
+            if (a.dR) Chunk<BF16>::store(static_cast<T *>(a.dR) + at + col, d, F - col);
+            if (a.dX) {
+                if constexpr (DROP) {
+                    uint32_t words[4];
+                    gen.words((uint32_t)(col / kChunk), (uint32_t)row, words);
+                    drop8(d, words, a.threshold, a.drop_scale);
+                }
+                Chunk<BF16>::store(static_cast<T *>(a.dX) + at + col, d, F - col);
+            }
+        }
+    }
+}
+
+// part[y][col] = sum over the rows y, y + gridDim.y, ... of dY n: wide rows, a workgroup holds 2048 columns.
+template <bool BF16>
+__global__ __launch_bounds__(kBlock) void k_norm_dw_wide(NormBwdArgs a)
+{
+    typedef typename Chunk<BF16>::elem T;
+    const int F = a.F, col = (int)(blockIdx.x * kBlock + threadIdx.x) * kChunk;
+    if (col >= F) return;
+    float dw[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int64_t row = blockIdx.y; row < a.M; row += gridDim.y) {
+        Chunk<BF16> q;
+        float n[8], y[8];
+        const float rstd = a.rstd[row];
+        q.load(static_cast<const T *>(a.S) + row * F + col, F - col);
+        q.get(n);
+        q.load(static_cast<const T *>(a.dY) + row * F + col, F - col);
+        q.get(y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[j] = fmaf(y[j], n[j] * rstd, dw[j]);
+    }
+    Chunk<false>::store(a.part + (int64_t)blockIdx.y * F + col, dw, F - col);
+}
+
+// dw[col] = sum of part[0 .. n)[col] in fp64: 16 columns a workgroup, 64 threads a column, a fixed order.
+__global__ __launch_bounds__(1024) void k_norm_dw(const float *__restrict__ part, int32_t n, int32_t F, float *__restrict__ dw)
+{
+    __shared__ double sums[64][kReduceCols + 1];
+    const int c = threadIdx.x % kReduceCols, s = threadIdx.x / kReduceCols;
+    const int col = blockIdx.x * kReduceCols + c;
+    double v = 0.0;
+    if (col < F) {
+#pragma unroll 8
+        for (int i = s; i < n; i += 64) v += (double)part[(int64_t)i * F + col];
+    }
+    sums[s][c] = v;
+    __syncthreads();
+    if (s < 8) {
+        v = 0.0;
+        for (int i = 0; i < 8; ++i) v += sums[s * 8 + i][c];
+    }
+    __syncthreads();
+    if (s < 8) sums[s][c] = v;
+    __syncthreads();
+    if (s == 0 && col < F) {
+        v = 0.0;
+        for (int i = 0; i < 8; ++i) v += sums[i][c];
+        dw[col] = (float)v;
+    }
+}
+
+// ------------------------------------------------------------------------------------ host side
+// How a row of F columns is spread over lanes: f(integral_constant LG, integral_constant NC); false beyond registers.
+template <class GO>
+bool spread(int64_t F, GO go)
+{
+    const int64_t chunks = ceil_div(F, kChunk);
+    auto is = [&](auto lg, auto nc) {
+        go(lg, nc);
+        return true;
+    };
+    using std::integral_constant;
+    if (chunks <= 1) return is(integral_constant<int, 0>(), integral_constant<int, 1>());
+    if (chunks <= 8) return is(integral_constant<int, 3>(), integral_constant<int, 1>());
+    if (chunks <= 16) return is(integral_constant<int, 4>(), integral_constant<int, 1>());
+    if (chunks <= 32) return is(integral_constant<int, 5>(), integral_constant<int, 1>());
+    if (chunks <= 64) return is(integral_constant<int, 6>(), integral_constant<int, 1>());
+    if (chunks <= 128) return is(integral_constant<int, 6>(), integral_constant<int, 2>());
+    if (chunks <= 256) return is(integral_constant<int, 8>(), integral_constant<int, 1>());
+    if (chunks <= 512) return is(integral_constant<int, 8>(), integral_constant<int, 2>());
+    if (chunks <= 1024) return is(integral_constant<int, 8>(), integral_constant<int, 4>());
+    return false;
+}
+
+int rows_per_group(int64_t F)
+{
+    int rows = 1;
+    spread(F, [&](auto lg, auto) { rows = kBlock >> decltype(lg)::value; });
+    return rows;
+}
+
+// Workgroups of the backward pass that leave column sums: a group of lanes has eight rows at least, so that the sums are
+// little beside the rows.
+int64_t bwd_groups(int64_t M, int64_t F)
+{
+    const int64_t most = ceil_div(M, rows_per_group(F)), some = ceil_div(most, 8);
+    const int64_t least = most < 256 ? most : 256;
+    const int64_t n = some > least ? some : least;
+    return n < kMaxGroupsOfRows ? n : kMaxGroupsOfRows;
+}
+
+bool misaligned_to(const void *p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
+
+fastgl_status check_rows(fastgl_dtype dtype, int64_t M, int64_t F, const int64_t *rng, double p, uint32_t *threshold, float *scale)
+{
+    if (dtype != FASTGL_F32 && dtype != FASTGL_BF16) {
+        set_error("bad dtype %d", (int)dtype);
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (M < 0 || F < 1) {
+        set_error("negative size or no columns (M=%lld F=%lld)", (long long)M, (long long)F);
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (M > kMaxIndex || F > (int64_t)1 << 24) {
+        set_error("M must stay below 2^31-1-1024 and F at 2^24 or below");
+        return FASTGL_ERR_UNSUPPORTED;
+    }
+    if (!drop_constants(p, threshold, scale)) {
+        set_error("the dropout probability must be in [0, 1]");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (p > 0.0 && (!rng || misaligned_to(rng, 8))) {
+        set_error("dropout needs rng: two int64 {seed, offset} in device memory, aligned to 8 bytes");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    return FASTGL_OK;
+}
+
+fastgl_status norm_fwd(bool e4m3, fastgl_dtype dtype, const void *X, const void *R, const float *w, int64_t M, int64_t F,
+                       float eps, const int64_t *rng, double p, void *sum_out, void *Y, float *row_scale, float *rstd, hipStream_t s)
+{
+    NormArgs a = {};
+    const fastgl_status st = check_rows(dtype, M, F, rng, p, &a.threshold, &a.drop_scale);
+    if (st != FASTGL_OK) return st;
+    if (!(eps >= 0.f) || eps > 3.4e38f) {
+        set_error("eps must be finite and not negative");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (M == 0) return FASTGL_OK;
+    const uintptr_t el = dtype == FASTGL_BF16 ? 2 : 4;
+    if (!X || !w || !Y || (e4m3 && !row_scale)) {
+        set_error("X, w or an output is NULL");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (misaligned_to(X, el) || misaligned_to(R, el) || misaligned_to(sum_out, el) || misaligned_to(Y, e4m3 ? 1 : el) ||
+        misaligned_to(w, 4) || misaligned_to(rstd, 4) || misaligned_to(row_scale, 4)) {
+        set_error("arrays must be aligned to their element size");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    a.X = X; a.R = R; a.w = w;
+    a.M = M; a.F = (int32_t)F;
+    a.eps = eps; a.inv_F = (float)(1.0 / (double)F);
+    a.rng = rng;
+    a.sum_out = sum_out; a.Y = Y; a.row_scale = row_scale; a.rstd = rstd;
+    const int64_t groups = ceil_div(M, rows_per_group(F));
+    const dim3 grid((unsigned)(groups < kMaxGroupsOfRows ? groups : kMaxGroupsOfRows));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, s, a); };
+    auto typed = [&](auto bf16, auto drop, auto to8) {
+        constexpr bool B = decltype(bf16)::value, D = decltype(drop)::value, E = decltype(to8)::value;
+        if (!spread(F, [&](auto lg, auto nc) { go(k_norm<B, decltype(lg)::value, decltype(nc)::value, D, E>); }))
+            go(k_norm_wide<B, D, E>);
+    };
+    auto dropped = [&](auto bf16, auto drop) { e4m3 ? typed(bf16, drop, std::true_type()) : typed(bf16, drop, std::false_type()); };
+    auto both = [&](auto bf16) { p > 0.0 ? dropped(bf16, std::true_type()) : dropped(bf16, std::false_type()); };
+    if (dtype == FASTGL_BF16) both(std::true_type());
+    else both(std::false_type());
+    FASTGL_LAUNCH_CHECK("fastgl_norm_fwd");
+    return FASTGL_OK;
+}
+
+}  // namespace
+}  // namespace fastgl
+
+using namespace fastgl;
+
+extern "C" {
+
+fastgl_status fastgl_norm_fwd(fastgl_dtype dtype, const void *X, const void *R, const float *w, int64_t M, int64_t F,
+                              float eps, const int64_t *rng, double p, void *sum_out, void *Y, float *rstd, void *stream)
+{
+    return norm_fwd(false, dtype, X, R, w, M, F, eps, rng, p, sum_out, Y, nullptr, rstd, (hipStream_t)stream);
+}
+
+fastgl_status fastgl_norm_fwd_e4m3(fastgl_dtype dtype, const void *X, const void *R, const float *w, int64_t M, int64_t F,
+                                   float eps, const int64_t *rng, double p, void *sum_out, uint8_t *Q, float *scale,
+                                   float *rstd, void *stream)
+{
+    return norm_fwd(true, dtype, X, R, w, M, F, eps, rng, p, sum_out, Q, scale, rstd, (hipStream_t)stream);
+}
+
+size_t fastgl_norm_bwd_workspace_bytes(int64_t M, int64_t F)
+{
+    if (M < 0 || F < 1 || M > kMaxIndex || F > (int64_t)1 << 24) return 0;
+    return align_up((size_t)bwd_groups(M, F) * (size_t)F * sizeof(float), 256);
+}
+
+fastgl_status fastgl_norm_bwd(fastgl_dtype dtype, const void *S, const float *w, const float *rstd, const void *dY,
+                              const void *dS, int64_t M, int64_t F, const int64_t *rng, double p, void *dX, void *dR,
+                              float *dw, void *workspace, size_t workspace_bytes, void *stream)
+{
+    NormBwdArgs a = {};
+    const fastgl_status st = check_rows(dtype, M, F, rng, p, &a.threshold, &a.drop_scale);
+    if (st != FASTGL_OK) return st;
+    const uintptr_t el = dtype == FASTGL_BF16 ? 2 : 4;
+    if (M > 0 && (!S || !w || !rstd || !dY)) {
+        set_error("S, w, rstd or dY is NULL");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (misaligned_to(S, el) || misaligned_to(dY, el) || misaligned_to(dS, el) || misaligned_to(dX, el) || misaligned_to(dR, el) ||
+        misaligned_to(w, 4) || misaligned_to(rstd, 4) || misaligned_to(dw, 4)) {
+        set_error("arrays must be aligned to their element size");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (dw && M > 0) {
+        if (!workspace || misaligned_to(workspace, 256)) {
+            set_error("workspace must be a 256-byte aligned device buffer");
+            return FASTGL_ERR_INVALID_ARG;
+        }
+        if (workspace_bytes < fastgl_norm_bwd_workspace_bytes(M, F)) {
+            set_error("workspace too small: %zu < %zu bytes", workspace_bytes, fastgl_norm_bwd_workspace_bytes(M, F));
+            return FASTGL_ERR_WORKSPACE;
+        }
+    }
+    if (!dX && !dR && !dw) return FASTGL_OK;
+    hipStream_t s = (hipStream_t)stream;
+    a.S = S; a.dY = dY; a.dS = dS;
+    a.w = w; a.rstd = rstd;
+    a.M = M; a.F = (int32_t)F;
+    a.inv_F = (float)(1.0 / (double)F);
+    a.rng = rng;
+    a.dX = dX; a.dR = dR;
+    a.part = dw ? (float *)workspace : nullptr;
+    const int64_t groups = bwd_groups(M, F);
+    if (M > 0) {
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kBlock), 0, s, a); };
+        auto typed = [&](auto bf16, auto drop) {
+            constexpr bool B = decltype(bf16)::value, D = decltype(drop)::value;
+            if (spread(F, [&](auto lg, auto nc) { go(k_norm_bwd<B, decltype(lg)::value, decltype(nc)::value, D>); })) return;
+            if (dX || dR) go(k_norm_bwd_wide<B, D>);
+            if (dw)
+                hipLaunchKernelGGL(k_norm_dw_wide<B>, dim3((unsigned)ceil_div(F, kBlock * kChunk), (unsigned)groups),
+                                   dim3(kBlock), 0, s, a);
+        };
+        auto both = [&](auto bf16) { p > 0.0 ? typed(bf16, std::true_type()) : typed(bf16, std::false_type()); };
+        if (dtype == FASTGL_BF16) both(std::true_type());
+        else both(std::false_type());
+        FASTGL_LAUNCH_CHECK("fastgl_norm_bwd");
+    }
+    if (dw) {
+        hipLaunchKernelGGL(k_norm_dw, dim3((unsigned)ceil_div(F, kReduceCols)), dim3(1024), 0, s, (const float *)workspace,
+                           (int32_t)(M > 0 ? groups : 0), (int32_t)F, dw);
+        FASTGL_LAUNCH_CHECK("fastgl_norm_bwd (dw)");
+    }
+    return FASTGL_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,158 @@
+// Device helpers of the row-wise kernels (norm, dropout): eight columns at a time, and the counter-based
+// generator that says which of them a dropout keeps.
+#pragma once
+#include "internal.h"
+
+namespace fastgl {
+
+constexpr int kChunk = 8;              // columns a lane holds at a time: one answer of the generator, 16 bytes of bf16
+
+// Philox 4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", SC 2011).
+// Key: the seed; counter: (block of eight columns, row, offset).  The mask is a function of these alone, so it is
+// computed again wherever it is needed and never stored, and does not depend on the launch or on the rows beside it.
+struct Philox {
+    uint32_t k0, k1, n2, n3;
+    __device__ __forceinline__ void load(const int64_t *state)      // the same address for every lane: scalar loads
+    {
+        const uint64_t seed = (uint64_t)state[0], offset = (uint64_t)state[1];
+        k0 = (uint32_t)seed;
+        k1 = (uint32_t)(seed >> 32);
+        n2 = (uint32_t)offset;
+        n3 = (uint32_t)(offset >> 32);
+    }
+    __device__ __forceinline__ void words(uint32_t block, uint32_t row, uint32_t (&w)[4]) const
+    {
+        uint32_t x0 = block, x1 = row, x2 = n2, x3 = n3, a = k0, b = k1;
+#pragma unroll
+        for (int r = 0; r < 10; ++r) {
+            const uint64_t p = (uint64_t)x0 * 0xD2511F53u, q = (uint64_t)x2 * 0xCD9E8D57u;
+            x0 = (uint32_t)(q >> 32) ^ x1 ^ a;
+            x1 = (uint32_t)q;
+            x2 = (uint32_t)(p >> 32) ^ x3 ^ b;
+            x3 = (uint32_t)p;
+            a += 0x9E3779B9u;
+            b += 0xBB67AE85u;
+        }
+        w[0] = x0;
+        w[1] = x1;
+        w[2] = x2;
+        w[3] = x3;
+    }
+};
+
+// Sixteen bits decide an element: kept where its half word is >= threshold = round(65536 p).  The probability is p to
+// 2^-17, and the scale 65536 / (65536 - threshold) is the reciprocal of the probability that is realised, so the
+// expectation is exact; 32 bits would cost twice the integer products, which is what bounds the generator.
+// What is dropped is 0 whatever it was (NaN and infinity too): a selection, not a product.
+__device__ __forceinline__ void drop8(float (&v)[8], const uint32_t (&w)[4], uint32_t threshold, float scale)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t h = j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xFFFFu;
+        v[j] = h >= threshold ? v[j] * scale : 0.f;
+    }
+}
+
+// Eight columns as they lie in memory, at any alignment to an element; columns from `left` on (left < 8 in a row's last
+// chunk) are neither read nor written, and read as 0.
+template <bool BF16>
+struct Chunk;
+
+template <>
+struct Chunk<true> {
+    typedef uint16_t elem;
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const uint16_t *p, int left)
+    {
+        if (left >= 8) {
+            const Words<2>::x4 q = *reinterpret_cast<const Words<2>::x4 *>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = q[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t x = 0;
+                if (2 * i < left) x = p[2 * i];
+                if (2 * i + 1 < left) x |= (uint32_t)p[2 * i + 1] << 16;
+                w[i] = x;
+            }
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    }
+    __device__ static __forceinline__ void store(uint16_t *p, const float (&v)[8], int left)
+    {
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            o[i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i]) |
+                   (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i + 1]) << 16;
+        if (left >= 8) {
+            *reinterpret_cast<Words<2>::x4 *>(p) = Words<2>::x4{o[0], o[1], o[2], o[3]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (j < left) p[j] = (uint16_t)(o[j >> 1] >> (16 * (j & 1)));
+        }
+    }
+};
+
+template <>
+struct Chunk<false> {
+    typedef float elem;
+    float w[8];
+    __device__ __forceinline__ void load(const float *p, int left)
+    {
+        if (left >= 8) {
+            const Words<4>::x4 a = *reinterpret_cast<const Words<4>::x4 *>(p), b = *reinterpret_cast<const Words<4>::x4 *>(p + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = __uint_as_float(a[i]);
+                w[i + 4] = __uint_as_float(b[i]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = j < left ? p[j] : 0.f;
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = w[j];
+    }
+    __device__ static __forceinline__ void store(float *p, const float (&v)[8], int left)
+    {
+        if (left >= 8) {
+            Words<4>::x4 a, b;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                a[i] = __float_as_uint(v[i]);
+                b[i] = __float_as_uint(v[i + 4]);
+            }
+            *reinterpret_cast<Words<4>::x4 *>(p) = a;
+            *reinterpret_cast<Words<4>::x4 *>(p + 4) = b;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (j < left) p[j] = v[j];
+        }
+    }
+};
+
+// Host side of a dropout probability: false where it is not in [0, 1].
+inline bool drop_constants(double p, uint32_t *threshold, float *scale)
+{
+    if (!(p >= 0.0 && p <= 1.0)) return false;
+    const double t = __builtin_nearbyint(65536.0 * p);
+    *threshold = (uint32_t)t;
+    *scale = t < 65536.0 ? (float)(65536.0 / (65536.0 - t)) : 0.f;
+    return true;
+}
+
+}  // namespace fastgl
