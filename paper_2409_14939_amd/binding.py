@@ -37,9 +37,11 @@ EXPORTS = [
     "fastgl_edge_workspace_bytes", "fastgl_edge_weight_grad", "fastgl_edge_softmax_fwd", "fastgl_edge_softmax_bwd",
     "fastgl_edge_softmax_long_row", "fastgl_edge_score_fwd", "fastgl_edge_score_bwd",
     "fastgl_norm_fwd", "fastgl_norm_fwd_e4m3", "fastgl_norm_bwd", "fastgl_norm_bwd_workspace_bytes", "fastgl_dropout",
-    "fastgl_gather_rows_e4m3",
+    "fastgl_gather_rows_e4m3", "fastgl_gated_fwd", "fastgl_gated_bwd", "fastgl_gated_fwd_workspace_bytes",
+    "fastgl_gated_bwd_workspace_bytes",
 ]
 MAX_REORDER_BATCHES = 64
+ACTS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
 IDMAP_MODES = {"ordered": 0, "fused": 1}
 
 
@@ -123,6 +125,12 @@ def lib() -> ctypes.CDLL:
         L.fastgl_norm_bwd.argtypes = [i32, p, p, p, p, p, i64, i64, p, f64, p, p, p, p, sz, p]
         L.fastgl_dropout.argtypes = [i32, p, p, i64, i64, p, f64, p, p]
         L.fastgl_gather_rows_e4m3.argtypes = [p, p, i64, p, i64, i64, i32, p, p]
+        L.fastgl_gated_fwd_workspace_bytes.argtypes = [i32, i64, i64, i64, i32]
+        L.fastgl_gated_fwd_workspace_bytes.restype = sz
+        L.fastgl_gated_bwd_workspace_bytes.argtypes = [i32, i64, i64, i64, i32]
+        L.fastgl_gated_bwd_workspace_bytes.restype = sz
+        L.fastgl_gated_fwd.argtypes = [i32, p, p, p, p, p, i64, i64, i64, i32, p, p, p, p, sz, p]
+        L.fastgl_gated_bwd.argtypes = [i32, p, p, p, p, p, p, i64, i64, i64, i32, p, p, p, p, p, p, sz, p]
         L.fastgl_idmap_table_slots.argtypes = [i64]
         L.fastgl_idmap_table_slots.restype = i64
         L.fastgl_idmap_workspace_bytes.argtypes = [i64, i64]
@@ -440,3 +448,31 @@ def fastgl_gather_rows_e4m3(table: torch.Tensor, scale: torch.Tensor, ids: torch
     """scale[ids] * table[ids] as "f32" or "bf16"; table torch.float8_e4m3fn with one float32 scale a row.  An ID
     outside the table gives a row of NaN."""
     return _native().gather_rows_e4m3(table, scale, ids, DTYPES[dtype], out)
+
+
+def fastgl_gated_fwd_workspace_bytes(dtype: str, M: int, K: int, N: int, aligned: bool = False) -> int:
+    return int(lib().fastgl_gated_fwd_workspace_bytes(DTYPES[dtype], M, K, N, int(aligned)))
+
+
+def fastgl_gated_bwd_workspace_bytes(dtype: str, M: int, K: int, N: int, aligned: bool = False) -> int:
+    return int(lib().fastgl_gated_bwd_workspace_bytes(DTYPES[dtype], M, K, N, int(aligned)))
+
+
+def fastgl_gated_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: Optional[torch.Tensor] = None,
+                     bu: Optional[torch.Tensor] = None, act: str = "silu", want_GU: bool = True,
+                     P: Optional[torch.Tensor] = None, G: Optional[torch.Tensor] = None, U: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None):
+    """(P, G, U): G = X Wg + bg, U = X Wu + bu, P = act(G) * U; act one of "silu", "gelu", "relu", "sigmoid".
+    want_GU=False leaves G and U (which the backward pass reads) unwritten and returns None for them."""
+    return _native().gated_fwd(X, Wg, Wu, bg, bu, ACTS[act], want_GU, P, G, U, workspace)
+
+
+def fastgl_gated_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G: torch.Tensor, U: torch.Tensor, dP: torch.Tensor,
+                     act: str = "silu", want=("dX", "dWg", "dWu", "dbg", "dbu"), dX: Optional[torch.Tensor] = None,
+                     dWg: Optional[torch.Tensor] = None, dWu: Optional[torch.Tensor] = None,
+                     dbg: Optional[torch.Tensor] = None, dbu: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None):
+    """(dX, dWg, dWu, dbg, dbu); parts not named in `want` (and not passed in) are None.  dX and the weight
+    gradients are of X's dtype, the bias gradients float32."""
+    return _native().gated_bwd(X, Wg, Wu, G, U, dP, ACTS[act], *(n in want for n in ("dX", "dWg", "dWu", "dbg", "dbu")),
+                               dX, dWg, dWu, dbg, dbu, workspace)

@@ -13,7 +13,7 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libfastgl_agg.so")
 HOST = os.path.join(HERE, "_host.so")
 SOURCES = ["api.hip", "bookkeeping.hip", "aggregate.hip", "update.hip", "update_narrow.hip", "update_rows.hip", "idmap.hip", "match.hip", "overlap.hip", "edge.hip",
-           "static_scratch.hip", "layer.hip", "norm.hip", "dropout.hip"]
+           "static_scratch.hip", "layer.hip", "norm.hip", "dropout.hip", "gated.hip"]
 
 
 def build_library(verbose: bool = False) -> str:

@@ -1,0 +1,640 @@
+// Gated feed-forward update, forward and backward (fastgl_gated.h has the formulas): what is around the products of
+// gated_tile.h.
+//
+//   forward   [operands packed] -> one product for G and U with the gate in its epilogue; few rows: k_gated_rows alone
+//   backward  k_gated_dz (dG, dU as the matrix cores take them, column sums) -> dX: one product over both halves
+//             -> dWg and dWu: one product over slabs of rows, partial sums added by k_gated_dw
+#include "gated_tile.h"
+#include "update_internal.h"
+
+namespace fastgl {
+namespace {
+
+constexpr int64_t kFewRows = 16;       // k_gated_rows up to here
+constexpr int kSumGroups = 2048;       // workgroups of the gradient of the gate
+constexpr int64_t kMostWidth = (int64_t)1 << 20;
+
+// x as three bf16 whose sum is x exactly (each rounding to nearest).
+__device__ __forceinline__ void pieces(float x, float (&p)[3])
+{
+    p[0] = (float)(__bf16)x;
+    const float r = x - p[0];
+    p[1] = (float)(__bf16)r;
+    p[2] = r - p[1];
+}
+
+// Eight columns into `planes` bf16 planes.
+template <int PLANES>
+__device__ __forceinline__ void store_planes(uint16_t *p, int64_t plane, const float (&v)[8])
+{
+    if constexpr (PLANES == 1) {
+        Chunk<true>::store(p, v, 8);
+    } else {
+        float q[3][8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float c[3];
+            pieces(v[j], c);
+            q[0][j] = c[0];
+            q[1][j] = c[1];
+            q[2][j] = c[2];
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i) Chunk<true>::store(p + i * plane, q[i], 8);
+    }
+}
+
+// ------------------------------------------------------------------------------------ packing
+// A matrix [rows][cols] as planes of bf16 with rows of ld elements, 0 beyond cols.
+template <bool BF16>
+__global__ __launch_bounds__(kBlock) void k_gated_pack(const void *src, int64_t rows, int32_t cols, int32_t ld, uint16_t *out)
+{
+    typedef typename Chunk<BF16>::elem T;
+    const int32_t chunks = ld / kChunk;
+    const int64_t n = rows * chunks;
+    for (int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x; u < n; u += (int64_t)gridDim.x * kBlock) {
+        const int64_t row = u / chunks;
+        const int col = (int)(u - row * chunks) * kChunk;
+        Chunk<BF16> c;
+        float v[8];
+        c.load(static_cast<const T *>(src) + row * cols + col, cols - col);
+        c.get(v);
+        store_planes<BF16 ? 1 : 3>(out + row * ld + col, rows * ld, v);
+    }
+}
+
+// ------------------------------------------------------------------------------------ few rows
+struct RowsArgs {
+    const void *X, *Wg, *Wu;
+    const float *bg, *bu;
+    void *P, *G, *U;
+    int32_t M, K, N, lg;             // 2^lg lanes of eight columns a strip
+};
+
+// MR rows of a strip of columns by one workgroup: every lane has eight columns of both weights and every n-th k; the sums
+// of a column are joined through the lanes of a wavefront, then through LDS, in a fixed order.
+template <bool BF16, int ACT, int MR>
+__global__ __launch_bounds__(kBlock) void k_gated_rows(RowsArgs a)
+{
+    typedef typename Chunk<BF16>::elem T;
+    const int lanes = 1 << a.lg, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int c = threadIdx.x & (lanes - 1), col = (int)(blockIdx.x * lanes + c) * kChunk, left = a.N - col;
+    const int m0 = blockIdx.y * MR;
+    const T *X = static_cast<const T *>(a.X), *Wg = static_cast<const T *>(a.Wg), *Wu = static_cast<const T *>(a.Wu);
+    float sg[MR][8], su[MR][8];
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sg[m][j] = su[m][j] = 0.f;
+    const int slots = kBlock >> a.lg;
+#pragma unroll 4
+    for (int k = threadIdx.x >> a.lg; k < a.K; k += slots) {
+        Chunk<BF16> qg, qu;
+        float g[8], u[8];
+        qg.load(Wg + (int64_t)k * a.N + col, left);
+        qu.load(Wu + (int64_t)k * a.N + col, left);
+        qg.get(g);
+        qu.get(u);
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+            const int row = m0 + m < a.M ? m0 + m : a.M - 1;
+            float x;
+            if constexpr (BF16) x = __uint_as_float((uint32_t)X[(int64_t)row * a.K + k] << 16);
+            else x = X[(int64_t)row * a.K + k];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sg[m][j] = fmaf(x, g[j], sg[m][j]);
+                su[m][j] = fmaf(x, u[j], su[m][j]);
+            }
+        }
+    }
+    __shared__ float sums[kBlock / kWave][MR][2][8 * 8];
+    for (int o = lanes; o < kWave; o <<= 1)
+#pragma unroll
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sg[m][j] += __shfl_xor(sg[m][j], o, kWave);
+                su[m][j] += __shfl_xor(su[m][j], o, kWave);
+            }
+    if (lane < lanes)
+#pragma unroll
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sums[wave][m][0][c * 8 + j] = sg[m][j];
+                sums[wave][m][1][c * 8 + j] = su[m][j];
+            }
+    __syncthreads();
+    for (int i = threadIdx.x; i < MR * lanes * 8; i += kBlock) {
+        const int m = i / (lanes * 8), j = i - m * lanes * 8, row = m0 + m;
+        const int64_t n = (int64_t)blockIdx.x * lanes * 8 + j;
+        if (row >= a.M || n >= a.N) continue;
+        float g = (sums[0][m][0][j] + sums[1][m][0][j]) + (sums[2][m][0][j] + sums[3][m][0][j]);
+        float u = (sums[0][m][1][j] + sums[1][m][1][j]) + (sums[2][m][1][j] + sums[3][m][1][j]);
+        if (a.bg) g += a.bg[n];
+        if (a.bu) u += a.bu[n];
+        const int64_t at = (int64_t)row * a.N + n;
+        auto put = [&](void *out, float v) {
+            if constexpr (BF16) static_cast<T *>(out)[at] = __builtin_bit_cast(uint16_t, (__bf16)v);
+            else static_cast<T *>(out)[at] = v;
+        };
+        put(a.P, gate<ACT, false>(g, nullptr) * u);
+        if (a.G) put(a.G, g);
+        if (a.U) put(a.U, u);
+    }
+}
+
+// ------------------------------------------------------------------------------------ gradient of the gate
+struct DzArgs {
+    const void *G, *U, *dP;
+    uint16_t *dG, *dU;               // planes [M][ld], or NULL
+    int64_t M, plane;
+    int32_t N, ld, lg;               // 2^lg lanes of eight columns a row
+    float *part;                     // [gridDim.y][2][N] column sums, or NULL
+};
+
+// dG = dP U act'(G), dU = dP act(G), rounded to what the matrix cores take (bf16, or three pieces); the column sums
+// are formed from the unrounded values.
+template <bool BF16, int ACT>
+__global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
+{
+    typedef typename Chunk<BF16>::elem T;
+    const int lanes = 1 << a.lg, c = threadIdx.x & (lanes - 1), rows = kBlock >> a.lg;
+    const int col = (int)(blockIdx.x * lanes + c) * kChunk, left = a.N - col;
+    const T *G = static_cast<const T *>(a.G), *U = static_cast<const T *>(a.U), *dP = static_cast<const T *>(a.dP);
+    float sg[8], su[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sg[j] = su[j] = 0.f;
+    if (left > 0) {
+        for (int64_t row = (int64_t)blockIdx.y * rows + (threadIdx.x >> a.lg); row < a.M; row += (int64_t)gridDim.y * rows) {
+            const int64_t at = row * a.N + col;
+            Chunk<BF16> qg, qu, qp;
+            float g[8], u[8], p[8];
+            qg.load(G + at, left);
+            qu.load(U + at, left);
+            qp.load(dP + at, left);
+            qg.get(g);
+            qu.get(u);
+            qp.get(p);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float grad;
+                const float v = gate<ACT, true>(g[j], &grad);
+                g[j] = p[j] * u[j] * grad;
+                u[j] = p[j] * v;
+                if (j >= left) g[j] = u[j] = 0.f;                  // padding
+                sg[j] += g[j];
+                su[j] += u[j];
+            }
+            if (a.dG) {
+                store_planes<BF16 ? 1 : 3>(a.dG + row * a.ld + col, a.plane, g);
+                store_planes<BF16 ? 1 : 3>(a.dU + row * a.ld + col, a.plane, u);
+            }
+        }
+    }
+    if (!a.part) return;
+    __shared__ float sums[2][kBlock * kChunk];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        sums[0][threadIdx.x * kChunk + j] = sg[j];
+        sums[1][threadIdx.x * kChunk + j] = su[j];
+    }
+    __syncthreads();
+    const int width = lanes * kChunk;
+    for (int i = threadIdx.x; i < 2 * width; i += kBlock) {
+        const int q = i >= width, j = i - q * width;
+        const int64_t n = (int64_t)blockIdx.x * width + j;
+        float v = 0.f;
+        for (int r = 0; r < rows; ++r) v += sums[q][r * width + j];
+        if (n < a.N) a.part[((int64_t)blockIdx.y * 2 + q) * a.N + n] = v;
+    }
+}
+
+// out[col] = sum of part[0 .. n)[col] in fp64 over 2 N columns: 16 columns a workgroup, a fixed order.
+__global__ __launch_bounds__(1024) void k_gated_db(const float *__restrict__ part, int32_t n, int32_t N, float *dbg, float *dbu)
+{
+    __shared__ double sums[64][17];
+    const int c = threadIdx.x % 16, s = threadIdx.x / 16;
+    const int64_t col = (int64_t)blockIdx.x * 16 + c;
+    double v = 0.0;
+    if (col < 2 * (int64_t)N) {
+#pragma unroll 8
+        for (int i = s; i < n; i += 64) v += (double)part[(int64_t)i * 2 * N + col];
+    }
+    sums[s][c] = v;
+    __syncthreads();
+    if (s == 0 && col < 2 * (int64_t)N) {
+        v = 0.0;
+        for (int i = 0; i < 64; ++i) v += sums[i][c];
+        float *out = col < N ? dbg : dbu;
+        if (out) out[col < N ? col : col - N] = (float)v;
+    }
+}
+
+// dW = sum over the slabs in fp64, in their order.
+template <bool BF16>
+__global__ __launch_bounds__(kBlock) void k_gated_dw(const float *__restrict__ part, int32_t slabs, int64_t stride, int64_t n, void *out)
+{
+    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (i >= n) return;
+    double v = 0.0;
+#pragma unroll 8
+    for (int s = 0; s < slabs; ++s) v += (double)part[(int64_t)s * stride + i];
+    if constexpr (BF16) static_cast<uint16_t *>(out)[i] = __builtin_bit_cast(uint16_t, (__bf16)(float)v);
+    else static_cast<float *>(out)[i] = (float)v;
+}
+
+// ------------------------------------------------------------------------------------ host side
+bool misaligned_to(const void *p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
+
+// Whether a product takes the tiles of 256 x 256 (else 128 x 128).
+bool large_tiles(int64_t tiles_large, int64_t slabs) { return tiles_large * slabs >= 192; }
+
+struct Slabs {
+    bool large;
+    int64_t rows, count;
+};
+
+// Slabs of rows for the weight gradients: enough tiles for the chip, and partial sums that cost less than they save.
+Slabs weight_slabs(int64_t M, int64_t K, int64_t N, int planes)
+{
+    Slabs best = {true, ceil_div(M > 0 ? M : 1, kStep) * kStep, 1};
+    double least = 1e300;
+    for (int large = 0; large < 2; ++large) {
+        const int64_t tile = large ? 256 : 128, slots = large ? 256 : 512;
+        const int64_t tiles = ceil_div(K, tile) * ceil_div(N, tile / 2);
+        for (int64_t want = 1; want <= 512; want = want < 16 ? want + 1 : want + want / 8) {
+            const int64_t rows = ceil_div(ceil_div(M > 0 ? M : 1, want), kStep) * kStep, count = ceil_div(M > 0 ? M : 1, rows);
+            const double step_us = (large ? 1.0 : 0.6) * (planes == 3 ? 6 : 1);
+            const double us = (double)ceil_div(tiles * count, slots) * ((double)(rows / kStep) * step_us + 4.0) +
+                              (count > 1 ? 2.0 + (double)count * (double)K * (double)N * 16.0 / 4e6 : 0.0);
+            if (us < least) {
+                least = us;
+                best = {large != 0, rows, count};
+            }
+        }
+    }
+    return best;
+}
+
+// Where a call's scratch lies; base NULL: only the size is wanted.
+struct Layout {
+    size_t used = 0;
+    char *base = nullptr;
+    template <class T>
+    T *take(size_t n)
+    {
+        char *p = base ? base + used : nullptr;
+        used += align_up(n * sizeof(T), 256);
+        return reinterpret_cast<T *>(p);
+    }
+};
+
+struct Shape {
+    bool bf16, aligned;
+    int planes;
+    int64_t M, K, N, ldk, ldn;
+    Shape(fastgl_dtype dtype, int64_t M_, int64_t K_, int64_t N_, bool aligned_)
+        : bf16(dtype == FASTGL_BF16), aligned(aligned_), planes(dtype == FASTGL_BF16 ? 1 : 3), M(M_), K(K_), N(N_),
+          ldk((int64_t)align_up((size_t)K_, 8)), ldn((int64_t)align_up((size_t)N_, 8))
+    {
+    }
+    bool pack_x() const { return !bf16 || !aligned || K % 8; }
+    bool pack_w() const { return !bf16 || !aligned || N % 8; }
+    // workgroups of k_gated_dz: (columns, rows); 2^lg lanes a row
+    int lg() const
+    {
+        int lg = 0;
+        while (lg < 5 && ((int64_t)8 << lg) < N) ++lg;
+        return lg;
+    }
+    int64_t dz_cols() const { return ceil_div(N, (int64_t)8 << lg()); }
+    int64_t dz_rows() const
+    {
+        const int64_t most = ceil_div(M, (int64_t)(kBlock >> lg()) * 4), some = ceil_div(kSumGroups, dz_cols() > 0 ? dz_cols() : 1);
+        return most < some ? (most > 0 ? most : 1) : some;
+    }
+};
+
+struct Scratch {
+    uint16_t *x, *wg, *wu, *dg, *du;
+    float *db, *dw;
+    int64_t dw_slab;
+};
+
+Scratch carve(const Shape &s, bool backward, Layout &l)
+{
+    Scratch o = {};
+    if (s.pack_x()) o.x = l.take<uint16_t>((size_t)(s.planes * s.M * s.ldk));
+    if (s.pack_w()) {
+        o.wg = l.take<uint16_t>((size_t)(s.planes * s.K * s.ldn));
+        o.wu = l.take<uint16_t>((size_t)(s.planes * s.K * s.ldn));
+    }
+    if (backward) {
+        o.dg = l.take<uint16_t>((size_t)(s.planes * s.M * s.ldn));
+        o.du = l.take<uint16_t>((size_t)(s.planes * s.M * s.ldn));
+        o.db = l.take<float>((size_t)(s.dz_rows() * 2 * s.N));
+        const Slabs b = weight_slabs(s.M, s.K, s.N, s.planes);
+        o.dw_slab = 2 * s.K * s.N;
+        if (b.count > 1) o.dw = l.take<float>((size_t)(b.count * o.dw_slab));
+    }
+    return o;
+}
+
+fastgl_status check(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, fastgl_act act)
+{
+    if (dtype != FASTGL_F32 && dtype != FASTGL_BF16) {
+        set_error("bad dtype %d", (int)dtype);
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if ((int)act < FASTGL_ACT_SILU || (int)act > FASTGL_ACT_SIGMOID) {
+        set_error("bad activation %d", (int)act);
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (M < 0 || K < 0 || N < 0) {
+        set_error("negative size (M=%lld K=%lld N=%lld)", (long long)M, (long long)K, (long long)N);
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (M > kMaxIndex || K > kMostWidth || N > kMostWidth) {
+        set_error("M must stay below 2^31-1-1024, K and N at 2^20 or below");
+        return FASTGL_ERR_UNSUPPORTED;
+    }
+    return FASTGL_OK;
+}
+
+fastgl_status check_workspace(const void *workspace, size_t bytes, size_t need)
+{
+    if (need == 0) return FASTGL_OK;
+    if (!workspace || misaligned_to(workspace, 256)) {
+        set_error("workspace must be a 256-byte aligned device buffer");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (bytes < need) {
+        set_error("workspace too small: %zu < %zu bytes", bytes, need);
+        return FASTGL_ERR_WORKSPACE;
+    }
+    return FASTGL_OK;
+}
+
+fastgl_status pack(const Shape &s, const void *src, int64_t rows, int64_t cols, int64_t ld, uint16_t *out, hipStream_t st)
+{
+    if (rows == 0 || cols == 0) return FASTGL_OK;
+    const int64_t blocks = ceil_div(rows * (ld / kChunk), kBlock);
+    const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, st, src, rows, (int32_t)cols, (int32_t)ld, out); };
+    if (s.bf16) go(k_gated_pack<true>);
+    else go(k_gated_pack<false>);
+    FASTGL_LAUNCH_CHECK("fastgl_gated (pack)");
+    return FASTGL_OK;
+}
+
+template <class F>
+void by_act(fastgl_act act, F f)
+{
+    switch (act) {
+        case FASTGL_ACT_SILU: f(std::integral_constant<int, FASTGL_ACT_SILU>()); break;
+        case FASTGL_ACT_GELU: f(std::integral_constant<int, FASTGL_ACT_GELU>()); break;
+        case FASTGL_ACT_RELU: f(std::integral_constant<int, FASTGL_ACT_RELU>()); break;
+        default: f(std::integral_constant<int, FASTGL_ACT_SIGMOID>()); break;
+    }
+}
+
+// One product.  `out32`: results in fp32 (else bf16).
+template <int MODE, class ACT>
+fastgl_status launch_tile(TileArgs g, bool large, bool out32, ACT, hipStream_t s, const char *what)
+{
+    constexpr int A = ACT::value;
+    const int64_t bm = large ? 256 : 128, bc = MODE == kRows ? bm : bm / 2;
+    const int64_t tr = ceil_div(g.R, bm), tc = ceil_div(g.C, bc), total = tr * tc * g.slabs;
+    if (total > 0x7FFFFFFFLL || 4 * tc > 0x7FFFFFFFLL) {
+        set_error("%s: too many tiles (%lld)", what, (long long)total);
+        return FASTGL_ERR_UNSUPPORTED;
+    }
+    g.tiles_r = (int32_t)tr;
+    g.tiles_c = (int32_t)tc;
+    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(threads), 0, s, g); };
+    if (large) {
+        if (out32) go(k_gated_tile<MODE, 8, float, A>, 512);
+        else go(k_gated_tile<MODE, 8, uint16_t, A>, 512);
+    } else {
+        if (out32) go(k_gated_tile<MODE, 4, float, A>, 256);
+        else go(k_gated_tile<MODE, 4, uint16_t, A>, 256);
+    }
+    FASTGL_LAUNCH_CHECK(what);
+    return FASTGL_OK;
+}
+
+bool starts_whole(std::initializer_list<const void *> ps)
+{
+    for (const void *p : ps)
+        if (misaligned_to(p, 16)) return false;
+    return true;
+}
+
+size_t workspace(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, bool aligned, bool backward)
+{
+    if (check(dtype, M, K, N, FASTGL_ACT_SILU) != FASTGL_OK) return 0;
+    if (!backward && M <= kFewRows) return 0;
+    Layout l;
+    carve(Shape(dtype, M, K, N, aligned), backward, l);
+    return l.used;
+}
+
+}  // namespace
+}  // namespace fastgl
+
+using namespace fastgl;
+
+extern "C" {
+
+size_t fastgl_gated_fwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned)
+{
+    return workspace(dtype, M, K, N, aligned != 0, false);
+}
+
+size_t fastgl_gated_bwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned)
+{
+    return workspace(dtype, M, K, N, aligned != 0, true);
+}
+
+fastgl_status fastgl_gated_fwd(fastgl_dtype dtype, const void *X, const void *Wg, const void *Wu, const float *bg,
+                               const float *bu, int64_t M, int64_t K, int64_t N, fastgl_act act, void *P, void *G, void *U,
+                               void *ws, size_t ws_bytes, void *stream)
+{
+    fastgl_status st = check(dtype, M, K, N, act);
+    if (st != FASTGL_OK) return st;
+    if (M == 0 || N == 0) return FASTGL_OK;
+    if (!P || (K > 0 && (!X || !Wg || !Wu))) {
+        set_error("X, Wg, Wu or P is NULL");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    const uintptr_t el = dtype == FASTGL_BF16 ? 2 : 4;
+    if (misaligned_to(X, el) || misaligned_to(Wg, el) || misaligned_to(Wu, el) || misaligned_to(P, el) || misaligned_to(G, el) ||
+        misaligned_to(U, el) || misaligned_to(bg, 4) || misaligned_to(bu, 4)) {
+        set_error("matrices must be aligned to their element size");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    hipStream_t s = (hipStream_t)stream;
+    if (M <= kFewRows) {
+        RowsArgs a = {X, Wg, Wu, bg, bu, P, G, U, (int32_t)M, (int32_t)K, (int32_t)N, 3};
+        while (a.lg > 0 && ceil_div(N, (int64_t)8 << a.lg) < 192) --a.lg;
+        const unsigned strips = (unsigned)ceil_div(N, (int64_t)8 << a.lg);
+        by_act(act, [&](auto A) {
+            constexpr int ACT = decltype(A)::value;
+            auto go = [&](auto kernel, int rows) { hipLaunchKernelGGL(kernel, dim3(strips, (unsigned)ceil_div(M, rows)), dim3(kBlock), 0, s, a); };
+            if (dtype == FASTGL_BF16) M == 1 ? go(k_gated_rows<true, ACT, 1>, 1) : go(k_gated_rows<true, ACT, 4>, 4);
+            else M == 1 ? go(k_gated_rows<false, ACT, 1>, 1) : go(k_gated_rows<false, ACT, 4>, 4);
+        });
+        FASTGL_LAUNCH_CHECK("fastgl_gated_fwd (few rows)");
+        return FASTGL_OK;
+    }
+    const Shape d(dtype, M, K, N, starts_whole({X, Wg, Wu}));
+    Layout l;
+    carve(d, false, l);
+    st = check_workspace(ws, ws_bytes, l.used);
+    if (st != FASTGL_OK) return st;
+    l = Layout();
+    l.base = (char *)ws;
+    const Scratch o = carve(d, false, l);
+    if (d.pack_x() && (st = pack(d, X, M, K, d.ldk, o.x, s)) != FASTGL_OK) return st;
+    if (d.pack_w()) {
+        if ((st = pack(d, Wg, K, N, d.ldn, o.wg, s)) != FASTGL_OK) return st;
+        if ((st = pack(d, Wu, K, N, d.ldn, o.wu, s)) != FASTGL_OK) return st;
+    }
+    TileArgs g = {};
+    g.a[0] = d.pack_x() ? o.x : (const uint16_t *)X;
+    g.b[0] = d.pack_w() ? o.wg : (const uint16_t *)Wg;
+    g.b[1] = d.pack_w() ? o.wu : (const uint16_t *)Wu;
+    g.a_plane = M * d.ldk; g.b_plane = K * d.ldn;
+    g.lda = d.ldk; g.ldb = d.ldn;
+    g.R = M; g.C = N; g.Kc = K;
+    g.pairs = d.bf16 ? 1 : 6; g.groups = 1; g.slabs = 1;
+    g.bias[0] = bg; g.bias[1] = bu;
+    g.out[0] = P; g.out[1] = G; g.out[2] = U;
+    const bool large = large_tiles(ceil_div(M, 256) * ceil_div(N, 128), 1);
+    by_act(act, [&](auto A) { st = launch_tile<kForward>(g, large, !d.bf16, A, s, "fastgl_gated_fwd"); });
+    return st;
+}
+
+fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg, const void *Wu, const void *G,
+                               const void *U, const void *dP, int64_t M, int64_t K, int64_t N, fastgl_act act, void *dX,
+                               void *dWg, void *dWu, float *dbg, float *dbu, void *ws, size_t ws_bytes, void *stream)
+{
+    fastgl_status st = check(dtype, M, K, N, act);
+    if (st != FASTGL_OK) return st;
+    const uintptr_t el = dtype == FASTGL_BF16 ? 2 : 4;
+    const bool want_x = dX && M > 0 && K > 0, want_w = (dWg || dWu) && K > 0 && N > 0, want_b = (dbg || dbu) && N > 0;
+    const bool terms = M > 0 && N > 0;
+    if (terms && (want_x || want_w || want_b) && (!G || !U || !dP)) {
+        set_error("G, U or dP is NULL");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (want_x && terms && (!Wg || !Wu)) {
+        set_error("dX needs Wg and Wu");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (want_w && terms && !X) {
+        set_error("dWg and dWu need X");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (misaligned_to(X, el) || misaligned_to(Wg, el) || misaligned_to(Wu, el) || misaligned_to(G, el) || misaligned_to(U, el) ||
+        misaligned_to(dP, el) || misaligned_to(dX, el) || misaligned_to(dWg, el) || misaligned_to(dWu, el) || misaligned_to(dbg, 4) ||
+        misaligned_to(dbu, 4)) {
+        set_error("matrices must be aligned to their element size");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    hipStream_t s = (hipStream_t)stream;
+    if (!terms) {                                     // sums without terms
+        const bool bf16 = dtype == FASTGL_BF16;
+        if (want_x && (st = launch_no_terms(bf16, dX, nullptr, M, K, false, s, "fastgl_gated_bwd (dX, N = 0)")) != FASTGL_OK) return st;
+        for (void *w : {dWg, dWu})
+            if (w && want_w && (st = launch_no_terms(bf16, w, nullptr, K, N, false, s, "fastgl_gated_bwd (dW, M = 0)")) != FASTGL_OK) return st;
+        for (float *b : {dbg, dbu})
+            if (b && want_b && (st = launch_no_terms(false, b, nullptr, 1, N, false, s, "fastgl_gated_bwd (db, M = 0)")) != FASTGL_OK) return st;
+        return FASTGL_OK;
+    }
+    if (!want_x && !want_w && !want_b) return FASTGL_OK;
+    const Shape d(dtype, M, K, N, starts_whole({want_w ? X : nullptr, want_x ? Wg : nullptr, want_x ? Wu : nullptr}));
+    Layout l;
+    carve(d, true, l);
+    st = check_workspace(ws, ws_bytes, l.used);
+    if (st != FASTGL_OK) return st;
+    l = Layout();
+    l.base = (char *)ws;
+    const Scratch o = carve(d, true, l);
+
+    DzArgs z = {};
+    z.G = G; z.U = U; z.dP = dP;
+    z.dG = want_x || want_w ? o.dg : nullptr;
+    z.dU = o.du;
+    z.M = M; z.plane = M * d.ldn;
+    z.N = (int32_t)N; z.ld = (int32_t)d.ldn; z.lg = d.lg();
+    z.part = want_b ? o.db : nullptr;
+    const dim3 dz((unsigned)d.dz_cols(), (unsigned)d.dz_rows());
+    by_act(act, [&](auto A) {
+        constexpr int ACT = decltype(A)::value;
+        if (d.bf16) hipLaunchKernelGGL((k_gated_dz<true, ACT>), dz, dim3(kBlock), 0, s, z);
+        else hipLaunchKernelGGL((k_gated_dz<false, ACT>), dz, dim3(kBlock), 0, s, z);
+    });
+    FASTGL_LAUNCH_CHECK("fastgl_gated_bwd (dG, dU)");
+    if (want_b) {
+        hipLaunchKernelGGL(k_gated_db, dim3((unsigned)ceil_div(2 * N, 16)), dim3(1024), 0, s, (const float *)o.db, (int32_t)dz.y,
+                           (int32_t)N, dbg, dbu);
+        FASTGL_LAUNCH_CHECK("fastgl_gated_bwd (db)");
+    }
+    const std::integral_constant<int, 0> none;
+    if (want_x) {
+        if (d.pack_w()) {
+            if ((st = pack(d, Wg, K, N, d.ldn, o.wg, s)) != FASTGL_OK) return st;
+            if ((st = pack(d, Wu, K, N, d.ldn, o.wu, s)) != FASTGL_OK) return st;
+        }
+        TileArgs g = {};
+        g.a[0] = o.dg; g.a[1] = o.du;
+        g.b[0] = d.pack_w() ? o.wg : (const uint16_t *)Wg;
+        g.b[1] = d.pack_w() ? o.wu : (const uint16_t *)Wu;
+        g.a_plane = M * d.ldn; g.b_plane = K * d.ldn;
+        g.lda = d.ldn; g.ldb = d.ldn;
+        g.R = M; g.C = K; g.Kc = N;
+        g.pairs = d.bf16 ? 1 : 6; g.groups = 2; g.slabs = 1;
+        g.out[0] = dX;
+        const bool large = large_tiles(ceil_div(M, 256) * ceil_div(K, 256), 1);
+        if ((st = launch_tile<kRows>(g, large, !d.bf16, none, s, "fastgl_gated_bwd (dX)")) != FASTGL_OK) return st;
+    }
+    if (want_w) {
+        if (d.pack_x() && (st = pack(d, X, M, K, d.ldk, o.x, s)) != FASTGL_OK) return st;
+        const Slabs b = weight_slabs(M, K, N, d.planes);
+        TileArgs g = {};
+        g.a[0] = d.pack_x() ? o.x : (const uint16_t *)X;
+        g.b[0] = o.dg; g.b[1] = o.du;
+        g.a_plane = M * d.ldk; g.b_plane = M * d.ldn;
+        g.lda = d.ldk; g.ldb = d.ldn;
+        g.R = K; g.C = N; g.Kc = M;
+        g.pairs = d.bf16 ? 1 : 6; g.groups = 1;
+        g.slab = b.rows; g.slabs = (int32_t)b.count;
+        if (b.count > 1) {
+            g.out[0] = dWg ? o.dw : nullptr;
+            g.out[1] = dWu ? o.dw + K * N : nullptr;
+            g.out_slab = o.dw_slab;
+        } else {
+            g.out[0] = dWg;
+            g.out[1] = dWu;
+        }
+        if ((st = launch_tile<kWeights>(g, b.large, !d.bf16 || b.count > 1, none, s, "fastgl_gated_bwd (dW)")) != FASTGL_OK) return st;
+        if (b.count > 1) {
+            const int64_t n = K * N;
+            for (int q = 0; q < 2; ++q) {
+                void *out = q ? dWu : dWg;
+                if (!out) continue;
+                const float *part = o.dw + q * n;
+                const dim3 grid((unsigned)ceil_div(n, kBlock));
+                if (d.bf16) hipLaunchKernelGGL(k_gated_dw<true>, grid, dim3(kBlock), 0, s, part, (int32_t)b.count, o.dw_slab, n, out);
+                else hipLaunchKernelGGL(k_gated_dw<false>, grid, dim3(kBlock), 0, s, part, (int32_t)b.count, o.dw_slab, n, out);
+                FASTGL_LAUNCH_CHECK("fastgl_gated_bwd (sum of slabs)");
+            }
+        }
+    }
+    return FASTGL_OK;
+}
+
+}  // extern "C"

@@ -23,6 +23,7 @@
 
 #include "fastgl_agg.h"
 #include "fastgl_edge.h"
+#include "fastgl_gated.h"
 #include "fastgl_idmap.h"
 #include "fastgl_match.h"
 #include "fastgl_norm.h"
@@ -758,6 +759,77 @@ PyObject *gather_rows_e4m3(PyObject *const *a)
     return wrap(out.t);
 }
 
+// ---------------------------------------------------------------------------- gated feed-forward
+const at::Tensor &matrix2(PyObject *o, at::ScalarType type, int64_t rows, int64_t cols, const char *name)
+{
+    const at::Tensor &t = dev(o, type, name);
+    if (!shape2(t, rows, cols)) {
+        PyErr_Format(PyExc_ValueError, "%s must be [%lld, %lld]", name, (long long)rows, (long long)cols);
+        throw Raised{};
+    }
+    return t;
+}
+
+int whole(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+// (X, Wg, Wu, bg, bu, act, want_GU, P, G, U, workspace) -> (P, G, U)
+PyObject *gated_fwd(PyObject *const *a)
+{
+    const at::Tensor &X = features2(a[0], "X");
+    const auto type = X.scalar_type();
+    const int64_t M = X.size(0), K = X.size(1);
+    const at::Tensor &Wg = dev(a[1], type, "Wg");
+    if (Wg.dim() != 2 || Wg.size(0) != K) fail(PyExc_ValueError, "Wg must be [K, N]");
+    const int64_t N = Wg.size(1);
+    const at::Tensor &Wu = matrix2(a[2], type, K, N, "Wu");
+    const float *bg = none(a[3]) ? nullptr : vector_f32(a[3], N, "bg"), *bu = none(a[4]) ? nullptr : vector_f32(a[4], N, "bu");
+    const auto act = (fastgl_act)integer(a[5]);
+    const bool want = truth(a[6]);
+    const Out P = out_of(a[7], type, {M, N}, X, "P");
+    Out G, U;
+    if (want || !none(a[8])) G = out_of(a[8], type, {M, N}, X, "G");
+    if (want || !none(a[9])) U = out_of(a[9], type, {M, N}, X, "U");
+    const fastgl_dtype dt = feat_dtype(X);
+    const Scratch ws(a[10], X, [&] {
+        return fastgl_gated_fwd_workspace_bytes(dt, M, K, N, whole(X.data_ptr()) && whole(Wg.data_ptr()) && whole(Wu.data_ptr()));
+    });
+    run([&](void *s) {
+        return fastgl_gated_fwd(dt, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), bg, bu, M, K, N, act, P.p(), G.p(), U.p(), ws.p(),
+                                ws.n(), s);
+    });
+    return tuple({P.t, G.t, U.t});
+}
+
+// (X, Wg, Wu, G, U, dP, act, want_dX, want_dWg, want_dWu, want_dbg, want_dbu, dX, dWg, dWu, dbg, dbu, workspace)
+// -> (dX, dWg, dWu, dbg, dbu)
+PyObject *gated_bwd(PyObject *const *a)
+{
+    const at::Tensor &X = features2(a[0], "X");
+    const auto type = X.scalar_type();
+    const int64_t M = X.size(0), K = X.size(1);
+    const at::Tensor &Wg = dev(a[1], type, "Wg");
+    if (Wg.dim() != 2 || Wg.size(0) != K) fail(PyExc_ValueError, "Wg must be [K, N]");
+    const int64_t N = Wg.size(1);
+    const at::Tensor &Wu = matrix2(a[2], type, K, N, "Wu"), &G = matrix2(a[3], type, M, N, "G"), &U = matrix2(a[4], type, M, N, "U");
+    const at::Tensor &dP = matrix2(a[5], type, M, N, "dP");
+    const auto act = (fastgl_act)integer(a[6]);
+    Out dX, dWg, dWu, dbg, dbu;
+    if (truth(a[7]) || !none(a[12])) dX = out_of(a[12], type, {M, K}, X, "dX");
+    if (truth(a[8]) || !none(a[13])) dWg = out_of(a[13], type, {K, N}, X, "dWg");
+    if (truth(a[9]) || !none(a[14])) dWu = out_of(a[14], type, {K, N}, X, "dWu");
+    if (truth(a[10]) || !none(a[15])) dbg = out_of(a[15], at::kFloat, {N}, X, "dbg");
+    if (truth(a[11]) || !none(a[16])) dbu = out_of(a[16], at::kFloat, {N}, X, "dbu");
+    const fastgl_dtype dt = feat_dtype(X);
+    const Scratch ws(a[17], X, [&] {
+        return fastgl_gated_bwd_workspace_bytes(dt, M, K, N, whole(X.data_ptr()) && whole(Wg.data_ptr()) && whole(Wu.data_ptr()));
+    });
+    run([&](void *s) {
+        return fastgl_gated_bwd(dt, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), G.data_ptr(), U.data_ptr(), dP.data_ptr(), M, K, N,
+                                act, dX.p(), dWg.p(), dWu.p(), (float *)dbg.p(), (float *)dbu.p(), ws.p(), ws.n(), s);
+    });
+    return tuple({dX.t, dWg.t, dWu.t, dbg.t, dbu.t});
+}
+
 // (error class): called once by binding.py
 PyObject *set_error_class(PyObject *const *a)
 {
@@ -773,7 +845,7 @@ PyMethodDef g_methods[] = {
     FN(update_fwd, 5), FN(layer_fwd, 14), FN(update_bwd, 12), FN(idmap, 7), FN(match, 7), FN(assemble_rows, 5),
     FN(overlap_counts, 3), FN(edge_weight_grad, 9), FN(edge_softmax_fwd, 4), FN(edge_softmax_bwd, 5),
     FN(edge_score_fwd, 6), FN(edge_score_bwd, 11), FN(norm_fwd, 13), FN(norm_bwd, 14), FN(dropout, 5),
-    FN(gather_rows_e4m3, 5), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
+    FN(gather_rows_e4m3, 5), FN(gated_fwd, 11), FN(gated_bwd, 18), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
 #undef FN
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host", "Native marshalling of the C ABI's calls.", -1, g_methods,
