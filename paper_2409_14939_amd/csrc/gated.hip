@@ -3,7 +3,8 @@
 //
 //   forward   [operands packed] -> one product for G and U with the gate in its epilogue; few rows: k_gated_rows alone
 //   backward  k_gated_dz (dG, dU as the matrix cores take them, column sums) -> dX: one product over both halves
-//             -> dWg and dWu: one product over slabs of rows, partial sums added by k_gated_dw
+//             -> dWg and dWu: one product
+//   where a product has few tiles, its steps are dealt to several workgroups a tile, whose sums are added in fp64 afterwards
 #include "gated_tile.h"
 #include "update_internal.h"
 
@@ -232,9 +233,9 @@ __global__ __launch_bounds__(1024) void k_gated_db(const float *__restrict__ par
     }
 }
 
-// dW = sum over the slabs in fp64, in their order.
+// out = sum over the slabs in fp64, in their order.
 template <bool BF16>
-__global__ __launch_bounds__(kBlock) void k_gated_dw(const float *__restrict__ part, int32_t slabs, int64_t stride, int64_t n, void *out)
+__global__ __launch_bounds__(kBlock) void k_gated_sum(const float *__restrict__ part, int32_t slabs, int64_t stride, int64_t n, void *out)
 {
     const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     if (i >= n) return;
@@ -245,33 +246,59 @@ __global__ __launch_bounds__(kBlock) void k_gated_dw(const float *__restrict__ p
     else static_cast<float *>(out)[i] = (float)v;
 }
 
+// The forward pass's slabs: sums, biases and the gate.
+template <bool BF16, int ACT>
+__global__ __launch_bounds__(kBlock) void k_gated_join(const float *__restrict__ part, int32_t slabs, int64_t n, int32_t N, const float *bg,
+                                                       const float *bu, void *P, void *G, void *U)
+{
+    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (i >= n) return;
+    const int c = (int)(i % N);
+    double sg = bg ? (double)bg[c] : 0.0, su = bu ? (double)bu[c] : 0.0;
+#pragma unroll 4
+    for (int s = 0; s < slabs; ++s) {
+        sg += (double)part[(int64_t)(2 * s) * n + i];
+        su += (double)part[(int64_t)(2 * s + 1) * n + i];
+    }
+    const float g = (float)sg, u = (float)su;
+    auto put = [&](void *out, float v) {
+        if constexpr (BF16) static_cast<uint16_t *>(out)[i] = __builtin_bit_cast(uint16_t, (__bf16)v);
+        else static_cast<float *>(out)[i] = v;
+    };
+    put(P, gate<ACT, false>(g, nullptr) * u);
+    if (G) put(G, g);
+    if (U) put(U, u);
+}
+
 // ------------------------------------------------------------------------------------ host side
 bool misaligned_to(const void *p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
 
-// Whether a product takes the tiles of 256 x 256 (else 128 x 128).
-bool large_tiles(int64_t tiles_large, int64_t slabs) { return tiles_large * slabs >= 192; }
-
-struct Slabs {
-    bool large;
-    int64_t rows, count;
+// The tile of a product and how many workgroups share the steps of one.
+struct Cut {
+    int size;
+    int64_t slabs;
 };
 
-// Slabs of rows for the weight gradients: enough tiles for the chip, and partial sums that cost less than they save.
-Slabs weight_slabs(int64_t M, int64_t K, int64_t N, int planes)
+// The cut that a model of the launch finds fastest: workgroups run in rounds of one (large tiles) or two a compute unit, a
+// workgroup costs its steps and a fixed part, and slabs cost the sums that they write and that are read again.
+Cut cut_of(int mode, int64_t R, int64_t C, int64_t Kc, int64_t segments)
 {
-    Slabs best = {true, ceil_div(M > 0 ? M : 1, kStep) * kStep, 1};
+    Cut best = {kLarge, 1};
     double least = 1e300;
-    for (int large = 0; large < 2; ++large) {
-        const int64_t tile = large ? 256 : 128, slots = large ? 256 : 512;
-        const int64_t tiles = ceil_div(K, tile) * ceil_div(N, tile / 2);
-        for (int64_t want = 1; want <= 512; want = want < 16 ? want + 1 : want + want / 8) {
-            const int64_t rows = ceil_div(ceil_div(M > 0 ? M : 1, want), kStep) * kStep, count = ceil_div(M > 0 ? M : 1, rows);
-            const double step_us = (large ? 1.0 : 0.6) * (planes == 3 ? 6 : 1);
-            const double us = (double)ceil_div(tiles * count, slots) * ((double)(rows / kStep) * step_us + 4.0) +
-                              (count > 1 ? 2.0 + (double)count * (double)K * (double)N * 16.0 / 4e6 : 0.0);
+    const int64_t all = ceil_div(Kc, kStep) * segments;
+    for (int size = kLarge; size <= kSmall; ++size) {
+        static const char *only = getenv("GSIZE");
+        if (only && atoi(only) != size) continue;
+        const int64_t bm = size == kLarge ? 256 : 128, bc = (size == kSmall ? 128 : 256) / (mode == kRows ? 1 : 2);
+        const int64_t tiles = ceil_div(R, bm) * ceil_div(C, bc), slots = size == kLarge ? 256 : 512;
+        const double step_us = size == kLarge ? 0.85 : size == kMiddle ? 0.95 : 0.6;
+        for (int64_t slabs = 1; slabs <= 64 && (slabs == 1 || all / slabs >= 4); slabs = slabs < 8 ? slabs + 1 : slabs * 5 / 4) {
+            const double rounds = (double)ceil_div(tiles * slabs, slots);
+            const double us = rounds * ((double)ceil_div(all, slabs) * step_us + 4.0) +
+                              (slabs > 1 ? 4.0 + (double)slabs * (double)R * (double)C * (mode == kRows ? 8.0 : 16.0) / 4e6 : 0.0);
             if (us < least) {
                 least = us;
-                best = {large != 0, rows, count};
+                best = {size, slabs};
             }
         }
     }
@@ -302,6 +329,10 @@ struct Shape {
     }
     bool pack_x() const { return !bf16 || !aligned || K % 8; }
     bool pack_w() const { return !bf16 || !aligned || N % 8; }
+    int64_t pairs() const { return bf16 ? 1 : 6; }
+    Cut forward_cut() const { return cut_of(kForward, M, N, K, pairs()); }
+    Cut rows_cut() const { return cut_of(kRows, M, K, N, 2 * pairs()); }
+    Cut weights_cut() const { return cut_of(kWeights, K, N, M, pairs()); }
     // workgroups of k_gated_dz: (columns, rows); 2^lg lanes a row
     int lg() const
     {
@@ -319,8 +350,7 @@ struct Shape {
 
 struct Scratch {
     uint16_t *x, *wg, *wu, *dg, *du;
-    float *db, *dw;
-    int64_t dw_slab;
+    float *db, *part;                // part: of one product at a time
 };
 
 Scratch carve(const Shape &s, bool backward, Layout &l)
@@ -331,14 +361,15 @@ Scratch carve(const Shape &s, bool backward, Layout &l)
         o.wg = l.take<uint16_t>((size_t)(s.planes * s.K * s.ldn));
         o.wu = l.take<uint16_t>((size_t)(s.planes * s.K * s.ldn));
     }
+    auto sums = [](const Cut &c, int64_t n) { return c.slabs > 1 ? (size_t)(c.slabs * n) : (size_t)0; };
     if (backward) {
         o.dg = l.take<uint16_t>((size_t)(s.planes * s.M * s.ldn));
         o.du = l.take<uint16_t>((size_t)(s.planes * s.M * s.ldn));
         o.db = l.take<float>((size_t)(s.dz_rows() * 2 * s.N));
-        const Slabs b = weight_slabs(s.M, s.K, s.N, s.planes);
-        o.dw_slab = 2 * s.K * s.N;
-        if (b.count > 1) o.dw = l.take<float>((size_t)(b.count * o.dw_slab));
-    }
+        const size_t x = sums(s.rows_cut(), s.M * s.K), w = sums(s.weights_cut(), 2 * s.K * s.N);
+        o.part = l.take<float>(x > w ? x : w);
+    } else
+        o.part = l.take<float>(sums(s.forward_cut(), 2 * s.M * s.N));
     return o;
 }
 
@@ -400,27 +431,39 @@ void by_act(fastgl_act act, F f)
     }
 }
 
-// One product.  `out32`: results in fp32 (else bf16).
+// One product: results in bf16 or fp32, or sums of slabs.
 template <int MODE, class ACT>
-fastgl_status launch_tile(TileArgs g, bool large, bool out32, ACT, hipStream_t s, const char *what)
+fastgl_status launch_tile(TileArgs g, const Cut &cut, bool bf16, ACT, hipStream_t s, const char *what)
 {
     constexpr int A = ACT::value;
-    const int64_t bm = large ? 256 : 128, bc = MODE == kRows ? bm : bm / 2;
-    const int64_t tr = ceil_div(g.R, bm), tc = ceil_div(g.C, bc), total = tr * tc * g.slabs;
+    const int64_t bm = cut.size == kLarge ? 256 : 128, bc = (cut.size == kSmall ? 128 : 256) / (MODE == kRows ? 1 : 2);
+    const int64_t tr = ceil_div(g.R, bm), tc = ceil_div(g.C, bc), total = tr * tc * cut.slabs;
     if (total > 0x7FFFFFFFLL || 4 * tc > 0x7FFFFFFFLL) {
         set_error("%s: too many tiles (%lld)", what, (long long)total);
         return FASTGL_ERR_UNSUPPORTED;
     }
     g.tiles_r = (int32_t)tr;
     g.tiles_c = (int32_t)tc;
-    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(threads), 0, s, g); };
-    if (large) {
-        if (out32) go(k_gated_tile<MODE, 8, float, A>, 512);
-        else go(k_gated_tile<MODE, 8, uint16_t, A>, 512);
-    } else {
-        if (out32) go(k_gated_tile<MODE, 4, float, A>, 256);
-        else go(k_gated_tile<MODE, 4, uint16_t, A>, 256);
-    }
+    g.slabs = (int32_t)cut.slabs;
+    auto sized = [&](auto size) {
+        constexpr int S = decltype(size)::value;
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(Tile<MODE, S>::THREADS), 0, s, g); };
+        if (cut.slabs > 1) go(k_gated_tile<MODE, S, float, 0, true>);
+        else if (bf16) go(k_gated_tile<MODE, S, uint16_t, A, false>);
+        else go(k_gated_tile<MODE, S, float, A, false>);
+    };
+    if (cut.size == kLarge) sized(std::integral_constant<int, kLarge>());
+    else if (cut.size == kMiddle) sized(std::integral_constant<int, kMiddle>());
+    else sized(std::integral_constant<int, kSmall>());
+    FASTGL_LAUNCH_CHECK(what);
+    return FASTGL_OK;
+}
+
+fastgl_status sum_slabs(const float *part, const Cut &cut, int64_t stride, int64_t n, bool bf16, void *out, hipStream_t s, const char *what)
+{
+    const dim3 grid((unsigned)ceil_div(n, kBlock));
+    if (bf16) hipLaunchKernelGGL(k_gated_sum<true>, grid, dim3(kBlock), 0, s, part, (int32_t)cut.slabs, stride, n, out);
+    else hipLaunchKernelGGL(k_gated_sum<false>, grid, dim3(kBlock), 0, s, part, (int32_t)cut.slabs, stride, n, out);
     FASTGL_LAUNCH_CHECK(what);
     return FASTGL_OK;
 }
@@ -509,12 +552,24 @@ fastgl_status fastgl_gated_fwd(fastgl_dtype dtype, const void *X, const void *Wg
     g.a_plane = M * d.ldk; g.b_plane = K * d.ldn;
     g.lda = d.ldk; g.ldb = d.ldn;
     g.R = M; g.C = N; g.Kc = K;
-    g.pairs = d.bf16 ? 1 : 6; g.groups = 1; g.slabs = 1;
+    g.pairs = (int32_t)d.pairs(); g.groups = 1;
     g.bias[0] = bg; g.bias[1] = bu;
     g.out[0] = P; g.out[1] = G; g.out[2] = U;
-    const bool large = large_tiles(ceil_div(M, 256) * ceil_div(N, 128), 1);
-    by_act(act, [&](auto A) { st = launch_tile<kForward>(g, large, !d.bf16, A, s, "fastgl_gated_fwd"); });
-    return st;
+    g.part = o.part;
+    const Cut cut = d.forward_cut();
+    by_act(act, [&](auto A) { st = launch_tile<kForward>(g, cut, d.bf16, A, s, "fastgl_gated_fwd"); });
+    if (st != FASTGL_OK || cut.slabs == 1) return st;
+    by_act(act, [&](auto A) {
+        constexpr int ACT = decltype(A)::value;
+        const dim3 grid((unsigned)ceil_div(M * N, kBlock));
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, s, (const float *)o.part, (int32_t)cut.slabs, M * N, (int32_t)N, bg, bu, P, G, U);
+        };
+        if (d.bf16) go(k_gated_join<true, ACT>);
+        else go(k_gated_join<false, ACT>);
+    });
+    FASTGL_LAUNCH_CHECK("fastgl_gated_fwd (sum of slabs)");
+    return FASTGL_OK;
 }
 
 fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg, const void *Wu, const void *G,
@@ -596,43 +651,32 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
         g.a_plane = M * d.ldn; g.b_plane = K * d.ldn;
         g.lda = d.ldn; g.ldb = d.ldn;
         g.R = M; g.C = K; g.Kc = N;
-        g.pairs = d.bf16 ? 1 : 6; g.groups = 2; g.slabs = 1;
+        g.pairs = (int32_t)d.pairs(); g.groups = 2;
         g.out[0] = dX;
-        const bool large = large_tiles(ceil_div(M, 256) * ceil_div(K, 256), 1);
-        if ((st = launch_tile<kRows>(g, large, !d.bf16, none, s, "fastgl_gated_bwd (dX)")) != FASTGL_OK) return st;
+        g.part = o.part;
+        const Cut cut = d.rows_cut();
+        if ((st = launch_tile<kRows>(g, cut, d.bf16, none, s, "fastgl_gated_bwd (dX)")) != FASTGL_OK) return st;
+        if (cut.slabs > 1 && (st = sum_slabs(o.part, cut, M * K, M * K, d.bf16, dX, s, "fastgl_gated_bwd (dX, sum of slabs)")) != FASTGL_OK) return st;
     }
     if (want_w) {
         if (d.pack_x() && (st = pack(d, X, M, K, d.ldk, o.x, s)) != FASTGL_OK) return st;
-        const Slabs b = weight_slabs(M, K, N, d.planes);
         TileArgs g = {};
         g.a[0] = d.pack_x() ? o.x : (const uint16_t *)X;
         g.b[0] = o.dg; g.b[1] = o.du;
         g.a_plane = M * d.ldk; g.b_plane = M * d.ldn;
         g.lda = d.ldk; g.ldb = d.ldn;
         g.R = K; g.C = N; g.Kc = M;
-        g.pairs = d.bf16 ? 1 : 6; g.groups = 1;
-        g.slab = b.rows; g.slabs = (int32_t)b.count;
-        if (b.count > 1) {
-            g.out[0] = dWg ? o.dw : nullptr;
-            g.out[1] = dWu ? o.dw + K * N : nullptr;
-            g.out_slab = o.dw_slab;
-        } else {
-            g.out[0] = dWg;
-            g.out[1] = dWu;
-        }
-        if ((st = launch_tile<kWeights>(g, b.large, !d.bf16 || b.count > 1, none, s, "fastgl_gated_bwd (dW)")) != FASTGL_OK) return st;
-        if (b.count > 1) {
-            const int64_t n = K * N;
+        g.pairs = (int32_t)d.pairs(); g.groups = 1;
+        g.out[0] = dWg; g.out[1] = dWu;
+        g.part = o.part;
+        const Cut cut = d.weights_cut();
+        if ((st = launch_tile<kWeights>(g, cut, d.bf16, none, s, "fastgl_gated_bwd (dW)")) != FASTGL_OK) return st;
+        if (cut.slabs > 1)
             for (int q = 0; q < 2; ++q) {
                 void *out = q ? dWu : dWg;
-                if (!out) continue;
-                const float *part = o.dw + q * n;
-                const dim3 grid((unsigned)ceil_div(n, kBlock));
-                if (d.bf16) hipLaunchKernelGGL(k_gated_dw<true>, grid, dim3(kBlock), 0, s, part, (int32_t)b.count, o.dw_slab, n, out);
-                else hipLaunchKernelGGL(k_gated_dw<false>, grid, dim3(kBlock), 0, s, part, (int32_t)b.count, o.dw_slab, n, out);
-                FASTGL_LAUNCH_CHECK("fastgl_gated_bwd (sum of slabs)");
+                if (out && (st = sum_slabs(o.part + q * K * N, cut, 2 * K * N, K * N, d.bf16, out, s, "fastgl_gated_bwd (dW, sum of slabs)")) != FASTGL_OK)
+                    return st;
             }
-        }
     }
     return FASTGL_OK;
 }

@@ -2,15 +2,15 @@
 //
 //   FORWARD  G, U [R,C]    = A [R,Kc] B0, B1 [Kc,C]         and the gate in the epilogue
 //   ROWS     dX   [R,C]    = sum over groups of A [R,Kc] B [C,Kc]^T
-//   WEIGHTS  dWg, dWu [R,C] = A [Kc,R]^T B0, B1 [Kc,C]       contracted range cut into slabs
+//   WEIGHTS  dWg, dWu [R,C] = A [Kc,R]^T B0, B1 [Kc,C]
 //
 // All operands are bf16 with rows of a multiple of 16 bytes; fp32 operands come as three planes of pieces, and a
 // product of two such is a sequence of six segments, each a product of one plane of either.
 //
-// * A tile is 256 x 256 (eight wavefronts, 64 x 128 each) or 128 x 128 (four, 64 x 64): of two results, half the
-//   columns each, so that a lane holds G and U of the same elements.  Contracted 64 at a time through two LDS buffers.
+// * A wavefront has 64 rows and 128 (or 64) columns of a tile: of two results, half the columns each, so that a lane
+//   holds G and U of the same elements.  Contracted 32 at a time through a ring of LDS buffers.
 // * Operands go from memory to LDS without passing registers (16 bytes a lane).  An operand whose contracted
-//   index is contiguous lies as [row][64], read 16 bytes a lane; one whose other index is contiguous lies as [64][column] and is
+//   index is contiguous lies as [row][32], read 16 bytes a lane; one whose other index is contiguous lies as [32][column] and is
 //   turned on its way out of LDS by the transposing reads.  The 16-byte pieces of a row are permuted (by the addresses they
 //   are loaded from) so that the lanes of a read meet different banks.
 // * Buffer resources end the operands: what lies beyond is read as 0.  A row's last pieces beyond the contracted
@@ -33,9 +33,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 enum TileMode { kForward = 0, kRows = 1, kWeights = 2 };
 
-constexpr int kStep = 64;                       // contracted elements of an LDS buffer
+constexpr int kStep = 32;                       // contracted elements of an LDS buffer
 constexpr uint32_t kNoSuchOffset = 0x7FFFFF00u; // beyond every buffer
-constexpr int64_t kMostRecords = 0x7FFF0000;
 constexpr int kTileRsrc = 0x00020000;
 
 struct TileArgs {
@@ -44,12 +43,10 @@ struct TileArgs {
     int64_t lda, ldb;              // elements between rows, multiples of 8; contiguous contracted elements are 0 from Kc to there
     int64_t R, C, Kc;
     int32_t pairs, groups;         // segments: groups x pairs; pairs is 1 (bf16) or 6 (three planes)
-    int64_t slab;                  // WEIGHTS: contracted elements of a slab, a multiple of kStep
-    int32_t tiles_r, tiles_c, slabs;
+    int32_t tiles_r, tiles_c, slabs;      // slabs: the steps of all segments are dealt to as many workgroups a tile
     const float *bias[2];          // FORWARD, or NULL
-    int32_t act;
-    void *out[3];                  // FORWARD: P, G, U (G, U or NULL); ROWS: dX; WEIGHTS: dWg, dWu, or their partial sums
-    int64_t out_slab;              // WEIGHTS with partial sums: elements between those of two slabs
+    void *out[3];                  // FORWARD: P, G, U (G, U or NULL); ROWS: dX; WEIGHTS: dWg, dWu
+    float *part;                   // slabs > 1: their sums, [slab][results][R][C]
 };
 
 // Segment i of six: the planes of A and of B, smallest products first.
@@ -89,35 +86,42 @@ __device__ __forceinline__ float gate(float g, float *grad)
     }
 }
 
-template <int MODE, int NW>
+// Tiles: rows, columns (of all results together), wavefronts, LDS buffers.  A compute unit has one workgroup of the large
+// tile, two of the others.
+enum TileSize { kLarge = 0, kMiddle = 1, kSmall = 2 };
+
+template <int MODE, int SIZE>
 struct Tile {
-    static constexpr int BM = NW == 8 ? 256 : 128, BNV = BM;             // rows and columns of all results together
-    static constexpr int WM = NW == 8 ? 4 : 2, WN = 2;
-    static constexpr int TM = BM / WM / 32, TN = BNV / WN / 32;
+    static constexpr int NW = SIZE == kLarge ? 8 : 4, BM = SIZE == kLarge ? 256 : 128, BNV = SIZE == kSmall ? 128 : 256;
+    static constexpr int BUFS = SIZE == kMiddle ? 3 : 5;
+    static constexpr int WM = SIZE == kLarge ? 4 : 2, WN = 2;
+    static constexpr int TM = BM / WM / 32, TN = BNV / WN / 32;          // blocks of 32 x 32 a wavefront
     static constexpr bool DUAL = MODE != kRows;
-    static constexpr int BC = DUAL ? BNV / 2 : BNV;                     // columns of one result
-    static constexpr bool A_T = MODE == kWeights, B_T = MODE != kRows;  // other index contiguous
+    static constexpr int RESULTS = DUAL ? 2 : 1, BC = BNV / RESULTS;     // columns of one result
+    static constexpr bool A_T = MODE == kWeights, B_T = MODE != kRows;   // other index contiguous
     static constexpr int A_BYTES = BM * kStep * 2, B_BYTES = BNV * kStep * 2, STAGE = A_BYTES + B_BYTES;
     static constexpr int THREADS = NW * kWave;
-    static constexpr int LOADS = A_BYTES / (THREADS * 16);              // 16-byte loads a lane, of either operand
-    static_assert(TM == 2 && LOADS == 4 && B_BYTES == A_BYTES, "tile shape");
+    static constexpr int LA = A_BYTES / (THREADS * 16), LB = B_BYTES / (THREADS * 16);      // 16-byte loads a lane
+    static_assert(TM == 2 && LA == 2, "tile shape");
 };
 
-// Which 16-byte piece of row k a [64][columns] buffer has at place p: rows of RB bytes.  Reads take 64 bytes of four
+// Which 16-byte piece of row k a [32][columns] buffer has at place p: rows of RB bytes.  Reads take 64 bytes of four
 // consecutive rows at a time, which this puts 64 bytes apart modulo 256.
 template <int RB>
 __device__ __forceinline__ int turned(int k) { return RB >= 256 ? 4 * (k & 3) : 4 * ((k >> 1) & 1); }
-// The same for a [row][64] buffer (rows of 128 bytes), read one piece of 32 consecutive rows at a time.
-__device__ __forceinline__ int twisted(int row) { return row & 7; }
+// The same for a [row][32] buffer (rows of 64 bytes), read one piece of 32 consecutive rows at a time: 16 rows meet all
+// the banks once.
+__device__ __forceinline__ int twisted(int row) { return (row >> 2) & 3; }
 
 namespace {
 
-template <int MODE, int NW, class OUT, int ACT>
-__global__ __launch_bounds__(NW * kWave, NW == 8 ? 2 : 2) void k_gated_tile(TileArgs g)
+template <int MODE, int SIZE, class OUT, int ACT, bool PART>
+__global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(TileArgs g)
 {
 #ifdef __HIP_DEVICE_COMPILE__                    // the host pass makes no launch stub of a body with these builtins
-    using T = Tile<MODE, NW>;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * T::STAGE];
+    using T = Tile<MODE, SIZE>;
+    constexpr int NW = T::NW;
+    __shared__ __attribute__((aligned(1024))) char lds[T::BUFS * T::STAGE];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int wm = wave / T::WN, wn = wave % T::WN, h = lane >> 5, l32 = lane & 31;
 
@@ -136,87 +140,100 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 2 : 2) void k_gated_tile(Tile
     at -= first * (uint32_t)g.tiles_c;
     const int64_t row0 = (int64_t)(first + at % high) * T::BM, col0 = (int64_t)(at / high) * T::BC;
 
-    const int64_t k_first = MODE == kWeights ? (int64_t)slab * g.slab : 0;
-    const int64_t k_len = MODE == kWeights ? (g.Kc - k_first < g.slab ? g.Kc - k_first : g.slab) : g.Kc;
-    const int steps = (int)((k_len + kStep - 1) / kStep), nseg = g.pairs * g.groups;
+    const int steps = (int)((g.Kc + kStep - 1) / kStep), nseg = g.pairs * g.groups;
+    const int first_step = PART ? (int)((int64_t)steps * nseg * slab / g.slabs) : 0;
+    const int all = (PART ? (int)((int64_t)steps * nseg * (slab + 1) / g.slabs) : steps * nseg) - first_step;
 
-    // Where this lane's 16-byte pieces come from, within a step, and to which step's pieces they belong.
-    uint32_t off_a[4], off_b[4];
-    const int piece_k = (lane & 7) ^ twisted(lane >> 3);                 // [row][64]: eight rows an instruction
-    auto place = [&](auto turned_layout, int64_t ld, int columns, uint32_t(&off)[4], bool dual) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (!decltype(turned_layout)::value) {
-                const int row = (i * NW + wave) * 8 + (lane >> 3);
-                off[i] = (uint32_t)(row * ld * 2) + 16u * (uint32_t)piece_k;
-            } else {
-                // dual: the first two instructions load one operand, the others the other
-                const int inst = dual ? (i & 1) * NW + wave : i * NW + wave;
-                const int per_row = columns / 8, k = (inst * kWave + lane) / per_row, p = lane & (per_row - 1);
-                const int c = p ^ (columns * 2 >= 256 ? turned<256>(k) : turned<128>(k));
-                off[i] = (uint32_t)(k * ld * 2) + 16u * (uint32_t)c;
-            }
+    // Where this lane's 16-byte pieces of a step come from.
+    uint32_t off_a[T::LA], off_b[T::LB];
+    const int piece_k = (lane & 3) ^ twisted(lane >> 2);                 // [row][32]: sixteen rows an instruction
+    auto place = [&](auto other, auto columns, int64_t ld, int inst) {
+        if constexpr (!decltype(other)::value) {
+            return (uint32_t)((inst * 16 + (lane >> 2)) * ld * 2) + 16u * (uint32_t)piece_k;
+        } else {
+            constexpr int COLS = decltype(columns)::value, PER_ROW = COLS / 8;
+            const int k = (inst * kWave + lane) / PER_ROW, c = (lane & (PER_ROW - 1)) ^ turned<COLS * 2>(k);
+            return (uint32_t)(k * ld * 2) + 16u * (uint32_t)c;
         }
     };
-    place(std::integral_constant<bool, T::A_T>(), g.lda, T::BM, off_a, false);
-    place(std::integral_constant<bool, T::B_T>(), g.ldb, T::BC, off_b, T::DUAL);
+    typedef std::integral_constant<int, T::BM> ColsA;
+    typedef std::integral_constant<int, T::BC> ColsB;
+#pragma unroll
+    for (int i = 0; i < T::LA; ++i) off_a[i] = place(std::integral_constant<bool, T::A_T>(), ColsA(), g.lda, i * NW + wave);
+#pragma unroll
+    for (int i = 0; i < T::LB; ++i)
+        off_b[i] = place(std::integral_constant<bool, T::B_T>(), ColsB(), g.ldb, i % (T::LB / T::RESULTS) * NW + wave);
 
-    // The operands' places at segment `seg`, step `t`, and the loads of that step into LDS buffer `buf`.
-    auto load_step = [&](int seg, int t, int buf) {
+    // The operands of the step that is loaded next.  Resources begin at the step's first element and end, for an operand
+    // whose contracted index is contiguous, with the tile's last row (a row's pieces beyond the contracted range are given an
+    // address beyond every end, in a segment's last step), for the others with the step's last contracted row.
+    int seg = PART ? first_step / (steps > 0 ? steps : 1) : 0, t = first_step - seg * steps, loaded = 0;
+    int into = 0;                                                        // bytes to the LDS buffer it goes to
+    const uint16_t *next_a, *next_b[2];
+    const int64_t step_a = T::A_T ? kStep * g.lda : kStep, step_b = T::B_T ? kStep * g.ldb : kStep;
+    const int last_rows = (int)(g.Kc - (int64_t)(steps - 1) * kStep);     // contracted elements of a segment's last step
+    const int64_t rows_a = g.R - row0 < T::BM ? g.R - row0 : T::BM, rows_b = g.C - col0 < T::BNV ? g.C - col0 : T::BNV;
+    const int bytes_a = (int)(2 * (T::A_T ? kStep * g.lda - row0 : rows_a * g.lda));
+    const int bytes_b = (int)(2 * (T::B_T ? kStep * g.ldb - col0 : rows_b * g.ldb));
+    const int last_a = T::A_T ? (int)(2 * (last_rows * g.lda - row0)) : bytes_a, last_b = T::B_T ? (int)(2 * (last_rows * g.ldb - col0)) : bytes_b;
+    const bool beyond = piece_k * 8 >= last_rows;                        // rows are padded with zeros to whole pieces
+    auto begin_segment = [&]() {
         const int grp = MODE == kRows ? seg / g.pairs : 0, pair = MODE == kRows ? seg - grp * g.pairs : seg;
         const int pa = g.pairs == 1 ? 0 : plane_a(pair), pb = g.pairs == 1 ? 0 : plane_b(pair);
-        const uint16_t *a = g.a[grp] + pa * g.a_plane;
-        const int64_t k = k_first + (int64_t)t * kStep, k_end = k_first + k_len;
-        auto rsrc = [&](const uint16_t *p, int64_t start, int64_t end) {
-            int64_t bytes = (end - start) * 2;
-            bytes = bytes < 0 ? 0 : bytes > kMostRecords ? kMostRecords : bytes;
-            return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p + start), 0, (int)bytes, kTileRsrc);
-        };
-        const bool tail = !(T::A_T && T::B_T) && k + kStep > k_end;
-        const uint32_t left = (uint32_t)(k_end - k + 7) / 8;             // pieces: rows are padded with zeros to a multiple of 8
-        FASTGL_LDS char *to = (FASTGL_LDS char *)lds + buf * T::STAGE + wave * 1024;
-        {
-            const auto r = T::A_T ? rsrc(a, k * g.lda + row0, k_end * g.lda) : rsrc(a, row0 * g.lda + k, g.R * g.lda);
+        next_a = g.a[grp] + pa * g.a_plane + (T::A_T ? row0 : row0 * g.lda) + t * step_a;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t o = off_a[i];
-                if (!T::A_T && tail && (uint32_t)piece_k >= left) o = kNoSuchOffset;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (FASTGL_LDS void *)(to + i * NW * 1024), 16, (int)o, 0, 0, 0);
-            }
+        for (int q = 0; q < T::RESULTS; ++q)
+            next_b[q] = (MODE == kRows ? g.b[grp] : g.b[q]) + pb * g.b_plane + (T::B_T ? col0 : col0 * g.ldb) + t * step_b;
+    };
+    auto load_next = [&]() {
+        if (loaded >= all) return;
+        const bool last = t + 1 == steps;
+        FASTGL_LDS char *to = (FASTGL_LDS char *)lds + into + wave * 1024;
+        auto rsrc = [&](const uint16_t *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p), 0, bytes, kTileRsrc); };
+        const auto ra = rsrc(next_a, last ? last_a : bytes_a);
+#pragma unroll
+        for (int i = 0; i < T::LA; ++i) {
+            const uint32_t o = !T::A_T && last && beyond ? kNoSuchOffset : off_a[i];
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (FASTGL_LDS void *)(to + i * NW * 1024), 16, (int)o, 0, 0, 0);
         }
 #pragma unroll
-        for (int q = 0; q < (T::DUAL ? 2 : 1); ++q) {
-            const uint16_t *b = (MODE == kRows ? g.b[grp] : g.b[q]) + pb * g.b_plane;
-            const auto r = T::B_T ? rsrc(b, k * g.ldb + col0, k_end * g.ldb) : rsrc(b, col0 * g.ldb + k, g.C * g.ldb);
+        for (int q = 0; q < T::RESULTS; ++q) {
+            const auto rb = rsrc(next_b[q], last ? last_b : bytes_b);
 #pragma unroll
-            for (int i = T::DUAL ? 2 * q : 0; i < (T::DUAL ? 2 * q + 2 : 4); ++i) {
-                uint32_t o = off_b[i];
-                if (!T::B_T && tail && (uint32_t)piece_k >= left) o = kNoSuchOffset;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (FASTGL_LDS void *)(to + T::A_BYTES + i * NW * 1024), 16, (int)o, 0, 0, 0);
+            for (int i = q * (T::LB / T::RESULTS); i < (q + 1) * (T::LB / T::RESULTS); ++i) {
+                const uint32_t o = !T::B_T && last && beyond ? kNoSuchOffset : off_b[i];
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (FASTGL_LDS void *)(to + T::A_BYTES + i * NW * 1024), 16, (int)o, 0, 0, 0);
             }
+            next_b[q] += step_b;
+        }
+        next_a += step_a;
+        ++loaded;
+        into = into == (T::BUFS - 1) * T::STAGE ? 0 : into + T::STAGE;
+        if (++t == steps) {
+            t = 0;
+            ++seg;
+            if (loaded < all) begin_segment();
         }
     };
 
     // Where a lane reads its fragments: row (or column) l32 of a block of 32, contracted elements 8 h .. 8 h + 7 of 16.
-    // [row][64]: piece 2 kk + h.  [64][column]: two transposing reads of four contracted rows each; of sixteen lanes four read one
+    // [row][32]: piece 2 kk + h.  [32][column]: two transposing reads of four contracted rows each; of sixteen lanes four read one
     // row, and lane i gets column i of the four rows.
     const int i16 = lane & 15, g2 = (lane >> 4) & 1;
-    uint32_t read_k[4];
+    uint32_t read_k[2];
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) read_k[kk] = (uint32_t)(l32 * 128 + (((2 * kk + h) ^ twisted(l32)) << 4));
-    auto read_t = [&](auto row_bytes, int block) {                      // block: of 32 columns
-        constexpr int RB = decltype(row_bytes)::value;
+    for (int kk = 0; kk < 2; ++kk) read_k[kk] = (uint32_t)(l32 * 64 + (((2 * kk + h) ^ twisted(l32)) << 4));
+    auto read_t = [&](auto columns, int block) {                        // block: of 32 columns
+        constexpr int RB = decltype(columns)::value * 2;
         const int k = 8 * h + (i16 >> 2), piece = (4 * block + 2 * g2 + ((i16 & 3) >> 1)) ^ turned<RB>(k);
         return (uint32_t)(k * RB + piece * 16 + (i16 & 1) * 8);
     };
-    typedef std::integral_constant<int, T::BM * 2> RowA;
-    typedef std::integral_constant<int, T::BC * 2> RowB;
-    constexpr int HALF_N = T::DUAL ? T::TN / 2 : T::TN;                   // column blocks of one result
-    uint32_t at_a[T::TM], at_b[HALF_N];
+    constexpr int ONE = T::TN / T::RESULTS;                               // column blocks of one result
+    uint32_t at_a[T::TM], at_b[ONE];
 #pragma unroll
-    for (int i = 0; i < T::TM; ++i) at_a[i] = T::A_T ? read_t(RowA(), wm * T::TM + i) : 0;
+    for (int i = 0; i < T::TM; ++i) at_a[i] = T::A_T ? read_t(ColsA(), wm * T::TM + i) : 0;
 #pragma unroll
-    for (int j = 0; j < HALF_N; ++j) at_b[j] = T::B_T ? read_t(RowB(), wn * HALF_N + j) : 0;
+    for (int j = 0; j < ONE; ++j) at_b[j] = T::B_T ? read_t(ColsB(), wn * ONE + j) : 0;
 
     auto frag_k = [&](uint32_t base) { return *(FASTGL_LDS bf16x8 *)((FASTGL_LDS char *)lds + base); };
     auto frag_t = [&](uint32_t base, int row_bytes) {
@@ -225,76 +242,111 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 2 : 2) void k_gated_tile(Tile
         struct { i16x4 l, h; } both = {lo, hi};
         return __builtin_bit_cast(bf16x8, both);
     };
-
-    f32x16 acc[T::TM][T::TN];
-#pragma unroll
-    for (int i = 0; i < T::TM; ++i)
-#pragma unroll
-        for (int j = 0; j < T::TN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-
     struct Frags { bf16x8 a[T::TM], b[T::TN]; };
     auto read = [&](int buf, int kk) {
         Frags f;
-        const uint32_t base = (uint32_t)(buf * T::STAGE);
+        const uint32_t base = (uint32_t)buf;
 #pragma unroll
         for (int i = 0; i < T::TM; ++i) {
-            if constexpr (T::A_T) f.a[i] = frag_t(base + at_a[i] + (uint32_t)(kk * 16 * RowA::value), RowA::value);
-            else f.a[i] = frag_k(base + read_k[kk] + (uint32_t)((wm * T::TM + i) * 32 * 128));
+            if constexpr (T::A_T) f.a[i] = frag_t(base + at_a[i] + (uint32_t)(kk * 16 * 2 * T::BM), 2 * T::BM);
+            else f.a[i] = frag_k(base + read_k[kk] + (uint32_t)((wm * T::TM + i) * 32 * 64));
         }
 #pragma unroll
         for (int j = 0; j < T::TN; ++j) {
-            if constexpr (T::B_T) {
-                const int q = T::DUAL && j >= HALF_N ? 1 : 0;
-                f.b[j] = frag_t(base + T::A_BYTES + q * (T::B_BYTES / 2) + at_b[j - q * HALF_N] + (uint32_t)(kk * 16 * RowB::value), RowB::value);
-            } else
-                f.b[j] = frag_k(base + T::A_BYTES + read_k[kk] + (uint32_t)((wn * T::TN + j) * 32 * 128));
+            if constexpr (T::B_T)
+                f.b[j] = frag_t(base + T::A_BYTES + j / ONE * (T::B_BYTES / T::RESULTS) + at_b[j % ONE] + (uint32_t)(kk * 16 * 2 * T::BC), 2 * T::BC);
+            else f.b[j] = frag_k(base + T::A_BYTES + read_k[kk] + (uint32_t)((wn * T::TN + j) * 32 * 64));
         }
         return f;
     };
-    // the columns first: a lane then holds four consecutive columns of one row
+
+    // Sums start from the biases.  Operands are multiplied columns first: lane l then holds, of row l32 of a block, columns
+    // 8 q + 4 h + (0 .. 3) in elements 4 q + (0 .. 3).
+    f32x16 acc[T::TM][T::TN];
+#pragma unroll
+    for (int j = 0; j < T::TN; ++j) {
+        f32x16 start;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) start[e] = 0.f;
+        if constexpr (MODE == kForward && !PART)
+            if (const float *bias = g.bias[j / ONE]) {
+                const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(bias), 0, (int)(g.C * 4), kTileRsrc);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)(4 * (col0 + (wn * ONE + j % ONE) * 32 + 8 * q + 4 * h)), 0, 0);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) start[4 * q + x] = __uint_as_float(v[x]);
+                }
+            }
+#pragma unroll
+        for (int i = 0; i < T::TM; ++i) acc[i][j] = start;
+    }
     auto multiply = [&](const Frags &f) {
 #pragma unroll
         for (int j = 0; j < T::TN; ++j)
 #pragma unroll
             for (int i = 0; i < T::TM; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[j], f.a[i], acc[i][j], 0, 0, 0);
     };
-
-    const int all = steps * nseg;
-    int seg = 0, t = 0;
-    if (all > 0) load_step(0, 0, 0);
-    for (int s = 0; s < all; ++s) {
-        const int buf = s & 1;
-        __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt 0: this wavefront's loads of the step are in LDS
-        __builtin_amdgcn_s_barrier();                // everybody's are, and the other buffer has been read
-        __builtin_amdgcn_sched_barrier(0);
-        if (++t == steps) {
-            t = 0;
-            ++seg;
-        }
-        if (s + 1 < all) load_step(seg, t, buf ^ 1);
-        Frags f = read(buf, 0);
+    // The reads of the next fragments go between the matrix instructions of this one, the first of them in front.
+    auto interleave = [&]() {
+        constexpr int READS = T::TM * (T::A_T ? 2 : 1) + T::TN * (T::B_T ? 2 : 1), MATRIX = T::TM * T::TN;
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            Frags n;
-            if (kk < 3) n = read(buf, kk + 1);
+        for (int i = 0; i < MATRIX; ++i) {
+            if (i * 2 < READS) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+        if (READS > 2 * MATRIX) __builtin_amdgcn_sched_group_barrier(0x100, READS - 2 * MATRIX, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // A step multiplies what lies in its buffer.  Its barrier says that everybody's loads of the next step have arrived, so
+    // that the first fragments of that one are read before the next barrier and matrix instructions follow at once; the loads
+    // that the step begins go where the step before it was, and have BUFS - 2 steps to arrive.
+    constexpr int IN_FLIGHT = T::LA + T::LB;                 // loads of a step
+    if (all > 0) {
+        begin_segment();
+#pragma unroll
+        for (int i = 0; i < T::BUFS - 1; ++i) load_next();
+        if (all >= T::BUFS - 1) __builtin_amdgcn_s_waitcnt(0x0F70 | (T::BUFS - 2) * IN_FLIGHT);
+        else __builtin_amdgcn_s_waitcnt(0x0F70);
+        __builtin_amdgcn_s_barrier();
+        Frags f = read(0, 0);
+        int now = 0;                                         // bytes to the step's buffer
+        auto step = [&]() {
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            load_next();
+            __builtin_amdgcn_sched_barrier(0);
+            const Frags n = read(now, 1);
             multiply(f);
-            f = n;
+            interleave();
+            now = now == (T::BUFS - 1) * T::STAGE ? 0 : now + T::STAGE;
+            f = read(now, 0);                                // of no use after the last step
+            multiply(n);
+            interleave();
+        };
+        int s = 0;
+        for (; s < all - (T::BUFS - 2); ++s) {
+            __builtin_amdgcn_s_waitcnt(0x0F70 | (T::BUFS - 3) * IN_FLIGHT);      // the next step has arrived
+            step();
+        }
+        for (; s < all; ++s) {
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+            step();
         }
     }
 
     // ------------------------------------------------------------------ epilogue
     __builtin_amdgcn_s_waitcnt(0xC07F);              // lgkmcnt 0
     __builtin_amdgcn_s_barrier();                    // the LDS buffers are free: each wavefront has a part for itself
-    constexpr int OB = (int)sizeof(OUT), PART = 2 * T::STAGE / NW;         // 16 KB a wavefront
+    constexpr int OB = (int)sizeof(OUT), PARTB = T::BUFS * T::STAGE / NW & ~1023;
     constexpr int ROWB = 64 * OB;                                        // 64 columns of a row
-    static_assert(64 * ROWB <= PART, "a block of 64 x 64 results fits a wavefront's part");
-    FASTGL_LDS char *mine = (FASTGL_LDS char *)lds + wave * PART;
+    static_assert(64 * ROWB <= PARTB, "a block of 64 x 64 results fits a wavefront's part");
+    FASTGL_LDS char *mine = (FASTGL_LDS char *)lds + wave * PARTB;
     const int64_t r_base = row0 + wm * 64;
-    // Columns c .. c + 32 B - 1 (B = 1 or 2 blocks) of the wavefront's 64 rows, element by element from `value(i, block, e)`.
-    auto store_block = [&](auto blocks, void *out, int64_t ld, int64_t c_base, auto value) {
-        constexpr int NB = decltype(blocks)::value, LPR = NB * 32 * OB / 16;        // lanes a row: 16 bytes each
+    // NB blocks of 32 columns from column c_base of the wavefront's 64 rows, element by element from value(i, block, e).
+    auto store_block = [&](auto blocks, void *out, int64_t c_base, auto value) {
+        constexpr int NB = decltype(blocks)::value, LPR = NB * 32 * OB / 16, PER = 16 / OB;      // lanes a row: PER elements each
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = 0; i < T::TM; ++i)
@@ -323,20 +375,32 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 2 : 2) void k_gated_tile(Tile
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         typedef typename Words<OB>::x4 W4;
+        constexpr int ROUNDS = 64 * LPR / kWave, ROWS = kWave / LPR;       // rows a round
+        const int row = lane / LPR, c = lane % LPR;
+        FASTGL_LDS char *from = mine + row * ROWB;
+        auto piece = [&](int n) { return *(FASTGL_LDS u32x4 *)(from + n * ROWS * ROWB + ((c ^ ((row + n * ROWS) & 7)) * 16)); };
+        OUT *base = static_cast<OUT *>(out) + r_base * g.C + c_base;
+        if (r_base + 64 <= g.R && c_base + NB * 32 <= g.C) {              // all of it exists
+            uint32_t o = (uint32_t)((row * g.C + c * PER) * OB);
+            const uint32_t down = (uint32_t)(ROWS * g.C * OB);
 #pragma unroll
-        for (int n = 0; n < 64 * LPR / kWave; ++n) {
-            const int row = (n * kWave + lane) / LPR, c = lane % LPR;
-            const u32x4 o = *(FASTGL_LDS u32x4 *)(mine + row * ROWB + ((c ^ (row & 7)) * 16));
-            const int64_t r = r_base + row, col = c_base + c * (16 / OB);
-            if (r < g.R && col < g.C) {
-                OUT *p = static_cast<OUT *>(out) + r * ld + col;
-                if (col + 16 / OB <= g.C) {
-                    *reinterpret_cast<W4 *>(p) = W4{o[0], o[1], o[2], o[3]};
+            for (int n = 0; n < ROUNDS; ++n, o += down) {
+                const u32x4 v = piece(n);
+                *reinterpret_cast<W4 *>(reinterpret_cast<char *>(base) + o) = W4{v[0], v[1], v[2], v[3]};
+            }
+        } else {
+            const int64_t left = g.C - c_base - c * PER;
+            for (int n = 0; n < ROUNDS; ++n) {
+                if (r_base + row + n * ROWS >= g.R || left <= 0) continue;
+                const u32x4 v = piece(n);
+                OUT *p = base + (row + n * ROWS) * g.C + c * PER;
+                if (left >= PER) {
+                    *reinterpret_cast<W4 *>(p) = W4{v[0], v[1], v[2], v[3]};
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 16 / OB - 1; ++e)
-                        if (col + e < g.C) {
-                            const uint32_t word = o[e * OB / 4];             // a copy: a bit cast of o[e] itself takes o[0]
+                    for (int e = 0; e < PER - 1; ++e)
+                        if (e < left) {
+                            const uint32_t word = v[e * OB / 4];           // a copy: a bit cast of v[e] itself takes v[0]
                             if constexpr (OB == 2) p[e] = (uint16_t)(word >> (16 * (e & 1)));
                             else p[e] = __uint_as_float(word);
                         }
@@ -345,40 +409,25 @@ __global__ __launch_bounds__(NW * kWave, NW == 8 ? 2 : 2) void k_gated_tile(Tile
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
-    if constexpr (MODE == kForward) {
-        const int64_t c_base = col0 + wn * HALF_N * 32;
-        typedef std::integral_constant<int, HALF_N> NB;
+    typedef std::integral_constant<int, ONE < 2 ? 1 : 2> NB;             // 64 columns at a time at most
+    auto store_result = [&](int q, void *out, auto value) {               // value(i, block, e): of this result's blocks
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            if (!g.bias[q]) continue;
-            const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(g.bias[q]), 0, (int)(g.C * 4), kTileRsrc);
+        for (int n = 0; n < ONE; n += NB::value)
+            store_block(NB(), out, col0 + (wn * ONE + n) * 32, [&](int i, int b, int e) { return value(i, n + b, e); });
+    };
+    if constexpr (PART) {
 #pragma unroll
-            for (int b = 0; b < HALF_N; ++b)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)(4 * (c_base + b * 32 + 8 * e + 4 * h)), 0, 0);
-#pragma unroll
-                    for (int i = 0; i < T::TM; ++i)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) acc[i][q * HALF_N + b][4 * e + x] += __uint_as_float(v[x]);
-                }
-        }
-        if (g.out[1]) store_block(NB(), g.out[1], g.C, c_base, [&](int i, int b, int e) { return acc[i][b][e]; });
-        if (g.out[2]) store_block(NB(), g.out[2], g.C, c_base, [&](int i, int b, int e) { return acc[i][HALF_N + b][e]; });
-        store_block(NB(), g.out[0], g.C, c_base,
-                    [&](int i, int b, int e) { return gate<ACT, false>(acc[i][b][e], nullptr) * acc[i][HALF_N + b][e]; });
-    } else if constexpr (MODE == kRows) {
-#pragma unroll
-        for (int n = 0; n < T::TN / 2; ++n)
-            store_block(std::integral_constant<int, 2>(), g.out[0], g.C, col0 + (wn * T::TN + 2 * n) * 32,
-                        [&](int i, int b, int e) { return acc[i][2 * n + b][e]; });
+        for (int q = 0; q < T::RESULTS; ++q)
+            if (MODE == kForward || g.out[q])
+                store_result(q, g.part + ((int64_t)slab * T::RESULTS + q) * g.R * g.C, [&](int i, int b, int e) { return acc[i][q * ONE + b][e]; });
+    } else if constexpr (MODE == kForward) {
+        if (g.out[1]) store_result(0, g.out[1], [&](int i, int b, int e) { return acc[i][b][e]; });
+        if (g.out[2]) store_result(1, g.out[2], [&](int i, int b, int e) { return acc[i][ONE + b][e]; });
+        store_result(0, g.out[0], [&](int i, int b, int e) { return gate<ACT, false>(acc[i][b][e], nullptr) * acc[i][ONE + b][e]; });
     } else {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            if (!g.out[q]) continue;
-            store_block(std::integral_constant<int, HALF_N>(), static_cast<OUT *>(g.out[q]) + (int64_t)slab * g.out_slab, g.C,
-                        col0 + wn * HALF_N * 32, [&](int i, int b, int e) { return acc[i][q * HALF_N + b][e]; });
-        }
+        for (int q = 0; q < T::RESULTS; ++q)
+            if (g.out[q]) store_result(q, g.out[q], [&](int i, int b, int e) { return acc[i][q * ONE + b][e]; });
     }
 #endif
 }
