@@ -212,38 +212,50 @@ __global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
     }
 }
 
-// out[col] = sum of part[0 .. n)[col] in fp64 over 2 N columns: 16 columns a workgroup, a fixed order.
-__global__ __launch_bounds__(1024) void k_gated_db(const float *__restrict__ part, int32_t n, int32_t N, float *dbg, float *dbu)
-{
-    __shared__ double sums[64][17];
-    const int c = threadIdx.x % 16, s = threadIdx.x / 16;
-    const int64_t col = (int64_t)blockIdx.x * 16 + c;
-    double v = 0.0;
-    if (col < 2 * (int64_t)N) {
-#pragma unroll 8
-        for (int i = s; i < n; i += 64) v += (double)part[(int64_t)i * 2 * N + col];
-    }
-    sums[s][c] = v;
-    __syncthreads();
-    if (s == 0 && col < 2 * (int64_t)N) {
-        v = 0.0;
-        for (int i = 0; i < 64; ++i) v += sums[i][c];
-        float *out = col < N ? dbg : dbu;
-        if (out) out[col < N ? col : col - N] = (float)v;
-    }
-}
+// What a backward pass adds up at its end, in fp64 and a fixed order: slabs of up to two results of n elements, and the
+// column sums of dG and dU.
+struct SumArgs {
+    const float *part;               // slab s of result q at part + s * stride + q * n
+    void *out[2];                    // or NULL
+    int64_t n, stride;
+    int32_t slabs, results;
+    int32_t blocks;                  // workgroups of the slabs, before those of the columns
+    const float *db;                 // [rows][2][N]
+    float *dbg, *dbu;
+    int32_t rows, N;
+};
 
-// out = sum over the slabs in fp64, in their order.
 template <bool BF16>
-__global__ __launch_bounds__(kBlock) void k_gated_sum(const float *__restrict__ part, int32_t slabs, int64_t stride, int64_t n, void *out)
+__global__ __launch_bounds__(kBlock) void k_gated_sum(SumArgs a)
 {
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (i >= n) return;
-    double v = 0.0;
+    if ((int)blockIdx.x < a.blocks) {
+        const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+        if (i >= a.n * a.results) return;
+        const int q = i >= a.n;
+        if (!a.out[q]) return;
+        double v = 0.0;
 #pragma unroll 8
-    for (int s = 0; s < slabs; ++s) v += (double)part[(int64_t)s * stride + i];
-    if constexpr (BF16) static_cast<uint16_t *>(out)[i] = __builtin_bit_cast(uint16_t, (__bf16)(float)v);
-    else static_cast<float *>(out)[i] = (float)v;
+        for (int s = 0; s < a.slabs; ++s) v += (double)a.part[(int64_t)s * a.stride + i];
+        if constexpr (BF16) static_cast<uint16_t *>(a.out[q])[i - q * a.n] = __builtin_bit_cast(uint16_t, (__bf16)(float)v);
+        else static_cast<float *>(a.out[q])[i - q * a.n] = (float)v;
+        return;
+    }
+    __shared__ double sums[kBlock / 8][9];                             // eight columns, 32 threads a column
+    const int c = threadIdx.x & 7, r = threadIdx.x >> 3;
+    const int64_t col = ((int64_t)blockIdx.x - a.blocks) * 8 + c;
+    double v = 0.0;
+    if (col < 2 * (int64_t)a.N) {
+#pragma unroll 8
+        for (int i = r; i < a.rows; i += kBlock / 8) v += (double)a.db[(int64_t)i * 2 * a.N + col];
+    }
+    sums[r][c] = v;
+    __syncthreads();
+    if (r == 0 && col < 2 * (int64_t)a.N) {
+        v = 0.0;
+        for (int i = 0; i < kBlock / 8; ++i) v += sums[i][c];
+        float *out = col < a.N ? a.dbg : a.dbu;
+        if (out) out[col < a.N ? col : col - a.N] = (float)v;
+    }
 }
 
 // The forward pass's slabs: sums, biases and the gate.
@@ -279,23 +291,25 @@ struct Cut {
     int64_t slabs;
 };
 
-// The cut that a model of the launch finds fastest: workgroups run in rounds of one (large tiles) or two a compute unit, a
-// workgroup costs its steps and a fixed part, and slabs cost the sums that they write and that are read again.
+// The cut that a model of the launch finds fastest.  A compute unit needs `step_us` for a step of a tile, whether it has one
+// or two workgroups at a time, and `tile_us` for what is around the steps; slabs cost the sums that they write and that are read
+// again, and a launch.  Measured (kernel times, bf16, us for large / middle / small tiles):
+//   forward 16 384 x 1024 -> 4096, G and U kept 271 / 268 / -, alone 227 / 240 / -;  115 000 x 256 -> 1024 196 / 186 / -, 154 / 139 / -
+//   dX 16 384 x 4096 -> 1024 242 / 284 / 344;  dWg, dWu of 16 384 rows 1024 x 4096 206 / 240 / 416 (the first two in two slabs)
+//   backward call of 300 rows 256 -> 1024 33 / 29 / 27, of 2000 rows 56 / 51 / 47, of 8000 rows 256 -> 683 79 / 72 / 76
 Cut cut_of(int mode, int64_t R, int64_t C, int64_t Kc, int64_t segments)
 {
+    static const double step_us[3][3] = {{0.80, 0.46, 0.32}, {0.93, 0.55, 0.34}, {0.80, 0.46, 0.40}};
+    static const double tile_us[2][3] = {{6.0, 2.6, 1.6}, {4.0, 2.0, 1.2}};
     Cut best = {kLarge, 1};
     double least = 1e300;
     const int64_t all = ceil_div(Kc, kStep) * segments;
     for (int size = kLarge; size <= kSmall; ++size) {
-        static const char *only = getenv("GSIZE");
-        if (only && atoi(only) != size) continue;
         const int64_t bm = size == kLarge ? 256 : 128, bc = (size == kSmall ? 128 : 256) / (mode == kRows ? 1 : 2);
-        const int64_t tiles = ceil_div(R, bm) * ceil_div(C, bc), slots = size == kLarge ? 256 : 512;
-        const double step_us = size == kLarge ? 0.85 : size == kMiddle ? 0.95 : 0.6;
-        for (int64_t slabs = 1; slabs <= 64 && (slabs == 1 || all / slabs >= 4); slabs = slabs < 8 ? slabs + 1 : slabs * 5 / 4) {
-            const double rounds = (double)ceil_div(tiles * slabs, slots);
-            const double us = rounds * ((double)ceil_div(all, slabs) * step_us + 4.0) +
-                              (slabs > 1 ? 4.0 + (double)slabs * (double)R * (double)C * (mode == kRows ? 8.0 : 16.0) / 4e6 : 0.0);
+        const int64_t tiles = ceil_div(R, bm) * ceil_div(C, bc);
+        for (int64_t slabs = 1; slabs <= 64 && (slabs == 1 || (all / slabs >= 4 && R * C <= (int64_t)1 << 30)); slabs = slabs < 8 ? slabs + 1 : slabs * 5 / 4) {
+            const double us = (double)ceil_div(tiles * slabs, 256) * ((double)ceil_div(all, slabs) * step_us[mode][size] + tile_us[mode != kForward][size]) +
+                              (slabs > 1 ? 5.0 + (double)slabs * (double)R * (double)C * (mode == kRows ? 8.0 : 16.0) / 4e6 : 0.0);
             if (us < least) {
                 least = us;
                 best = {size, slabs};
@@ -321,10 +335,10 @@ struct Layout {
 struct Shape {
     bool bf16, aligned;
     int planes;
-    int64_t M, K, N, ldk, ldn;
+    int64_t M, K, N, ldk, ldn, ldz;
     Shape(fastgl_dtype dtype, int64_t M_, int64_t K_, int64_t N_, bool aligned_)
         : bf16(dtype == FASTGL_BF16), aligned(aligned_), planes(dtype == FASTGL_BF16 ? 1 : 3), M(M_), K(K_), N(N_),
-          ldk((int64_t)align_up((size_t)K_, 8)), ldn((int64_t)align_up((size_t)N_, 8))
+          ldk((int64_t)align_up((size_t)K_, 8)), ldn((int64_t)align_up((size_t)N_, 8)), ldz(ldn + (ldn % 512 == 0 ? 64 : 0))
     {
     }
     bool pack_x() const { return !bf16 || !aligned || K % 8; }
@@ -363,8 +377,8 @@ Scratch carve(const Shape &s, bool backward, Layout &l)
     }
     auto sums = [](const Cut &c, int64_t n) { return c.slabs > 1 ? (size_t)(c.slabs * n) : (size_t)0; };
     if (backward) {
-        o.dg = l.take<uint16_t>((size_t)(s.planes * s.M * s.ldn));
-        o.du = l.take<uint16_t>((size_t)(s.planes * s.M * s.ldn));
+        o.dg = l.take<uint16_t>((size_t)(s.planes * s.M * s.ldz));
+        o.du = l.take<uint16_t>((size_t)(s.planes * s.M * s.ldz));
         o.db = l.take<float>((size_t)(s.dz_rows() * 2 * s.N));
         const size_t x = sums(s.rows_cut(), s.M * s.K), w = sums(s.weights_cut(), 2 * s.K * s.N);
         o.part = l.take<float>(x > w ? x : w);
@@ -432,11 +446,17 @@ void by_act(fastgl_act act, F f)
 }
 
 // One product: results in bf16 or fp32, or sums of slabs.
+//
+// Results of the forward pass go past the caches where the tiles' rows are whole 128-byte lines.  us a call, bf16, through the caches /
+// past them: 115 000 rows 256 -> 1024, G and U kept 250 / 186, alone 168 / 139; 8000 rows 18.6 / 16.2, 15.6 / 11.9; 16 384 rows
+// 1024 -> 4096 307 / 268.  Rows that are not: 60 000 rows 128 -> 520 49 / 95; 20 000 rows 100 -> 1000 35 / 70.
 template <int MODE, class ACT>
 fastgl_status launch_tile(TileArgs g, const Cut &cut, bool bf16, ACT, hipStream_t s, const char *what)
 {
     constexpr int A = ACT::value;
     const int64_t bm = cut.size == kLarge ? 256 : 128, bc = (cut.size == kSmall ? 128 : 256) / (MODE == kRows ? 1 : 2);
+    const int64_t line = bf16 ? 64 : 32;                             // elements
+    const bool once = cut.size != kSmall && g.C % line == 0 && !misaligned_to(g.out[0], 128) && !misaligned_to(g.out[1], 128) && !misaligned_to(g.out[2], 128);
     const int64_t tr = ceil_div(g.R, bm), tc = ceil_div(g.C, bc), total = tr * tc * cut.slabs;
     if (total > 0x7FFFFFFFLL || 4 * tc > 0x7FFFFFFFLL) {
         set_error("%s: too many tiles (%lld)", what, (long long)total);
@@ -448,9 +468,12 @@ fastgl_status launch_tile(TileArgs g, const Cut &cut, bool bf16, ACT, hipStream_
     auto sized = [&](auto size) {
         constexpr int S = decltype(size)::value;
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(Tile<MODE, S>::THREADS), 0, s, g); };
-        if (cut.slabs > 1) go(k_gated_tile<MODE, S, float, 0, true>);
-        else if (bf16) go(k_gated_tile<MODE, S, uint16_t, A, false>);
-        else go(k_gated_tile<MODE, S, float, A, false>);
+        if (cut.slabs > 1) return go(k_gated_tile<MODE, S, float, 0, true, false>);
+        if constexpr (MODE == kForward) {
+            if (once) return bf16 ? go(k_gated_tile<MODE, S, uint16_t, A, false, true>) : go(k_gated_tile<MODE, S, float, A, false, true>);
+        }
+        if (bf16) go(k_gated_tile<MODE, S, uint16_t, A, false, false>);
+        else go(k_gated_tile<MODE, S, float, A, false, false>);
     };
     if (cut.size == kLarge) sized(std::integral_constant<int, kLarge>());
     else if (cut.size == kMiddle) sized(std::integral_constant<int, kMiddle>());
@@ -459,11 +482,12 @@ fastgl_status launch_tile(TileArgs g, const Cut &cut, bool bf16, ACT, hipStream_
     return FASTGL_OK;
 }
 
-fastgl_status sum_slabs(const float *part, const Cut &cut, int64_t stride, int64_t n, bool bf16, void *out, hipStream_t s, const char *what)
+fastgl_status launch_sum(SumArgs a, bool bf16, hipStream_t s, const char *what)
 {
-    const dim3 grid((unsigned)ceil_div(n, kBlock));
-    if (bf16) hipLaunchKernelGGL(k_gated_sum<true>, grid, dim3(kBlock), 0, s, part, (int32_t)cut.slabs, stride, n, out);
-    else hipLaunchKernelGGL(k_gated_sum<false>, grid, dim3(kBlock), 0, s, part, (int32_t)cut.slabs, stride, n, out);
+    a.blocks = (int32_t)ceil_div(a.n * a.results, kBlock);
+    const dim3 grid((unsigned)(a.blocks + (a.db ? ceil_div(2 * (int64_t)a.N, 8) : 0)));
+    if (bf16) hipLaunchKernelGGL(k_gated_sum<true>, grid, dim3(kBlock), 0, s, a);
+    else hipLaunchKernelGGL(k_gated_sum<false>, grid, dim3(kBlock), 0, s, a);
     FASTGL_LAUNCH_CHECK(what);
     return FASTGL_OK;
 }
@@ -623,8 +647,8 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
     z.G = G; z.U = U; z.dP = dP;
     z.dG = want_x || want_w ? o.dg : nullptr;
     z.dU = o.du;
-    z.M = M; z.plane = M * d.ldn;
-    z.N = (int32_t)N; z.ld = (int32_t)d.ldn; z.lg = d.lg();
+    z.M = M; z.plane = M * d.ldz;
+    z.N = (int32_t)N; z.ld = (int32_t)d.ldz; z.lg = d.lg();
     z.part = want_b ? o.db : nullptr;
     const dim3 dz((unsigned)d.dz_cols(), (unsigned)d.dz_rows());
     by_act(act, [&](auto A) {
@@ -633,10 +657,11 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
         else hipLaunchKernelGGL((k_gated_dz<false, ACT>), dz, dim3(kBlock), 0, s, z);
     });
     FASTGL_LAUNCH_CHECK("fastgl_gated_bwd (dG, dU)");
+    SumArgs last = {};                                 // the sums at the end
     if (want_b) {
-        hipLaunchKernelGGL(k_gated_db, dim3((unsigned)ceil_div(2 * N, 16)), dim3(1024), 0, s, (const float *)o.db, (int32_t)dz.y,
-                           (int32_t)N, dbg, dbu);
-        FASTGL_LAUNCH_CHECK("fastgl_gated_bwd (db)");
+        last.db = o.db;
+        last.dbg = dbg; last.dbu = dbu;
+        last.rows = (int32_t)dz.y; last.N = (int32_t)N;
     }
     const std::integral_constant<int, 0> none;
     if (want_x) {
@@ -648,36 +673,43 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
         g.a[0] = o.dg; g.a[1] = o.du;
         g.b[0] = d.pack_w() ? o.wg : (const uint16_t *)Wg;
         g.b[1] = d.pack_w() ? o.wu : (const uint16_t *)Wu;
-        g.a_plane = M * d.ldn; g.b_plane = K * d.ldn;
-        g.lda = d.ldn; g.ldb = d.ldn;
+        g.a_plane = M * d.ldz; g.b_plane = K * d.ldn;
+        g.lda = d.ldz; g.ldb = d.ldn;
         g.R = M; g.C = K; g.Kc = N;
         g.pairs = (int32_t)d.pairs(); g.groups = 2;
         g.out[0] = dX;
         g.part = o.part;
         const Cut cut = d.rows_cut();
         if ((st = launch_tile<kRows>(g, cut, d.bf16, none, s, "fastgl_gated_bwd (dX)")) != FASTGL_OK) return st;
-        if (cut.slabs > 1 && (st = sum_slabs(o.part, cut, M * K, M * K, d.bf16, dX, s, "fastgl_gated_bwd (dX, sum of slabs)")) != FASTGL_OK) return st;
+        if (cut.slabs > 1) {
+            SumArgs a = {};
+            a.part = o.part; a.out[0] = dX;
+            a.n = a.stride = M * K;
+            a.slabs = (int32_t)cut.slabs; a.results = 1;
+            if ((st = launch_sum(a, d.bf16, s, "fastgl_gated_bwd (dX, sums)")) != FASTGL_OK) return st;
+        }
     }
     if (want_w) {
         if (d.pack_x() && (st = pack(d, X, M, K, d.ldk, o.x, s)) != FASTGL_OK) return st;
         TileArgs g = {};
         g.a[0] = d.pack_x() ? o.x : (const uint16_t *)X;
         g.b[0] = o.dg; g.b[1] = o.du;
-        g.a_plane = M * d.ldk; g.b_plane = M * d.ldn;
-        g.lda = d.ldk; g.ldb = d.ldn;
+        g.a_plane = M * d.ldk; g.b_plane = M * d.ldz;
+        g.lda = d.ldk; g.ldb = d.ldz;
         g.R = K; g.C = N; g.Kc = M;
         g.pairs = (int32_t)d.pairs(); g.groups = 1;
         g.out[0] = dWg; g.out[1] = dWu;
         g.part = o.part;
         const Cut cut = d.weights_cut();
         if ((st = launch_tile<kWeights>(g, cut, d.bf16, none, s, "fastgl_gated_bwd (dW)")) != FASTGL_OK) return st;
-        if (cut.slabs > 1)
-            for (int q = 0; q < 2; ++q) {
-                void *out = q ? dWu : dWg;
-                if (out && (st = sum_slabs(o.part + q * K * N, cut, 2 * K * N, K * N, d.bf16, out, s, "fastgl_gated_bwd (dW, sum of slabs)")) != FASTGL_OK)
-                    return st;
-            }
+        if (cut.slabs > 1) {
+            last.part = o.part;
+            last.out[0] = dWg; last.out[1] = dWu;
+            last.n = K * N; last.stride = 2 * K * N;
+            last.slabs = (int32_t)cut.slabs; last.results = 2;
+        }
     }
+    if (want_b || last.results) return launch_sum(last, d.bf16, s, "fastgl_gated_bwd (sums)");
     return FASTGL_OK;
 }
 

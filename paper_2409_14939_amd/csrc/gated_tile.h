@@ -115,7 +115,8 @@ __device__ __forceinline__ int twisted(int row) { return (row >> 2) & 3; }
 
 namespace {
 
-template <int MODE, int SIZE, class OUT, int ACT, bool PART>
+// PART: sums of a slab instead of results.  ONCE: whole lines of results go past the caches.
+template <int MODE, int SIZE, class OUT, int ACT, bool PART, bool ONCE>
 __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(TileArgs g)
 {
 #ifdef __HIP_DEVICE_COMPILE__                    // the host pass makes no launch stub of a body with these builtins
@@ -299,9 +300,9 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
         __builtin_amdgcn_sched_barrier(0);
     };
 
-    // A step multiplies what lies in its buffer.  Its barrier says that everybody's loads of the next step have arrived, so
-    // that the first fragments of that one are read before the next barrier and matrix instructions follow at once; the loads
-    // that the step begins go where the step before it was, and have BUFS - 2 steps to arrive.
+    // A step multiplies what lies in its buffer, in two halves.  Between them is its barrier: everybody has read the buffer,
+    // and everybody's loads of the next step have arrived, so that the next step's first fragments are read during the second half.
+    // The loads that a step begins go where the step before it was, and have BUFS - 3/2 steps to arrive.
     constexpr int IN_FLIGHT = T::LA + T::LB;                 // loads of a step
     if (all > 0) {
         begin_segment();
@@ -312,28 +313,23 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
         __builtin_amdgcn_s_barrier();
         Frags f = read(0, 0);
         int now = 0;                                         // bytes to the step's buffer
-        auto step = [&]() {
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_sched_barrier(0);
+        auto step = [&](auto arrived) {
             load_next();
             __builtin_amdgcn_sched_barrier(0);
             const Frags n = read(now, 1);
             multiply(f);
             interleave();
+            __builtin_amdgcn_s_waitcnt(decltype(arrived)::value);       // and lgkmcnt 0: the fragments are here
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
             now = now == (T::BUFS - 1) * T::STAGE ? 0 : now + T::STAGE;
             f = read(now, 0);                                // of no use after the last step
             multiply(n);
             interleave();
         };
         int s = 0;
-        for (; s < all - (T::BUFS - 2); ++s) {
-            __builtin_amdgcn_s_waitcnt(0x0F70 | (T::BUFS - 3) * IN_FLIGHT);      // the next step has arrived
-            step();
-        }
-        for (; s < all; ++s) {
-            __builtin_amdgcn_s_waitcnt(0x0F70);
-            step();
-        }
+        for (; s < all - (T::BUFS - 1); ++s) step(std::integral_constant<int, 0x0070 | (T::BUFS - 2) * IN_FLIGHT>());
+        for (; s < all; ++s) step(std::integral_constant<int, 0x0070>());
     }
 
     // ------------------------------------------------------------------ epilogue
@@ -386,7 +382,9 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
 #pragma unroll
             for (int n = 0; n < ROUNDS; ++n, o += down) {
                 const u32x4 v = piece(n);
-                *reinterpret_cast<W4 *>(reinterpret_cast<char *>(base) + o) = W4{v[0], v[1], v[2], v[3]};
+                W4 *p = reinterpret_cast<W4 *>(reinterpret_cast<char *>(base) + o);
+                if constexpr (ONCE) __builtin_nontemporal_store(W4{v[0], v[1], v[2], v[3]}, p);
+                else *p = W4{v[0], v[1], v[2], v[3]};
             }
         } else {
             const int64_t left = g.C - c_base - c * PER;
