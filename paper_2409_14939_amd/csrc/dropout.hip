@@ -78,18 +78,19 @@ struct Gather8Args {
     const int64_t *ids;
     int64_t n;
     int32_t F;
-    int32_t slices;                 // of 16 columns a row
+    int32_t slices;                 // of 16 bytes a row of the result
     int32_t lg;                     // 2^lg lanes a row
     void *out;
 };
 
-// Sixteen columns of one row (rows of 16 and more: the last slice starts 16 before the row's end, and what two
-// slices share is written twice alike; shorter rows: column by column).
+// A lane writes 16 bytes of a row: V columns.  In rows of V and more the last slice starts V before the row's end, and
+// what two slices share is written twice alike; shorter rows go column by column.
 template <bool BF16, bool SHORT>
 __global__ __launch_bounds__(kBlock) void k_gather_e4m3(Gather8Args a)
 {
-    typedef uint32_t bytes16 __attribute__((ext_vector_type(4), aligned(1)));
+    typedef uint32_t bytes4 __attribute__((aligned(1)));
     typedef typename Chunk<BF16>::elem T;
+    constexpr int V = 16 / (int)sizeof(T);
     const int64_t row = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> a.lg;
     if (row >= a.n) return;
     const int lanes = 1 << a.lg;
@@ -107,21 +108,24 @@ __global__ __launch_bounds__(kBlock) void k_gather_e4m3(Gather8Args a)
         }
     } else {
         for (int c = threadIdx.x & (lanes - 1); c < a.slices; c += lanes) {
-            const int col = c * 16 < a.F - 16 ? c * 16 : a.F - 16;
-            bytes16 w = {0u, 0u, 0u, 0u};
-            if (there) w = *reinterpret_cast<const bytes16 *>(q + col);
-            float v[2][8];
+            const int col = c * V < a.F - V ? c * V : a.F - V;
+            uint32_t w[V / 4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < V / 4; ++i) w[i] = there ? *reinterpret_cast<const bytes4 *>(q + col + 4 * i) : 0u;
+            float v[V];
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i) {
                 const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
-                float *o = v[i / 2] + 4 * (i % 2);
-                o[0] = lo[0] * scale;
-                o[1] = lo[1] * scale;
-                o[2] = hi[0] * scale;
-                o[3] = hi[1] * scale;
+                v[4 * i] = lo[0] * scale;
+                v[4 * i + 1] = lo[1] * scale;
+                v[4 * i + 2] = hi[0] * scale;
+                v[4 * i + 3] = hi[1] * scale;
             }
-            Chunk<BF16>::store(out + col, v[0], 8);
-            Chunk<BF16>::store(out + col + 8, v[1], 8);
+            if constexpr (BF16) {
+                Chunk<true>::store(out + col, v, 8);
+            } else
+                *reinterpret_cast<Words<4>::x4 *>(out + col) =
+                    Words<4>::x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
         }
     }
 }
@@ -213,8 +217,9 @@ fastgl_status fastgl_gather_rows_e4m3(const uint8_t *table, const float *scale, 
     Gather8Args a = {};
     a.table = table; a.scale = scale; a.table_rows = table_rows;
     a.ids = ids; a.n = n; a.F = (int32_t)F; a.out = out;
-    a.slices = (int32_t)ceil_div(F, 16);
-    const int64_t units = F < 16 ? F : a.slices;
+    const int64_t V = dtype == FASTGL_BF16 ? 8 : 4;
+    a.slices = (int32_t)ceil_div(F, V);
+    const int64_t units = F < V ? F : a.slices;
     while (a.lg < 6 && ((int64_t)1 << a.lg) < units) ++a.lg;
     const int64_t blocks = ceil_div(n << a.lg, kBlock);
     if (blocks > 0x7FFFFFFFLL) {
@@ -222,8 +227,8 @@ fastgl_status fastgl_gather_rows_e4m3(const uint8_t *table, const float *scale, 
         return FASTGL_ERR_UNSUPPORTED;
     }
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, (hipStream_t)stream, a); };
-    if (dtype == FASTGL_BF16) F < 16 ? go(k_gather_e4m3<true, true>) : go(k_gather_e4m3<true, false>);
-    else F < 16 ? go(k_gather_e4m3<false, true>) : go(k_gather_e4m3<false, false>);
+    if (dtype == FASTGL_BF16) F < V ? go(k_gather_e4m3<true, true>) : go(k_gather_e4m3<true, false>);
+    else F < V ? go(k_gather_e4m3<false, true>) : go(k_gather_e4m3<false, false>);
     FASTGL_LAUNCH_CHECK("fastgl_gather_rows_e4m3");
     return FASTGL_OK;
 }
