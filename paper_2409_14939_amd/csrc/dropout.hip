@@ -48,10 +48,10 @@ __global__ __launch_bounds__(kBlock) void k_dropout(DropArgs a)
         left[i] = row < a.M ? a.F - col : 0;
     }
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) x[i].load(static_cast<const T *>(a.X) + at[i], left[i]);
+    for (int i = 0; i < kUnits; ++i) load_row(x[i], static_cast<const T *>(a.X), at[i], left[i], a.M * a.F);
     if (a.R) {
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) r[i].load(static_cast<const T *>(a.R) + at[i], left[i]);
+        for (int i = 0; i < kUnits; ++i) load_row(r[i], static_cast<const T *>(a.R), at[i], left[i], a.M * a.F);
     }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {

@@ -58,8 +58,10 @@ __global__ __launch_bounds__(kBlock) void k_gated_pack(const void *src, int64_t 
         const int col = (int)(u - row * chunks) * kChunk;
         Chunk<BF16> c;
         float v[8];
-        c.load(static_cast<const T *>(src) + row * cols + col, cols - col);
+        load_row(c, static_cast<const T *>(src), row * cols + col, cols - col, rows * cols);
         c.get(v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < cols - col ? v[j] : 0.f;
         store_planes<BF16 ? 1 : 3>(out + row * ld + col, rows * ld, v);
     }
 }
@@ -164,6 +166,7 @@ __global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
     const int lanes = 1 << a.lg, c = threadIdx.x & (lanes - 1), rows = kBlock >> a.lg;
     const int col = (int)(blockIdx.x * lanes + c) * kChunk, left = a.N - col;
     const T *G = static_cast<const T *>(a.G), *U = static_cast<const T *>(a.U), *dP = static_cast<const T *>(a.dP);
+    const int64_t end = a.M * a.N;
     float sg[8], su[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) sg[j] = su[j] = 0.f;
@@ -172,9 +175,9 @@ __global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
             const int64_t at = row * a.N + col;
             Chunk<BF16> qg, qu, qp;
             float g[8], u[8], p[8];
-            qg.load(G + at, left);
-            qu.load(U + at, left);
-            qp.load(dP + at, left);
+            load_row(qg, G, at, left, end);
+            load_row(qu, U, at, left, end);
+            load_row(qp, dP, at, left, end);
             qg.get(g);
             qu.get(u);
             qp.get(p);

@@ -42,6 +42,13 @@ struct NormBwdArgs {
     float *part;               // [workgroups][F] column sums of dY n, or NULL
 };
 
+// What load_row() read beyond the row counts as 0.
+__device__ __forceinline__ void only(float (&v)[8], int left)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < left ? v[j] : 0.f;
+}
+
 struct Plus {
     __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
 };
@@ -103,20 +110,21 @@ __global__ __launch_bounds__(kBlock) void k_norm(NormArgs a)
         q.load(a.w + col, F - col);
         q.get(w[c]);
     }
-    const int64_t step = (int64_t)gridDim.x * ROWS;
+    const int64_t step = (int64_t)gridDim.x * ROWS, end = a.M * F;
+    const bool ragged = F % kChunk != 0;
     for (int64_t row = (int64_t)blockIdx.x * ROWS + (threadIdx.x >> LG); row < a.M; row += step) {
         const int64_t at = row * F;
         Chunk<BF16> x[NC], r[NC];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int col = (c * LANES + lane) * kChunk;
-            x[c].load(X + at + col, F - col);
+            load_row(x[c], X, at + col, F - col, end);
         }
         if (R) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (c * LANES + lane) * kChunk;
-                r[c].load(R + at + col, F - col);
+                load_row(r[c], R, at + col, F - col, end);
             }
         }
         float h[NC][8], sq = 0.f;
@@ -133,6 +141,7 @@ __global__ __launch_bounds__(kBlock) void k_norm(NormArgs a)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h[c][j] += v[j];
             }
+            if (ragged) only(h[c], F - col);
             if (a.sum_out) Chunk<BF16>::store(static_cast<T *>(a.sum_out) + at + col, h[c], F - col);
 #pragma unroll
             for (int j = 0; j < 8; ++j) sq = fmaf(h[c][j], h[c][j], sq);
@@ -269,7 +278,8 @@ __global__ __launch_bounds__(kBlock) void k_norm_bwd(NormBwdArgs a)
 #pragma unroll
         for (int j = 0; j < 8; ++j) dw[c][j] = 0.f;
     }
-    const int64_t step = (int64_t)gridDim.x * ROWS;
+    const int64_t step = (int64_t)gridDim.x * ROWS, end = a.M * F;
+    const bool ragged = F % kChunk != 0;
     for (int64_t row = (int64_t)blockIdx.x * ROWS + (threadIdx.x >> LG); row < a.M; row += step) {
         const int64_t at = row * F;
         Chunk<BF16> qs[NC], qy[NC], qd[NC];
@@ -277,14 +287,14 @@ __global__ __launch_bounds__(kBlock) void k_norm_bwd(NormBwdArgs a)
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int col = (c * LANES + lane) * kChunk;
-            qs[c].load(S + at + col, F - col);
-            qy[c].load(dY + at + col, F - col);
+            load_row(qs[c], S, at + col, F - col, end);
+            load_row(qy[c], dY, at + col, F - col, end);
         }
         if (dS) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (c * LANES + lane) * kChunk;
-                qd[c].load(dS + at + col, F - col);
+                load_row(qd[c], dS, at + col, F - col, end);
             }
         }
         float n[NC][8], t[NC][8], dot = 0.f;
@@ -292,6 +302,10 @@ __global__ __launch_bounds__(kBlock) void k_norm_bwd(NormBwdArgs a)
         for (int c = 0; c < NC; ++c) {
             qs[c].get(n[c]);
             qy[c].get(t[c]);
+            if (ragged) {
+                only(n[c], F - (c * LANES + lane) * kChunk);
+                only(t[c], F - (c * LANES + lane) * kChunk);
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 n[c][j] *= rstd;
@@ -477,9 +491,13 @@ bool spread(int64_t F, GO go)
     if (chunks <= 1) return is(integral_constant<int, 0>(), integral_constant<int, 1>());
     if (chunks <= 8) return is(integral_constant<int, 3>(), integral_constant<int, 1>());
     if (chunks <= 16) return is(integral_constant<int, 4>(), integral_constant<int, 1>());
+    if (chunks <= 24) return is(integral_constant<int, 3>(), integral_constant<int, 3>());
     if (chunks <= 32) return is(integral_constant<int, 5>(), integral_constant<int, 1>());
+    if (chunks <= 48) return is(integral_constant<int, 4>(), integral_constant<int, 3>());
     if (chunks <= 64) return is(integral_constant<int, 6>(), integral_constant<int, 1>());
+    if (chunks <= 96) return is(integral_constant<int, 5>(), integral_constant<int, 3>());
     if (chunks <= 128) return is(integral_constant<int, 6>(), integral_constant<int, 2>());
+    if (chunks <= 192) return is(integral_constant<int, 6>(), integral_constant<int, 3>());
     if (chunks <= 256) return is(integral_constant<int, 8>(), integral_constant<int, 1>());
     if (chunks <= 512) return is(integral_constant<int, 8>(), integral_constant<int, 2>());
     if (chunks <= 1024) return is(integral_constant<int, 8>(), integral_constant<int, 4>());
@@ -493,13 +511,12 @@ int rows_per_group(int64_t F)
     return rows;
 }
 
-// Workgroups of the backward pass that leave column sums: a group of lanes has eight rows at least, so that the sums are
-// little beside the rows.
+// Workgroups of the backward pass that leave column sums: one has eight rows at least, so that the sums are little beside the
+// rows, unless that leaves compute units without one.
 int64_t bwd_groups(int64_t M, int64_t F)
 {
-    const int64_t most = ceil_div(M, rows_per_group(F)), some = ceil_div(most, 8);
-    const int64_t least = most < 256 ? most : 256;
-    const int64_t n = some > least ? some : least;
+    const int64_t most = ceil_div(M, rows_per_group(F)), some = ceil_div(M, 8);
+    const int64_t enough = some > 256 ? some : 256, n = most < enough ? most : enough;
     return n < kMaxGroupsOfRows ? n : kMaxGroupsOfRows;
 }
 

@@ -170,6 +170,15 @@ struct Chunk<false> {
     }
 };
 
+// A chunk of a row that begins at element `at` of an array of `end`: a row's last chunk is read beyond the row, as one
+// word, where the array goes on, and masked where it is used (not here: nothing should wait for the load yet); by load() only at
+// the array's end.  us a call, by load() throughout / so: gradient of the plain norm of 115 000 bf16 rows of 602 116 / 94.
+template <class C, class T>
+__device__ __forceinline__ void load_row(C &c, const T *p, int64_t at, int left, int64_t end)
+{
+    c.load(p + at, left > 0 && at + kChunk <= end ? kChunk : left);
+}
+
 // Host side of a dropout probability: false where it is not in [0, 1].
 inline bool drop_constants(double p, uint32_t *threshold, float *scale)
 {
