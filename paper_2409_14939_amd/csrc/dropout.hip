@@ -30,6 +30,7 @@ __global__ __launch_bounds__(kBlock) void k_dropout(DropArgs a)
     const uint64_t first = (uint64_t)blockIdx.x * (kBlock * kUnits);
     const int64_t row0 = (int64_t)(first / (uint32_t)a.chunks);
     const uint32_t c0 = (uint32_t)(first - (uint64_t)row0 * (uint32_t)a.chunks);
+    const bool inside = first + kBlock * kUnits + kChunk <= (uint64_t)a.M * (uint32_t)a.chunks;      // units follow, of an element at least
     Chunk<BF16> x[kUnits], r[kUnits];
     int64_t at[kUnits];
     uint32_t rows[kUnits], cs[kUnits];
@@ -48,10 +49,10 @@ __global__ __launch_bounds__(kBlock) void k_dropout(DropArgs a)
         left[i] = row < a.M ? a.F - col : 0;
     }
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) load_row(x[i], static_cast<const T *>(a.X), at[i], left[i], a.M * a.F);
+    for (int i = 0; i < kUnits; ++i) load_row(x[i], static_cast<const T *>(a.X), at[i], left[i], inside);
     if (a.R) {
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) load_row(r[i], static_cast<const T *>(a.R), at[i], left[i], a.M * a.F);
+        for (int i = 0; i < kUnits; ++i) load_row(r[i], static_cast<const T *>(a.R), at[i], left[i], inside);
     }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {

@@ -11,7 +11,11 @@
 namespace fastgl {
 namespace {
 
-constexpr int64_t kFewRows = 16;       // k_gated_rows up to here
+// Rows that k_gated_rows takes: fewer where the tiles need no packed operands.  us a call, k_gated_rows / tiles:
+//   bf16, nothing to pack: 256 -> 1024 1 row 5.5 / 5.7, 16 rows 5.5 / 5.7, 32 rows 8.0 / 5.8; 1024 -> 4096 1 row 7.4 / 10.5, 8 rows
+//   10.1 / 11.0, 16 rows 14.6 / 11.3;   float32: 256 -> 1024 1 row 5.4 / 19, 32 rows 8.3 / 20; 1024 -> 4096 1 row 9.4 / 40, 32 rows
+//   25 / 41, 64 rows 43 / 53
+constexpr int64_t kFewRows = 8, kFewRowsPacked = 48;
 constexpr int kSumGroups = 2048;       // workgroups of the gradient of the gate
 constexpr int64_t kMostWidth = (int64_t)1 << 20;
 
@@ -46,11 +50,23 @@ __device__ __forceinline__ void store_planes(uint16_t *p, int64_t plane, const f
 }
 
 // ------------------------------------------------------------------------------------ packing
-// A matrix [rows][cols] as planes of bf16 with rows of ld elements, 0 beyond cols.
+// Matrices [rows][cols] as planes of bf16 with rows of ld elements, 0 beyond cols.
+struct PackArgs {
+    const void *src[3];
+    uint16_t *out[3];
+    int64_t rows[3];
+    int32_t cols[3], ld[3];
+};
+
 template <bool BF16>
-__global__ __launch_bounds__(kBlock) void k_gated_pack(const void *src, int64_t rows, int32_t cols, int32_t ld, uint16_t *out)
+__global__ __launch_bounds__(kBlock) void k_gated_pack(PackArgs a)
 {
     typedef typename Chunk<BF16>::elem T;
+    const int m = blockIdx.y;
+    const T *src = static_cast<const T *>(m == 0 ? a.src[0] : m == 1 ? a.src[1] : a.src[2]);
+    uint16_t *out = m == 0 ? a.out[0] : m == 1 ? a.out[1] : a.out[2];
+    const int64_t rows = m == 0 ? a.rows[0] : m == 1 ? a.rows[1] : a.rows[2];
+    const int32_t cols = m == 0 ? a.cols[0] : m == 1 ? a.cols[1] : a.cols[2], ld = m == 0 ? a.ld[0] : m == 1 ? a.ld[1] : a.ld[2];
     const int32_t chunks = ld / kChunk;
     const int64_t n = rows * chunks;
     for (int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x; u < n; u += (int64_t)gridDim.x * kBlock) {
@@ -58,7 +74,9 @@ __global__ __launch_bounds__(kBlock) void k_gated_pack(const void *src, int64_t 
         const int col = (int)(u - row * chunks) * kChunk;
         Chunk<BF16> c;
         float v[8];
-        load_row(c, static_cast<const T *>(src), row * cols + col, cols - col, rows * cols);
+        const int64_t wave_u = u - (threadIdx.x & (kWave - 1));
+        const bool inside = __builtin_amdgcn_readfirstlane((int)(wave_u + kWave + kChunk <= n));
+        load_row(c, src, row * cols + col, cols - col, inside);
         c.get(v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = j < cols - col ? v[j] : 0.f;
@@ -71,78 +89,102 @@ struct RowsArgs {
     const void *X, *Wg, *Wu;
     const float *bg, *bu;
     void *P, *G, *U;
-    int32_t M, K, N, lg;             // 2^lg lanes of eight columns a strip
+    int32_t M, K, N, act;
+    int32_t strips, groups;          // strips of columns, groups of rows
 };
 
-// MR rows of a strip of columns by one workgroup: every lane has eight columns of both weights and every n-th k; the sums
-// of a column are joined through the lanes of a wavefront, then through LDS, in a fixed order.
-template <bool BF16, int ACT, int MR>
+// Sums v[0 .. N) over the lanes that differ in the bits O, O / 2, ... FROM: at each bit a lane keeps one half of what it holds and
+// gives the other away, so that N - 1 exchanges (not N for each bit) are enough.  A lane ends with N FROM / 64 values (one at
+// least), of the returned index onwards.
+template <int N, int O, int FROM, int NV>
+__device__ __forceinline__ int scatter_sum(float (&v)[NV], int lane)
+{
+    if constexpr (O < FROM) {
+        return 0;
+    } else if constexpr (N > 1) {
+        const bool up = lane & O;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const float give = up ? v[i] : v[i + N / 2], keep = up ? v[i + N / 2] : v[i];
+            v[i] = keep + __shfl_xor(give, O, kWave);
+        }
+        return (up ? N / 2 : 0) + scatter_sum<N / 2, O / 2, FROM>(v, lane);
+    } else {
+        v[0] += __shfl_xor(v[0], O, kWave);
+        return scatter_sum<1, O / 2, FROM>(v, lane);
+    }
+}
+
+// MR rows of a strip of columns by one workgroup: 2^LG lanes hold eight columns of both weights each, the lanes beyond them
+// the next k; the sums of a column are joined through the lanes of a wavefront, then through LDS, in a fixed order.
+// Bound by the weights: neighbouring strips, which share lines, are given to one L2 domain.
+template <bool BF16, int MR, int LG>
 __global__ __launch_bounds__(kBlock) void k_gated_rows(RowsArgs a)
 {
     typedef typename Chunk<BF16>::elem T;
-    const int lanes = 1 << a.lg, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int c = threadIdx.x & (lanes - 1), col = (int)(blockIdx.x * lanes + c) * kChunk, left = a.N - col;
-    const int m0 = blockIdx.y * MR;
+    constexpr int LANES = 1 << LG, SLOTS = kBlock >> LG, NV = MR * 16, LEFT = NV * LANES > kWave ? NV * LANES / kWave : 1;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    uint32_t at = blockIdx.x;
+    {
+        const uint32_t total = (uint32_t)a.strips * (uint32_t)a.groups, q = total / kXcds, rest = total % kXcds, x = at % kXcds;
+        at = x * q + (x < rest ? x : rest) + at / kXcds;
+    }
+    const int strip = (int)(at / (uint32_t)a.groups), m0 = (int)(at - (uint32_t)strip * (uint32_t)a.groups) * MR;
+    const int c = threadIdx.x & (LANES - 1), col = (strip * LANES + c) * kChunk, left = a.N - col;
     const T *X = static_cast<const T *>(a.X), *Wg = static_cast<const T *>(a.Wg), *Wu = static_cast<const T *>(a.Wu);
-    float sg[MR][8], su[MR][8];
+    float v[NV];                                                     // [row][gate, up][column]
 #pragma unroll
-    for (int m = 0; m < MR; ++m)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sg[m][j] = su[m][j] = 0.f;
-    const int slots = kBlock >> a.lg;
+    for (int i = 0; i < NV; ++i) v[i] = 0.f;
 #pragma unroll 4
-    for (int k = threadIdx.x >> a.lg; k < a.K; k += slots) {
+    for (int k = threadIdx.x >> LG; k < a.K; k += SLOTS) {
+        const bool inside = k - (int)(threadIdx.x >> LG) + wave_first(LG) + (kWave >> LG) + kChunk <= a.K;
         Chunk<BF16> qg, qu;
         float g[8], u[8];
-        qg.load(Wg + (int64_t)k * a.N + col, left);
-        qu.load(Wu + (int64_t)k * a.N + col, left);
+        load_row(qg, Wg, (int64_t)k * a.N + col, left, inside);       // columns that do not exist are summed and not stored
+        load_row(qu, Wu, (int64_t)k * a.N + col, left, inside);
+        float x[MR];
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+            const int64_t row = m0 + m < a.M ? m0 + m : a.M - 1;
+            if constexpr (BF16) x[m] = __uint_as_float((uint32_t)X[row * a.K + k] << 16);
+            else x[m] = X[row * a.K + k];
+        }
         qg.get(g);
         qu.get(u);
 #pragma unroll
-        for (int m = 0; m < MR; ++m) {
-            const int row = m0 + m < a.M ? m0 + m : a.M - 1;
-            float x;
-            if constexpr (BF16) x = __uint_as_float((uint32_t)X[(int64_t)row * a.K + k] << 16);
-            else x = X[(int64_t)row * a.K + k];
+        for (int m = 0; m < MR; ++m)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                sg[m][j] = fmaf(x, g[j], sg[m][j]);
-                su[m][j] = fmaf(x, u[j], su[m][j]);
+                v[m * 16 + j] = fmaf(x[m], g[j], v[m * 16 + j]);
+                v[m * 16 + 8 + j] = fmaf(x[m], u[j], v[m * 16 + 8 + j]);
             }
-        }
     }
-    __shared__ float sums[kBlock / kWave][MR][2][8 * 8];
-    for (int o = lanes; o < kWave; o <<= 1)
+    __shared__ float sums[kBlock / kWave][LANES][NV];
+    const int first = scatter_sum<NV, kWave / 2, LANES>(v, lane);
 #pragma unroll
-        for (int m = 0; m < MR; ++m)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                sg[m][j] += __shfl_xor(sg[m][j], o, kWave);
-                su[m][j] += __shfl_xor(su[m][j], o, kWave);
-            }
-    if (lane < lanes)
-#pragma unroll
-        for (int m = 0; m < MR; ++m)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                sums[wave][m][0][c * 8 + j] = sg[m][j];
-                sums[wave][m][1][c * 8 + j] = su[m][j];
-            }
+    for (int i = 0; i < LEFT; ++i) sums[wave][c][first + i] = v[i];
     __syncthreads();
-    for (int i = threadIdx.x; i < MR * lanes * 8; i += kBlock) {
-        const int m = i / (lanes * 8), j = i - m * lanes * 8, row = m0 + m;
-        const int64_t n = (int64_t)blockIdx.x * lanes * 8 + j;
+    for (int i = threadIdx.x; i < MR * LANES * 8; i += kBlock) {
+        const int m = i / (LANES * 8), j = i - m * (LANES * 8), row = m0 + m, e = m * 16 + (j & 7), l = j >> 3;
+        const int64_t n = (int64_t)strip * (LANES * 8) + j;
         if (row >= a.M || n >= a.N) continue;
-        float g = (sums[0][m][0][j] + sums[1][m][0][j]) + (sums[2][m][0][j] + sums[3][m][0][j]);
-        float u = (sums[0][m][1][j] + sums[1][m][1][j]) + (sums[2][m][1][j] + sums[3][m][1][j]);
+        float g = (sums[0][l][e] + sums[1][l][e]) + (sums[2][l][e] + sums[3][l][e]);
+        float u = (sums[0][l][e + 8] + sums[1][l][e + 8]) + (sums[2][l][e + 8] + sums[3][l][e + 8]);
         if (a.bg) g += a.bg[n];
         if (a.bu) u += a.bu[n];
-        const int64_t at = (int64_t)row * a.N + n;
-        auto put = [&](void *out, float v) {
-            if constexpr (BF16) static_cast<T *>(out)[at] = __builtin_bit_cast(uint16_t, (__bf16)v);
-            else static_cast<T *>(out)[at] = v;
+        const int64_t to = (int64_t)row * a.N + n;
+        auto put = [&](void *out, float x) {
+            if constexpr (BF16) static_cast<T *>(out)[to] = __builtin_bit_cast(uint16_t, (__bf16)x);
+            else static_cast<T *>(out)[to] = x;
         };
-        put(a.P, gate<ACT, false>(g, nullptr) * u);
+        float act;
+        switch (a.act) {
+            case FASTGL_ACT_SILU: act = gate<FASTGL_ACT_SILU, false>(g, nullptr); break;
+            case FASTGL_ACT_GELU: act = gate<FASTGL_ACT_GELU, false>(g, nullptr); break;
+            case FASTGL_ACT_RELU: act = gate<FASTGL_ACT_RELU, false>(g, nullptr); break;
+            default: act = gate<FASTGL_ACT_SIGMOID, false>(g, nullptr); break;
+        }
+        put(a.P, act * u);
         if (a.G) put(a.G, g);
         if (a.U) put(a.U, u);
     }
@@ -166,18 +208,18 @@ __global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
     const int lanes = 1 << a.lg, c = threadIdx.x & (lanes - 1), rows = kBlock >> a.lg;
     const int col = (int)(blockIdx.x * lanes + c) * kChunk, left = a.N - col;
     const T *G = static_cast<const T *>(a.G), *U = static_cast<const T *>(a.U), *dP = static_cast<const T *>(a.dP);
-    const int64_t end = a.M * a.N;
     float sg[8], su[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) sg[j] = su[j] = 0.f;
     if (left > 0) {
         for (int64_t row = (int64_t)blockIdx.y * rows + (threadIdx.x >> a.lg); row < a.M; row += (int64_t)gridDim.y * rows) {
             const int64_t at = row * a.N + col;
+            const bool inside = row - (threadIdx.x >> a.lg) + wave_first(a.lg) + (kWave >> a.lg) + kChunk <= a.M;
             Chunk<BF16> qg, qu, qp;
             float g[8], u[8], p[8];
-            load_row(qg, G, at, left, end);
-            load_row(qu, U, at, left, end);
-            load_row(qp, dP, at, left, end);
+            load_row(qg, G, at, left, inside);
+            load_row(qu, U, at, left, inside);
+            load_row(qp, dP, at, left, inside);
             qg.get(g);
             qu.get(u);
             qp.get(p);
@@ -294,15 +336,17 @@ struct Cut {
     int64_t slabs;
 };
 
-// The cut that a model of the launch finds fastest.  A compute unit needs `step_us` for a step of a tile, whether it has one
-// or two workgroups at a time, and `tile_us` for what is around the steps; slabs cost the sums that they write and that are read
-// again, and a launch.  Measured (kernel times, bf16, us for large / middle / small tiles):
+// The cut that a model of the launch finds fastest.  A compute unit needs single_us for a step of a workgroup that it has alone and
+// pair_us for one of each of two (large tiles: one at a time), and tile_us for what is around the steps; slabs cost the sums that they
+// write and that are read again (4 bytes each way at some 6 TB/s), and a launch.
+// Measured (kernel times, bf16, us for large / middle / small tiles):
 //   forward 16 384 x 1024 -> 4096, G and U kept 271 / 268 / -, alone 227 / 240 / -;  115 000 x 256 -> 1024 196 / 186 / -, 154 / 139 / -
 //   dX 16 384 x 4096 -> 1024 242 / 284 / 344;  dWg, dWu of 16 384 rows 1024 x 4096 206 / 240 / 416 (the first two in two slabs)
 //   backward call of 300 rows 256 -> 1024 33 / 29 / 27, of 2000 rows 56 / 51 / 47, of 8000 rows 256 -> 683 79 / 72 / 76
 Cut cut_of(int mode, int64_t R, int64_t C, int64_t Kc, int64_t segments)
 {
-    static const double step_us[3][3] = {{0.80, 0.46, 0.32}, {0.93, 0.55, 0.34}, {0.80, 0.46, 0.40}};
+    static const double single_us[3][3] = {{0.80, 0.60, 0.36}, {0.93, 0.65, 0.38}, {0.80, 0.60, 0.42}};      // [mode][size]
+    static const double pair_us[3][3] = {{1.60, 0.92, 0.64}, {1.86, 1.10, 0.70}, {1.60, 0.92, 0.80}};
     static const double tile_us[2][3] = {{6.0, 2.6, 1.6}, {4.0, 2.0, 1.2}};
     Cut best = {kLarge, 1};
     double least = 1e300;
@@ -311,8 +355,10 @@ Cut cut_of(int mode, int64_t R, int64_t C, int64_t Kc, int64_t segments)
         const int64_t bm = size == kLarge ? 256 : 128, bc = (size == kSmall ? 128 : 256) / (mode == kRows ? 1 : 2);
         const int64_t tiles = ceil_div(R, bm) * ceil_div(C, bc);
         for (int64_t slabs = 1; slabs <= 64 && (slabs == 1 || (all / slabs >= 4 && R * C <= (int64_t)1 << 30)); slabs = slabs < 8 ? slabs + 1 : slabs * 5 / 4) {
-            const double us = (double)ceil_div(tiles * slabs, 256) * ((double)ceil_div(all, slabs) * step_us[mode][size] + tile_us[mode != kForward][size]) +
-                              (slabs > 1 ? 5.0 + (double)slabs * (double)R * (double)C * (mode == kRows ? 8.0 : 16.0) / 4e6 : 0.0);
+            const int64_t of_unit = ceil_div(tiles * slabs, 256);
+            const double step = (double)(of_unit / 2) * pair_us[mode][size] + (double)(of_unit % 2) * single_us[mode][size];
+            const double us = (double)ceil_div(all, slabs) * step + (double)of_unit * tile_us[mode != kForward][size] +
+                              (slabs > 1 ? 4.0 + (double)slabs * (double)R * (double)C * (mode == kRows ? 1.3e-6 : 2.6e-6) : 0.0);
             if (us < least) {
                 least = us;
                 best = {size, slabs};
@@ -346,6 +392,7 @@ struct Shape {
     }
     bool pack_x() const { return !bf16 || !aligned || K % 8; }
     bool pack_w() const { return !bf16 || !aligned || N % 8; }
+    bool few_rows() const { return M <= (pack_x() || pack_w() ? kFewRowsPacked : kFewRows); }
     int64_t pairs() const { return bf16 ? 1 : 6; }
     Cut forward_cut() const { return cut_of(kForward, M, N, K, pairs()); }
     Cut rows_cut() const { return cut_of(kRows, M, K, N, 2 * pairs()); }
@@ -425,14 +472,31 @@ fastgl_status check_workspace(const void *workspace, size_t bytes, size_t need)
     return FASTGL_OK;
 }
 
-fastgl_status pack(const Shape &s, const void *src, int64_t rows, int64_t cols, int64_t ld, uint16_t *out, hipStream_t st)
+// What of X, Wg and Wu a product needs packed, in one launch.
+fastgl_status pack(const Shape &d, const Scratch &o, const void *X, const void *Wg, const void *Wu, bool x, bool w, hipStream_t st)
 {
-    if (rows == 0 || cols == 0) return FASTGL_OK;
-    const int64_t blocks = ceil_div(rows * (ld / kChunk), kBlock);
-    const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, st, src, rows, (int32_t)cols, (int32_t)ld, out); };
-    if (s.bf16) go(k_gated_pack<true>);
-    else go(k_gated_pack<false>);
+    PackArgs a = {};
+    int n = 0;
+    int64_t most = 0;
+    auto add = [&](const void *src, uint16_t *out, int64_t rows, int64_t cols, int64_t ld) {
+        if (rows == 0 || cols == 0) return;
+        a.src[n] = src;
+        a.out[n] = out;
+        a.rows[n] = rows;
+        a.cols[n] = (int32_t)cols;
+        a.ld[n++] = (int32_t)ld;
+        if (rows * (ld / kChunk) > most) most = rows * (ld / kChunk);
+    };
+    if (x && d.pack_x()) add(X, o.x, d.M, d.K, d.ldk);
+    if (w && d.pack_w()) {
+        add(Wg, o.wg, d.K, d.N, d.ldn);
+        add(Wu, o.wu, d.K, d.N, d.ldn);
+    }
+    if (n == 0) return FASTGL_OK;
+    const int64_t blocks = ceil_div(most, kBlock);
+    const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384), (unsigned)n);
+    if (d.bf16) hipLaunchKernelGGL(k_gated_pack<true>, grid, dim3(kBlock), 0, st, a);
+    else hipLaunchKernelGGL(k_gated_pack<false>, grid, dim3(kBlock), 0, st, a);
     FASTGL_LAUNCH_CHECK("fastgl_gated (pack)");
     return FASTGL_OK;
 }
@@ -505,10 +569,12 @@ bool starts_whole(std::initializer_list<const void *> ps)
 size_t workspace(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, bool aligned, bool backward)
 {
     if (check(dtype, M, K, N, FASTGL_ACT_SILU) != FASTGL_OK) return 0;
-    if (!backward && M <= kFewRows) return 0;
+    const Shape d(dtype, M, K, N, aligned);
     Layout l;
-    carve(Shape(dtype, M, K, N, aligned), backward, l);
-    return l.used;
+    if (backward || !d.few_rows()) carve(d, backward, l);
+    if (aligned) return l.used;
+    const size_t whole = workspace(dtype, M, K, N, true, backward);      // the tiles may be taken from fewer rows on
+    return l.used > whole ? l.used : whole;
 }
 
 }  // namespace
@@ -546,20 +612,34 @@ fastgl_status fastgl_gated_fwd(fastgl_dtype dtype, const void *X, const void *Wg
         return FASTGL_ERR_INVALID_ARG;
     }
     hipStream_t s = (hipStream_t)stream;
-    if (M <= kFewRows) {
-        RowsArgs a = {X, Wg, Wu, bg, bu, P, G, U, (int32_t)M, (int32_t)K, (int32_t)N, 3};
-        while (a.lg > 0 && ceil_div(N, (int64_t)8 << a.lg) < 192) --a.lg;
-        const unsigned strips = (unsigned)ceil_div(N, (int64_t)8 << a.lg);
-        by_act(act, [&](auto A) {
-            constexpr int ACT = decltype(A)::value;
-            auto go = [&](auto kernel, int rows) { hipLaunchKernelGGL(kernel, dim3(strips, (unsigned)ceil_div(M, rows)), dim3(kBlock), 0, s, a); };
-            if (dtype == FASTGL_BF16) M == 1 ? go(k_gated_rows<true, ACT, 1>, 1) : go(k_gated_rows<true, ACT, 4>, 4);
-            else M == 1 ? go(k_gated_rows<false, ACT, 1>, 1) : go(k_gated_rows<false, ACT, 4>, 4);
-        });
+    const Shape d(dtype, M, K, N, starts_whole({X, Wg, Wu}));
+    if (d.few_rows()) {
+        int lg = 3;                                     // strips as wide as leaves enough of them
+        while (lg > 0 && ceil_div(N, (int64_t)8 << lg) < 192) --lg;
+        const int rows = M == 1 ? 1 : M == 2 ? 2 : 4;
+        RowsArgs a = {X, Wg, Wu, bg, bu, P, G, U, (int32_t)M, (int32_t)K, (int32_t)N, (int32_t)act, (int32_t)ceil_div(N, (int64_t)8 << lg),
+                      (int32_t)ceil_div(M, rows)};
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(a.strips * a.groups)), dim3(kBlock), 0, s, a); };
+        auto wide = [&](auto bf16, auto mr) {
+            constexpr bool B = decltype(bf16)::value;
+            constexpr int R = decltype(mr)::value;
+            switch (lg) {
+                case 0: go(k_gated_rows<B, R, 0>); break;
+                case 1: go(k_gated_rows<B, R, 1>); break;
+                case 2: go(k_gated_rows<B, R, 2>); break;
+                default: go(k_gated_rows<B, R, 3>); break;
+            }
+        };
+        auto typed = [&](auto bf16) {
+            if (rows == 1) wide(bf16, std::integral_constant<int, 1>());
+            else if (rows == 2) wide(bf16, std::integral_constant<int, 2>());
+            else wide(bf16, std::integral_constant<int, 4>());
+        };
+        if (dtype == FASTGL_BF16) typed(std::true_type());
+        else typed(std::false_type());
         FASTGL_LAUNCH_CHECK("fastgl_gated_fwd (few rows)");
         return FASTGL_OK;
     }
-    const Shape d(dtype, M, K, N, starts_whole({X, Wg, Wu}));
     Layout l;
     carve(d, false, l);
     st = check_workspace(ws, ws_bytes, l.used);
@@ -567,11 +647,7 @@ fastgl_status fastgl_gated_fwd(fastgl_dtype dtype, const void *X, const void *Wg
     l = Layout();
     l.base = (char *)ws;
     const Scratch o = carve(d, false, l);
-    if (d.pack_x() && (st = pack(d, X, M, K, d.ldk, o.x, s)) != FASTGL_OK) return st;
-    if (d.pack_w()) {
-        if ((st = pack(d, Wg, K, N, d.ldn, o.wg, s)) != FASTGL_OK) return st;
-        if ((st = pack(d, Wu, K, N, d.ldn, o.wu, s)) != FASTGL_OK) return st;
-    }
+    if ((st = pack(d, o, X, Wg, Wu, true, true, s)) != FASTGL_OK) return st;
     TileArgs g = {};
     g.a[0] = d.pack_x() ? o.x : (const uint16_t *)X;
     g.b[0] = d.pack_w() ? o.wg : (const uint16_t *)Wg;
@@ -666,12 +742,9 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
         last.dbg = dbg; last.dbu = dbu;
         last.rows = (int32_t)dz.y; last.N = (int32_t)N;
     }
+    if ((st = pack(d, o, X, Wg, Wu, want_w, want_x, s)) != FASTGL_OK) return st;
     const std::integral_constant<int, 0> none;
     if (want_x) {
-        if (d.pack_w()) {
-            if ((st = pack(d, Wg, K, N, d.ldn, o.wg, s)) != FASTGL_OK) return st;
-            if ((st = pack(d, Wu, K, N, d.ldn, o.wu, s)) != FASTGL_OK) return st;
-        }
         TileArgs g = {};
         g.a[0] = o.dg; g.a[1] = o.du;
         g.b[0] = d.pack_w() ? o.wg : (const uint16_t *)Wg;
@@ -693,7 +766,6 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
         }
     }
     if (want_w) {
-        if (d.pack_x() && (st = pack(d, X, M, K, d.ldk, o.x, s)) != FASTGL_OK) return st;
         TileArgs g = {};
         g.a[0] = d.pack_x() ? o.x : (const uint16_t *)X;
         g.b[0] = o.dg; g.b[1] = o.du;

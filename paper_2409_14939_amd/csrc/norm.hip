@@ -110,21 +110,24 @@ __global__ __launch_bounds__(kBlock) void k_norm(NormArgs a)
         q.load(a.w + col, F - col);
         q.get(w[c]);
     }
-    const int64_t step = (int64_t)gridDim.x * ROWS, end = a.M * F;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
     const bool ragged = F % kChunk != 0;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + (threadIdx.x >> LG); row < a.M; row += step) {
+    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 + (threadIdx.x >> LG) < a.M; row0 += step) {
+        const int64_t row = row0 + (threadIdx.x >> LG);
         const int64_t at = row * F;
+        // of the rows of a wavefront, each of an element at least, the last is followed by eight
+        const bool inside = row0 + (int64_t)wave_first(LG) + (kWave >> (LG < 6 ? LG : 6)) + kChunk <= a.M;
         Chunk<BF16> x[NC], r[NC];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int col = (c * LANES + lane) * kChunk;
-            load_row(x[c], X, at + col, F - col, end);
+            load_row(x[c], X, at + col, F - col, inside);
         }
         if (R) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (c * LANES + lane) * kChunk;
-                load_row(r[c], R, at + col, F - col, end);
+                load_row(r[c], R, at + col, F - col, inside);
             }
         }
         float h[NC][8], sq = 0.f;
@@ -278,23 +281,26 @@ __global__ __launch_bounds__(kBlock) void k_norm_bwd(NormBwdArgs a)
 #pragma unroll
         for (int j = 0; j < 8; ++j) dw[c][j] = 0.f;
     }
-    const int64_t step = (int64_t)gridDim.x * ROWS, end = a.M * F;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
     const bool ragged = F % kChunk != 0;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + (threadIdx.x >> LG); row < a.M; row += step) {
+    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 + (threadIdx.x >> LG) < a.M; row0 += step) {
+        const int64_t row = row0 + (threadIdx.x >> LG);
         const int64_t at = row * F;
+        // of the rows of a wavefront, each of an element at least, the last is followed by eight
+        const bool inside = row0 + (int64_t)wave_first(LG) + (kWave >> (LG < 6 ? LG : 6)) + kChunk <= a.M;
         Chunk<BF16> qs[NC], qy[NC], qd[NC];
         const float rstd = a.rstd[row];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int col = (c * LANES + lane) * kChunk;
-            load_row(qs[c], S, at + col, F - col, end);
-            load_row(qy[c], dY, at + col, F - col, end);
+            load_row(qs[c], S, at + col, F - col, inside);
+            load_row(qy[c], dY, at + col, F - col, inside);
         }
         if (dS) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (c * LANES + lane) * kChunk;
-                load_row(qd[c], dS, at + col, F - col, end);
+                load_row(qd[c], dS, at + col, F - col, inside);
             }
         }
         float n[NC][8], t[NC][8], dot = 0.f;

@@ -170,14 +170,22 @@ struct Chunk<false> {
     }
 };
 
-// A chunk of a row that begins at element `at` of an array of `end`: a row's last chunk is read beyond the row, as one
-// word, where the array goes on, and masked where it is used (not here: nothing should wait for the load yet); by load() only at
-// the array's end.  us a call, by load() throughout / so: gradient of the plain norm of 115 000 bf16 rows of 602 116 / 94.
+// A chunk of a row, at element `at` of an array: where the array goes on for eight elements at least (`inside`, the same for a
+// whole wavefront), a row's last chunk is read beyond the row, as one word, and masked where it is used (not here: nothing should
+// wait for the load yet); by load() only at the array's end.
+// us a call, by load() throughout / so: gradient of the plain norm of 115 000 bf16 rows of 602 116 / 94.
 template <class C, class T>
-__device__ __forceinline__ void load_row(C &c, const T *p, int64_t at, int left, int64_t end)
+__device__ __forceinline__ void load_row(C &c, const T *p, int64_t at, int left, bool inside)
 {
-    c.load(p + at, left > 0 && at + kChunk <= end ? kChunk : left);
+    if (__builtin_expect(inside, 1)) {
+        c = C{};                                       // columns that do not exist: 0
+        if (left > 0) c.load(p + at, kChunk);
+    } else
+        c.load(p + at, left);
 }
+
+// The number of a wavefront's first thread, over 2^lg.
+__device__ __forceinline__ int wave_first(int lg) { return __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> lg; }
 
 // Host side of a dropout probability: false where it is not in [0, 1].
 inline bool drop_constants(double p, uint32_t *threshold, float *scale)

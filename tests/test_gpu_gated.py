@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 SENTINEL = -776.0
 U32 = ref.U32
 # rows: below, at and beyond the line of the few-rows kernel and of a tile; widths: multiples of 8 and not, below and beyond a step of 64
-SHAPES = [(1, 1, 1), (1, 256, 1024), (2, 5, 9), (3, 64, 64), (7, 100, 47), (16, 130, 200), (17, 8, 8), (17, 1, 1), (33, 7, 5), (64, 64, 64),
+SHAPES = [(1, 1, 1), (1, 256, 1024), (2, 5, 9), (3, 64, 64), (7, 100, 47), (16, 130, 200), (17, 8, 8), (17, 1, 1), (33, 7, 5), (48, 72, 80), (49, 33, 31), (64, 64, 64),
           (65, 72, 40), (100, 63, 65), (127, 128, 130), (129, 200, 48), (255, 256, 256), (257, 100, 136), (300, 602, 91), (513, 48, 700),
           (1000, 256, 683), (2100, 520, 264)]
 
@@ -182,7 +182,7 @@ def test_refusals_of_the_binding():
     with pytest.raises(KeyError):
         B.fastgl_gated_fwd(x, w, w, act="tanh")
     with pytest.raises(B.FastglError):
-        B.fastgl_gated_fwd(x, w, w, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        B.fastgl_gated_fwd(x.repeat(5, 1), w, w, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError):
         B.fastgl_gated_bwd(x, w, w, torch.ones(20, 16).cuda(), torch.ones(20, 15).cuda(), torch.ones(20, 16).cuda())
 
