@@ -358,8 +358,8 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
                     FASTGL_LDS char *p = mine + row * ROWB + piece * 16 + within;
                     if constexpr (OB == 2) {
                         u32x2 o;
-                        o[0] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[0]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[1]) << 16;
-                        o[1] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[3]) << 16;
+                        o[0] = pack_bf16(v[0], v[1]);
+                        o[1] = pack_bf16(v[2], v[3]);
                         *(FASTGL_LDS u32x2 *)p = o;
                     } else {
                         u32x4 o;

@@ -56,14 +56,25 @@ struct Max {
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
 
+// The value of another lane of the same sixteen: CTRL 0xB1 the neighbour, 0x4E the neighbour pair's, 0x141 and 0x140 the
+// mirrored place of eight and of sixteen (sums of four and of eight lanes, which their lanes all hold, meet their others).
+template <int CTRL>
+__device__ __forceinline__ float lane_of_16(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+
 // Over the 2^LG lanes of a row (LG = 8: the workgroup, through `buf`, two halves in turn so that one barrier is
 // enough); the order of the terms is fixed.
 template <int LG, class OP>
 __device__ __forceinline__ float row_reduce(float v, OP op, float (&buf)[2][4], int &turn)
 {
-    constexpr int IN = LG < 6 ? LG : 6;
-#pragma unroll
-    for (int o = 0; o < IN; ++o) v = op(v, __shfl_xor(v, 1 << o, kWave));
+    if constexpr (LG > 0) v = op(v, lane_of_16<0xB1>(v));
+    if constexpr (LG > 1) v = op(v, lane_of_16<0x4E>(v));
+    if constexpr (LG > 2) v = op(v, lane_of_16<0x141>(v));
+    if constexpr (LG > 3) v = op(v, lane_of_16<0x140>(v));
+    if constexpr (LG > 4) v = op(v, __shfl_xor(v, 16, kWave));
+    if constexpr (LG > 5) v = op(v, __shfl_xor(v, 32, kWave));
     if constexpr (LG == 8) {
         if ((threadIdx.x & (kWave - 1)) == 0) buf[turn][threadIdx.x / kWave] = v;
         __syncthreads();
@@ -112,24 +123,39 @@ __global__ __launch_bounds__(kBlock) void k_norm(NormArgs a)
     }
     const int64_t step = (int64_t)gridDim.x * ROWS;
     const bool ragged = F % kChunk != 0;
-    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 + (threadIdx.x >> LG) < a.M; row0 += step) {
-        const int64_t row = row0 + (threadIdx.x >> LG);
-        const int64_t at = row * F;
+    // the rows of a step; the next step's are under way while this one's are worked on, where registers allow
+    auto fetch = [&](int64_t row0, Chunk<BF16>(&x)[NC], Chunk<BF16>(&r)[NC]) {
+        const int64_t row = row0 + (threadIdx.x >> LG), at = row * F;
         // of the rows of a wavefront, each of an element at least, the last is followed by eight
         const bool inside = row0 + (int64_t)wave_first(LG) + (kWave >> (LG < 6 ? LG : 6)) + kChunk <= a.M;
-        Chunk<BF16> x[NC], r[NC];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int col = (c * LANES + lane) * kChunk;
-            load_row(x[c], X, at + col, F - col, inside);
+            load_row(x[c], X, at + col, row < a.M ? F - col : 0, inside);
         }
         if (R) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (c * LANES + lane) * kChunk;
-                load_row(r[c], R, at + col, F - col, inside);
+                load_row(r[c], R, at + col, row < a.M ? F - col : 0, inside);
             }
         }
+    };
+    constexpr bool AHEAD = BF16 ? NC <= 3 : NC == 1;
+    Chunk<BF16> x[NC], r[NC], next_x[NC], next_r[NC];
+    if (AHEAD) fetch((int64_t)blockIdx.x * ROWS, next_x, next_r);
+    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.M; row0 += step) {
+        const int64_t row = row0 + (threadIdx.x >> LG), at = row * F;
+        const bool live = row < a.M;                                  // no row: nothing is read or written
+        if (AHEAD) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                x[c] = next_x[c];
+                r[c] = next_r[c];
+            }
+            if (row0 + step < a.M) fetch(row0 + step, next_x, next_r);
+        } else
+            fetch(row0, x, r);
         float h[NC][8], sq = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
@@ -144,14 +170,14 @@ __global__ __launch_bounds__(kBlock) void k_norm(NormArgs a)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h[c][j] += v[j];
             }
-            if (ragged) only(h[c], F - col);
-            if (a.sum_out) Chunk<BF16>::store(static_cast<T *>(a.sum_out) + at + col, h[c], F - col);
+            if (ragged) only(h[c], live ? F - col : 0);
+            if (a.sum_out) Chunk<BF16>::store(static_cast<T *>(a.sum_out) + at + col, h[c], live ? F - col : 0);
 #pragma unroll
             for (int j = 0; j < 8; ++j) sq = fmaf(h[c][j], h[c][j], sq);
         }
         sq = row_reduce<LG>(sq, Plus(), buf, turn);
         const float rstd = 1.f / sqrtf(sq * a.inv_F + a.eps);
-        if (a.rstd && lane == 0) a.rstd[row] = rstd;
+        if (a.rstd && lane == 0 && live) a.rstd[row] = rstd;
         float most = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
@@ -163,19 +189,19 @@ __global__ __launch_bounds__(kBlock) void k_norm(NormArgs a)
         if constexpr (E4M3) {
             most = row_reduce<LG>(most, Max(), buf, turn);
             const float scale = fmaxf(most / 448.f, 0x1p-126f), inv = 1.f / scale;
-            if (lane == 0) a.row_scale[row] = scale;
+            if (lane == 0 && live) a.row_scale[row] = scale;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (c * LANES + lane) * kChunk;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h[c][j] *= inv;
-                store_e4m3(static_cast<uint8_t *>(a.Y) + at + col, h[c], F - col);
+                store_e4m3(static_cast<uint8_t *>(a.Y) + at + col, h[c], live ? F - col : 0);
             }
         } else {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (c * LANES + lane) * kChunk;
-                Chunk<BF16>::store(static_cast<T *>(a.Y) + at + col, h[c], F - col);
+                Chunk<BF16>::store(static_cast<T *>(a.Y) + at + col, h[c], live ? F - col : 0);
             }
         }
     }
@@ -283,26 +309,30 @@ __global__ __launch_bounds__(kBlock) void k_norm_bwd(NormBwdArgs a)
     }
     const int64_t step = (int64_t)gridDim.x * ROWS;
     const bool ragged = F % kChunk != 0;
-    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 + (threadIdx.x >> LG) < a.M; row0 += step) {
-        const int64_t row = row0 + (threadIdx.x >> LG);
-        const int64_t at = row * F;
-        // of the rows of a wavefront, each of an element at least, the last is followed by eight
+    auto fetch = [&](int64_t row0, Chunk<BF16>(&qs)[NC], Chunk<BF16>(&qy)[NC], Chunk<BF16>(&qd)[NC], float &rstd) {
+        const int64_t row = row0 + (threadIdx.x >> LG), at = row * F;
         const bool inside = row0 + (int64_t)wave_first(LG) + (kWave >> (LG < 6 ? LG : 6)) + kChunk <= a.M;
-        Chunk<BF16> qs[NC], qy[NC], qd[NC];
-        const float rstd = a.rstd[row];
+        rstd = row < a.M ? a.rstd[row] : 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int col = (c * LANES + lane) * kChunk;
-            load_row(qs[c], S, at + col, F - col, inside);
-            load_row(qy[c], dY, at + col, F - col, inside);
+            const int col = (c * LANES + lane) * kChunk, left = row < a.M ? F - col : 0;
+            load_row(qs[c], S, at + col, left, inside);
+            load_row(qy[c], dY, at + col, left, inside);
         }
         if (dS) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (c * LANES + lane) * kChunk;
-                load_row(qd[c], dS, at + col, F - col, inside);
+                load_row(qd[c], dS, at + col, row < a.M ? F - col : 0, inside);
             }
         }
+    };
+    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.M; row0 += step) {
+        const int64_t row = row0 + (threadIdx.x >> LG), at = row * F;
+        const bool live = row < a.M;
+        Chunk<BF16> qs[NC], qy[NC], qd[NC];
+        float rstd;
+        fetch(row0, qs, qy, qd, rstd);                               // loading a step ahead gained nothing here
         float n[NC][8], t[NC][8], dot = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
@@ -332,14 +362,14 @@ __global__ __launch_bounds__(kBlock) void k_norm_bwd(NormBwdArgs a)
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) d[j] = fmaf(rstd, t[c][j] - n[c][j] * dot, d[j]);
-            if (a.dR) Chunk<BF16>::store(static_cast<T *>(a.dR) + at + col, d, F - col);
+            if (a.dR) Chunk<BF16>::store(static_cast<T *>(a.dR) + at + col, d, live ? F - col : 0);
             if (a.dX) {
                 if constexpr (DROP) {
                     uint32_t words[4];
                     gen.words((uint32_t)(col / kChunk), (uint32_t)row, words);
                     drop8(d, words, a.threshold, a.drop_scale);
                 }
-                Chunk<BF16>::store(static_cast<T *>(a.dX) + at + col, d, F - col);
+                Chunk<BF16>::store(static_cast<T *>(a.dX) + at + col, d, live ? F - col : 0);
             }
         }
     }
