@@ -1,12 +1,23 @@
 // Dropout from the counter-based generator, with an optional addition (fastgl_norm.h has the formula), and the row
 // gather of tables held in 8 bits.  Both are one pass over memory.
+//
+// Dropout is bound by memory: 1.15 M fp32 rows of 100 take 175 us, 5.3 TB/s (a copy runs at 4.7 to 5.0 here).  An answer of the
+// generator serves eight elements: its twenty 32-bit products take about as long as the moves of eight bf16, and fit beside them.
+// A workgroup has consecutive chunks whatever the rows' length, four a lane under way at once.
+//
+// The gather is bound by its random rows: 390 000 rows of 128 from a table of 2.6 GB take 37 us, 4.1 TB/s of what has to move (each row's scale,
+// 4 bytes, costs a sector of its own).
 #include "fastgl_norm.h"
 #include "rows_device.h"
+
+#include <type_traits>
 
 namespace fastgl {
 namespace {
 
 constexpr int kUnits = 4;           // chunks of eight columns a lane of the dropout takes
+constexpr int kMany = 4;            // rows that a lane of the gather has under way where the result has kManyBytes at least
+constexpr int64_t kManyBytes = (int64_t)64 << 20;
 constexpr int kWide = 2048;         // chunks a row from which a workgroup's units touch at most two rows
 
 struct DropArgs {
@@ -84,49 +95,68 @@ struct Gather8Args {
     void *out;
 };
 
-// A lane writes 16 bytes of a row: V columns.  In rows of V and more the last slice starts V before the row's end, and
-// what two slices share is written twice alike; shorter rows go column by column.
-template <bool BF16, bool SHORT>
+// A lane writes 16 bytes of a row: V columns, of MANY rows whose IDs, scales and columns are under way together.  In rows of V
+// and more the last slice starts V before the row's end, and what two slices share is written twice alike; shorter rows go
+// column by column.
+template <bool BF16, bool SHORT, int MANY>
 __global__ __launch_bounds__(kBlock) void k_gather_e4m3(Gather8Args a)
 {
     typedef uint32_t bytes4 __attribute__((aligned(1)));
     typedef typename Chunk<BF16>::elem T;
     constexpr int V = 16 / (int)sizeof(T);
-    const int64_t row = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> a.lg;
-    if (row >= a.n) return;
-    const int lanes = 1 << a.lg;
-    const int64_t id = a.ids[row];
-    const bool there = (uint64_t)id < (uint64_t)a.table_rows;
-    const float scale = there ? a.scale[id] : __uint_as_float(0x7FC00000u);
-    const uint8_t *q = a.table + (there ? id : 0) * a.F;
-    T *out = static_cast<T *>(a.out) + row * a.F;
+    const int groups = kBlock >> a.lg, lanes = 1 << a.lg;
+    const int64_t first = (int64_t)blockIdx.x * (groups * MANY) + (threadIdx.x >> a.lg);
+    const uint8_t *q[MANY];
+    float scale[MANY];
+    bool there[MANY];
+#pragma unroll
+    for (int m = 0; m < MANY; ++m) {
+        const int64_t row = first + m * groups;
+        const int64_t id = row < a.n ? a.ids[row] : -1;
+        there[m] = (uint64_t)id < (uint64_t)a.table_rows;
+        q[m] = a.table + (there[m] ? id : 0) * a.F;
+        scale[m] = there[m] ? a.scale[id] : __uint_as_float(0x7FC00000u);
+    }
     if constexpr (SHORT) {
-        for (int c = threadIdx.x & (lanes - 1); c < a.F; c += lanes) {
-            const uint32_t b = there ? q[c] : 0u;
-            const float v = __builtin_amdgcn_cvt_f32_fp8((int)b, 0) * scale;
-            if constexpr (BF16) out[c] = __builtin_bit_cast(uint16_t, (__bf16)v);
-            else out[c] = v;
-        }
+        for (int c = threadIdx.x & (lanes - 1); c < a.F; c += lanes)
+#pragma unroll
+            for (int m = 0; m < MANY; ++m) {
+                const int64_t row = first + m * groups;
+                if (row >= a.n) continue;
+                const uint32_t b = there[m] ? q[m][c] : 0u;
+                const float v = __builtin_amdgcn_cvt_f32_fp8((int)b, 0) * scale[m];
+                T *out = static_cast<T *>(a.out) + row * a.F + c;
+                if constexpr (BF16) *out = __builtin_bit_cast(uint16_t, (__bf16)v);
+                else *out = v;
+            }
     } else {
         for (int c = threadIdx.x & (lanes - 1); c < a.slices; c += lanes) {
             const int col = c * V < a.F - V ? c * V : a.F - V;
-            uint32_t w[V / 4];
+            uint32_t w[MANY][V / 4];
 #pragma unroll
-            for (int i = 0; i < V / 4; ++i) w[i] = there ? *reinterpret_cast<const bytes4 *>(q + col + 4 * i) : 0u;
-            float v[V];
+            for (int m = 0; m < MANY; ++m)
 #pragma unroll
-            for (int i = 0; i < V / 4; ++i) {
-                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
-                v[4 * i] = lo[0] * scale;
-                v[4 * i + 1] = lo[1] * scale;
-                v[4 * i + 2] = hi[0] * scale;
-                v[4 * i + 3] = hi[1] * scale;
+                for (int i = 0; i < V / 4; ++i) w[m][i] = there[m] ? *reinterpret_cast<const bytes4 *>(q[m] + col + 4 * i) : 0u;
+#pragma unroll
+            for (int m = 0; m < MANY; ++m) {
+                const int64_t row = first + m * groups;
+                if (row >= a.n) continue;
+                T *out = static_cast<T *>(a.out) + row * a.F + col;
+                float v[V];
+#pragma unroll
+                for (int i = 0; i < V / 4; ++i) {
+                    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[m][i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[m][i], true);
+                    v[4 * i] = lo[0] * scale[m];
+                    v[4 * i + 1] = lo[1] * scale[m];
+                    v[4 * i + 2] = hi[0] * scale[m];
+                    v[4 * i + 3] = hi[1] * scale[m];
+                }
+                if constexpr (BF16) {
+                    Chunk<true>::store(out, v, 8);
+                } else
+                    *reinterpret_cast<Words<4>::x4 *>(out) =
+                        Words<4>::x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
             }
-            if constexpr (BF16) {
-                Chunk<true>::store(out + col, v, 8);
-            } else
-                *reinterpret_cast<Words<4>::x4 *>(out + col) =
-                    Words<4>::x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
         }
     }
 }
@@ -222,14 +252,23 @@ fastgl_status fastgl_gather_rows_e4m3(const uint8_t *table, const float *scale, 
     a.slices = (int32_t)ceil_div(F, V);
     const int64_t units = F < V ? F : a.slices;
     while (a.lg < 6 && ((int64_t)1 << a.lg) < units) ++a.lg;
-    const int64_t blocks = ceil_div(n << a.lg, kBlock);
+    // us a call, one row under way / four: 390 000 rows of 128 to bf16 42 / 37, to fp32 81 / 63; 30 000 of 2048 to fp32 79 / 64;
+    // 80 000 of 128 to fp32 11.3 / 11.6; 100 000 of 16 to bf16 5.8 / 6.6
+    const bool many = n * F * (dtype == FASTGL_BF16 ? 2 : 4) >= kManyBytes;
+    const int64_t blocks = ceil_div(n, (int64_t)(kBlock >> a.lg) * (many ? kMany : 1));
     if (blocks > 0x7FFFFFFFLL) {
         set_error("gather too large for one launch");
         return FASTGL_ERR_UNSUPPORTED;
     }
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, (hipStream_t)stream, a); };
-    if (dtype == FASTGL_BF16) F < V ? go(k_gather_e4m3<true, true>) : go(k_gather_e4m3<true, false>);
-    else F < V ? go(k_gather_e4m3<false, true>) : go(k_gather_e4m3<false, false>);
+    auto typed = [&](auto bf16, auto many_rows) {
+        constexpr bool B = decltype(bf16)::value;
+        constexpr int N = decltype(many_rows)::value;
+        F < V ? go(k_gather_e4m3<B, true, N>) : go(k_gather_e4m3<B, false, N>);
+    };
+    auto both = [&](auto bf16) { many ? typed(bf16, std::integral_constant<int, kMany>()) : typed(bf16, std::integral_constant<int, 1>()); };
+    if (dtype == FASTGL_BF16) both(std::true_type());
+    else both(std::false_type());
     FASTGL_LAUNCH_CHECK("fastgl_gather_rows_e4m3");
     return FASTGL_OK;
 }

@@ -199,8 +199,9 @@ struct DzArgs {
     float *part;                     // [gridDim.y][2][N] column sums, or NULL
 };
 
-// dG = dP U act'(G), dU = dP act(G), rounded to what the matrix cores take (bf16, or three pieces); the column sums
-// are formed from the unrounded values.
+// dG = dP U act'(G), dU = dP act(G), rounded to what the matrix cores take (bf16, or three pieces): a rounding of 2^-8 of terms that the
+// products add up at random, which bf16 weights and inputs have too.  The column sums are formed from the unrounded values.
+// Bound by memory: 16 384 x 4096 bf16 117 us, 671 MB at 5.7 TB/s.
 template <bool BF16, int ACT>
 __global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
 {
