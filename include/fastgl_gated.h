@@ -12,14 +12,14 @@
  * sigmoid s(g).  X [M,K], Wg, Wu [K,N], G, U, P, dP [M,N]: dense row-major without
  * padding, fp32 or (bit patterns in uint16_t) bf16, all of one dtype; biases and their
  * gradients fp32 [N].  The weight gradients are of the weights' dtype: with bf16 their terms
- * dG, dU are already rounded to bf16, so that more bits would hold nothing.
+ * dG, dU are already rounded to bf16, so that more bits would hold little.
  *
  * Both products of a pass share one kernel.  They run on the bf16 matrix cores with fp32
  * accumulation; fp32 elements are cut into three bf16 pieces whose sum is the element
  * exactly, and six of the nine piece products are added, smallest first (relative error of a
  * product at most 2^-23).  Few rows are multiplied with plain fp32 multiply-adds.  bf16
- * results are rounded once, from fp32; dG and dU are rounded to bf16 once in between, their
- * column sums are formed before that.  Elements that are not finite: every sum such an
+ * results are rounded once, from fp32; dG and dU are rounded to bf16 once in between (to two
+ * pieces where dX or dWg has at most 1024 elements or dG at most 16384), their column sums are formed before that.  Elements that are not finite: every sum such an
  * element enters is not finite, and no other changes (from fp32 pieces it is NaN, also for
  * finite elements above 3.39e38); act of an infinite G is what IEEE arithmetic makes of the formula.
  *

@@ -17,6 +17,9 @@ namespace {
 //   25 / 41, 64 rows 43 / 53
 constexpr int64_t kFewRows = 8, kFewRowsPacked = 48;
 constexpr int kSumGroups = 2048;       // workgroups of the gradient of the gate
+// Elements of dX or dWg, and of dG, up to which bf16 calls keep dG and dU in two pieces.  us a backward call, one piece / two: 1 row
+// 256 -> 1024 23 / 23; 30 rows 100 -> 300 27 / 26; but 300 rows 256 -> 1024 28 / 37, 130 000 rows 32 -> 64 72 / 119.
+constexpr int64_t kFewResults = 1024, kFewTerms = 16384;
 constexpr int64_t kMostWidth = (int64_t)1 << 20;
 
 // x as three bf16 whose sum is x exactly (each rounding to nearest).
@@ -45,7 +48,7 @@ __device__ __forceinline__ void store_planes(uint16_t *p, int64_t plane, const f
             q[2][j] = c[2];
         }
 #pragma unroll
-        for (int i = 0; i < 3; ++i) Chunk<true>::store(p + i * plane, q[i], 8);
+        for (int i = 0; i < PLANES; ++i) Chunk<true>::store(p + i * plane, q[i], 8);
     }
 }
 
@@ -199,10 +202,11 @@ struct DzArgs {
     float *part;                     // [gridDim.y][2][N] column sums, or NULL
 };
 
-// dG = dP U act'(G), dU = dP act(G), rounded to what the matrix cores take (bf16, or three pieces): a rounding of 2^-8 of terms that the
-// products add up at random, which bf16 weights and inputs have too.  The column sums are formed from the unrounded values.
+// dG = dP U act'(G), dU = dP act(G), rounded to what the matrix cores take: three pieces of fp32, or bf16, whose rounding adds an error
+// of the size of the results' own (2^-9 root mean square, sqrt 2 together).  Where bf16 gradients have few elements,
+// whose errors do not average, two pieces are kept (2^-17).  The column sums are formed from the unrounded values.
 // Bound by memory: 16 384 x 4096 bf16 117 us, 671 MB at 5.7 TB/s.
-template <bool BF16, int ACT>
+template <bool BF16, int ACT, int PLANES>
 __global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
 {
     typedef typename Chunk<BF16>::elem T;
@@ -235,8 +239,8 @@ __global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
                 su[j] += u[j];
             }
             if (a.dG) {
-                store_planes<BF16 ? 1 : 3>(a.dG + row * a.ld + col, a.plane, g);
-                store_planes<BF16 ? 1 : 3>(a.dU + row * a.ld + col, a.plane, u);
+                store_planes<PLANES>(a.dG + row * a.ld + col, a.plane, g);
+                store_planes<PLANES>(a.dU + row * a.ld + col, a.plane, u);
             }
         }
     }
@@ -394,10 +398,12 @@ struct Shape {
     bool pack_x() const { return !bf16 || !aligned || K % 8; }
     bool pack_w() const { return !bf16 || !aligned || N % 8; }
     bool few_rows() const { return M <= (pack_x() || pack_w() ? kFewRowsPacked : kFewRows); }
+    int z_planes() const { return bf16 ? (M * K <= kFewResults || K * N <= kFewResults || M * N <= kFewTerms ? 2 : 1) : 3; }               // of dG and dU
     int64_t pairs() const { return bf16 ? 1 : 6; }
+    int64_t z_pairs() const { return bf16 ? z_planes() : 6; }
     Cut forward_cut() const { return cut_of(kForward, M, N, K, pairs()); }
-    Cut rows_cut() const { return cut_of(kRows, M, K, N, 2 * pairs()); }
-    Cut weights_cut() const { return cut_of(kWeights, K, N, M, pairs()); }
+    Cut rows_cut() const { return cut_of(kRows, M, K, N, 2 * z_pairs()); }
+    Cut weights_cut() const { return cut_of(kWeights, K, N, M, z_pairs()); }
     // workgroups of k_gated_dz: (columns, rows); 2^lg lanes a row
     int lg() const
     {
@@ -428,8 +434,8 @@ Scratch carve(const Shape &s, bool backward, Layout &l)
     }
     auto sums = [](const Cut &c, int64_t n) { return c.slabs > 1 ? (size_t)(c.slabs * n) : (size_t)0; };
     if (backward) {
-        o.dg = l.take<uint16_t>((size_t)(s.planes * s.M * s.ldz));
-        o.du = l.take<uint16_t>((size_t)(s.planes * s.M * s.ldz));
+        o.dg = l.take<uint16_t>((size_t)(s.z_planes() * s.M * s.ldz));
+        o.du = l.take<uint16_t>((size_t)(s.z_planes() * s.M * s.ldz));
         o.db = l.take<float>((size_t)(s.dz_rows() * 2 * s.N));
         const size_t x = sums(s.rows_cut(), s.M * s.K), w = sums(s.weights_cut(), 2 * s.K * s.N);
         o.part = l.take<float>(x > w ? x : w);
@@ -657,6 +663,10 @@ fastgl_status fastgl_gated_fwd(fastgl_dtype dtype, const void *X, const void *Wg
     g.lda = d.ldk; g.ldb = d.ldn;
     g.R = M; g.C = N; g.Kc = K;
     g.pairs = (int32_t)d.pairs(); g.groups = 1;
+    if (!d.bf16) {
+        g.planes_a = kSixA;
+        g.planes_b = kSixB;
+    }
     g.bias[0] = bg; g.bias[1] = bu;
     g.out[0] = P; g.out[1] = G; g.out[2] = U;
     g.part = o.part;
@@ -733,8 +743,9 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
     const dim3 dz((unsigned)d.dz_cols(), (unsigned)d.dz_rows());
     by_act(act, [&](auto A) {
         constexpr int ACT = decltype(A)::value;
-        if (d.bf16) hipLaunchKernelGGL((k_gated_dz<true, ACT>), dz, dim3(kBlock), 0, s, z);
-        else hipLaunchKernelGGL((k_gated_dz<false, ACT>), dz, dim3(kBlock), 0, s, z);
+        if (d.z_planes() == 1) hipLaunchKernelGGL((k_gated_dz<true, ACT, 1>), dz, dim3(kBlock), 0, s, z);
+        else if (d.bf16) hipLaunchKernelGGL((k_gated_dz<true, ACT, 2>), dz, dim3(kBlock), 0, s, z);
+        else hipLaunchKernelGGL((k_gated_dz<false, ACT, 3>), dz, dim3(kBlock), 0, s, z);
     });
     FASTGL_LAUNCH_CHECK("fastgl_gated_bwd (dG, dU)");
     SumArgs last = {};                                 // the sums at the end
@@ -753,7 +764,9 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
         g.a_plane = M * d.ldz; g.b_plane = K * d.ldn;
         g.lda = d.ldz; g.ldb = d.ldn;
         g.R = M; g.C = K; g.Kc = N;
-        g.pairs = (int32_t)d.pairs(); g.groups = 2;
+        g.pairs = (int32_t)d.z_pairs(); g.groups = 2;
+        g.planes_a = !d.bf16 ? kSixA : d.z_planes() == 2 ? kTwo : 0;
+        g.planes_b = !d.bf16 ? kSixB : 0;
         g.out[0] = dX;
         g.part = o.part;
         const Cut cut = d.rows_cut();
@@ -773,7 +786,9 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
         g.a_plane = M * d.ldk; g.b_plane = M * d.ldz;
         g.lda = d.ldk; g.ldb = d.ldz;
         g.R = K; g.C = N; g.Kc = M;
-        g.pairs = (int32_t)d.pairs(); g.groups = 1;
+        g.pairs = (int32_t)d.z_pairs(); g.groups = 1;
+        g.planes_a = !d.bf16 ? kSixA : 0;
+        g.planes_b = !d.bf16 ? kSixB : d.z_planes() == 2 ? kTwo : 0;
         g.out[0] = dWg; g.out[1] = dWu;
         g.part = o.part;
         const Cut cut = d.weights_cut();

@@ -16,7 +16,7 @@
 // * Buffer resources end the operands: what lies beyond is read as 0.  A row's last pieces beyond the contracted
 //   range are given an address beyond the end.
 // * What bounds it: the matrix instructions at the clock that the card holds under them (1.7 to 1.9 GHz of 2.4).  dWg, dWu of 16 384 rows
-//   1024 x 4096 bf16: 206 us, 1334 TFLOP/s, the matrix cores busy 87 % of a compute unit's cycles; dX there 237 us, 1160 TFLOP/s, 59 % (rows of
+//   1024 x 4096 bf16: 206 us, 1334 TFLOP/s, the matrix cores busy 82 to 87 % of a compute unit's cycles; dX there 237 us, 1160 TFLOP/s, 59 % (rows of
 //   64 bytes a step from two operands; a library product of that shape 205 us); forward 115 000 rows 256 -> 1024 178 us, bound by its 706 MB
 //   of results (4.3 TB/s with what is read); 16 384 rows 1024 -> 4096 227 us without G and U, 1211 TFLOP/s.  No LDS bank conflicts in dX
 //   and dW.  fp32 runs at a sixth: 222 TFLOP/s at 16 384 rows 1024 -> 4096.
@@ -47,16 +47,16 @@ struct TileArgs {
     int64_t a_plane, b_plane;      // elements between planes of pieces
     int64_t lda, ldb;              // elements between rows, multiples of 8; contiguous contracted elements are 0 from Kc to there
     int64_t R, C, Kc;
-    int32_t pairs, groups;         // segments: groups x pairs; pairs is 1 (bf16) or 6 (three planes)
+    int32_t pairs, groups;         // segments: groups x pairs of a plane of A and a plane of B
+    uint32_t planes_a, planes_b;   // the planes of pair i: four bits each from bit 4 i
     int32_t tiles_r, tiles_c, slabs;      // slabs: the steps of all segments are dealt to as many workgroups a tile
     const float *bias[2];          // FORWARD, or NULL
     void *out[3];                  // FORWARD: P, G, U (G, U or NULL); ROWS: dX; WEIGHTS: dWg, dWu
     float *part;                   // slabs > 1: their sums, [slab][results][R][C]
 };
 
-// Segment i of six: the planes of A and of B, smallest products first.
-__device__ __forceinline__ int plane_a(int i) { return (0x001120 >> (4 * i)) & 15; }       // 0 2 1 1 0 0
-__device__ __forceinline__ int plane_b(int i) { return (0x010102 >> (4 * i)) & 15; }       // 2 0 1 0 1 0
+// Pairs of planes, smallest products first: six of three planes and three (0 2, 2 0, 1 1, 0 1, 1 0, 0 0), and two of two and one.
+constexpr uint32_t kSixA = 0x001120, kSixB = 0x010102, kTwo = 0x01;
 
 // exp(-x), x >= 0 or any: 2^(-x log2 e).  Relative error 2^-23 (1 + |x|): the rounding of the exponent.
 __device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(-1.44269504089f * x); }
@@ -185,7 +185,7 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
     const bool beyond = piece_k * 8 >= last_rows;                        // rows are padded with zeros to whole pieces
     auto begin_segment = [&]() {
         const int grp = MODE == kRows ? seg / g.pairs : 0, pair = MODE == kRows ? seg - grp * g.pairs : seg;
-        const int pa = g.pairs == 1 ? 0 : plane_a(pair), pb = g.pairs == 1 ? 0 : plane_b(pair);
+        const int pa = (int)(g.planes_a >> (4 * pair)) & 15, pb = (int)(g.planes_b >> (4 * pair)) & 15;
         next_a = g.a[grp] + pa * g.a_plane + (T::A_T ? row0 : row0 * g.lda) + t * step_a;
 #pragma unroll
         for (int q = 0; q < T::RESULTS; ++q)
