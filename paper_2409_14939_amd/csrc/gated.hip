@@ -197,8 +197,8 @@ __global__ __launch_bounds__(kBlock) void k_gated_rows(RowsArgs a)
 struct DzArgs {
     const void *G, *U, *dP;
     uint16_t *dG, *dU;               // planes [M][ld], or NULL
-    int64_t M, plane;
-    int32_t N, ld, lg;               // 2^lg lanes of eight columns a row
+    int64_t M, plane, ld, block;     // ld: elements between rows, block: between blocks of 32 columns (32: rows lie whole)
+    int32_t N, lg;                   // 2^lg lanes of eight columns a row
     float *part;                     // [gridDim.y][2][N] column sums, or NULL
 };
 
@@ -239,8 +239,9 @@ __global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
                 su[j] += u[j];
             }
             if (a.dG) {
-                store_planes<PLANES>(a.dG + row * a.ld + col, a.plane, g);
-                store_planes<PLANES>(a.dU + row * a.ld + col, a.plane, u);
+                const int64_t to = (col >> 5) * a.block + row * a.ld + (col & 31);
+                store_planes<PLANES>(a.dG + to, a.plane, g);
+                store_planes<PLANES>(a.dU + to, a.plane, u);
             }
         }
     }
@@ -346,7 +347,7 @@ struct Cut {
 // write and that are read again (4 bytes each way at some 6 TB/s), and a launch.
 // Measured (kernel times, bf16, us for large / middle / small tiles):
 //   forward 16 384 x 1024 -> 4096, G and U kept 271 / 268 / -, alone 227 / 240 / -;  115 000 x 256 -> 1024 196 / 186 / -, 154 / 139 / -
-//   dX 16 384 x 4096 -> 1024 242 / 284 / 344;  dWg, dWu of 16 384 rows 1024 x 4096 206 / 240 / 416 (the first two in two slabs)
+//   dX 16 384 x 4096 -> 1024 242 / 284 / 344 (221 with dG, dU in blocks);  dWg, dWu of 16 384 rows 1024 x 4096 206 / 240 / 416 (the first two in two slabs)
 //   backward call of 300 rows 256 -> 1024 33 / 29 / 27, of 2000 rows 56 / 51 / 47, of 8000 rows 256 -> 683 79 / 72 / 76
 Cut cut_of(int mode, int64_t R, int64_t C, int64_t Kc, int64_t segments)
 {
@@ -392,12 +393,17 @@ struct Shape {
     int64_t M, K, N, ldk, ldn, ldz;
     Shape(fastgl_dtype dtype, int64_t M_, int64_t K_, int64_t N_, bool aligned_)
         : bf16(dtype == FASTGL_BF16), aligned(aligned_), planes(dtype == FASTGL_BF16 ? 1 : 3), M(M_), K(K_), N(N_),
-          ldk((int64_t)align_up((size_t)K_, 8)), ldn((int64_t)align_up((size_t)N_, 8)), ldz(ldn + (ldn % 512 == 0 ? 64 : 0))
+          ldk((int64_t)align_up((size_t)K_, 8)), ldn((int64_t)align_up((size_t)N_, 8)), ldz((int64_t)align_up((size_t)N_, 32))
     {
     }
     bool pack_x() const { return !bf16 || !aligned || K % 8; }
     bool pack_w() const { return !bf16 || !aligned || N % 8; }
     bool few_rows() const { return M <= (pack_x() || pack_w() ? kFewRowsPacked : kFewRows); }
+    // Elements of a block of 32 columns of dG and dU, which lie [block][row][32]: dX then reads whole lines although it takes 32
+    // columns a step (16 384 x 8192 times 8192 x 1024: 245 -> 221 us).  A block is 2304 bytes more than a multiple of 4096: the tiles
+    // of the weight gradients read the same rows of many blocks at a time, which should not meet in the same memory channels.  0: rows lie whole, where there are few (nothing to gain) or four blocks pass 32-bit offsets.
+    int64_t z_block() const { return M >= 1024 && M <= (int64_t)1 << 22 ? (int64_t)(align_up((size_t)M * 64, 4096) + 2304) / 2 : 0; }
+    int64_t z_plane() const { return z_block() ? ldz / 32 * z_block() : M * ldz; }
     int z_planes() const { return bf16 ? (M * K <= kFewResults || K * N <= kFewResults || M * N <= kFewTerms ? 2 : 1) : 3; }               // of dG and dU
     int64_t pairs() const { return bf16 ? 1 : 6; }
     int64_t z_pairs() const { return bf16 ? z_planes() : 6; }
@@ -434,8 +440,8 @@ Scratch carve(const Shape &s, bool backward, Layout &l)
     }
     auto sums = [](const Cut &c, int64_t n) { return c.slabs > 1 ? (size_t)(c.slabs * n) : (size_t)0; };
     if (backward) {
-        o.dg = l.take<uint16_t>((size_t)(s.z_planes() * s.M * s.ldz));
-        o.du = l.take<uint16_t>((size_t)(s.z_planes() * s.M * s.ldz));
+        o.dg = l.take<uint16_t>((size_t)(s.z_planes() * s.z_plane()));
+        o.du = l.take<uint16_t>((size_t)(s.z_planes() * s.z_plane()));
         o.db = l.take<float>((size_t)(s.dz_rows() * 2 * s.N));
         const size_t x = sums(s.rows_cut(), s.M * s.K), w = sums(s.weights_cut(), 2 * s.K * s.N);
         o.part = l.take<float>(x > w ? x : w);
@@ -737,8 +743,10 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
     z.G = G; z.U = U; z.dP = dP;
     z.dG = want_x || want_w ? o.dg : nullptr;
     z.dU = o.du;
-    z.M = M; z.plane = M * d.ldz;
-    z.N = (int32_t)N; z.ld = (int32_t)d.ldz; z.lg = d.lg();
+    z.M = M; z.plane = d.z_plane();
+    z.N = (int32_t)N; z.lg = d.lg();
+    z.ld = d.z_block() ? 32 : d.ldz;
+    z.block = d.z_block() ? d.z_block() : 32;
     z.part = want_b ? o.db : nullptr;
     const dim3 dz((unsigned)d.dz_cols(), (unsigned)d.dz_rows());
     by_act(act, [&](auto A) {
@@ -761,8 +769,9 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
         g.a[0] = o.dg; g.a[1] = o.du;
         g.b[0] = d.pack_w() ? o.wg : (const uint16_t *)Wg;
         g.b[1] = d.pack_w() ? o.wu : (const uint16_t *)Wu;
-        g.a_plane = M * d.ldz; g.b_plane = K * d.ldn;
+        g.a_plane = d.z_plane(); g.b_plane = K * d.ldn;
         g.lda = d.ldz; g.ldb = d.ldn;
+        g.a_blocks = d.z_block();
         g.R = M; g.C = K; g.Kc = N;
         g.pairs = (int32_t)d.z_pairs(); g.groups = 2;
         g.planes_a = !d.bf16 ? kSixA : d.z_planes() == 2 ? kTwo : 0;
@@ -783,8 +792,9 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
         TileArgs g = {};
         g.a[0] = d.pack_x() ? o.x : (const uint16_t *)X;
         g.b[0] = o.dg; g.b[1] = o.du;
-        g.a_plane = M * d.ldk; g.b_plane = M * d.ldz;
+        g.a_plane = M * d.ldk; g.b_plane = d.z_plane();
         g.lda = d.ldk; g.ldb = d.ldz;
+        g.b_blocks = d.z_block();
         g.R = K; g.C = N; g.Kc = M;
         g.pairs = (int32_t)d.z_pairs(); g.groups = 1;
         g.planes_a = !d.bf16 ? kSixA : 0;

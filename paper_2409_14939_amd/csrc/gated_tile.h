@@ -13,11 +13,11 @@
 //   index is contiguous lies as [row][32], read 16 bytes a lane; one whose other index is contiguous lies as [32][column] and is
 //   turned on its way out of LDS by the transposing reads.  The 16-byte pieces of a row are permuted (by the addresses they
 //   are loaded from) so that the lanes of a read meet different banks.
-// * Buffer resources end the operands: what lies beyond is read as 0.  A row's last pieces beyond the contracted
-//   range are given an address beyond the end.
+// * Buffer resources end the operands: what lies beyond is read as 0.  Pieces beyond the contracted range that lie inside an
+//   operand are given an address beyond the end.
 // * What bounds it: the matrix instructions at the clock that the card holds under them (1.7 to 1.9 GHz of 2.4).  dWg, dWu of 16 384 rows
-//   1024 x 4096 bf16: 206 us, 1334 TFLOP/s, the matrix cores busy 82 to 87 % of a compute unit's cycles; dX there 237 us, 1160 TFLOP/s, 59 % (rows of
-//   64 bytes a step from two operands; a library product of that shape 205 us); forward 115 000 rows 256 -> 1024 178 us, bound by its 706 MB
+//   1024 x 4096 bf16: 206 us, 1334 TFLOP/s, the matrix cores busy 82 to 87 % of a compute unit's cycles; dX there 221 us, 1244 TFLOP/s (245 with dG and dU in whole rows, of which a
+//   step takes 64 bytes; a library product of that shape 205); forward 115 000 rows 256 -> 1024 178 us, bound by its 706 MB
 //   of results (4.3 TB/s with what is read); 16 384 rows 1024 -> 4096 227 us without G and U, 1211 TFLOP/s.  No LDS bank conflicts in dX
 //   and dW.  fp32 runs at a sixth: 222 TFLOP/s at 16 384 rows 1024 -> 4096.
 // * Results are turned through LDS, 64 x 64 at a time for each wavefront alone, into whole 128-byte lines.
@@ -45,7 +45,8 @@ constexpr int kTileRsrc = 0x00020000;
 struct TileArgs {
     const uint16_t *a[2], *b[2];   // FORWARD, WEIGHTS: a[0] and b[0], b[1]; ROWS: group g has a[g], b[g]
     int64_t a_plane, b_plane;      // elements between planes of pieces
-    int64_t lda, ldb;              // elements between rows, multiples of 8; contiguous contracted elements are 0 from Kc to there
+    int64_t lda, ldb;              // elements between rows, multiples of 8; contiguous contracted elements are 0 from Kc on to a multiple of 8
+    int64_t a_blocks, b_blocks;    // 0, or ROWS' A and WEIGHTS' B lie in blocks of 32 columns, [block][row][32], so many elements a block
     int64_t R, C, Kc;
     int32_t pairs, groups;         // segments: groups x pairs of a plane of A and a plane of B
     uint32_t planes_a, planes_b;   // the planes of pair i: four bits each from bit 4 i
@@ -150,25 +151,29 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
     const int first_step = PART ? (int)((int64_t)steps * nseg * slab / g.slabs) : 0;
     const int all = (PART ? (int)((int64_t)steps * nseg * (slab + 1) / g.slabs) : steps * nseg) - first_step;
 
+    const int64_t a_blocks = MODE == kRows ? g.a_blocks : 0, b_blocks = MODE == kWeights ? g.b_blocks : 0;
+
     // Where this lane's 16-byte pieces of a step come from.
     uint32_t off_a[T::LA], off_b[T::LB];
     const int piece_k = (lane & 3) ^ twisted(lane >> 2);                 // [row][32]: sixteen rows an instruction
-    auto place = [&](auto other, auto columns, int64_t ld, int inst) {
+    auto place = [&](auto other, auto columns, int64_t ld, int64_t blocks, int inst) __attribute__((always_inline)) {
+        if (blocks) ld = 32;
         if constexpr (!decltype(other)::value) {
             return (uint32_t)((inst * 16 + (lane >> 2)) * ld * 2) + 16u * (uint32_t)piece_k;
         } else {
             constexpr int COLS = decltype(columns)::value, PER_ROW = COLS / 8;
             const int k = (inst * kWave + lane) / PER_ROW, c = (lane & (PER_ROW - 1)) ^ turned<COLS * 2>(k);
+            if (blocks) return (uint32_t)(k * 64 + (c >> 2) * blocks * 2) + 16u * (uint32_t)(c & 3);
             return (uint32_t)(k * ld * 2) + 16u * (uint32_t)c;
         }
     };
     typedef std::integral_constant<int, T::BM> ColsA;
     typedef std::integral_constant<int, T::BC> ColsB;
 #pragma unroll
-    for (int i = 0; i < T::LA; ++i) off_a[i] = place(std::integral_constant<bool, T::A_T>(), ColsA(), g.lda, i * NW + wave);
+    for (int i = 0; i < T::LA; ++i) off_a[i] = place(std::integral_constant<bool, T::A_T>(), ColsA(), g.lda, a_blocks, i * NW + wave);
 #pragma unroll
     for (int i = 0; i < T::LB; ++i)
-        off_b[i] = place(std::integral_constant<bool, T::B_T>(), ColsB(), g.ldb, i % (T::LB / T::RESULTS) * NW + wave);
+        off_b[i] = place(std::integral_constant<bool, T::B_T>(), ColsB(), g.ldb, b_blocks, i % (T::LB / T::RESULTS) * NW + wave);
 
     // The operands of the step that is loaded next.  Resources begin at the step's first element and end, for an operand
     // whose contracted index is contiguous, with the tile's last row (a row's pieces beyond the contracted range are given an
@@ -176,22 +181,33 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
     int seg = PART ? first_step / (steps > 0 ? steps : 1) : 0, t = first_step - seg * steps, loaded = 0;
     int into = 0;                                                        // bytes to the LDS buffer it goes to
     const uint16_t *next_a, *next_b[2];
-    const int64_t step_a = T::A_T ? kStep * g.lda : kStep, step_b = T::B_T ? kStep * g.ldb : kStep;
+    const int64_t step_a = T::A_T ? kStep * g.lda : a_blocks ? a_blocks : kStep, step_b = T::B_T ? kStep * (b_blocks ? 32 : g.ldb) : kStep;
+    const int64_t row_a = a_blocks ? 32 : g.lda;
     const int last_rows = (int)(g.Kc - (int64_t)(steps - 1) * kStep);     // contracted elements of a segment's last step
     const int64_t rows_a = g.R - row0 < T::BM ? g.R - row0 : T::BM, rows_b = g.C - col0 < T::BNV ? g.C - col0 : T::BNV;
-    const int bytes_a = (int)(2 * (T::A_T ? kStep * g.lda - row0 : rows_a * g.lda));
-    const int bytes_b = (int)(2 * (T::B_T ? kStep * g.ldb - col0 : rows_b * g.ldb));
-    const int last_a = T::A_T ? (int)(2 * (last_rows * g.lda - row0)) : bytes_a, last_b = T::B_T ? (int)(2 * (last_rows * g.ldb - col0)) : bytes_b;
+    const int bytes_a = (int)(2 * (T::A_T ? kStep * g.lda - row0 : rows_a * row_a));
+    // blocks of columns: what the tile has of them; where a block's own rows end, only masks tell
+    int64_t left_blocks = b_blocks ? (g.C - col0 + 31) / 32 : 0;
+    left_blocks = left_blocks < T::BC / 32 ? left_blocks : T::BC / 32;
+    const int bytes_b = (int)(2 * (b_blocks ? left_blocks * b_blocks : T::B_T ? kStep * g.ldb - col0 : rows_b * g.ldb));
+    const int64_t base_b = b_blocks ? col0 / 32 * b_blocks : T::B_T ? col0 : col0 * g.ldb;
+    const int last_a = T::A_T ? (int)(2 * (last_rows * g.lda - row0)) : bytes_a, last_b = T::B_T && !b_blocks ? (int)(2 * (last_rows * g.ldb - col0)) : bytes_b;
     const bool beyond = piece_k * 8 >= last_rows;                        // rows are padded with zeros to whole pieces
-    auto begin_segment = [&]() {
+    uint32_t last_off_b[T::LB];
+#pragma unroll
+    for (int i = 0; i < T::LB; ++i) {
+        const int k = (i % (T::LB / T::RESULTS) * NW * kWave + wave * kWave + lane) / (T::BC / 8);         // of this lane's piece
+        last_off_b[i] = (T::B_T ? MODE == kWeights && k >= last_rows : beyond) ? kNoSuchOffset : off_b[i];
+    }
+    auto begin_segment = [&]() __attribute__((always_inline)) {
         const int grp = MODE == kRows ? seg / g.pairs : 0, pair = MODE == kRows ? seg - grp * g.pairs : seg;
         const int pa = (int)(g.planes_a >> (4 * pair)) & 15, pb = (int)(g.planes_b >> (4 * pair)) & 15;
-        next_a = g.a[grp] + pa * g.a_plane + (T::A_T ? row0 : row0 * g.lda) + t * step_a;
+        next_a = g.a[grp] + pa * g.a_plane + (T::A_T ? row0 : row0 * row_a) + t * step_a;
 #pragma unroll
         for (int q = 0; q < T::RESULTS; ++q)
-            next_b[q] = (MODE == kRows ? g.b[grp] : g.b[q]) + pb * g.b_plane + (T::B_T ? col0 : col0 * g.ldb) + t * step_b;
+            next_b[q] = (MODE == kRows ? g.b[grp] : g.b[q]) + pb * g.b_plane + base_b + t * step_b;
     };
-    auto load_next = [&]() {
+    auto load_next = [&]() __attribute__((always_inline)) {
         if (loaded >= all) return;
         const bool last = t + 1 == steps;
         FASTGL_LDS char *to = (FASTGL_LDS char *)lds + into + wave * 1024;
@@ -207,7 +223,7 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
             const auto rb = rsrc(next_b[q], last ? last_b : bytes_b);
 #pragma unroll
             for (int i = q * (T::LB / T::RESULTS); i < (q + 1) * (T::LB / T::RESULTS); ++i) {
-                const uint32_t o = !T::B_T && last && beyond ? kNoSuchOffset : off_b[i];
+                const uint32_t o = MODE != kForward && last ? last_off_b[i] : off_b[i];
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (FASTGL_LDS void *)(to + T::A_BYTES + i * NW * 1024), 16, (int)o, 0, 0, 0);
             }
             next_b[q] += step_b;
@@ -249,7 +265,7 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
         return __builtin_bit_cast(bf16x8, both);
     };
     struct Frags { bf16x8 a[T::TM], b[T::TN]; };
-    auto read = [&](int buf, int kk) {
+    auto read = [&](int buf, int kk) __attribute__((always_inline)) {
         Frags f;
         const uint32_t base = (uint32_t)buf;
 #pragma unroll
@@ -318,7 +334,7 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
         __builtin_amdgcn_s_barrier();
         Frags f = read(0, 0);
         int now = 0;                                         // bytes to the step's buffer
-        auto step = [&](auto arrived) {
+        auto step = [&](auto arrived) __attribute__((always_inline)) {
             load_next();
             __builtin_amdgcn_sched_barrier(0);
             const Frags n = read(now, 1);

@@ -128,7 +128,7 @@ def test_many_tiles_and_slabs(dtype, M, K, N):
 
 def test_what_is_not_finite_stays_in_its_row_and_column():
     for dtype in ("f32", "bf16"):
-        for M in (9, 300):
+        for M in (9, 300, 1100):
             x, wg, wu, bg, bu = (v.cuda() for v in inputs(M, 72, 88, dtype, 40))
             clean = B.fastgl_gated_fwd(x, wg, wu, bg, bu, "silu")
             bad = x.clone()
