@@ -49,7 +49,7 @@ __global__ __launch_bounds__(kBlock) void k_dropout(DropArgs a)
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
         // c0 + the unit's place: below chunks + kBlock * kUnits, so below kWide chunks the product with `inv` is exact
-        // (3072 * 2048 < 2^32) and beyond them the quotient is 0 or 1; one chunk a row divides by itself
+        // (both factors below 2^12) and beyond them the quotient is 0 or 1; one chunk a row divides by itself
         const uint32_t u = c0 + (uint32_t)(i * kBlock) + threadIdx.x;
         const uint32_t q = a.chunks == 1 ? u : a.chunks < kWide ? __umulhi(u, a.inv) : (u >= (uint32_t)a.chunks ? 1u : 0u);
         const int64_t row = row0 + q;
