@@ -208,3 +208,23 @@ def test_replays_of_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(out, step()):
             assert torch.equal(a, b), k
+
+
+def test_more_rows_than_blocks_of_columns_take():
+    """Beyond 2^22 rows dG and dU lie in whole rows."""
+    M, K, N = (1 << 22) + 33, 8, 40
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, G, U, dp = (torch.randn(M, n, generator=g, device="cuda", dtype=torch.float32).bfloat16() for n in (K, N, N, N))
+    wg, wu = (torch.randn(K, N, generator=g, device="cuda", dtype=torch.float32).bfloat16() for _ in range(2))
+    dx, dwg, dwu, dbg, dbu = B.fastgl_gated_bwd(x, wg, wu, G, U, dp, "silu")
+    want = ref.backward(x, wg, wu, G, U, dp, "silu")
+    dg, du = want[5], want[6]
+    size = dg.abs() @ wg.double().abs().T + du.abs() @ wu.double().abs().T
+    off = size * (2.0 ** -8 * 1.01 + U32 * 4 * N) + 1e-6
+    assert bool(((dx.double() - want[0]).abs() <= off + 2.0 ** -8 * (want[0].abs() + off)).all())
+    for got, exact, term in ((dwg, want[1], dg), (dwu, want[2], du)):
+        # independent roundings of 2^-8 at most of each term, float32 sums of slabs of some 10^5 terms, one rounding of the result
+        noise = (x.double().square().T @ term.square()).sqrt() * 2.0 ** -8
+        assert bool(((got.double() - exact).abs() <= 6 * noise + 2.0 ** -8 * exact.abs() + (x.double().abs().T @ term.abs()) * 2.0 ** -20).all())
+    for got, exact, term in ((dbg, want[3], dg), (dbu, want[4], du)):
+        assert bool(((got.double() - exact).abs() <= term.abs().sum(0) * 2.0 ** -18).all())
