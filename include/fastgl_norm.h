@@ -48,7 +48,7 @@ fastgl_status fastgl_norm_fwd(fastgl_dtype dtype, const void *X, const void *R, 
                               float eps, const int64_t *rng, double p, void *sum_out, void *Y, float *rstd, void *stream);
 
 /* The same with Y as e4m3 values (OCP, 448 the largest) and one scale a row:
- * scale[i] = max(max |Y[i,:]| / 448, 2^-126), Q = Y / scale to the nearest, even.
+ * scale[i] = max(max |Y[i,:]| / 448, 2^-126), Q the fp32 quotient Y / scale to the nearest, even.
  * NaN stays NaN and does not enter the maximum. */
 fastgl_status fastgl_norm_fwd_e4m3(fastgl_dtype dtype, const void *X, const void *R, const float *w, int64_t M, int64_t F,
                                    float eps, const int64_t *rng, double p, void *sum_out, uint8_t *Q, float *scale,

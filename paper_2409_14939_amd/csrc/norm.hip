@@ -7,8 +7,8 @@
 // the grid's stride, so that the weights stay in registers and the backward pass keeps its column sums there.
 //
 // Bound by memory; a copy runs at 4.7 to 5.0 TB/s on the same cards.  us a call and TB/s of what has to move: 512 000 bf16 rows of 256
-// with residual and dropout 207 (5.1); gradient of 115 000 fp32 rows of 602 with both 283 (4.9); 400 003 bf16 rows of 128 to 8 bits 33
-// (4.7); plain norm of 115 000 bf16 rows of 602 47 (5.9).  One row: 1.9 us of kernel, the rest of a call is the host.
+// with residual and dropout 207 (5.1); gradient of 115 000 fp32 rows of 602 with both 283 (4.9); 400 003 bf16 rows of 128 to 8 bits 37
+// (4.2); plain norm of 115 000 bf16 rows of 602 47 (5.9).  One row: 1.9 us of kernel, the rest of a call is the host.
 #include "fastgl_norm.h"
 #include "rows_device.h"
 
@@ -87,6 +87,35 @@ __device__ __forceinline__ float row_reduce(float v, OP op, float (&buf)[2][4], 
     }
     return v;
 }
+
+// The scale of a row of e4m3 values and quotients by it, all rounded as a division rounds them: the product with the rounded reciprocal,
+// then what that leaves of the dividend (exact), times the reciprocal.  us a call for 400 003 bf16 rows of 128, by divisions 46, so 37, by
+// the product alone 34, which stores a value or two in 10^7 of normal data a step off.
+struct RowScale {
+    float scale, s, inv;
+    bool tiny;
+    __device__ __forceinline__ explicit RowScale(float most)
+    {
+        const float q = most * (1.f / 448.f);
+        scale = fmaxf(most < __builtin_inff() ? fmaf(fmaf(-q, 448.f, most), 1.f / 448.f, q) : most, 0x1p-126f);
+        tiny = scale < 0x1p-90f;                        // what is left would not be a whole number of the least subnormal
+        s = tiny ? scale * 0x1p64f : scale;
+        inv = 1.f / s;
+        s = inv > 0.f ? s : 0.f;                        // an infinite scale: the product alone, 0 (or NaN)
+    }
+    __device__ __forceinline__ void divide(float (&v)[8]) const
+    {
+        if (tiny) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= 0x1p64f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float q = v[j] * inv;
+            v[j] = fmaf(fmaf(-q, s, v[j]), inv, q);
+        }
+    }
+};
 
 // y of eight columns as e4m3.
 __device__ __forceinline__ void store_e4m3(uint8_t *p, const float (&v)[8], int left)
@@ -192,13 +221,12 @@ __global__ __launch_bounds__(kBlock) void k_norm(NormArgs a)
             }
         if constexpr (E4M3) {
             most = row_reduce<LG>(most, Max(), buf, turn);
-            const float scale = fmaxf(most / 448.f, 0x1p-126f), inv = 1.f / scale;
-            if (lane == 0 && live) a.row_scale[row] = scale;
+            const RowScale by(most);
+            if (lane == 0 && live) a.row_scale[row] = by.scale;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (c * LANES + lane) * kChunk;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) h[c][j] *= inv;
+                by.divide(h[c]);
                 store_e4m3(static_cast<uint8_t *>(a.Y) + at + col, h[c], live ? F - col : 0);
             }
         } else {
@@ -260,9 +288,8 @@ __global__ __launch_bounds__(kBlock) void k_norm_wide(NormArgs a)
         sq = row_reduce<8>(sq, Plus(), buf, turn);
         const float rstd = 1.f / sqrtf(sq * a.inv_F + a.eps);
         if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
-        float inv = 1.f;
+        float most = 0.f;
         if constexpr (E4M3) {
-            float most = 0.f;
             for (int col = threadIdx.x * kChunk; col < F; col += kBlock * kChunk) {
                 float h[8];
                 sum(col, h);
@@ -271,17 +298,16 @@ __global__ __launch_bounds__(kBlock) void k_norm_wide(NormArgs a)
                 for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(h[j]));
             }
             most = row_reduce<8>(most, Max(), buf, turn);
-            const float scale = fmaxf(most / 448.f, 0x1p-126f);
-            inv = 1.f / scale;
-            if (threadIdx.x == 0) a.row_scale[row] = scale;
         }
+        const RowScale by(most);
+        if constexpr (E4M3)
+            if (threadIdx.x == 0) a.row_scale[row] = by.scale;
         for (int col = threadIdx.x * kChunk; col < F; col += kBlock * kChunk) {
             float h[8];
             sum(col, h);
             scaled(col, rstd, h);
             if constexpr (E4M3) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) h[j] *= inv;
+                by.divide(h);
                 store_e4m3(static_cast<uint8_t *>(a.Y) + at + col, h, F - col);
             } else
                 Chunk<BF16>::store(static_cast<T *>(a.Y) + at + col, h, F - col);

@@ -249,3 +249,39 @@ def test_replays_of_a_graph_take_the_offset_they_find():
             assert torch.equal(a, b), k
         seen.append(out[-1].clone())
     assert not torch.equal(seen[0], seen[1])
+
+
+# --------------------------------------------------------------------------------- e4m3: the quotient
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("F", [8, 64, 128, 256, 1024, 2048, 8192, 16_384])
+def test_e4m3_is_the_rounded_quotient(F, dtype):
+    """Rows of ones have rstd = 1 where eps = 0 and F is a power of two, so that Y is the weights: any values, here those next to
+    the middle of two e4m3 values times the scale.  Q is then the float32 quotient, rounded, bit for bit."""
+    rng = np.random.default_rng(F)
+    x = torch.ones(3, F, dtype=ref.DTYPES[dtype], device="cuda")
+    middles = np.array([(1 + (2 * i + 1) / 16) * 2.0 ** e for e in range(-6, 9) for i in range(8)] + [(i + 0.5) * 2.0 ** -9 for i in range(8)])
+    middles = middles[middles < 448]
+    for k in range(24):
+        most = np.float32(rng.uniform(1, 2) * 2.0 ** rng.integers(-118, 120) if k % 3 else rng.uniform(0.5, 8))
+        scale = max(most / np.float32(448), np.float32(2.0 ** -126))
+        y = (rng.choice(middles, F) * scale).astype(np.float32)
+        for _ in range(2):                                          # up to two values away from it
+            y = np.choose(rng.integers(0, 3, F), [y, np.nextafter(y, np.float32(0)), np.nextafter(y, np.float32(np.inf))])
+        y = np.minimum(y, most) * rng.choice([-1, 1], F).astype(np.float32)
+        y[rng.integers(F)] = most
+        Q, got_scale, _, rstd = B.fastgl_norm_fwd_e4m3(x, torch.from_numpy(y).cuda(), 0.0)
+        assert bool((rstd == 1).all()) and bool((got_scale.cpu() == float(scale)).all()), k
+        want = torch.from_numpy(y / scale).to(torch.float8_e4m3fn).view(torch.uint8)
+        assert all(torch.equal(row, want) for row in Q.view(torch.uint8).cpu()), (k, most, scale)
+
+
+def test_e4m3_of_weights_that_are_not_finite():
+    """An infinite weight makes the scale infinite: every finite value over it is 0, itself NaN."""
+    for F in (64, 1024, 16_384):
+        w = torch.linspace(0.5, 1.5, F)
+        w[3], w[F - 1] = float("inf"), float("nan")
+        Q, scale, _, _ = B.fastgl_norm_fwd_e4m3(torch.ones(2, F, device="cuda"), w.cuda(), 0.0)
+        q = Q.float().cpu()
+        assert bool(torch.isinf(scale).all()) and bool(torch.isnan(q[:, [3, F - 1]]).all())
+        q[:, [3, F - 1]] = 0
+        assert bool((q == 0).all())
