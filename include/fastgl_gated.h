@@ -23,6 +23,9 @@
  * element enters is not finite, and no other changes (from fp32 pieces it is NaN, also for
  * finite elements above 3.39e38); act of an infinite G is what IEEE arithmetic makes of the formula.
  *
+ * act(G) from G, before it is rounded to its type, is within 20 x 2^-24 of itself for GELU (bf16: another
+ * 4e-5 + g^2 2^-23), (8 + 2 |g|) x 2^-24 for SiLU and the sigmoid, also far below 0 (values below 2^-120 may be 0).
+ *
  * Conventions are those of fastgl_agg.h: caller-owned DEVICE memory aligned to the element
  * size; nothing is allocated, scratch comes from `workspace` (256-byte aligned); work is enqueued
  * on `stream` without synchronising the host; outputs are overwritten in full and must not

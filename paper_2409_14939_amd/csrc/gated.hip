@@ -182,10 +182,10 @@ __global__ __launch_bounds__(kBlock) void k_gated_rows(RowsArgs a)
         };
         float act;
         switch (a.act) {
-            case FASTGL_ACT_SILU: act = gate<FASTGL_ACT_SILU, false>(g, nullptr); break;
-            case FASTGL_ACT_GELU: act = gate<FASTGL_ACT_GELU, false>(g, nullptr); break;
-            case FASTGL_ACT_RELU: act = gate<FASTGL_ACT_RELU, false>(g, nullptr); break;
-            default: act = gate<FASTGL_ACT_SIGMOID, false>(g, nullptr); break;
+            case FASTGL_ACT_SILU: act = gate<FASTGL_ACT_SILU, false, BF16>(g, nullptr); break;
+            case FASTGL_ACT_GELU: act = gate<FASTGL_ACT_GELU, false, BF16>(g, nullptr); break;
+            case FASTGL_ACT_RELU: act = gate<FASTGL_ACT_RELU, false, BF16>(g, nullptr); break;
+            default: act = gate<FASTGL_ACT_SIGMOID, false, BF16>(g, nullptr); break;
         }
         put(a.P, act * u);
         if (a.G) put(a.G, g);
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 float grad;
-                const float v = gate<ACT, true>(g[j], &grad);
+                const float v = gate<ACT, true, BF16>(g[j], &grad);
                 g[j] = p[j] * u[j] * grad;
                 u[j] = p[j] * v;
                 if (j >= left) g[j] = u[j] = 0.f;                  // padding
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(kBlock) void k_gated_join(const float *__restrict__
         if constexpr (BF16) static_cast<uint16_t *>(out)[i] = __builtin_bit_cast(uint16_t, (__bf16)v);
         else static_cast<float *>(out)[i] = v;
     };
-    put(P, gate<ACT, false>(g, nullptr) * u);
+    put(P, gate<ACT, false, BF16>(g, nullptr) * u);
     if (G) put(G, g);
     if (U) put(U, u);
 }

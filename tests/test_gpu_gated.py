@@ -228,3 +228,63 @@ def test_more_rows_than_blocks_of_columns_take():
         assert bool(((got.double() - exact).abs() <= 6 * noise + 2.0 ** -8 * exact.abs() + (x.double().abs().T @ term.abs()) * 2.0 ** -20).all())
     for got, exact, term in ((dbg, want[3], dg), (dbu, want[4], du)):
         assert bool(((got.double() - exact).abs() <= term.abs().sum(0) * 2.0 ** -18).all())
+
+
+# --------------------------------------------------------------------------------- the gate alone
+def gate_points(dtype):
+    """2^14 gates in -10 .. 10, dense below 0."""
+    v = torch.cat([torch.linspace(-10, 0, 10_000), torch.linspace(0, 10, 6384)])
+    return v.to(rows_ref.DTYPES[dtype])
+
+
+def gate_bounds(name, dtype, g):
+    """Relative error of act(g) before it is rounded to its type.  GELU: the tail 8.4 U32 (two roundings of t, which count three times at
+    most in the polynomial, one of it and of the exponential, which the hardware gives within 2^-23, and the exponent), bf16 4e-5 of the
+    fit; 1 - tail doubles the absolute share at most; the product.  SiLU, sigmoid: exponent, exponential, sum, reciprocal, product."""
+    if name == "gelu":
+        return 20 * U32 + (4e-5 + 2 * U32 * g.square() if dtype == "bf16" else 0.0) * torch.ones_like(g)
+    return (0.0 if name == "relu" else 8 * U32 + 2 * U32 * g.abs()) * torch.ones_like(g)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", ref.ACTS)
+def test_gates_keep_their_digits(name, dtype):
+    """P without columns of X is act(bg) * 1, and the column sums of one row are dU = act(G), dG = act'(G): exact in relative terms, far below 0
+    too."""
+    t = rows_ref.DTYPES[dtype]
+    g = gate_points(dtype)
+    N, ones = g.numel(), torch.ones(g.numel()).cuda()
+    gd = g.double()
+    a, da = ref.act(name, gd)
+    rel = gate_bounds(name, dtype, gd)
+    e = lambda *s: torch.empty(*s, device="cuda", dtype=t)  # noqa: E731
+    for M in (1, 300):                                              # the kernel of few rows, the tiles
+        P, _, _ = B.fastgl_gated_fwd(e(M, 0), e(0, N), e(0, N), g.float().cuda(), ones, name)
+        off = rel * a.abs()
+        for row in (P[0], P[M - 1]):
+            within(row, a, off + ref.HALF[t] * (a.abs() + off) + 1e-37, (name, M))
+    one = torch.ones(1, N, device="cuda", dtype=t)
+    _, _, _, dbg, dbu = B.fastgl_gated_bwd(one[:, :1].contiguous(), e(1, N), e(1, N), g.cuda().view(1, N), one, one, name, want=("dbg", "dbu"))
+    within(dbu, a, rel * a.abs() + 2 * U32 * a.abs() + 1e-37, (name, "dbu"))
+    if name == "gelu":
+        cdf, pdf = 0.5 * torch.special.erfc(-gd / 2 ** 0.5), torch.exp(-0.5 * gd * gd) / (2 * torch.pi) ** 0.5
+        off = rel * cdf + gd.abs() * pdf * (12 * U32 + (2 * U32 * gd.square() if dtype == "bf16" else 0.0)) + 3 * U32 * da.abs()
+    elif name == "silu":
+        s = torch.sigmoid(gd)
+        off = rel * s * (1 + gd.abs()) + 4 * U32 * (s * (1 + gd.abs() * (1 - s))) + s * gd.abs() * (U32 + rel * s)
+    else:
+        off = rel * a.abs() * (1 + a.abs()) + 4 * U32 * a.abs() + U32 * a.abs()
+    within(dbg, da, (off if name != "relu" else 0.0 * gd) + 1e-37, (name, "dbg"))
+
+
+def test_gate_of_what_is_not_finite_and_far_out():
+    inf = float("inf")
+    for dtype in ("f32", "bf16"):
+        t = rows_ref.DTYPES[dtype]
+        g = torch.tensor([inf, 3e38, 1e20, 100.0, 0.0, -0.0, -100.0, -1e20, -3e38, -inf, float("nan")])
+        N = g.numel()
+        e = lambda *s: torch.empty(*s, device="cuda", dtype=t)  # noqa: E731
+        for M in (2, 300):
+            P, _, _ = B.fastgl_gated_fwd(e(M, 0), e(0, N), e(0, N), g.cuda(), torch.ones(N).cuda(), "gelu")
+            p = P[M - 1].float().cpu()
+            assert torch.equal(p[:4], g[:4].to(t).float()) and bool((p[4:9] == 0).all()) and bool(torch.isnan(p[9:]).all())
