@@ -38,7 +38,7 @@ EXPORTS = [
     "fastgl_edge_softmax_long_row", "fastgl_edge_score_fwd", "fastgl_edge_score_bwd",
     "fastgl_norm_fwd", "fastgl_norm_fwd_e4m3", "fastgl_norm_bwd", "fastgl_norm_bwd_workspace_bytes", "fastgl_dropout",
     "fastgl_gather_rows_e4m3", "fastgl_gated_fwd", "fastgl_gated_bwd", "fastgl_gated_fwd_workspace_bytes",
-    "fastgl_gated_bwd_workspace_bytes",
+    "fastgl_gated_bwd_workspace_bytes", "fastgl_gated_bwd_fine", "fastgl_gated_bwd_fine_workspace_bytes",
 ]
 MAX_REORDER_BATCHES = 64
 ACTS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
@@ -127,10 +127,12 @@ def lib() -> ctypes.CDLL:
         L.fastgl_gather_rows_e4m3.argtypes = [p, p, i64, p, i64, i64, i32, p, p]
         L.fastgl_gated_fwd_workspace_bytes.argtypes = [i32, i64, i64, i64, i32]
         L.fastgl_gated_fwd_workspace_bytes.restype = sz
-        L.fastgl_gated_bwd_workspace_bytes.argtypes = [i32, i64, i64, i64, i32]
-        L.fastgl_gated_bwd_workspace_bytes.restype = sz
+        for f in (L.fastgl_gated_bwd_workspace_bytes, L.fastgl_gated_bwd_fine_workspace_bytes):
+            f.argtypes = [i32, i64, i64, i64, i32]
+            f.restype = sz
         L.fastgl_gated_fwd.argtypes = [i32, p, p, p, p, p, i64, i64, i64, i32, p, p, p, p, sz, p]
-        L.fastgl_gated_bwd.argtypes = [i32, p, p, p, p, p, p, i64, i64, i64, i32, p, p, p, p, p, p, sz, p]
+        for f in (L.fastgl_gated_bwd, L.fastgl_gated_bwd_fine):
+            f.argtypes = [i32, p, p, p, p, p, p, i64, i64, i64, i32, p, p, p, p, p, p, sz, p]
         L.fastgl_idmap_table_slots.argtypes = [i64]
         L.fastgl_idmap_table_slots.restype = i64
         L.fastgl_idmap_workspace_bytes.argtypes = [i64, i64]
@@ -454,8 +456,9 @@ def fastgl_gated_fwd_workspace_bytes(dtype: str, M: int, K: int, N: int, aligned
     return int(lib().fastgl_gated_fwd_workspace_bytes(DTYPES[dtype], M, K, N, int(aligned)))
 
 
-def fastgl_gated_bwd_workspace_bytes(dtype: str, M: int, K: int, N: int, aligned: bool = False) -> int:
-    return int(lib().fastgl_gated_bwd_workspace_bytes(DTYPES[dtype], M, K, N, int(aligned)))
+def fastgl_gated_bwd_workspace_bytes(dtype: str, M: int, K: int, N: int, aligned: bool = False, fine: bool = False) -> int:
+    size = lib().fastgl_gated_bwd_fine_workspace_bytes if fine else lib().fastgl_gated_bwd_workspace_bytes
+    return int(size(DTYPES[dtype], M, K, N, int(aligned)))
 
 
 def fastgl_gated_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: Optional[torch.Tensor] = None,
@@ -471,8 +474,9 @@ def fastgl_gated_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G: tor
                      act: str = "silu", want=("dX", "dWg", "dWu", "dbg", "dbu"), dX: Optional[torch.Tensor] = None,
                      dWg: Optional[torch.Tensor] = None, dWu: Optional[torch.Tensor] = None,
                      dbg: Optional[torch.Tensor] = None, dbu: Optional[torch.Tensor] = None,
-                     workspace: Optional[torch.Tensor] = None):
+                     workspace: Optional[torch.Tensor] = None, fine: bool = False):
     """(dX, dWg, dWu, dbg, dbu); parts not named in `want` (and not passed in) are None.  dX and the weight
-    gradients are of X's dtype, the bias gradients float32."""
+    gradients are of X's dtype, the bias gradients float32.  In bfloat16 the gradients of G and U are rounded to bfloat16 before
+    the products; fine=True keeps them to 2^-17, for twice the products."""
     return _native().gated_bwd(X, Wg, Wu, G, U, dP, ACTS[act], *(n in want for n in ("dX", "dWg", "dWu", "dbg", "dbu")),
-                               dX, dWg, dWu, dbg, dbu, workspace)
+                               dX, dWg, dWu, dbg, dbu, workspace, fine)

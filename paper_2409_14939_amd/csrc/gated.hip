@@ -17,9 +17,6 @@ namespace {
 //   25 / 41, 64 rows 43 / 53
 constexpr int64_t kFewRows = 8, kFewRowsPacked = 48;
 constexpr int kSumGroups = 2048;       // workgroups of the gradient of the gate
-// Elements of dX or dWg, and of dG, up to which bf16 calls keep dG and dU in two pieces.  us a backward call, one piece / two: 1 row
-// 256 -> 1024 23 / 23; 30 rows 100 -> 300 27 / 26; but 300 rows 256 -> 1024 28 / 37, 130 000 rows 32 -> 64 72 / 119.
-constexpr int64_t kFewResults = 1024, kFewTerms = 16384;
 constexpr int64_t kMostWidth = (int64_t)1 << 20;
 
 // x as three bf16 whose sum is x exactly (each rounding to nearest).
@@ -203,8 +200,11 @@ struct DzArgs {
 };
 
 // dG = dP U act'(G), dU = dP act(G), rounded to what the matrix cores take: three pieces of fp32, or bf16, whose rounding adds an error
-// of the size of the results' own (2^-9 root mean square, sqrt 2 together).  Where bf16 gradients have few elements,
-// whose errors do not average, two pieces are kept (2^-17).  The column sums are formed from the unrounded values.
+// of the size of the results' own, as rounding any bf16 tensor between two products does (results are off by sqrt 2 of what their own
+// rounding costs, root mean square), or, where the caller asks for it, two pieces (2^-17) at twice the products: us a bf16 call, one piece /
+// two: 1 row 256 -> 1024 22 / 22, 300 rows 28 / 37, 8000 rows 72 / 91, 130 000 rows 32 -> 64 72 / 119, 16 384 rows 1024 -> 4096 586 / 1042.
+// One rule for all sizes: a row's gradient has the same error in a small batch and in a large one.  The column sums are formed from the
+// unrounded values.
 // Bound by memory: 16 384 x 4096 bf16 117 us, 671 MB at 5.7 TB/s.
 template <bool BF16, int ACT, int PLANES>
 __global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
@@ -388,11 +388,11 @@ struct Layout {
 };
 
 struct Shape {
-    bool bf16, aligned;
+    bool bf16, aligned, fine;
     int planes;
     int64_t M, K, N, ldk, ldn, ldz;
-    Shape(fastgl_dtype dtype, int64_t M_, int64_t K_, int64_t N_, bool aligned_)
-        : bf16(dtype == FASTGL_BF16), aligned(aligned_), planes(dtype == FASTGL_BF16 ? 1 : 3), M(M_), K(K_), N(N_),
+    Shape(fastgl_dtype dtype, int64_t M_, int64_t K_, int64_t N_, bool aligned_, bool fine_ = false)
+        : bf16(dtype == FASTGL_BF16), aligned(aligned_), fine(fine_), planes(dtype == FASTGL_BF16 ? 1 : 3), M(M_), K(K_), N(N_),
           ldk((int64_t)align_up((size_t)K_, 8)), ldn((int64_t)align_up((size_t)N_, 8)), ldz((int64_t)align_up((size_t)N_, 32))
     {
     }
@@ -404,7 +404,7 @@ struct Shape {
     // of the weight gradients read the same rows of many blocks at a time, which should not meet in the same memory channels.  0: rows lie whole, where there are few (nothing to gain) or four blocks pass 32-bit offsets.
     int64_t z_block() const { return M >= 1024 && M <= (int64_t)1 << 22 ? (int64_t)(align_up((size_t)M * 64, 4096) + 2304) / 2 : 0; }
     int64_t z_plane() const { return z_block() ? ldz / 32 * z_block() : M * ldz; }
-    int z_planes() const { return bf16 ? (M * K <= kFewResults || K * N <= kFewResults || M * N <= kFewTerms ? 2 : 1) : 3; }               // of dG and dU
+    int z_planes() const { return !bf16 ? 3 : fine ? 2 : 1; }               // of dG and dU
     int64_t pairs() const { return bf16 ? 1 : 6; }
     int64_t z_pairs() const { return bf16 ? z_planes() : 6; }
     Cut forward_cut() const { return cut_of(kForward, M, N, K, pairs()); }
@@ -579,15 +579,137 @@ bool starts_whole(std::initializer_list<const void *> ps)
     return true;
 }
 
-size_t workspace(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, bool aligned, bool backward)
+size_t workspace(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, bool aligned, bool backward, bool fine = false)
 {
     if (check(dtype, M, K, N, FASTGL_ACT_SILU) != FASTGL_OK) return 0;
-    const Shape d(dtype, M, K, N, aligned);
+    const Shape d(dtype, M, K, N, aligned, fine);
     Layout l;
     if (backward || !d.few_rows()) carve(d, backward, l);
     if (aligned) return l.used;
-    const size_t whole = workspace(dtype, M, K, N, true, backward);      // the tiles may be taken from fewer rows on
+    const size_t whole = workspace(dtype, M, K, N, true, backward, fine);      // the tiles may be taken from fewer rows on
     return l.used > whole ? l.used : whole;
+}
+
+fastgl_status gated_bwd(bool fine, fastgl_dtype dtype, const void *X, const void *Wg, const void *Wu, const void *G, const void *U,
+                        const void *dP, int64_t M, int64_t K, int64_t N, fastgl_act act, void *dX, void *dWg, void *dWu, float *dbg,
+                        float *dbu, void *ws, size_t ws_bytes, void *stream)
+{
+    fastgl_status st = check(dtype, M, K, N, act);
+    if (st != FASTGL_OK) return st;
+    const uintptr_t el = dtype == FASTGL_BF16 ? 2 : 4;
+    const bool want_x = dX && M > 0 && K > 0, want_w = (dWg || dWu) && K > 0 && N > 0, want_b = (dbg || dbu) && N > 0;
+    const bool terms = M > 0 && N > 0;
+    if (terms && (want_x || want_w || want_b) && (!G || !U || !dP)) {
+        set_error("G, U or dP is NULL");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (want_x && terms && (!Wg || !Wu)) {
+        set_error("dX needs Wg and Wu");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (want_w && terms && !X) {
+        set_error("dWg and dWu need X");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (misaligned_to(X, el) || misaligned_to(Wg, el) || misaligned_to(Wu, el) || misaligned_to(G, el) || misaligned_to(U, el) ||
+        misaligned_to(dP, el) || misaligned_to(dX, el) || misaligned_to(dWg, el) || misaligned_to(dWu, el) || misaligned_to(dbg, 4) ||
+        misaligned_to(dbu, 4)) {
+        set_error("matrices must be aligned to their element size");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    hipStream_t s = (hipStream_t)stream;
+    if (!terms) {                                     // sums without terms
+        const bool bf16 = dtype == FASTGL_BF16;
+        if (want_x && (st = launch_no_terms(bf16, dX, nullptr, M, K, false, s, "fastgl_gated_bwd (dX, N = 0)")) != FASTGL_OK) return st;
+        for (void *w : {dWg, dWu})
+            if (w && want_w && (st = launch_no_terms(bf16, w, nullptr, K, N, false, s, "fastgl_gated_bwd (dW, M = 0)")) != FASTGL_OK) return st;
+        for (float *b : {dbg, dbu})
+            if (b && want_b && (st = launch_no_terms(false, b, nullptr, 1, N, false, s, "fastgl_gated_bwd (db, M = 0)")) != FASTGL_OK) return st;
+        return FASTGL_OK;
+    }
+    if (!want_x && !want_w && !want_b) return FASTGL_OK;
+    const Shape d(dtype, M, K, N, starts_whole({want_w ? X : nullptr, want_x ? Wg : nullptr, want_x ? Wu : nullptr}), fine);
+    Layout l;
+    carve(d, true, l);
+    st = check_workspace(ws, ws_bytes, l.used);
+    if (st != FASTGL_OK) return st;
+    l = Layout();
+    l.base = (char *)ws;
+    const Scratch o = carve(d, true, l);
+
+    DzArgs z = {};
+    z.G = G; z.U = U; z.dP = dP;
+    z.dG = want_x || want_w ? o.dg : nullptr;
+    z.dU = o.du;
+    z.M = M; z.plane = d.z_plane();
+    z.N = (int32_t)N; z.lg = d.lg();
+    z.ld = d.z_block() ? 32 : d.ldz;
+    z.block = d.z_block() ? d.z_block() : 32;
+    z.part = want_b ? o.db : nullptr;
+    const dim3 dz((unsigned)d.dz_cols(), (unsigned)d.dz_rows());
+    by_act(act, [&](auto A) {
+        constexpr int ACT = decltype(A)::value;
+        if (d.z_planes() == 1) hipLaunchKernelGGL((k_gated_dz<true, ACT, 1>), dz, dim3(kBlock), 0, s, z);
+        else if (d.bf16) hipLaunchKernelGGL((k_gated_dz<true, ACT, 2>), dz, dim3(kBlock), 0, s, z);
+        else hipLaunchKernelGGL((k_gated_dz<false, ACT, 3>), dz, dim3(kBlock), 0, s, z);
+    });
+    FASTGL_LAUNCH_CHECK("fastgl_gated_bwd (dG, dU)");
+    SumArgs last = {};                                 // the sums at the end
+    if (want_b) {
+        last.db = o.db;
+        last.dbg = dbg; last.dbu = dbu;
+        last.rows = (int32_t)dz.y; last.N = (int32_t)N;
+    }
+    if ((st = pack(d, o, X, Wg, Wu, want_w, want_x, s)) != FASTGL_OK) return st;
+    const std::integral_constant<int, 0> none;
+    if (want_x) {
+        TileArgs g = {};
+        g.a[0] = o.dg; g.a[1] = o.du;
+        g.b[0] = d.pack_w() ? o.wg : (const uint16_t *)Wg;
+        g.b[1] = d.pack_w() ? o.wu : (const uint16_t *)Wu;
+        g.a_plane = d.z_plane(); g.b_plane = K * d.ldn;
+        g.lda = d.ldz; g.ldb = d.ldn;
+        g.a_blocks = d.z_block();
+        g.R = M; g.C = K; g.Kc = N;
+        g.pairs = (int32_t)d.z_pairs(); g.groups = 2;
+        g.planes_a = !d.bf16 ? kSixA : d.z_planes() == 2 ? kTwo : 0;
+        g.planes_b = !d.bf16 ? kSixB : 0;
+        g.out[0] = dX;
+        g.part = o.part;
+        const Cut cut = d.rows_cut();
+        if ((st = launch_tile<kRows>(g, cut, d.bf16, none, s, "fastgl_gated_bwd (dX)")) != FASTGL_OK) return st;
+        if (cut.slabs > 1) {
+            SumArgs a = {};
+            a.part = o.part; a.out[0] = dX;
+            a.n = a.stride = M * K;
+            a.slabs = (int32_t)cut.slabs; a.results = 1;
+            if ((st = launch_sum(a, d.bf16, s, "fastgl_gated_bwd (dX, sums)")) != FASTGL_OK) return st;
+        }
+    }
+    if (want_w) {
+        TileArgs g = {};
+        g.a[0] = d.pack_x() ? o.x : (const uint16_t *)X;
+        g.b[0] = o.dg; g.b[1] = o.du;
+        g.a_plane = M * d.ldk; g.b_plane = d.z_plane();
+        g.lda = d.ldk; g.ldb = d.ldz;
+        g.b_blocks = d.z_block();
+        g.R = K; g.C = N; g.Kc = M;
+        g.pairs = (int32_t)d.z_pairs(); g.groups = 1;
+        g.planes_a = !d.bf16 ? kSixA : 0;
+        g.planes_b = !d.bf16 ? kSixB : d.z_planes() == 2 ? kTwo : 0;
+        g.out[0] = dWg; g.out[1] = dWu;
+        g.part = o.part;
+        const Cut cut = d.weights_cut();
+        if ((st = launch_tile<kWeights>(g, cut, d.bf16, none, s, "fastgl_gated_bwd (dW)")) != FASTGL_OK) return st;
+        if (cut.slabs > 1) {
+            last.part = o.part;
+            last.out[0] = dWg; last.out[1] = dWu;
+            last.n = K * N; last.stride = 2 * K * N;
+            last.slabs = (int32_t)cut.slabs; last.results = 2;
+        }
+    }
+    if (want_b || last.results) return launch_sum(last, d.bf16, s, "fastgl_gated_bwd (sums)");
+    return FASTGL_OK;
 }
 
 }  // namespace
@@ -605,6 +727,11 @@ size_t fastgl_gated_fwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K
 size_t fastgl_gated_bwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned)
 {
     return workspace(dtype, M, K, N, aligned != 0, true);
+}
+
+size_t fastgl_gated_bwd_fine_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned)
+{
+    return workspace(dtype, M, K, N, aligned != 0, true, true);
 }
 
 fastgl_status fastgl_gated_fwd(fastgl_dtype dtype, const void *X, const void *Wg, const void *Wu, const float *bg,
@@ -696,122 +823,14 @@ fastgl_status fastgl_gated_bwd(fastgl_dtype dtype, const void *X, const void *Wg
                                const void *U, const void *dP, int64_t M, int64_t K, int64_t N, fastgl_act act, void *dX,
                                void *dWg, void *dWu, float *dbg, float *dbu, void *ws, size_t ws_bytes, void *stream)
 {
-    fastgl_status st = check(dtype, M, K, N, act);
-    if (st != FASTGL_OK) return st;
-    const uintptr_t el = dtype == FASTGL_BF16 ? 2 : 4;
-    const bool want_x = dX && M > 0 && K > 0, want_w = (dWg || dWu) && K > 0 && N > 0, want_b = (dbg || dbu) && N > 0;
-    const bool terms = M > 0 && N > 0;
-    if (terms && (want_x || want_w || want_b) && (!G || !U || !dP)) {
-        set_error("G, U or dP is NULL");
-        return FASTGL_ERR_INVALID_ARG;
-    }
-    if (want_x && terms && (!Wg || !Wu)) {
-        set_error("dX needs Wg and Wu");
-        return FASTGL_ERR_INVALID_ARG;
-    }
-    if (want_w && terms && !X) {
-        set_error("dWg and dWu need X");
-        return FASTGL_ERR_INVALID_ARG;
-    }
-    if (misaligned_to(X, el) || misaligned_to(Wg, el) || misaligned_to(Wu, el) || misaligned_to(G, el) || misaligned_to(U, el) ||
-        misaligned_to(dP, el) || misaligned_to(dX, el) || misaligned_to(dWg, el) || misaligned_to(dWu, el) || misaligned_to(dbg, 4) ||
-        misaligned_to(dbu, 4)) {
-        set_error("matrices must be aligned to their element size");
-        return FASTGL_ERR_INVALID_ARG;
-    }
-    hipStream_t s = (hipStream_t)stream;
-    if (!terms) {                                     // sums without terms
-        const bool bf16 = dtype == FASTGL_BF16;
-        if (want_x && (st = launch_no_terms(bf16, dX, nullptr, M, K, false, s, "fastgl_gated_bwd (dX, N = 0)")) != FASTGL_OK) return st;
-        for (void *w : {dWg, dWu})
-            if (w && want_w && (st = launch_no_terms(bf16, w, nullptr, K, N, false, s, "fastgl_gated_bwd (dW, M = 0)")) != FASTGL_OK) return st;
-        for (float *b : {dbg, dbu})
-            if (b && want_b && (st = launch_no_terms(false, b, nullptr, 1, N, false, s, "fastgl_gated_bwd (db, M = 0)")) != FASTGL_OK) return st;
-        return FASTGL_OK;
-    }
-    if (!want_x && !want_w && !want_b) return FASTGL_OK;
-    const Shape d(dtype, M, K, N, starts_whole({want_w ? X : nullptr, want_x ? Wg : nullptr, want_x ? Wu : nullptr}));
-    Layout l;
-    carve(d, true, l);
-    st = check_workspace(ws, ws_bytes, l.used);
-    if (st != FASTGL_OK) return st;
-    l = Layout();
-    l.base = (char *)ws;
-    const Scratch o = carve(d, true, l);
+    return gated_bwd(false, dtype, X, Wg, Wu, G, U, dP, M, K, N, act, dX, dWg, dWu, dbg, dbu, ws, ws_bytes, stream);
+}
 
-    DzArgs z = {};
-    z.G = G; z.U = U; z.dP = dP;
-    z.dG = want_x || want_w ? o.dg : nullptr;
-    z.dU = o.du;
-    z.M = M; z.plane = d.z_plane();
-    z.N = (int32_t)N; z.lg = d.lg();
-    z.ld = d.z_block() ? 32 : d.ldz;
-    z.block = d.z_block() ? d.z_block() : 32;
-    z.part = want_b ? o.db : nullptr;
-    const dim3 dz((unsigned)d.dz_cols(), (unsigned)d.dz_rows());
-    by_act(act, [&](auto A) {
-        constexpr int ACT = decltype(A)::value;
-        if (d.z_planes() == 1) hipLaunchKernelGGL((k_gated_dz<true, ACT, 1>), dz, dim3(kBlock), 0, s, z);
-        else if (d.bf16) hipLaunchKernelGGL((k_gated_dz<true, ACT, 2>), dz, dim3(kBlock), 0, s, z);
-        else hipLaunchKernelGGL((k_gated_dz<false, ACT, 3>), dz, dim3(kBlock), 0, s, z);
-    });
-    FASTGL_LAUNCH_CHECK("fastgl_gated_bwd (dG, dU)");
-    SumArgs last = {};                                 // the sums at the end
-    if (want_b) {
-        last.db = o.db;
-        last.dbg = dbg; last.dbu = dbu;
-        last.rows = (int32_t)dz.y; last.N = (int32_t)N;
-    }
-    if ((st = pack(d, o, X, Wg, Wu, want_w, want_x, s)) != FASTGL_OK) return st;
-    const std::integral_constant<int, 0> none;
-    if (want_x) {
-        TileArgs g = {};
-        g.a[0] = o.dg; g.a[1] = o.du;
-        g.b[0] = d.pack_w() ? o.wg : (const uint16_t *)Wg;
-        g.b[1] = d.pack_w() ? o.wu : (const uint16_t *)Wu;
-        g.a_plane = d.z_plane(); g.b_plane = K * d.ldn;
-        g.lda = d.ldz; g.ldb = d.ldn;
-        g.a_blocks = d.z_block();
-        g.R = M; g.C = K; g.Kc = N;
-        g.pairs = (int32_t)d.z_pairs(); g.groups = 2;
-        g.planes_a = !d.bf16 ? kSixA : d.z_planes() == 2 ? kTwo : 0;
-        g.planes_b = !d.bf16 ? kSixB : 0;
-        g.out[0] = dX;
-        g.part = o.part;
-        const Cut cut = d.rows_cut();
-        if ((st = launch_tile<kRows>(g, cut, d.bf16, none, s, "fastgl_gated_bwd (dX)")) != FASTGL_OK) return st;
-        if (cut.slabs > 1) {
-            SumArgs a = {};
-            a.part = o.part; a.out[0] = dX;
-            a.n = a.stride = M * K;
-            a.slabs = (int32_t)cut.slabs; a.results = 1;
-            if ((st = launch_sum(a, d.bf16, s, "fastgl_gated_bwd (dX, sums)")) != FASTGL_OK) return st;
-        }
-    }
-    if (want_w) {
-        TileArgs g = {};
-        g.a[0] = d.pack_x() ? o.x : (const uint16_t *)X;
-        g.b[0] = o.dg; g.b[1] = o.du;
-        g.a_plane = M * d.ldk; g.b_plane = d.z_plane();
-        g.lda = d.ldk; g.ldb = d.ldz;
-        g.b_blocks = d.z_block();
-        g.R = K; g.C = N; g.Kc = M;
-        g.pairs = (int32_t)d.z_pairs(); g.groups = 1;
-        g.planes_a = !d.bf16 ? kSixA : 0;
-        g.planes_b = !d.bf16 ? kSixB : d.z_planes() == 2 ? kTwo : 0;
-        g.out[0] = dWg; g.out[1] = dWu;
-        g.part = o.part;
-        const Cut cut = d.weights_cut();
-        if ((st = launch_tile<kWeights>(g, cut, d.bf16, none, s, "fastgl_gated_bwd (dW)")) != FASTGL_OK) return st;
-        if (cut.slabs > 1) {
-            last.part = o.part;
-            last.out[0] = dWg; last.out[1] = dWu;
-            last.n = K * N; last.stride = 2 * K * N;
-            last.slabs = (int32_t)cut.slabs; last.results = 2;
-        }
-    }
-    if (want_b || last.results) return launch_sum(last, d.bf16, s, "fastgl_gated_bwd (sums)");
-    return FASTGL_OK;
+fastgl_status fastgl_gated_bwd_fine(fastgl_dtype dtype, const void *X, const void *Wg, const void *Wu, const void *G,
+                                    const void *U, const void *dP, int64_t M, int64_t K, int64_t N, fastgl_act act, void *dX,
+                                    void *dWg, void *dWu, float *dbg, float *dbu, void *ws, size_t ws_bytes, void *stream)
+{
+    return gated_bwd(true, dtype, X, Wg, Wu, G, U, dP, M, K, N, act, dX, dWg, dWu, dbg, dbu, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

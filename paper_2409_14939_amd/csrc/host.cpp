@@ -800,7 +800,7 @@ PyObject *gated_fwd(PyObject *const *a)
     return tuple({P.t, G.t, U.t});
 }
 
-// (X, Wg, Wu, G, U, dP, act, want_dX, want_dWg, want_dWu, want_dbg, want_dbu, dX, dWg, dWu, dbg, dbu, workspace)
+// (X, Wg, Wu, G, U, dP, act, want_dX, want_dWg, want_dWu, want_dbg, want_dbu, dX, dWg, dWu, dbg, dbu, workspace, fine)
 // -> (dX, dWg, dWu, dbg, dbu)
 PyObject *gated_bwd(PyObject *const *a)
 {
@@ -813,6 +813,7 @@ PyObject *gated_bwd(PyObject *const *a)
     const at::Tensor &Wu = matrix2(a[2], type, K, N, "Wu"), &G = matrix2(a[3], type, M, N, "G"), &U = matrix2(a[4], type, M, N, "U");
     const at::Tensor &dP = matrix2(a[5], type, M, N, "dP");
     const auto act = (fastgl_act)integer(a[6]);
+    const bool fine = truth(a[18]);
     Out dX, dWg, dWu, dbg, dbu;
     if (truth(a[7]) || !none(a[12])) dX = out_of(a[12], type, {M, K}, X, "dX");
     if (truth(a[8]) || !none(a[13])) dWg = out_of(a[13], type, {K, N}, X, "dWg");
@@ -821,11 +822,13 @@ PyObject *gated_bwd(PyObject *const *a)
     if (truth(a[11]) || !none(a[16])) dbu = out_of(a[16], at::kFloat, {N}, X, "dbu");
     const fastgl_dtype dt = feat_dtype(X);
     const Scratch ws(a[17], X, [&] {
-        return fastgl_gated_bwd_workspace_bytes(dt, M, K, N, whole(X.data_ptr()) && whole(Wg.data_ptr()) && whole(Wu.data_ptr()));
+        const int aligned = whole(X.data_ptr()) && whole(Wg.data_ptr()) && whole(Wu.data_ptr());
+        return fine ? fastgl_gated_bwd_fine_workspace_bytes(dt, M, K, N, aligned) : fastgl_gated_bwd_workspace_bytes(dt, M, K, N, aligned);
     });
     run([&](void *s) {
-        return fastgl_gated_bwd(dt, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), G.data_ptr(), U.data_ptr(), dP.data_ptr(), M, K, N,
-                                act, dX.p(), dWg.p(), dWu.p(), (float *)dbg.p(), (float *)dbu.p(), ws.p(), ws.n(), s);
+        return (fine ? fastgl_gated_bwd_fine : fastgl_gated_bwd)(dt, X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), G.data_ptr(),
+                                                                 U.data_ptr(), dP.data_ptr(), M, K, N, act, dX.p(), dWg.p(), dWu.p(),
+                                                                 (float *)dbg.p(), (float *)dbu.p(), ws.p(), ws.n(), s);
     });
     return tuple({dX.t, dWg.t, dWu.t, dbg.t, dbu.t});
 }
@@ -845,7 +848,7 @@ PyMethodDef g_methods[] = {
     FN(update_fwd, 5), FN(layer_fwd, 14), FN(update_bwd, 12), FN(idmap, 7), FN(match, 7), FN(assemble_rows, 5),
     FN(overlap_counts, 3), FN(edge_weight_grad, 9), FN(edge_softmax_fwd, 4), FN(edge_softmax_bwd, 5),
     FN(edge_score_fwd, 6), FN(edge_score_bwd, 11), FN(norm_fwd, 13), FN(norm_bwd, 14), FN(dropout, 5),
-    FN(gather_rows_e4m3, 5), FN(gated_fwd, 11), FN(gated_bwd, 18), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
+    FN(gather_rows_e4m3, 5), FN(gated_fwd, 11), FN(gated_bwd, 19), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
 #undef FN
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host", "Native marshalling of the C ABI's calls.", -1, g_methods,

@@ -105,3 +105,16 @@ def test_workspace_sizes():
     assert f("bf16", -1, 8, 8) == 0 and b("bf16", 8, -1, 8) == 0 and b("bf16", 8, 8, 2 ** 21) == 0
     for M, K, N in ((16_384, 1024, 4096), (1, 2 ** 20, 2 ** 20), (300_000, 64, 64)):
         assert b("bf16", M, K, N) < 40 * (M * (K + 2 * N) + 4 * K * N) + (1 << 26)
+
+
+def test_fine_calls_are_checked_alike():
+    def fine(dt=1, M=64, K=8, N=8, act=0, G=FAKE, X=FAKE, ws=FAKE, wsb=1 << 40):
+        return B.lib().fastgl_gated_bwd_fine(dt, X, FAKE, FAKE, G, FAKE, FAKE, M, K, N, act, FAKE, FAKE, FAKE, None, None, ws, wsb, None)
+    for kw, status in ((dict(dt=2), INVALID), (dict(act=4), INVALID), (dict(M=-1), INVALID), (dict(K=2 ** 20 + 1), UNSUPPORTED), (dict(G=None), INVALID),
+                       (dict(X=ODD), INVALID), (dict(ws=None), INVALID), (dict(wsb=64), WORKSPACE)):
+        assert fine(**kw) == status
+    size = B.fastgl_gated_bwd_workspace_bytes
+    for M, K, N in ((1, 8, 16), (300, 33, 32), (5000, 256, 683)):
+        assert size("bf16", M, K, N, fine=True) >= 2 * 2 * 2 * M * N                           # two pieces of both
+        assert size("f32", M, K, N, fine=True) == size("f32", M, K, N)
+    assert fine(M=300, K=33, N=32, wsb=size("bf16", 300, 33, 32)) == WORKSPACE

@@ -288,3 +288,27 @@ def test_gate_of_what_is_not_finite_and_far_out():
             P, _, _ = B.fastgl_gated_fwd(e(M, 0), e(0, N), e(0, N), g.cuda(), torch.ones(N).cuda(), "gelu")
             p = P[M - 1].float().cpu()
             assert torch.equal(p[:4], g[:4].to(t).float()) and bool((p[4:9] == 0).all()) and bool(torch.isnan(p[9:]).all())
+
+
+# --------------------------------------------------------------------------------- what dG and dU are rounded to
+@pytest.mark.parametrize("M,K,N", [(1, 8, 16), (1, 256, 1024), (4, 16, 300), (16, 64, 1024), (17, 64, 1024), (30, 100, 300), (300, 32, 32), (300, 33, 32),
+                                   (1030, 40, 72), (20_000, 256, 200)])
+def test_terms_of_bf16_gradients(M, K, N):
+    """One rule at every size.  With ReLU dG = dP U and dU = dP G are exact in float32, so that their roundings to bfloat16 are known: the plain call
+    gives the products of those, the fine one those of the unrounded terms."""
+    x, wg, wu, _, _ = inputs(M, K, N, "bf16", 60)
+    g, u, dp = make((M, N), "bf16", 71), make((M, N), "bf16", 72), make((M, N), "bf16", 73)
+    on = (g > 0).double()
+    dg, du = dp.double() * u.double() * on, dp.double() * g.double() * on
+    args = [v.cuda() for v in (x, wg, wu, g, u, dp)]
+    for fine, half in ((False, 0.0), (True, 2.0 ** -17)):
+        a, b = (v if fine else v.bfloat16().double() for v in (dg, du))
+        out = B.fastgl_gated_bwd(*args, "relu", want=("dX", "dWg", "dWu"), fine=fine)
+        xd, wgd, wud = x.double(), wg.double(), wu.double()
+        for got, want, size, terms, what in ((out[0], a @ wgd.T + b @ wud.T, a.abs() @ wgd.abs().T + b.abs() @ wud.abs().T, 2 * N, "dX"),
+                                             (out[1], xd.T @ a, xd.abs().T @ a.abs(), M, "dWg"), (out[2], xd.T @ b, xd.abs().T @ b.abs(), M, "dWu")):
+            off = size * (half + U32 * 1.3 * (terms * (2 if fine else 1) + 4))
+            within(got, want, off + 2.0 ** -8 * (want.abs() + off) + 1e-37, (fine, what))
+    f32 = [v.float() for v in args]
+    for p, q in zip(B.fastgl_gated_bwd(*f32, "relu"), B.fastgl_gated_bwd(*f32, "relu", fine=True)):
+        assert torch.equal(p, q)
