@@ -433,8 +433,8 @@ def fastgl_norm_bwd(S: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, d
                     want=("dX", "dR", "dw"), dX: Optional[torch.Tensor] = None, dR: Optional[torch.Tensor] = None,
                     dw: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """(dX, dR, dw); parts not named in `want` (and not passed in) are None.  S: what the forward pass returned as h
-    (X where that was None); dS: the gradient that reaches h from elsewhere.  Without dropout dX and dR are the
-    same values, and one tensor unless they were passed in."""
+    (X where that was None); dS: the gradient that reaches h from elsewhere.  Without dropout dX and dR hold the same
+    values, each in a tensor of its own: a caller to whom one of them is enough asks for one."""
     return _native().norm_bwd(S, weight, rstd, dY, dS, rng, p, dX is None and "dX" in want, dR is None and "dR" in want,
                               dw is None and "dw" in want, dX, dR, dw, workspace)
 

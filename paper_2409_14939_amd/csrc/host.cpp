@@ -716,16 +716,14 @@ PyObject *norm_bwd(PyObject *const *a)
     const int64_t *rng = rng_state(a[5]);
     const double p = to_double(a[6]);
     Out dX, dR, dw;
-    const bool one = p == 0.0 && none(a[10]) && none(a[11]);          // without dropout both are the same gradient
-    if (!none(a[10]) || (truth(a[7]) && !one)) dX = out_of(a[10], S.scalar_type(), {M, F}, S, "dX");
-    if (!none(a[11]) || truth(a[8]) || (truth(a[7]) && one)) dR = out_of(a[11], S.scalar_type(), {M, F}, S, "dR");
+    if (!none(a[10]) || truth(a[7])) dX = out_of(a[10], S.scalar_type(), {M, F}, S, "dX");
+    if (!none(a[11]) || truth(a[8])) dR = out_of(a[11], S.scalar_type(), {M, F}, S, "dR");
     if (!none(a[12]) || truth(a[9])) dw = out_of(a[12], at::kFloat, {F}, S, "dw");
     const Scratch ws(a[13], S, [&] { return dw.t.defined() ? fastgl_norm_bwd_workspace_bytes(M, F) : 0; });
     run([&](void *s) {
         return fastgl_norm_bwd(feat_dtype(S), S.data_ptr(), w, rstd, dY, dS, M, F, rng, p, dX.p(), dR.p(), (float *)dw.p(),
                                ws.p(), ws.n(), s);
     });
-    if (one) return tuple({truth(a[7]) ? dR.t : at::Tensor(), truth(a[8]) ? dR.t : at::Tensor(), dw.t});
     return tuple({dX.t, dR.t, dw.t});
 }
 

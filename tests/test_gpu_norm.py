@@ -285,3 +285,19 @@ def test_e4m3_of_weights_that_are_not_finite():
         assert bool(torch.isinf(scale).all()) and bool(torch.isnan(q[:, [3, F - 1]]).all())
         q[:, [3, F - 1]] = 0
         assert bool((q == 0).all())
+
+
+def test_gradients_are_tensors_of_their_own():
+    """Also without dropout, where dX and dR are the same values: a change of one leaves the other as it is."""
+    S, dY, w = make(50, 72, "f32", 1).cuda(), make(50, 72, "f32", 2).cuda(), torch.ones(72).cuda()
+    rstd = (1.0 / torch.sqrt(S.double().square().mean(1) + EPS)).float()
+    for p in (0.0, 0.3):
+        dX, dR, dw = B.fastgl_norm_bwd(S, w, rstd, dY, rng=state(), p=p)
+        kept = dR.clone()
+        assert p > 0 or torch.equal(dX, dR)
+        dX.zero_()
+        assert torch.equal(dR, kept)
+        for want, i in (("dX", 0), ("dR", 1)):                     # one of them alone
+            alone = B.fastgl_norm_bwd(S, w, rstd, dY, rng=state(), p=p, want=(want,))
+            assert [v is not None for v in alone] == [i == 0, i == 1, False]
+            assert torch.equal(alone[1], kept) if i else p > 0 or torch.equal(alone[0], kept)
