@@ -8,7 +8,7 @@
  *   rstd = 1 / sqrt(mean over the row of h^2 + eps)
  *   Y    = h * rstd * w
  *   drop(x)[i,j] = x[i,j] * 65536 / (65536 - t) where keep(i,j), else 0;
- *                  t = round(65536 p), 0 <= p <= 1
+ *                  t = round(65536 p), 0 <= p <= 1; the factor is rounded to fp32 first
  *   keep(i,j): half word j % 8 of Philox4x32-10(key = seed, counter =
  *                  (j / 8, i, offset)) is >= t; low half words first
  *
