@@ -11,11 +11,20 @@
 namespace fastgl {
 namespace {
 
-// Rows that k_gated_rows takes: fewer where the tiles need no packed operands.  us a call, k_gated_rows / tiles:
-//   bf16, nothing to pack: 256 -> 1024 1 row 5.5 / 5.7, 16 rows 5.5 / 5.7, 32 rows 8.0 / 5.8; 1024 -> 4096 1 row 7.4 / 10.5, 8 rows
-//   10.1 / 11.0, 16 rows 14.6 / 11.3;   float32: 256 -> 1024 1 row 5.4 / 19, 32 rows 8.3 / 20; 1024 -> 4096 1 row 9.4 / 40, 32 rows
-//   25 / 41, 64 rows 43 / 53
-constexpr int64_t kFewRows = 8, kFewRowsPacked = 48;
+// Rows that k_gated_rows takes, by the elements of a weight matrix: its time grows with the rows, that of the tiles hardly, but they pack
+// operands that are fp32 or no multiple of 16 bytes.  us a call, k_gated_rows / tiles, on both sides of each line:
+//   bf16, nothing to pack: 1024 -> 4096 2 rows 8.2 / 10.5, 3 rows 11.4 / 10.5, 8 rows 12.8 / 11.0; 2048 -> 1024 8 rows 9.3 / 9.9; 512 -> 2048 8 rows
+//   6.6 / 9.0; 256 -> 1024 8 rows 5.6 / 5.6, 16 rows 5.6 / 5.6, 32 rows 7.2 / 5.6
+//   bf16, packed: 1000 -> 4095 12 rows 16.6 / 19.0, 16 rows 19.6 / 18.9, 32 rows 34.5 / 19.2; 500 -> 2001 24 rows 13.8 / 15.5, 32 rows 17.1 / 15.5, 48 rows
+//   23.0 / 15.7; 257 -> 1023 32 rows 8.3 / 9.6, 48 rows 12.1 / 9.8; 2000 -> 300 32 rows 11.8 / 13.1, 64 rows 15.6 / 13.6; 100 -> 300 64 rows 5.6 / 9.1
+//   fp32: 1024 -> 4096 48 rows 34.5 / 48.4, 64 rows 43.6 / 48.9, 80 rows 51.9 / 49.4; 1000 -> 1000 64 rows 23.1 / 26.3, 80 rows 27.1 / 26.4; 256 -> 1024
+//   64 rows 11.0 / 15.8, 128 rows 17.1 / 18.0; 100 -> 300 64 rows 5.6 / 12.5
+inline int64_t few_rows_of(bool bf16, bool packed, int64_t weights)
+{
+    if (bf16 && !packed) return weights > (int64_t)1 << 21 ? 2 : 8;
+    if (bf16 && weights > (int64_t)1 << 16) return weights > (int64_t)1 << 21 ? 16 : 32;
+    return 60;
+}
 constexpr int kSumGroups = 2048;       // workgroups of the gradient of the gate
 constexpr int64_t kMostWidth = (int64_t)1 << 20;
 
@@ -398,10 +407,13 @@ struct Shape {
     }
     bool pack_x() const { return !bf16 || !aligned || K % 8; }
     bool pack_w() const { return !bf16 || !aligned || N % 8; }
-    bool few_rows() const { return M <= (pack_x() || pack_w() ? kFewRowsPacked : kFewRows); }
+    bool few_rows() const { return M <= few_rows_of(bf16, pack_x() || pack_w(), K * N); }
     // Elements of a block of 32 columns of dG and dU, which lie [block][row][32]: dX then reads whole lines although it takes 32
     // columns a step (16 384 x 8192 times 8192 x 1024: 245 -> 221 us).  A block is 2304 bytes more than a multiple of 4096: the tiles
-    // of the weight gradients read the same rows of many blocks at a time, which should not meet in the same memory channels.  0: rows lie whole, where there are few (nothing to gain) or four blocks pass 32-bit offsets.
+    // of the weight gradients read the same rows of many blocks at a time, which should not meet in the same memory channels.  0: rows lie
+    // whole, where there are few or four blocks pass 32-bit offsets.  us a backward call, blocks / whole rows, 1024 -> 4096: 512 rows bf16
+    // 50.5 / 50.2, fp32 154 / 155; 1024 rows 65.7 / 66.4, 249 / 253; 2000 rows 110 / 109, 403 / 413; 4000 rows 189 / 190, 752 / 779; 16 000 rows
+    // 574 / 594, 2750 / 2839; bf16 256 -> 1024 1000 rows 35.8 / 37.1, 4000 rows 53.1 / 51.5, 16 000 rows 96.9 / 101.7.
     int64_t z_block() const { return M >= 1024 && M <= (int64_t)1 << 22 ? (int64_t)(align_up((size_t)M * 64, 4096) + 2304) / 2 : 0; }
     int64_t z_plane() const { return z_block() ? ldz / 32 * z_block() : M * ldz; }
     int z_planes() const { return !bf16 ? 3 : fine ? 2 : 1; }               // of dG and dU

@@ -31,8 +31,8 @@ SHAPES_F32 = [(17_719, 34, 193),       # L, S p, S p
               (17_433, 263, 68),       # L p, S, M p
               (17_250, 9, 83),         # M, S, S p
               (22_255, 9, 128),        # M o, S, S p
-              (50, 1528, 1728),        # M p, M p, M
-              (50, 72, 9),             # S p, S, S
+              (50, 1528, 1728),        # few rows, M p, M
+              (50, 72, 9),             # few rows, S, S
               (39_388, 145, 9),        # S, L, S p
               (17_322, 136, 128),      # M o, L p, S p
               (18_948, 151, 8),        # S, M, S p
@@ -41,7 +41,10 @@ SHAPES_F32 = [(17_719, 34, 193),       # L, S p, S p
               (5131, 908, 65),         # S p, M, L p
               (9, 1326, 1480),         # few rows, S p, M
               (1327, 9, 455),          # S, S p, M p
-              (372, 1046, 4427), (33_388, 82, 2900), (70_001, 64, 24), (4000, 1024, 1500)]
+              (64, 1528, 1728),        # S p, S p, M
+              (64, 72, 9),             # S p, S, S
+              (372, 1046, 4427),       # M p, S p, L
+              (61, 300, 100), (33_388, 82, 2900), (70_001, 64, 24), (4000, 1024, 1500)]
 # dG and dU lie in blocks of 32 columns from 1024 rows on.
 LINES = [(1023, 40, 100), (1024, 40, 100), (1025, 33, 65)]
 SHAPES = [("bf16", *s) for s in SHAPES_BF16 + LINES] + [("f32", *s) for s in SHAPES_F32 + LINES]
