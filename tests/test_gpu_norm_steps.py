@@ -15,9 +15,9 @@ def factor(p):
     return float(np.float32(ref.drop_scale(p)))
 
 
-# Every spread of a row over lanes, with rows for more than two launches' worth of groups and no multiple of a step: 1, 8, 16, 32, 64 and 256
+# Every spread of a row over lanes, with rows for more than two launches' worth of groups and no multiple of a step: 1, 2, 4, ... 64 and 256
 # lanes, one to four chunks a lane, and rows that are read twice.
-SHAPES = [(1_100_003, 5), (140_001, 47), (70_001, 100), (140_003, 160), (40_001, 256), (70_003, 300), (17_001, 500), (20_001, 602), (17_003, 1000), (17_003, 1500),
+SHAPES = [(1_100_003, 5), (600_001, 9), (600_007, 16), (300_001, 17), (300_003, 24), (300_007, 32), (140_001, 47), (70_001, 100), (140_003, 160), (40_001, 256), (70_003, 300), (17_001, 500), (20_001, 602), (17_003, 1000), (17_003, 1500),
           (4500, 2000), (4500, 2050), (4501, 5000), (2100, 8197)]
 
 
@@ -28,10 +28,10 @@ def setting(M, F, dtype, p):
     rng = torch.tensor([0x1234_5678_9ABC, (1 << 40) + F], dtype=torch.int64, device="cuda")
     keep = B.fastgl_dropout(torch.ones(M, F, device="cuda"), rng, p) != 0 if p > 0 else torch.ones(M, F, dtype=torch.bool, device="cuda")
     if p > 0:                                                       # the mask itself, in the last rows
-        at = np.arange(M - 3, M, dtype=np.uint64)[:, None]
+        at = np.arange(max(0, M - 3), M, dtype=np.uint64)[:, None]
         w = ref.philox(np.arange(-(-F // 8), dtype=np.uint64)[None, :], at, np.uint64(int(rng[1]) & 0xFFFFFFFF), np.uint64(int(rng[1]) >> 32),
                        int(rng[0]) & 0xFFFFFFFF, int(rng[0]) >> 32)
-        halves = np.stack([h for v in w for h in (v & np.uint64(0xFFFF), v >> np.uint64(16))], -1).reshape(3, -1)[:, :F]
+        halves = np.stack([h for v in w for h in (v & np.uint64(0xFFFF), v >> np.uint64(16))], -1).reshape(at.shape[0], -1)[:, :F]
         assert torch.equal(keep[-3:].cpu(), torch.from_numpy(halves >= ref.threshold(p)))
     return make, 1.0 + 0.3 * torch.randn(F, generator=g, device="cuda"), rng, keep
 
@@ -100,6 +100,14 @@ def test_weight_gradient_counts_every_row_once(M, F, dtype):
     _, _, dw = B.fastgl_norm_bwd(S, torch.ones(F, device="cuda"), rstd, dY, want=("dw",))
     want = (S.double() * dY.double() * rstd.double()[:, None]).sum(0)
     assert 8 * M < 1 << 24 and torch.equal(dw.double(), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,F", [(M, F) for M in (1, 2, 3, 31, 64, 129) for F in (9, 15, 16, 17, 25, 32)])
+def test_few_narrow_rows(M, F, dtype):
+    test_forward_in_steps(M, F, dtype)
+    test_backward_in_steps(M, F, dtype)
+    test_weight_gradient_counts_every_row_once(M, F, dtype)
 
 
 @pytest.mark.parametrize("dtype,n,F", [("bf16", 270_003, 131), ("bf16", 33_001, 1031), ("bf16", 6_800_003, 5), ("bf16", 4_300_001, 8), ("f32", 130_007, 133),
