@@ -77,3 +77,19 @@ def test_rows_of_the_table():
         bound = y.abs() * (2.0 ** -4 * 1.001 + half) + scale.double()[ids][:, None] * 2.0 ** -10 * 1.01
         assert bool(((rows - y).abs() <= bound).all())
     assert np.isfinite(rows.cpu().numpy()).all()
+
+
+def test_a_mini_batch_of_reused_rows_and_rows_of_an_8_bit_table():
+    """Match, the gather of what has to be loaded, assembly: the same calls as with a float32 table, and the same rows as a gather of all."""
+    g = torch.Generator().manual_seed(3)
+    rows, F = 5000, 100
+    table = torch.randn(rows, F, generator=g).cuda()
+    Q, scale, _, _ = B.fastgl_norm_fwd_e4m3(table, torch.ones(F).cuda(), ex.EPS, want_rstd=False)
+    first, second = (torch.randperm(rows, generator=g)[:n].cuda() for n in (1500, 1777))
+    for dtype in ("f32", "bf16"):
+        X = B.fastgl_gather_rows_e4m3(Q, scale, first, dtype)
+        src_row, _, load_gid, result = B.fastgl_match(first, second)
+        n_load, violations = result.tolist()
+        assert violations == 0 and 0 < n_load < second.numel()
+        load = B.fastgl_gather_rows_e4m3(Q, scale, load_gid[:n_load], dtype)
+        assert torch.equal(B.fastgl_assemble_rows(X, load, src_row, n_load), B.fastgl_gather_rows_e4m3(Q, scale, second, dtype))
