@@ -214,7 +214,7 @@ struct DzArgs {
 // two: 1 row 256 -> 1024 22 / 22, 300 rows 28 / 37, 8000 rows 72 / 91, 130 000 rows 32 -> 64 72 / 119, 16 384 rows 1024 -> 4096 586 / 1042.
 // One rule for all sizes: a row's gradient has the same error in a small batch and in a large one.  The column sums are formed from the
 // unrounded values.
-// Bound by memory: 16 384 x 4096 bf16 117 us, 671 MB at 5.7 TB/s.
+// Bound by memory: 16 384 x 4096 bf16 119 us, 671 MB at 5.6 TB/s.
 template <bool BF16, int ACT, int PLANES>
 __global__ __launch_bounds__(kBlock) void k_gated_dz(DzArgs a)
 {
@@ -354,10 +354,10 @@ struct Cut {
 // The cut that a model of the launch finds fastest.  A compute unit needs single_us for a step of a workgroup that it has alone and
 // pair_us for one of each of two (large tiles: one at a time), and tile_us for what is around the steps; slabs cost the sums that they
 // write and that are read again (4 bytes each way at some 6 TB/s), and a launch.
-// Measured (kernel times, bf16, us for large / middle / small tiles):
-//   forward 16 384 x 1024 -> 4096, G and U kept 271 / 268 / -, alone 227 / 240 / -;  115 000 x 256 -> 1024 196 / 186 / -, 154 / 139 / -
-//   dX 16 384 x 4096 -> 1024 242 / 284 / 344 (221 with dG, dU in blocks);  dWg, dWu of 16 384 rows 1024 x 4096 206 / 240 / 416 (the first two in two slabs)
-//   backward call of 300 rows 256 -> 1024 33 / 29 / 27, of 2000 rows 56 / 51 / 47, of 8000 rows 256 -> 683 79 / 72 / 76
+// Measured (bf16, us for large / middle / small tiles; kernel times, the least of 150 passes on one card):
+//   forward 16 384 rows 1024 -> 4096, G and U kept 273 / 269 / -, alone 241 / 253 / -;  115 000 rows 256 -> 1024 193 / 174 / -, 162 / 140 / -
+//   dX of 16 384 rows 1024 -> 4096 223 / 278 / 310, dWg and dWu there 218 / 241 / 401 (the first two in two slabs)
+//   all kernels of a backward call of 300 rows 256 -> 1024 (medians) 36 / 32 / 31, of 2000 rows 52 / 47 / 43, of 8000 rows 256 -> 683 73 / 67 / 60
 Cut cut_of(int mode, int64_t R, int64_t C, int64_t Kc, int64_t segments)
 {
     static const double single_us[3][3] = {{0.80, 0.60, 0.36}, {0.93, 0.65, 0.38}, {0.80, 0.60, 0.42}};      // [mode][size]
@@ -539,9 +539,9 @@ void by_act(fastgl_act act, F f)
 
 // One product: results in bf16 or fp32, or sums of slabs.
 //
-// Results of the forward pass go past the caches where the tiles' rows are whole 128-byte lines.  us a call, bf16, through the caches /
-// past them: 115 000 rows 256 -> 1024, G and U kept 250 / 186, alone 168 / 139; 8000 rows 18.6 / 16.2, 15.6 / 11.9; 16 384 rows
-// 1024 -> 4096 307 / 268.  Rows that are not: 60 000 rows 128 -> 520 49 / 95; 20 000 rows 100 -> 1000 35 / 70.
+// Results of the forward pass go past the caches where the tiles' rows are whole 128-byte lines.  us, through the caches / past them (bf16; kernel
+// times, the least of 150 passes on one card): 115 000 rows 256 -> 1024, G and U kept 246 / 174, alone 167 / 141; 8000 rows 16.9 / 16.2, 13.8 / 12.4;
+// 16 384 rows 1024 -> 4096 302 / 273, 253 / 242.  Rows that are not: 60 000 rows 128 -> 520 49 / 92; 20 000 rows 104 -> 1000 31 / 63.
 template <int MODE, class ACT>
 fastgl_status launch_tile(TileArgs g, const Cut &cut, bool bf16, ACT, hipStream_t s, const char *what)
 {

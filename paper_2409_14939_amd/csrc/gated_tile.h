@@ -15,11 +15,11 @@
 //   are loaded from) so that the lanes of a read meet different banks.
 // * Buffer resources end the operands: what lies beyond is read as 0.  Pieces beyond the contracted range that lie inside an
 //   operand are given an address beyond the end.
-// * What bounds it: the matrix instructions at the clock that the card holds under them (1.7 to 1.9 GHz of 2.4).  dWg, dWu of 16 384 rows
-//   1024 x 4096 bf16: 206 us, 1334 TFLOP/s, the matrix cores busy 82 to 87 % of a compute unit's cycles; dX there 221 us, 1244 TFLOP/s (245 with dG and dU in whole rows, of which a
-//   step takes 64 bytes; a library product of that shape 205); forward 115 000 rows 256 -> 1024 178 us, bound by its 706 MB
-//   of results (4.3 TB/s with what is read); 16 384 rows 1024 -> 4096 227 us without G and U, 1211 TFLOP/s.  No LDS bank conflicts in dX
-//   and dW.  fp32 runs at a sixth: 222 TFLOP/s at 16 384 rows 1024 -> 4096.
+// * What bounds it: the matrix instructions at the clock that the card holds under them (1.7 to 1.9 GHz of 2.4).  Kernel times, the least of
+//   150 passes on one card: dWg, dWu of 16 384 rows 1024 x 4096 bf16 215 us, 1279 TFLOP/s, the matrix cores busy 82 to 87 % of a compute unit's
+//   cycles; dX there 222 us, 1238 TFLOP/s (a library product of that shape 215); forward 16 384 rows 1024 -> 4096 242 us without G and U, 1136
+//   TFLOP/s; 115 000 rows 256 -> 1024 with them 174 us, bound by its 706 MB of results (4.4 TB/s with what is read).  No LDS bank conflicts
+//   in dX and dW.  fp32 runs at a sixth: 207 TFLOP/s at 16 384 rows 1024 -> 4096 with GELU.
 // * Results are turned through LDS, 64 x 64 at a time for each wavefront alone, into whole 128-byte lines.
 #pragma once
 #include <type_traits>

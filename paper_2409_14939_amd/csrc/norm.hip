@@ -3,7 +3,8 @@
 //
 // A row is read once: its columns stay in registers between the sum of squares and the result.  A lane holds eight
 // columns at a time (one 16-byte word of bf16, two of fp32, one answer of the generator).  A row has 1 to 64 lanes
-// of a wavefront, NC chunks each, and beyond 1536 columns a workgroup; beyond 8192 it is read twice.  Groups of lanes walk the rows with
+// of a wavefront, NC chunks each, and beyond 1536 columns a workgroup; beyond 8192 it is read twice (to 8 bits
+// three times, backward with column sums three times).  Groups of lanes walk the rows with
 // the grid's stride, so that the weights stay in registers and the backward pass keeps its column sums there.
 //
 // Bound by memory; a copy runs at 4.7 to 5.0 TB/s on the same cards.  us a call and TB/s of what has to move: 512 000 bf16 rows of 256
