@@ -229,7 +229,7 @@ def _own(s):
         dkv = torch.empty_like(s["KV"])
         k = s["K"].shape[1]
         into = dict(dK=dkv[:, :k], dV=dkv[:, k:])
-    dq, dk, dv, dbias = B.fastgl_attn_bwd(*block, s["Q"], s["K"], s["V"], lse, s["dO"], **how, **into)
+    dq, dk, dv, dbias = B.fastgl_attn_bwd(*block, s["Q"], s["K"], s["V"], s["dO"], **how, **into)
     out = [o, lse, dq] + ([dkv] if c["one_array"] else [dk, dv])
     return out + ([dbias] if c["buckets"] else [])
 
