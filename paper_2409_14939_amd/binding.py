@@ -39,6 +39,7 @@ EXPORTS = [
     "fastgl_norm_fwd", "fastgl_norm_fwd_e4m3", "fastgl_norm_bwd", "fastgl_norm_bwd_workspace_bytes", "fastgl_dropout",
     "fastgl_gather_rows_e4m3", "fastgl_gated_fwd", "fastgl_gated_bwd", "fastgl_gated_fwd_workspace_bytes",
     "fastgl_gated_bwd_workspace_bytes", "fastgl_gated_bwd_fine", "fastgl_gated_bwd_fine_workspace_bytes",
+    "fastgl_attn_fwd", "fastgl_attn_bwd", "fastgl_attn_workspace_bytes",
 ]
 MAX_REORDER_BATCHES = 64
 ACTS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
@@ -55,6 +56,15 @@ class BlockDesc(ctypes.Structure):
     _fields_ = [("indptr", ctypes.c_void_p), ("indices", ctypes.c_void_p), ("num_dst", ctypes.c_int64),
                 ("num_src", ctypes.c_int64), ("num_edges", ctypes.c_int64), ("parts", ctypes.c_int),
                 ("plan_mem", ctypes.c_void_p), ("plan_bytes", ctypes.c_size_t)]
+
+
+class AttnDesc(ctypes.Structure):
+    _fields_ = [("indptr", ctypes.c_void_p), ("indices", ctypes.c_void_p), ("num_dst", ctypes.c_int64),
+                ("num_src", ctypes.c_int64), ("num_edges", ctypes.c_int64), ("bucket", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p), ("num_buckets", ctypes.c_int64), ("heads", ctypes.c_int64),
+                ("kv_heads", ctypes.c_int64), ("width", ctypes.c_int64), ("scale", ctypes.c_float), ("dtype", ctypes.c_int),
+                ("Q", ctypes.c_void_p), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("ldq", ctypes.c_int64),
+                ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64)]
 
 
 class PlanView(ctypes.Structure):
@@ -133,6 +143,11 @@ def lib() -> ctypes.CDLL:
         L.fastgl_gated_fwd.argtypes = [i32, p, p, p, p, p, i64, i64, i64, i32, p, p, p, p, sz, p]
         for f in (L.fastgl_gated_bwd, L.fastgl_gated_bwd_fine):
             f.argtypes = [i32, p, p, p, p, p, p, i64, i64, i64, i32, p, p, p, p, p, p, sz, p]
+        desc = ctypes.POINTER(AttnDesc)
+        L.fastgl_attn_workspace_bytes.argtypes = [desc, i32]
+        L.fastgl_attn_workspace_bytes.restype = sz
+        L.fastgl_attn_fwd.argtypes = [desc, p, i64, p, p, p, sz, p]
+        L.fastgl_attn_bwd.argtypes = [desc, p, i64, p, i64, p, i64, p, i64, p, p, p, sz, p]
         L.fastgl_idmap_table_slots.argtypes = [i64]
         L.fastgl_idmap_table_slots.restype = i64
         L.fastgl_idmap_workspace_bytes.argtypes = [i64, i64]
@@ -480,3 +495,34 @@ def fastgl_gated_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G: tor
     the products; fine=True keeps them to 2^-17, for twice the products."""
     return _native().gated_bwd(X, Wg, Wu, G, U, dP, ACTS[act], *(n in want for n in ("dX", "dWg", "dWu", "dbg", "dbu")),
                                dX, dWg, dWu, dbg, dbu, workspace, fine)
+
+
+def fastgl_attn_workspace_bytes(num_dst: int, num_src: int, num_edges: int, heads: int, width: int, dtype: str,
+                                kv_heads: Optional[int] = None, num_buckets: int = 0, backward: bool = False) -> int:
+    """num_buckets: of the bias, 0 without one."""
+    d = AttnDesc(num_dst=num_dst, num_src=num_src, num_edges=num_edges, heads=heads, kv_heads=kv_heads or heads, width=width,
+                 dtype=DTYPES[dtype], num_buckets=num_buckets, bucket=num_buckets and 4, bias=num_buckets and 4)
+    return int(lib().fastgl_attn_workspace_bytes(ctypes.byref(d), int(backward)))
+
+
+def fastgl_attn_fwd(indptr, indices, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, heads: int,
+                    kv_heads: Optional[int] = None, scale: Optional[float] = None, bucket: Optional[torch.Tensor] = None,
+                    bias: Optional[torch.Tensor] = None, want_lse: bool = True, O: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, plan: Optional[Plan] = None, workspace: Optional[torch.Tensor] = None):
+    """(O, lse) of attention over a block's edges: softmax(scale * <q, k> + bias[bucket]) per row and head, applied to V.
+    Q [num_dst, heads * width], K and V [num_src, kv_heads * width], ranges of another tensor's columns included; scale None:
+    1 / sqrt(width); bucket int32 [num_edges], a negative one leaves its edge out; bias float32 [num_buckets, heads]; lse float32
+    [num_dst, heads]: the logarithm of what the weights are divided by."""
+    return _native().attn_fwd(indptr, indices, Q, K, V, heads, kv_heads, scale, bucket, bias, want_lse, O, lse, plan, workspace)
+
+
+def fastgl_attn_bwd(indptr, indices, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, dO: torch.Tensor, heads: int,
+                    kv_heads: Optional[int] = None, scale: Optional[float] = None,
+                    bucket: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                    want=("dQ", "dK", "dV", "dbias"), dQ: Optional[torch.Tensor] = None, dK: Optional[torch.Tensor] = None,
+                    dV: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None, plan: Optional[Plan] = None,
+                    workspace: Optional[torch.Tensor] = None):
+    """(dQ, dK, dV, dbias); parts not named in `want` (and not passed in) are None, dbias also without a bias.  plan: PLAN_ALL,
+    with buckets PLAN_ALL | PLAN_PERM."""
+    return _native().attn_bwd(indptr, indices, Q, K, V, heads, kv_heads, scale, bucket, bias, dO,
+                              *(n in want for n in ("dQ", "dK", "dV", "dbias")), dQ, dK, dV, dbias, plan, workspace)

@@ -17,11 +17,13 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <exception>
 #include <new>
 #include <vector>
 
 #include "fastgl_agg.h"
+#include "fastgl_attn.h"
 #include "fastgl_edge.h"
 #include "fastgl_gated.h"
 #include "fastgl_idmap.h"
@@ -831,6 +833,121 @@ PyObject *gated_bwd(PyObject *const *a)
     return tuple({dX.t, dWg.t, dWu.t, dbg.t, dbu.t});
 }
 
+// --------------------------------------------------------- attention over sampled neighbours
+// A matrix of contiguous rows that may lie further apart than they are long: a range of another's columns.
+struct Rows {
+    at::Tensor t;
+    int64_t ld = 0;
+    Rows() = default;
+    Rows(PyObject *o, at::ScalarType type, int64_t rows, int64_t cols, const char *name) : t(tensor(o, name))
+    {
+        if (!t.is_cuda() || t.scalar_type() != type) {
+            PyErr_Format(PyExc_TypeError, "%s must be a device tensor of %s", name, dtype_name(type));
+            throw Raised{};
+        }
+        if (t.dim() != 2 || (rows >= 0 && t.size(0) != rows) || t.size(1) != cols) {
+            if (rows >= 0) PyErr_Format(PyExc_ValueError, "%s must be [%lld, %lld]", name, (long long)rows, (long long)cols);
+            else PyErr_Format(PyExc_ValueError, "%s must have two dimensions and %lld columns", name, (long long)cols);
+            throw Raised{};
+        }
+        const bool one = t.size(0) <= 1;
+        if ((cols > 1 && t.numel() > 0 && t.stride(1) != 1) || (!one && t.numel() > 0 && t.stride(0) < cols)) {
+            PyErr_Format(PyExc_ValueError, "%s must have contiguous rows that do not overlap", name);
+            throw Raised{};
+        }
+        ld = one || t.stride(0) < cols ? cols : t.stride(0);
+    }
+    void *p() const { return t.defined() ? t.data_ptr() : nullptr; }
+};
+
+Rows rows_out(PyObject *o, bool want, at::ScalarType type, int64_t rows, int64_t cols, const at::Tensor &like, const char *name)
+{
+    if (!none(o)) return Rows(o, type, rows, cols, name);
+    Rows r;
+    if (!want) return r;
+    r.t = at::empty({rows, cols}, like.options().dtype(type));
+    r.ld = cols;
+    return r;
+}
+
+// (indptr, indices, Q, K, V, heads, kv_heads or None, scale or None, bucket, bias): what both passes of attention take.
+struct Attention {
+    fastgl_attn_desc d = {};
+    Rows Q, K, V;
+    at::ScalarType type;
+    explicit Attention(PyObject *const *a)
+    {
+        const at::Tensor &ip = dev(a[0], at::kInt, "indptr"), &ix = dev(a[1], at::kInt, "indices"), &q = tensor(a[2], "Q");
+        type = q.scalar_type();
+        d.dtype = feat_dtype(q);
+        if (ip.dim() != 1 || ip.size(0) < 1 || ix.dim() != 1) fail(PyExc_ValueError, "indptr must be [num_dst + 1] and indices [num_edges]");
+        d.indptr = (const int32_t *)ip.data_ptr();
+        d.indices = (const int32_t *)ix.data_ptr();
+        d.num_dst = ip.size(0) - 1;
+        d.num_edges = ix.size(0);
+        d.heads = integer(a[5]);
+        d.kv_heads = none(a[6]) ? d.heads : integer(a[6]);
+        if (q.dim() != 2 || d.heads < 1 || d.kv_heads < 1 || d.heads % d.kv_heads || q.size(1) % d.heads)
+            fail(PyExc_ValueError, "Q must be [num_dst, heads * width], and heads a multiple of kv_heads");
+        d.width = q.size(1) / d.heads;
+        d.scale = none(a[7]) ? (float)(1.0 / std::sqrt((double)(d.width > 0 ? d.width : 1))) : to_real(a[7]);
+        Q = Rows(a[2], type, d.num_dst, d.heads * d.width, "Q");
+        K = Rows(a[3], type, -1, d.kv_heads * d.width, "K");
+        d.num_src = K.t.size(0);
+        V = Rows(a[4], type, d.num_src, d.kv_heads * d.width, "V");
+        d.Q = Q.p(); d.K = K.p(); d.V = V.p();
+        d.ldq = Q.ld; d.ldk = K.ld; d.ldv = V.ld;
+        if (!none(a[8])) {
+            const at::Tensor &b = dev(a[8], at::kInt, "bucket");
+            if (!shape1(b, d.num_edges)) fail(PyExc_ValueError, "bucket must be [num_edges]");
+            d.bucket = (const int32_t *)b.data_ptr();
+        }
+        if (!none(a[9])) {
+            const at::Tensor &b = dev(a[9], at::kFloat, "bias");
+            if (b.dim() != 2 || b.size(1) != d.heads || b.size(0) < 1) fail(PyExc_ValueError, "bias must be [num_buckets, heads]");
+            if (none(a[8])) fail(PyExc_ValueError, "a bias needs buckets");
+            d.bias = (const float *)b.data_ptr();
+            d.num_buckets = b.size(0);
+        }
+    }
+};
+
+// (the ten above, want_lse, O, lse, plan, workspace) -> (O, lse)
+PyObject *attn_fwd(PyObject *const *a)
+{
+    const Attention c(a);
+    const fastgl_attn_desc &d = c.d;
+    const Rows O = rows_out(a[11], true, c.type, d.num_dst, d.heads * d.width, c.Q.t, "O");
+    Out lse;
+    if (truth(a[10]) || !none(a[12])) lse = out_of(a[12], at::kFloat, {d.num_dst, d.heads}, c.Q.t, "lse");
+    const fastgl_plan *p = plan_of(a[13]);
+    const Scratch ws(a[14], c.Q.t, [&] { return fastgl_attn_workspace_bytes(&d, 0); });
+    run([&](void *s) { return fastgl_attn_fwd(&d, O.p(), O.ld, (float *)lse.p(), p, ws.p(), ws.n(), s); });
+    return tuple({O.t, lse.t});
+}
+
+// (the ten above, dO, want_dQ, want_dK, want_dV, want_dbias, dQ, dK, dV, dbias, plan, workspace) -> (dQ, dK, dV, dbias)
+PyObject *attn_bwd(PyObject *const *a)
+{
+    const Attention c(a);
+    const fastgl_attn_desc &d = c.d;
+    const int64_t n = d.heads * d.width, k = d.kv_heads * d.width;
+    const Rows dO(a[10], c.type, d.num_dst, n, "dO");
+    const Rows dQ = rows_out(a[15], truth(a[11]), c.type, d.num_dst, n, c.Q.t, "dQ");
+    const Rows dK = rows_out(a[16], truth(a[12]), c.type, d.num_src, k, c.Q.t, "dK");
+    const Rows dV = rows_out(a[17], truth(a[13]), c.type, d.num_src, k, c.Q.t, "dV");
+    Out dbias;
+    if (!none(a[18]) && !d.bias) fail(PyExc_ValueError, "dbias needs the bias and its buckets");
+    if (d.bias && (truth(a[14]) || !none(a[18]))) dbias = out_of(a[18], at::kFloat, {d.num_buckets, d.heads}, c.Q.t, "dbias");
+    const fastgl_plan *p = plan_of(a[19]);
+    const Scratch ws(a[20], c.Q.t, [&] { return fastgl_attn_workspace_bytes(&d, 1); });
+    run([&](void *s) {
+        return fastgl_attn_bwd(&d, dO.p(), dO.ld, dQ.p(), dQ.ld, dK.p(), dK.ld, dV.p(), dV.ld,
+                               (float *)dbias.p(), p, ws.p(), ws.n(), s);
+    });
+    return tuple({dQ.t, dK.t, dV.t, dbias.t});
+}
+
 // (error class): called once by binding.py
 PyObject *set_error_class(PyObject *const *a)
 {
@@ -846,7 +963,7 @@ PyMethodDef g_methods[] = {
     FN(update_fwd, 5), FN(layer_fwd, 14), FN(update_bwd, 12), FN(idmap, 7), FN(match, 7), FN(assemble_rows, 5),
     FN(overlap_counts, 3), FN(edge_weight_grad, 9), FN(edge_softmax_fwd, 4), FN(edge_softmax_bwd, 5),
     FN(edge_score_fwd, 6), FN(edge_score_bwd, 11), FN(norm_fwd, 13), FN(norm_bwd, 14), FN(dropout, 5),
-    FN(gather_rows_e4m3, 5), FN(gated_fwd, 11), FN(gated_bwd, 19), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
+    FN(gather_rows_e4m3, 5), FN(gated_fwd, 11), FN(gated_bwd, 19), FN(attn_fwd, 15), FN(attn_bwd, 21), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
 #undef FN
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host", "Native marshalling of the C ABI's calls.", -1, g_methods,

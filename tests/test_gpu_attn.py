@@ -1,0 +1,297 @@
+"""Attention over a block's edges on the GPU against its plain 64-bit form (tests/attn_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+import blockgen as bg
+from attn_ref import HALF, Attention
+from gpu_util import dev_i32
+from paper_2409_14939_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+SENTINEL = -776.0
+# heads, key heads, width: below and beyond 16 bytes, multiples of it and not, every number of lanes a head
+HEADS = [(1, 1, 1), (2, 1, 3), (12, 4, 2), (3, 3, 5), (1, 1, 7), (4, 4, 8), (6, 3, 9), (4, 4, 16), (5, 5, 20), (8, 8, 32), (6, 2, 47), (4, 1, 47), (4, 2, 64),
+         (2, 2, 100), (8, 1, 128), (3, 1, 200), (2, 2, 255), (1, 1, 256)]
+
+
+def hubs(seed=3, nd=500, ns=700):
+    """Empty rows, short ones, rows of several chunks; sources of several chunks and none."""
+    return bg.random_block(np.random.default_rng(seed), nd, ns, 5.0, empty_frac=0.15, hub_rows=6, hub_deg=900)
+
+
+class Case:
+    """A block's inputs, on the CPU and on the GPU; K and V columns of one array, dQ and the like columns of wider ones."""
+
+    def __init__(self, blk, heads, kv, D, dtype, buckets, seed=0, scale=None, size=1.0):
+        g = torch.Generator().manual_seed(seed)
+        t = DTYPES[dtype]
+        make = lambda *s: (size * torch.randn(*s, generator=g)).to(t)
+        self.blk, self.heads, self.kv, self.D, self.t = blk, heads, kv, D, t
+        self.scale = D ** -0.5 if scale is None else scale
+        n, k = heads * D, kv * D
+        self.Q, self.KV, self.dO = make(blk.num_dst, n), make(blk.num_src, 2 * k + 3), make(blk.num_dst, n)
+        self.bucket = self.bias = None
+        if buckets is not None:                                # -1 and what lies beyond the table leave an edge out
+            self.bucket = torch.randint(-1, max(buckets, 1) + (buckets > 0), (blk.num_edges,), generator=g, dtype=torch.int32)
+            if buckets:
+                self.bias = torch.randn(buckets, heads, generator=g)
+        self.k = k
+
+    def columns(self, x):
+        return x[:, :self.k], x[:, self.k + 3:]
+
+    def reference(self, backward=True):
+        K, V = self.columns(self.KV)
+        a = Attention(self.blk.indptr, self.blk.indices, self.Q, K, V, self.heads, self.kv, self.scale, self.bucket, self.bias)
+        return a.backward(self.dO) if backward else a
+
+    def on_gpu(self, parts=None):
+        cuda = lambda x: None if x is None else x.cuda()
+        self.ip, self.ix = dev_i32(self.blk.indptr), dev_i32(self.blk.indices)
+        self.gKV = self.KV.cuda()
+        K, V = self.columns(self.gKV)
+        self.args = (self.ip, self.ix, self.Q.cuda(), K, V)
+        self.gdO = self.dO.cuda()
+        parts = B.PLAN_ALL | (B.PLAN_PERM if self.bucket is not None else 0) if parts is None else parts
+        self.plan = B.fastgl_block_plan_create(self.ip, self.ix, self.blk.num_src, parts) if parts else None
+        self.how = dict(heads=self.heads, kv_heads=self.kv, scale=self.scale, bucket=cuda(self.bucket), bias=cuda(self.bias), plan=self.plan)
+        return self
+
+    def forward(self, **kw):
+        return B.fastgl_attn_fwd(*self.args, **self.how, **kw)
+
+    def gradients(self, **kw):
+        return B.fastgl_attn_bwd(*self.args, self.gdO, **self.how, **kw)
+
+
+def within(got, want, bound, t, what):
+    got, want = got.double().cpu().reshape(want.shape), want.double()
+    same = (got == want) | (got.isnan() & want.isnan())
+    off = torch.where(same, 0.0, (got - want).abs())
+    # a weight below 2^-126 is 0 in float32: 2^-126 times at most 2^10 terms of products below 2^14
+    limit = (bound + HALF[t] * (want.abs() + bound) if t else bound) + 2.0 ** -102
+    bad = ~((off <= limit) | same)
+    assert not bool(bad.any()), (what, int(bad.sum()), off[bad][:4], limit[bad][:4], want[bad][:4], got[bad][:4])
+
+
+def check(c, grads=True, **kw):
+    ref = c.reference(grads)
+    O, lse = c.forward(**kw)
+    within(O, ref.O, ref.off_O, c.t, "O")
+    within(lse, ref.lse, ref.off_lse, None, "lse")
+    if not grads:
+        return O, lse
+    n = c.heads * c.D
+    wide = torch.full((c.blk.num_dst, n + 5), SENTINEL, dtype=c.t, device="cuda")
+    both = torch.full((c.blk.num_src, 2 * c.k + 3), SENTINEL, dtype=c.t, device="cuda")
+    dK, dV = c.columns(both)
+    dQ, dK, dV, dbias = c.gradients(dQ=wide[:, 2:2 + n], dK=dK, dV=dV)
+    within(dQ, ref.dQ, ref.off_dQ, c.t, "dQ")
+    within(dK, ref.dK, ref.off_dK, c.t, "dK")
+    within(dV, ref.dV, ref.off_dV, c.t, "dV")
+    if c.bias is not None:
+        within(dbias, ref.dbias, ref.off_dbias, torch.float32, "dbias")
+    else:
+        assert dbias is None
+    assert bool((wide[:, :2] == SENTINEL).all()) and bool((wide[:, 2 + n:] == SENTINEL).all())
+    assert bool((both[:, c.k:c.k + 3] == SENTINEL).all())
+    return O, lse, dQ, dK, dV, dbias
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,kv,D", HEADS)
+def test_heads_and_widths(heads, kv, D, dtype):
+    check(Case(hubs(), heads, kv, D, dtype, None, seed=D).on_gpu())
+    check(Case(hubs(4), heads, kv, D, dtype, 6, seed=D + 1).on_gpu())
+
+
+@pytest.mark.parametrize("buckets", [0, 1, 2, 63, 64, 65, 130, 1000])
+@pytest.mark.parametrize("heads", [1, 3, 8, 33])
+def test_buckets(buckets, heads):
+    check(Case(hubs(5), heads, heads, 12, "f32", buckets, seed=buckets).on_gpu())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nd,ns,degree", [(1, 1, 1), (1, 1, 0), (1, 16, 15), (2, 3, 256), (2, 3, 257), (1, 5, 1000), (3, 2, 129), (300, 1, 3), (70, 4000, 2),
+                                          (1, 2, 255), (1, 300, 20_001)])
+def test_lengths(nd, ns, degree, dtype):
+    rng = np.random.default_rng(degree)
+    blk = bg.Block((np.arange(nd + 1) * degree).astype(np.int32), rng.integers(0, ns, nd * degree).astype(np.int32), nd, ns)
+    for heads, kv, D in ((2, 1, 24), (3, 3, 6)):
+        check(Case(blk, heads, kv, D, dtype, None, seed=1).on_gpu())
+        check(Case(blk, heads, kv, D, dtype, 3, seed=2).on_gpu())
+
+
+def test_blocks_without_rows_or_edges():
+    for nd, ns in ((0, 0), (0, 5), (4, 0), (4, 5)):
+        blk = bg.Block(np.zeros(nd + 1, np.int32), np.zeros(0, np.int32), nd, ns)
+        c = Case(blk, 2, 2, 8, "f32", 3).on_gpu()
+        O, lse = c.forward()
+        dQ, dK, dV, dbias = c.gradients()
+        assert O.shape == (nd, 16) and dK.shape == (ns, 16) and not bool(O.any()) and bool((lse == -torch.inf).all())
+        assert not bool(dQ.any() | dK.any() | dV.any() | dbias.any()) and dbias.shape == (3, 2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_nothing_is_left_of_and_what_is_left_out(dtype):
+    """Rows all of whose edges are left out; sources that only left-out edges have hold NaN and infinities, and are neighbours of every row."""
+    blk = hubs(6)
+    c = Case(blk, 4, 2, 24, dtype, 5, seed=3)
+    rows = torch.repeat_interleave(torch.arange(blk.num_dst), torch.as_tensor(np.diff(blk.indptr)).long())
+    src = torch.as_tensor(blk.indices).long()
+    c.bucket = torch.where((rows % 5 == 0) | (src % 7 == 0), torch.where(rows % 2 == 0, -1, 5), c.bucket.clamp(0, 4)).int()
+    ref = c.reference()
+    c.KV[::7], c.KV[7::21] = float("nan"), float("inf")
+    c.reference = lambda backward=True: ref
+    O, lse, dQ, dK, dV, _ = check(c.on_gpu())
+    empty = ref.n[:, 0] == 0
+    assert bool(empty[::5].all()) and not bool(O.cpu()[empty].any()) and bool((lse.cpu()[empty] == -torch.inf).all())
+    assert not bool(dQ.cpu()[empty].any()) and not bool(dK[::7].any()) and not bool(dV[::7].any())
+
+
+def test_a_bias_of_the_lowest_value_and_of_minus_infinity():
+    """-inf leaves an edge out; the type's lowest value gives weight 0 where another edge remains, and a row of nothing else its mean."""
+    blk = bg.Block(np.array([0, 3, 5, 7, 9], np.int32), np.array([0, 1, 2, 1, 2, 0, 1, 2, 0], np.int32), 4, 3)
+    c = Case(blk, 1, 1, 8, "f32", 3)
+    c.bias = torch.tensor([[0.5], [torch.finfo(torch.float32).min], [-torch.inf]])
+    c.bucket = torch.tensor([0, 1, 2, 2, 2, 1, 1, 0, 0], dtype=torch.int32)
+    c.on_gpu()
+    O, lse = c.forward()
+    V = c.columns(c.gKV)[1]
+    assert torch.equal(O[0], V[0]) and not bool(O[1].any()) and lse[1, 0] == -torch.inf
+    # the lowest value swallows the dot products: both edges weigh the same
+    torch.testing.assert_close(O[2], (V[0] + V[1]) / 2, rtol=4 * 2.0 ** -24, atol=2.0 ** -22)
+    dQ, dK, dV, dbias = c.gradients()
+    for x in (O, dQ, dK, dV, dbias):
+        assert bool(torch.isfinite(x).all())
+    assert not bool(dQ[1].any()) and dbias[2, 0] == 0
+    # the row of lowest values weighs both edges 1/2 in the backward pass too: dV of its sources without the other rows
+    c.gdO[[0, 1, 3]] = 0
+    dV = c.gradients()[2]
+    torch.testing.assert_close(dV[0], c.gdO[2] / 2, rtol=2.0 ** -22, atol=0)
+    torch.testing.assert_close(dV[1], c.gdO[2] / 2, rtol=2.0 ** -22, atol=0)
+
+
+def test_rows_that_are_not_finite_change_no_other():
+    blk = bg.Block(np.array([0, 3, 6, 9], np.int32), np.array([0, 1, 2, 3, 4, 5, 6, 7, 8], np.int32), 3, 9)
+    c = Case(blk, 2, 2, 20, "f32", None)
+    clean = c.on_gpu()
+    O, lse = clean.forward()
+    dQ = clean.gradients()[0]
+    c.KV[4] = float("nan")
+    c.on_gpu()
+    O2, lse2 = c.forward()
+    dQ2 = c.gradients()[0]
+    for a, b in ((O, O2), (lse, lse2), (dQ, dQ2)):
+        assert torch.equal(a[[0, 2]], b[[0, 2]]) and bool(b[1].isnan().all())
+
+
+@pytest.mark.parametrize("size,scale", [(8.0, 1.0), (1.0, -0.3), (30.0, 0.1), (1e-3, 1.0), (1.0, 0.0)])
+def test_sizes_of_scores(size, scale):
+    """Scores of several hundred, of either sign of the scale, and all the same."""
+    for dtype in ("f32", "bf16"):
+        check(Case(hubs(7, 120, 200), 3, 3, 24, dtype, 4, seed=5, scale=scale, size=size).on_gpu())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_same_results_with_every_plan_and_again(dtype):
+    c = Case(hubs(8), 6, 2, 20, dtype, 7)
+    first = check(c.on_gpu())
+    again = check(c.on_gpu())
+    none = check(c.on_gpu(parts=0))
+    for other in (again, none):
+        assert all(torch.equal(a, b) for a, b in zip(first, other))
+    c.on_gpu(parts=B.PLAN_FWD)
+    O, lse = c.forward()
+    assert torch.equal(O, first[0]) and torch.equal(lse, first[1])
+    check(c.on_gpu(parts=B.PLAN_ALL | B.PLAN_PERM | B.PLAN_SHORT_DST_ROWS))
+
+
+def test_parts_of_the_gradient():
+    c = Case(hubs(9), 4, 2, 16, "bf16", 5).on_gpu()
+    _, lse = c.forward()
+    whole = c.gradients()
+    names = ("dQ", "dK", "dV", "dbias")
+    for i, name in enumerate(names):
+        got = c.gradients(want=(name,))
+        assert [x is not None for x in got] == [j == i for j in range(4)] and torch.equal(got[i], whole[i])
+    O = c.forward(want_lse=False)
+    assert O[1] is None and torch.equal(O[0], c.forward()[0])
+
+
+def test_gradient_against_differences():
+    """Along the gradient itself: the change of <O, dO> of the kernels' own forward pass, in float32."""
+    c = Case(hubs(10, 60, 90), 4, 2, 12, "f32", 5).on_gpu()
+    _, lse = c.forward()
+    grads = c.gradients()
+    for name, x, grad in (("Q", c.args[2], grads[0]), ("K", c.args[3], grads[1]), ("V", c.args[4], grads[2]), ("bias", c.how["bias"], grads[3])):
+        keep, way = x.clone(), grad.double() / grad.double().norm()
+        step = 0.02 * keep.double().norm().item() / way.numel() ** 0.5
+        values = []
+        for sign in (1, -1):
+            x.copy_(keep.double() + sign * step * way)
+            values.append((c.forward()[0].double() * c.gdO.double()).sum().item())
+        x.copy_(keep)
+        # a central difference over a fiftieth of an element's size: third order; float32 noise of some hundred outputs
+        assert abs((values[0] - values[1]) / (2 * step) - grad.double().norm().item()) < 2e-3 * grad.double().norm().item() + 1e-3, name
+
+
+def test_a_captured_step_replayed_with_other_inputs():
+    c = Case(hubs(11), 4, 2, 16, "bf16", 5).on_gpu()
+    other = Case(hubs(11), 4, 2, 16, "bf16", 5, seed=9).on_gpu()
+    ws = torch.empty(B.fastgl_attn_workspace_bytes(500, 700, c.blk.num_edges, 4, 16, "bf16", kv_heads=2, num_buckets=5, backward=True),
+                     dtype=torch.uint8, device="cuda")
+
+    def step():
+        O, lse = c.forward(workspace=ws)
+        return [O, lse, *c.gradients(workspace=ws)]
+    eager = [[t.clone() for t in step()]]
+    _, lse = other.forward()
+    eager.append([other.forward()[0], lse, *other.gradients()])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        step()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            got = step()
+    torch.cuda.current_stream().wait_stream(side)
+    first = [t.clone() for t in (c.args[2], c.gKV, c.gdO, c.how["bucket"], c.how["bias"])]
+    second = [other.args[2], other.gKV, other.gdO, other.how["bucket"], other.how["bias"]]
+    for n in (0, 1, 0, 1):
+        for to, x in zip((c.args[2], c.gKV, c.gdO, c.how["bucket"], c.how["bias"]), second if n else first):
+            to.copy_(x)
+        for t in got:
+            t.zero_()
+        ws.random_(0, 255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, eager[n])), n
+
+
+def test_what_the_binding_refuses():
+    c = Case(hubs(12, 20, 30), 2, 2, 8, "f32", 3).on_gpu()
+    ip, ix, Q, K, V = c.args
+    _, lse = c.forward()
+    bad = [(TypeError, (ip.long(), ix, Q, K, V)), (TypeError, (ip, ix.cpu(), Q, K, V)), (TypeError, (ip, ix, Q, K.bfloat16(), V)), (TypeError, (ip, ix, Q.double(), K, V)),
+           (ValueError, (ip, ix, Q[:-1], K, V)), (ValueError, (ip, ix, Q, K[:, :-1], V)), (ValueError, (ip, ix, Q, K, V[:-1])),
+           (ValueError, (ip, ix, Q.T.contiguous().T, K, V)), (ValueError, (ip, ix, Q, K[:1].expand(30, 16), V)), (ValueError, (ip[:0], ix, Q, K, V))]
+    for kind, args in bad:
+        with pytest.raises(kind):
+            B.fastgl_attn_fwd(*args, **c.how)
+    for kw in (dict(heads=3), dict(kv_heads=3), dict(heads=0), dict(bucket=c.how["bucket"][:-1]), dict(bias=c.how["bias"][:, :1].contiguous()), dict(bucket=None),
+               dict(bias=c.how["bias"][:0]), dict(O=Q[:, :-1]), dict(lse=lse[:-1])):
+        with pytest.raises(ValueError):
+            B.fastgl_attn_fwd(*c.args, **{**c.how, **kw})
+    with pytest.raises(ValueError):
+        B.fastgl_attn_bwd(*c.args, c.gdO[:, :-1], **c.how)
+    with pytest.raises(ValueError):
+        B.fastgl_attn_bwd(*c.args, c.gdO, **{**c.how, "bias": None}, dbias=c.how["bias"])
+    with pytest.raises(B.FastglError, match="parts"):
+        B.fastgl_attn_bwd(*c.args, c.gdO, **{**c.how, "plan": B.fastgl_block_plan_create(ip, ix, 30, B.PLAN_ALL)})
+    with pytest.raises(B.FastglError, match="different block"):
+        B.fastgl_attn_fwd(*c.args, **{**c.how, "plan": B.fastgl_block_plan_create(ip.clone(), ix, 30)})
