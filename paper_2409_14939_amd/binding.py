@@ -40,6 +40,7 @@ EXPORTS = [
     "fastgl_gather_rows_e4m3", "fastgl_gated_fwd", "fastgl_gated_bwd", "fastgl_gated_fwd_workspace_bytes",
     "fastgl_gated_bwd_workspace_bytes", "fastgl_gated_bwd_fine", "fastgl_gated_bwd_fine_workspace_bytes",
     "fastgl_attn_fwd", "fastgl_attn_bwd", "fastgl_attn_workspace_bytes",
+    "fastgl_loss_fwd", "fastgl_loss_bwd", "fastgl_loss_fwd_workspace_bytes", "fastgl_loss_bwd_workspace_bytes",
 ]
 MAX_REORDER_BATCHES = 64
 ACTS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
@@ -148,6 +149,11 @@ def lib() -> ctypes.CDLL:
         L.fastgl_attn_workspace_bytes.restype = sz
         L.fastgl_attn_fwd.argtypes = [desc, p, i64, p, p, p, sz, p]
         L.fastgl_attn_bwd.argtypes = [desc, p, i64, p, i64, p, i64, p, i64, p, p, p, sz, p]
+        for f in (L.fastgl_loss_fwd_workspace_bytes, L.fastgl_loss_bwd_workspace_bytes):
+            f.argtypes = [i32, i64, i64, i64, i32]
+            f.restype = sz
+        L.fastgl_loss_fwd.argtypes = [i32, p, p, p, p, i64, i64, i64, p, p, p, sz, p]
+        L.fastgl_loss_bwd.argtypes = [i32, p, p, p, p, p, p, i64, i64, i64, p, p, p, p, sz, p]
         L.fastgl_idmap_table_slots.argtypes = [i64]
         L.fastgl_idmap_table_slots.restype = i64
         L.fastgl_idmap_workspace_bytes.argtypes = [i64, i64]
@@ -526,3 +532,28 @@ def fastgl_attn_bwd(indptr, indices, Q: torch.Tensor, K: torch.Tensor, V: torch.
     with buckets PLAN_ALL | PLAN_PERM."""
     return _native().attn_bwd(indptr, indices, Q, K, V, heads, kv_heads, scale, bucket, bias, dO,
                               *(n in want for n in ("dQ", "dK", "dV", "dbias")), dQ, dK, dV, dbias, plan, workspace)
+
+
+def fastgl_loss_fwd_workspace_bytes(dtype: str, M: int, K: int, N: int, aligned: bool = False) -> int:
+    return int(lib().fastgl_loss_fwd_workspace_bytes(DTYPES[dtype], M, K, N, int(aligned)))
+
+
+def fastgl_loss_bwd_workspace_bytes(dtype: str, M: int, K: int, N: int, aligned: bool = False) -> int:
+    return int(lib().fastgl_loss_bwd_workspace_bytes(DTYPES[dtype], M, K, N, int(aligned)))
+
+
+def fastgl_loss_fwd(H: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor], label: torch.Tensor, want_lse: bool = True,
+                    loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None):
+    """(loss, lse), float32 [M]: softmax cross entropy of the class scores H W + b, which are not kept.  label int64 [M]; a negative
+    one leaves its row out (loss 0), one that is no class gives NaN.  lse is what the backward pass reads."""
+    return _native().loss_fwd(H, W, b, label, want_lse, loss, lse, workspace)
+
+
+def fastgl_loss_bwd(H: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor], label: torch.Tensor, lse: torch.Tensor,
+                    dloss: torch.Tensor, want=("dH", "dW", "db"), dH: Optional[torch.Tensor] = None,
+                    dW: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None):
+    """(dH, dW, db) for the gradient dloss [M] of loss (1 / rows for a mean); parts not named in `want` (and not passed in)
+    are None.  dH and dW are of H's dtype, db float32."""
+    return _native().loss_bwd(H, W, b, label, lse, dloss, *(n in want for n in ("dH", "dW", "db")), dH, dW, db, workspace)

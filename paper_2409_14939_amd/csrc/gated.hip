@@ -102,28 +102,6 @@ struct RowsArgs {
     int32_t strips, groups;          // strips of columns, groups of rows
 };
 
-// Sums v[0 .. N) over the lanes that differ in the bits O, O / 2, ... FROM: at each bit a lane keeps one half of what it holds and
-// gives the other away, so that N - 1 exchanges (not N for each bit) are enough.  A lane ends with N FROM / 64 values (one at
-// least), of the returned index onwards.
-template <int N, int O, int FROM, int NV>
-__device__ __forceinline__ int scatter_sum(float (&v)[NV], int lane)
-{
-    if constexpr (O < FROM) {
-        return 0;
-    } else if constexpr (N > 1) {
-        const bool up = lane & O;
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const float give = up ? v[i] : v[i + N / 2], keep = up ? v[i + N / 2] : v[i];
-            v[i] = keep + __shfl_xor(give, O, kWave);
-        }
-        return (up ? N / 2 : 0) + scatter_sum<N / 2, O / 2, FROM>(v, lane);
-    } else {
-        v[0] += __shfl_xor(v[0], O, kWave);
-        return scatter_sum<1, O / 2, FROM>(v, lane);
-    }
-}
-
 // MR rows of a strip of columns by one workgroup: 2^LG lanes hold eight columns of both weights each, the lanes beyond them
 // the next k; the sums of a column are joined through the lanes of a wavefront, then through LDS, in a fixed order.
 // Bound by the weights: neighbouring strips, which share lines, are given to one L2 domain.
@@ -344,44 +322,6 @@ __global__ __launch_bounds__(kBlock) void k_gated_join(const float *__restrict__
 
 // ------------------------------------------------------------------------------------ host side
 bool misaligned_to(const void *p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
-
-// The tile of a product and how many workgroups share the steps of one.
-struct Cut {
-    int size;
-    int64_t slabs;
-};
-
-// The cut that a model of the launch finds fastest.  A compute unit needs single_us for a step of a workgroup that it has alone and
-// pair_us for one of each of two (large tiles: one at a time), and tile_us for what is around the steps; slabs cost the sums that they
-// write and that are read again (4 bytes each way at some 6 TB/s), and a launch.
-// Measured (bf16, us for large / middle / small tiles; kernel times, the least of 150 passes on one card):
-//   forward 16 384 rows 1024 -> 4096, G and U kept 273 / 269 / -, alone 241 / 253 / -;  115 000 rows 256 -> 1024 193 / 174 / -, 162 / 140 / -
-//   dX of 16 384 rows 1024 -> 4096 223 / 278 / 310, dWg and dWu there 218 / 241 / 401 (the first two in two slabs)
-//   all kernels of a backward call of 300 rows 256 -> 1024 (medians) 36 / 32 / 31, of 2000 rows 52 / 47 / 43, of 8000 rows 256 -> 683 73 / 67 / 60
-Cut cut_of(int mode, int64_t R, int64_t C, int64_t Kc, int64_t segments)
-{
-    static const double single_us[3][3] = {{0.80, 0.60, 0.36}, {0.93, 0.65, 0.38}, {0.80, 0.60, 0.42}};      // [mode][size]
-    static const double pair_us[3][3] = {{1.60, 0.92, 0.64}, {1.86, 1.10, 0.70}, {1.60, 0.92, 0.80}};
-    static const double tile_us[2][3] = {{6.0, 2.6, 1.6}, {4.0, 2.0, 1.2}};
-    Cut best = {kLarge, 1};
-    double least = 1e300;
-    const int64_t all = ceil_div(Kc, kStep) * segments;
-    for (int size = kLarge; size <= kSmall; ++size) {
-        const int64_t bm = size == kLarge ? 256 : 128, bc = (size == kSmall ? 128 : 256) / (mode == kRows ? 1 : 2);
-        const int64_t tiles = ceil_div(R, bm) * ceil_div(C, bc);
-        for (int64_t slabs = 1; slabs <= 64 && (slabs == 1 || (all / slabs >= 4 && R * C <= (int64_t)1 << 30)); slabs = slabs < 8 ? slabs + 1 : slabs * 5 / 4) {
-            const int64_t of_unit = ceil_div(tiles * slabs, 256);
-            const double step = (double)(of_unit / 2) * pair_us[mode][size] + (double)(of_unit % 2) * single_us[mode][size];
-            const double us = (double)ceil_div(all, slabs) * step + (double)of_unit * tile_us[mode != kForward][size] +
-                              (slabs > 1 ? 4.0 + (double)slabs * (double)R * (double)C * (mode == kRows ? 1.3e-6 : 2.6e-6) : 0.0);
-            if (us < least) {
-                least = us;
-                best = {size, slabs};
-            }
-        }
-    }
-    return best;
-}
 
 // Where a call's scratch lies; base NULL: only the size is wanted.
 struct Layout {

@@ -1,8 +1,15 @@
-// The matrix-core tile of the gated feed-forward update: three kinds of product of one shape of kernel.
+// The matrix-core tile of the gated feed-forward update and of a classifier's loss: three kinds of product of one shape of kernel.
 //
 //   FORWARD  G, U [R,C]    = A [R,Kc] B0, B1 [Kc,C]         and the gate in the epilogue
 //   ROWS     dX   [R,C]    = sum over groups of A [R,Kc] B [C,Kc]^T
 //   WEIGHTS  dWg, dWu [R,C] = A [Kc,R]^T B0, B1 [Kc,C]
+//
+// and with one result the loss's (fastgl_loss.h)
+//
+//   SCORES   z [R,C] = A [R,Kc] B [Kc,C], of which each wavefront leaves maximum and sum of exponentials of its columns of every row
+//   GRADIENT the same, of which dZ is left as the next products take it, and its column sums
+//   ROWS_ADD sums of slabs as ROWS has them, added to what a piece of the classes before left there
+//   WEIGHTS_ONE  dW [R,C] = A [Kc,R]^T B [Kc,C] into columns of a wider matrix
 //
 // All operands are bf16 with rows of a multiple of 16 bytes; fp32 operands come as three planes of pieces, and a
 // product of two such is a sequence of six segments, each a product of one plane of either.
@@ -36,7 +43,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #define FASTGL_LDS __attribute__((address_space(3)))
 
-enum TileMode { kForward = 0, kRows = 1, kWeights = 2 };
+enum TileMode { kForward = 0, kRows = 1, kWeights = 2, kScores = 3, kGradient = 4, kRowsAdd = 5, kWeightsOne = 6 };
 
 constexpr int kStep = 32;                       // contracted elements of an LDS buffer
 constexpr uint32_t kNoSuchOffset = 0x7FFFFF00u; // beyond every buffer
@@ -55,6 +62,25 @@ struct TileArgs {
     void *out[3];                  // FORWARD: P, G, U (G, U or NULL); ROWS: dX; WEIGHTS: dWg, dWu
     float *part;                   // slabs > 1: their sums, [slab][results][R][C]
 };
+
+struct LossTileArgs : TileArgs {
+    int64_t shift;                 // SCORES, GRADIENT: the column of B that column 0 is
+    int64_t ldo;                   // WEIGHTS_ONE: elements between rows of the result
+    int32_t add;                   // ROWS_ADD: whether `part` holds sums to add to
+    const int64_t *label;          // [R]
+    int64_t first, classes;        // the class of column 0, and all of them
+    float *stats;                  // SCORES: [column tile and wavefront][R][2]
+    float *picked;                 // SCORES: [R] the score of the label
+    const float *lse, *dloss;      // GRADIENT: [R]
+    uint16_t *dz;                  // GRADIENT: planes of dZ; column c of row r at (c >> 5) * dz_block + r * dz_ld + (c & 31)
+    int64_t dz_plane, dz_ld, dz_block;
+    float *db;                     // GRADIENT: [row tile and wavefront][C] column sums, or NULL
+};
+template <int MODE> struct TileArgsOf { typedef TileArgs type; };
+template <> struct TileArgsOf<kScores> { typedef LossTileArgs type; };
+template <> struct TileArgsOf<kGradient> { typedef LossTileArgs type; };
+template <> struct TileArgsOf<kRowsAdd> { typedef LossTileArgs type; };
+template <> struct TileArgsOf<kWeightsOne> { typedef LossTileArgs type; };
 
 // Pairs of planes, smallest products first: six of three planes and three (0 2, 2 0, 1 1, 0 1, 1 0, 0 0), and two of two and one.
 constexpr uint32_t kSixA = 0x001120, kSixB = 0x010102, kTwo = 0x01;
@@ -126,14 +152,54 @@ struct Tile {
     static constexpr int BUFS = SIZE == kMiddle ? 3 : 5;
     static constexpr int WM = SIZE == kLarge ? 4 : 2, WN = 2;
     static constexpr int TM = BM / WM / 32, TN = BNV / WN / 32;          // blocks of 32 x 32 a wavefront
-    static constexpr bool DUAL = MODE != kRows;
+    static constexpr bool FORWARD = MODE == kForward || MODE == kScores || MODE == kGradient, ROWS = MODE == kRows || MODE == kRowsAdd;
+    static constexpr bool WEIGHTS = MODE == kWeights || MODE == kWeightsOne, DUAL = MODE == kForward || MODE == kWeights;
     static constexpr int RESULTS = DUAL ? 2 : 1, BC = BNV / RESULTS;     // columns of one result
-    static constexpr bool A_T = MODE == kWeights, B_T = MODE != kRows;   // other index contiguous
+    static constexpr bool A_T = WEIGHTS, B_T = !ROWS;                    // other index contiguous
     static constexpr int A_BYTES = BM * kStep * 2, B_BYTES = BNV * kStep * 2, STAGE = A_BYTES + B_BYTES;
     static constexpr int THREADS = NW * kWave;
     static constexpr int LA = A_BYTES / (THREADS * 16), LB = B_BYTES / (THREADS * 16);      // 16-byte loads a lane
     static_assert(TM == 2 && LA == 2, "tile shape");
 };
+
+// The tile of a product and how many workgroups share the steps of one.
+struct Cut {
+    int size;
+    int64_t slabs;
+};
+
+// The cut that a model of the launch finds fastest.  A compute unit needs single_us for a step of a workgroup that it has alone and
+// pair_us for one of each of two (large tiles: one at a time), and tile_us for what is around the steps; slabs cost the sums that they
+// write and that are read again (4 bytes each way at some 6 TB/s), and a launch.
+// Measured (bf16, us for large / middle / small tiles; kernel times, the least of 150 passes on one card):
+//   forward 16 384 rows 1024 -> 4096, G and U kept 273 / 269 / -, alone 241 / 253 / -;  115 000 rows 256 -> 1024 193 / 174 / -, 162 / 140 / -
+//   dX of 16 384 rows 1024 -> 4096 223 / 278 / 310, dWg and dWu there 218 / 241 / 401 (the first two in two slabs)
+//   all kernels of a backward call of 300 rows 256 -> 1024 (medians) 36 / 32 / 31, of 2000 rows 52 / 47 / 43, of 8000 rows 256 -> 683 73 / 67 / 60
+// The loss's products have one result of twice the columns (`one`); scores are not summed over slabs (`whole`).
+inline Cut cut_of(int mode, int64_t R, int64_t C, int64_t Kc, int64_t segments, bool one = false, bool whole = false)
+{
+    static const double single_us[3][3] = {{0.80, 0.60, 0.36}, {0.93, 0.65, 0.38}, {0.80, 0.60, 0.42}};      // [mode][size]
+    static const double pair_us[3][3] = {{1.60, 0.92, 0.64}, {1.86, 1.10, 0.70}, {1.60, 0.92, 0.80}};
+    static const double tile_us[2][3] = {{6.0, 2.6, 1.6}, {4.0, 2.0, 1.2}};
+    Cut best = {kLarge, 1};
+    double least = 1e300;
+    const int64_t all = ceil_div(Kc, kStep) * segments;
+    for (int size = kLarge; size <= kSmall; ++size) {
+        const int64_t bm = size == kLarge ? 256 : 128, bc = (size == kSmall ? 128 : 256) / (mode == kRows || one ? 1 : 2);
+        const int64_t tiles = ceil_div(R, bm) * ceil_div(C, bc);
+        for (int64_t slabs = 1; slabs <= (whole ? 1 : 64) && (slabs == 1 || (all / slabs >= 4 && R * C <= (int64_t)1 << 30)); slabs = slabs < 8 ? slabs + 1 : slabs * 5 / 4) {
+            const int64_t of_unit = ceil_div(tiles * slabs, 256);
+            const double step = (double)(of_unit / 2) * pair_us[mode][size] + (double)(of_unit % 2) * single_us[mode][size];
+            const double us = (double)ceil_div(all, slabs) * step + (double)of_unit * tile_us[mode != kForward][size] +
+                              (slabs > 1 ? 4.0 + (double)slabs * (double)R * (double)C * (mode == kRows || one ? 1.3e-6 : 2.6e-6) : 0.0);
+            if (us < least) {
+                least = us;
+                best = {size, slabs};
+            }
+        }
+    }
+    return best;
+}
 
 // Which 16-byte piece of row k a [32][columns] buffer has at place p: rows of RB bytes.  Reads take 64 bytes of four
 // consecutive rows at a time, which this puts 64 bytes apart modulo 256.
@@ -145,9 +211,132 @@ __device__ __forceinline__ int twisted(int row) { return (row >> 2) & 3; }
 
 namespace {
 
+// Sums v[0 .. N) over the lanes that differ in the bits O, O / 2, ... FROM: at each bit a lane keeps one half of what it holds and
+// gives the other away, so that N - 1 exchanges (not N for each bit) are enough.  A lane ends with N FROM / 64 values (one at
+// least), of the returned index onwards.
+template <int N, int O, int FROM, int NV>
+__device__ __forceinline__ int scatter_sum(float (&v)[NV], int lane)
+{
+    if constexpr (O < FROM) {
+        return 0;
+    } else if constexpr (N > 1) {
+        const bool up = lane & O;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const float give = up ? v[i] : v[i + N / 2], keep = up ? v[i + N / 2] : v[i];
+            v[i] = keep + __shfl_xor(give, O, kWave);
+        }
+        return (up ? N / 2 : 0) + scatter_sum<N / 2, O / 2, FROM>(v, lane);
+    } else {
+        v[0] += __shfl_xor(v[0], O, kWave);
+        return scatter_sum<1, O / 2, FROM>(v, lane);
+    }
+}
+
+// A wavefront's scores: rows row0 + 32 i + lane % 32, columns col0 + 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4 in acc[i][j][e].
+// SCORES: maximum and sum of exponentials of its columns of each row, and the label's score where it is among them.
+// GRADIENT: dZ = g (exp(z - lse) - [label]), 0 in rows without a label and in columns that do not exist (to a multiple of 32), as
+// `planes` bf16 whose sum is it (one: rounded), and its column sums.
+template <int MODE, class T, int PLANES, class ARGS>
+__device__ __forceinline__ void loss_epilogue(const ARGS &g, f32x16 (&acc)[T::TM][T::TN], int64_t row0, int64_t col0, int64_t row_slot, int64_t col_slot)
+{
+    constexpr float kLog2e = 1.44269504089f;
+    const int lane = threadIdx.x & (kWave - 1), h = lane >> 5, l32 = lane & 31;
+    const int64_t far = g.C - col0;                                       // columns that exist, less this lane's first
+    const int left = (int)(far < T::TN * 32 ? far : T::TN * 32) - 4 * h;
+    if (far <= 0) return;                                                 // the same for a wavefront
+    float sums[T::TN * 16];
+    if constexpr (MODE == kGradient) {
+#pragma unroll
+        for (int c = 0; c < T::TN * 16; ++c) sums[c] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i) {
+        const int64_t row = row0 + i * 32 + l32;
+        const bool in = row < g.R;
+        const int64_t label = in ? g.label[row] : -1, at = label - g.first - col0 - 4 * h;      // of the label among this lane's columns
+        const int mine = label >= 0 && at >= 0 && at < T::TN * 32 ? (int)at : -1;
+        if constexpr (MODE == kScores) {
+            float most = -INFINITY, sum = 0.f, z = 0.f;
+            bool has = false;
+            if (far < T::TN * 32) {                                       // columns that do not exist weigh nothing
+#pragma unroll
+                for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * j + 8 * (e >> 2) + (e & 3) < left ? acc[i][j][e] : -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const bool is = 32 * j + 8 * (e >> 2) + (e & 3) == mine;
+                    most = fmaxf(most, acc[i][j][e]);
+                    z = is ? acc[i][j][e] : z;
+                    has = has || is;
+                }
+            most = fmaxf(most, __shfl_xor(most, 32, kWave));
+            const float base = most == -INFINITY ? 0.f : most;
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - base) * kLog2e);
+            sum += __shfl_xor(sum, 32, kWave);
+            if (h == 0 && in) {
+                float *to = g.stats + 2 * (col_slot * g.R + row);
+                to[0] = most;
+                to[1] = sum;
+            }
+            if (has && mine < left) g.picked[row] = z;
+        } else {
+            const float lse = in ? g.lse[row] : 0.f;
+            const float scale = label >= g.classes ? NAN : in ? g.dloss[row] : 0.f;
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j) {
+                if (32 * j >= far) break;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int c = 32 * j + 8 * q + e;
+                        const float p = __builtin_amdgcn_exp2f((acc[i][j][4 * q + e] - lse) * kLog2e);
+                        const float x = c == mine ? p - 1.f : p;
+                        v[e] = label >= 0 && c < left ? x * scale : 0.f;
+                        sums[16 * j + 4 * q + e] += v[e];
+                    }
+                    if (in) {
+                        uint16_t *to = g.dz + (col0 / 32 + j) * g.dz_block + row * g.dz_ld + 8 * q + 4 * h;
+#pragma unroll
+                        for (int p = 0; p < PLANES; ++p) {
+                            u32x2 o;
+                            o[0] = pack_bf16(v[0], v[1]);
+                            o[1] = pack_bf16(v[2], v[3]);
+                            *reinterpret_cast<u32x2 *>(to + p * g.dz_plane) = o;
+                            if (p + 1 < PLANES) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) v[e] -= __uint_as_float(e & 1 ? o[e >> 1] & 0xFFFF0000u : o[e >> 1] << 16);
+                            }
+                        }
+                    }
+                }
+            }
+        }
+    }
+    if constexpr (MODE == kGradient) {
+        if (!g.db) return;
+        constexpr int NV = T::TN * 16;
+        const int at = scatter_sum<NV, 16, 1>(sums, lane);
+#pragma unroll
+        for (int k = 0; k < NV / 32; ++k) {
+            const int e = at + k, c = 32 * (e >> 4) + 8 * ((e >> 2) & 3) + (e & 3);
+            if (c < left) g.db[row_slot * g.C + col0 + 4 * h + c] = sums[k];
+        }
+    }
+}
+
 // PART: sums of a slab instead of results.  ONCE: whole lines of results go past the caches.
 template <int MODE, int SIZE, class OUT, int ACT, bool PART, bool ONCE>
-__global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(TileArgs g)
+__global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(typename TileArgsOf<MODE>::type g)
 {
 #ifdef __HIP_DEVICE_COMPILE__                    // the host pass makes no launch stub of a body with these builtins
     using T = Tile<MODE, SIZE>;
@@ -175,7 +364,7 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
     const int first_step = PART ? (int)((int64_t)steps * nseg * slab / g.slabs) : 0;
     const int all = (PART ? (int)((int64_t)steps * nseg * (slab + 1) / g.slabs) : steps * nseg) - first_step;
 
-    const int64_t a_blocks = MODE == kRows ? g.a_blocks : 0, b_blocks = MODE == kWeights ? g.b_blocks : 0;
+    const int64_t a_blocks = T::ROWS ? g.a_blocks : 0, b_blocks = T::WEIGHTS ? g.b_blocks : 0;
 
     // Where this lane's 16-byte pieces of a step come from.
     uint32_t off_a[T::LA], off_b[T::LB];
@@ -213,23 +402,25 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
     // blocks of columns: what the tile has of them; where a block's own rows end, only masks tell
     int64_t left_blocks = b_blocks ? (g.C - col0 + 31) / 32 : 0;
     left_blocks = left_blocks < T::BC / 32 ? left_blocks : T::BC / 32;
-    const int bytes_b = (int)(2 * (b_blocks ? left_blocks * b_blocks : T::B_T ? kStep * g.ldb - col0 : rows_b * g.ldb));
-    const int64_t base_b = b_blocks ? col0 / 32 * b_blocks : T::B_T ? col0 : col0 * g.ldb;
-    const int last_a = T::A_T ? (int)(2 * (last_rows * g.lda - row0)) : bytes_a, last_b = T::B_T && !b_blocks ? (int)(2 * (last_rows * g.ldb - col0)) : bytes_b;
+    int64_t col_b = col0;                                                // of B
+    if constexpr (MODE == kScores || MODE == kGradient) col_b += g.shift;
+    const int bytes_b = (int)(2 * (b_blocks ? left_blocks * b_blocks : T::B_T ? kStep * g.ldb - col_b : rows_b * g.ldb));
+    const int64_t base_b = b_blocks ? col0 / 32 * b_blocks : T::B_T ? col_b : col0 * g.ldb;
+    const int last_a = T::A_T ? (int)(2 * (last_rows * g.lda - row0)) : bytes_a, last_b = T::B_T && !b_blocks ? (int)(2 * (last_rows * g.ldb - col_b)) : bytes_b;
     const bool beyond = piece_k * 8 >= last_rows;                        // rows are padded with zeros to whole pieces
     uint32_t last_off_b[T::LB];
 #pragma unroll
     for (int i = 0; i < T::LB; ++i) {
         const int k = (i % (T::LB / T::RESULTS) * NW * kWave + wave * kWave + lane) / (T::BC / 8);         // of this lane's piece
-        last_off_b[i] = (T::B_T ? MODE == kWeights && k >= last_rows : beyond) ? kNoSuchOffset : off_b[i];
+        last_off_b[i] = (T::B_T ? T::WEIGHTS && k >= last_rows : beyond) ? kNoSuchOffset : off_b[i];
     }
     auto begin_segment = [&]() __attribute__((always_inline)) {
-        const int grp = MODE == kRows ? seg / g.pairs : 0, pair = MODE == kRows ? seg - grp * g.pairs : seg;
+        const int grp = T::ROWS ? seg / g.pairs : 0, pair = T::ROWS ? seg - grp * g.pairs : seg;
         const int pa = (int)(g.planes_a >> (4 * pair)) & 15, pb = (int)(g.planes_b >> (4 * pair)) & 15;
         next_a = g.a[grp] + pa * g.a_plane + (T::A_T ? row0 : row0 * row_a) + t * step_a;
 #pragma unroll
         for (int q = 0; q < T::RESULTS; ++q)
-            next_b[q] = (MODE == kRows ? g.b[grp] : g.b[q]) + pb * g.b_plane + base_b + t * step_b;
+            next_b[q] = (T::ROWS ? g.b[grp] : g.b[q]) + pb * g.b_plane + base_b + t * step_b;
     };
     auto load_next = [&]() __attribute__((always_inline)) {
         if (loaded >= all) return;
@@ -247,7 +438,7 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
             const auto rb = rsrc(next_b[q], last ? last_b : bytes_b);
 #pragma unroll
             for (int i = q * (T::LB / T::RESULTS); i < (q + 1) * (T::LB / T::RESULTS); ++i) {
-                const uint32_t o = MODE != kForward && last ? last_off_b[i] : off_b[i];
+                const uint32_t o = !T::FORWARD && last ? last_off_b[i] : off_b[i];
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (FASTGL_LDS void *)(to + T::A_BYTES + i * NW * 1024), 16, (int)o, 0, 0, 0);
             }
             next_b[q] += step_b;
@@ -314,7 +505,7 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
         f32x16 start;
 #pragma unroll
         for (int e = 0; e < 16; ++e) start[e] = 0.f;
-        if constexpr (MODE == kForward && !PART)
+        if constexpr (T::FORWARD && !PART)
             if (const float *bias = g.bias[j / ONE]) {
                 const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(bias), 0, (int)(g.C * 4), kTileRsrc);
 #pragma unroll
@@ -385,6 +576,8 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
     static_assert(64 * ROWB <= PARTB, "a block of 64 x 64 results fits a wavefront's part");
     FASTGL_LDS char *mine = (FASTGL_LDS char *)lds + wave * PARTB;
     const int64_t r_base = row0 + wm * 64;
+    int64_t ldo = g.C;                                                   // elements between rows of the result
+    if constexpr (MODE == kWeightsOne && !PART) ldo = g.ldo;
     // NB blocks of 32 columns from column c_base of the wavefront's 64 rows, element by element from value(i, block, e).
     auto store_block = [&](auto blocks, void *out, int64_t c_base, auto value) {
         constexpr int NB = decltype(blocks)::value, LPR = NB * 32 * OB / 16, PER = 16 / OB;      // lanes a row: PER elements each
@@ -420,14 +613,20 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
         const int row = lane / LPR, c = lane % LPR;
         FASTGL_LDS char *from = mine + row * ROWB;
         auto piece = [&](int n) { return *(FASTGL_LDS u32x4 *)(from + n * ROWS * ROWB + ((c ^ ((row + n * ROWS) & 7)) * 16)); };
-        OUT *base = static_cast<OUT *>(out) + r_base * g.C + c_base;
+        OUT *base = static_cast<OUT *>(out) + r_base * ldo + c_base;
         if (r_base + 64 <= g.R && c_base + NB * 32 <= g.C) {              // all of it exists
-            uint32_t o = (uint32_t)((row * g.C + c * PER) * OB);
-            const uint32_t down = (uint32_t)(ROWS * g.C * OB);
+            uint32_t o = (uint32_t)((row * ldo + c * PER) * OB);
+            const uint32_t down = (uint32_t)(ROWS * ldo * OB);
 #pragma unroll
             for (int n = 0; n < ROUNDS; ++n, o += down) {
-                const u32x4 v = piece(n);
+                u32x4 v = piece(n);
                 W4 *p = reinterpret_cast<W4 *>(reinterpret_cast<char *>(base) + o);
+                if constexpr (MODE == kRowsAdd)
+                    if (g.add) {
+                        const W4 w = *p;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + __uint_as_float(w[e]));
+                    }
                 if constexpr (ONCE) __builtin_nontemporal_store(W4{v[0], v[1], v[2], v[3]}, p);
                 else *p = W4{v[0], v[1], v[2], v[3]};
             }
@@ -435,8 +634,14 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
             const int64_t left = g.C - c_base - c * PER;
             for (int n = 0; n < ROUNDS; ++n) {
                 if (r_base + row + n * ROWS >= g.R || left <= 0) continue;
-                const u32x4 v = piece(n);
-                OUT *p = base + (row + n * ROWS) * g.C + c * PER;
+                u32x4 v = piece(n);
+                OUT *p = base + (row + n * ROWS) * ldo + c * PER;
+                if constexpr (MODE == kRowsAdd)
+                    if (g.add) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (e < left) v[e] = __float_as_uint(__uint_as_float(v[e]) + p[e]);
+                    }
                 if (left >= PER) {
                     *reinterpret_cast<W4 *>(p) = W4{v[0], v[1], v[2], v[3]};
                 } else {
@@ -458,10 +663,12 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(T
         for (int n = 0; n < ONE; n += NB::value)
             store_block(NB(), out, col0 + (wn * ONE + n) * 32, [&](int i, int b, int e) { return value(i, n + b, e); });
     };
-    if constexpr (PART) {
+    if constexpr (MODE == kScores || MODE == kGradient) {
+        loss_epilogue<MODE, T, sizeof(OUT) == 4 ? 3 : 1>(g, acc, r_base, col0 + wn * T::TN * 32, (row0 / T::BM) * T::WM + wm, (col0 / T::BC) * T::WN + wn);
+    } else if constexpr (PART) {
 #pragma unroll
         for (int q = 0; q < T::RESULTS; ++q)
-            if (MODE == kForward || g.out[q])
+            if (MODE == kForward || MODE == kRowsAdd || MODE == kWeightsOne || g.out[q])
                 store_result(q, g.part + ((int64_t)slab * T::RESULTS + q) * g.R * g.C, [&](int i, int b, int e) { return acc[i][q * ONE + b][e]; });
     } else if constexpr (MODE == kForward) {
         if (g.out[1]) store_result(0, g.out[1], [&](int i, int b, int e) { return acc[i][b][e]; });

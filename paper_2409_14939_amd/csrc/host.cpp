@@ -27,6 +27,7 @@
 #include "fastgl_edge.h"
 #include "fastgl_gated.h"
 #include "fastgl_idmap.h"
+#include "fastgl_loss.h"
 #include "fastgl_match.h"
 #include "fastgl_norm.h"
 #include "fastgl_update.h"
@@ -948,6 +949,59 @@ PyObject *attn_bwd(PyObject *const *a)
     return tuple({dQ.t, dK.t, dV.t, dbias.t});
 }
 
+// ------------------------------------------------------------------------- a classifier's loss
+// (H, W, b, label): what both passes of the loss take.
+struct Loss {
+    const at::Tensor &H, &W, &label;
+    int64_t M, K, N;
+    const float *b;
+    fastgl_dtype dt;
+    explicit Loss(PyObject *const *a) : H(features2(a[0], "H")), W(dev(a[1], H.scalar_type(), "W")), label(dev(a[3], at::kLong, "label"))
+    {
+        M = H.size(0);
+        K = H.size(1);
+        if (W.dim() != 2 || W.size(0) != K) fail(PyExc_ValueError, "W must be [K, N]");
+        N = W.size(1);
+        if (!shape1(label, M)) fail(PyExc_ValueError, "label must be [M]");
+        b = none(a[2]) ? nullptr : vector_f32(a[2], N, "b");
+        dt = feat_dtype(H);
+    }
+    int aligned() const { return whole(H.data_ptr()) && whole(W.data_ptr()); }
+};
+
+// (H, W, b, label, want_lse, loss, lse, workspace) -> (loss, lse)
+PyObject *loss_fwd(PyObject *const *a)
+{
+    const Loss c(a);
+    const Out loss = out_of(a[5], at::kFloat, {c.M}, c.H, "loss");
+    Out lse;
+    if (truth(a[4]) || !none(a[6])) lse = out_of(a[6], at::kFloat, {c.M}, c.H, "lse");
+    const Scratch ws(a[7], c.H, [&] { return fastgl_loss_fwd_workspace_bytes(c.dt, c.M, c.K, c.N, c.aligned()); });
+    run([&](void *s) {
+        return fastgl_loss_fwd(c.dt, c.H.data_ptr(), c.W.data_ptr(), c.b, (const int64_t *)c.label.data_ptr(), c.M, c.K, c.N, (float *)loss.p(),
+                               (float *)lse.p(), ws.p(), ws.n(), s);
+    });
+    return tuple({loss.t, lse.t});
+}
+
+// (H, W, b, label, lse, dloss, want_dH, want_dW, want_db, dH, dW, db, workspace) -> (dH, dW, db)
+PyObject *loss_bwd(PyObject *const *a)
+{
+    const Loss c(a);
+    const float *lse = vector_f32(a[4], c.M, "lse"), *dloss = vector_f32(a[5], c.M, "dloss");
+    const auto type = c.H.scalar_type();
+    Out dH, dW, db;
+    if (truth(a[6]) || !none(a[9])) dH = out_of(a[9], type, {c.M, c.K}, c.H, "dH");
+    if (truth(a[7]) || !none(a[10])) dW = out_of(a[10], type, {c.K, c.N}, c.H, "dW");
+    if (truth(a[8]) || !none(a[11])) db = out_of(a[11], at::kFloat, {c.N}, c.H, "db");
+    const Scratch ws(a[12], c.H, [&] { return fastgl_loss_bwd_workspace_bytes(c.dt, c.M, c.K, c.N, c.aligned()); });
+    run([&](void *s) {
+        return fastgl_loss_bwd(c.dt, c.H.data_ptr(), c.W.data_ptr(), c.b, (const int64_t *)c.label.data_ptr(), lse, dloss, c.M, c.K, c.N, dH.p(),
+                               dW.p(), (float *)db.p(), ws.p(), ws.n(), s);
+    });
+    return tuple({dH.t, dW.t, db.t});
+}
+
 // (error class): called once by binding.py
 PyObject *set_error_class(PyObject *const *a)
 {
@@ -963,7 +1017,7 @@ PyMethodDef g_methods[] = {
     FN(update_fwd, 5), FN(layer_fwd, 14), FN(update_bwd, 12), FN(idmap, 7), FN(match, 7), FN(assemble_rows, 5),
     FN(overlap_counts, 3), FN(edge_weight_grad, 9), FN(edge_softmax_fwd, 4), FN(edge_softmax_bwd, 5),
     FN(edge_score_fwd, 6), FN(edge_score_bwd, 11), FN(norm_fwd, 13), FN(norm_bwd, 14), FN(dropout, 5),
-    FN(gather_rows_e4m3, 5), FN(gated_fwd, 11), FN(gated_bwd, 19), FN(attn_fwd, 15), FN(attn_bwd, 21), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
+    FN(gather_rows_e4m3, 5), FN(gated_fwd, 11), FN(gated_bwd, 19), FN(attn_fwd, 15), FN(attn_bwd, 21), FN(loss_fwd, 8), FN(loss_bwd, 13), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
 #undef FN
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host", "Native marshalling of the C ABI's calls.", -1, g_methods,

@@ -1,0 +1,500 @@
+// Softmax cross entropy of class scores that are not kept (fastgl_loss.h has the formulas): what is around the products of gated_tile.h.
+//
+//   forward   [operands packed] -> scores by tiles, of which maximum and sum of exponentials of some columns of each row remain -> k_loss_join
+//   backward  for a piece of the classes at a time: [W packed] -> scores again, of which dZ remains (as the matrix cores take it, with column sums)
+//             -> dH += dZ W^T -> dW = H^T dZ -> k_loss_sum
+//
+// The rows of H are packed once for all pieces of a backward pass, 0 where there is no label: dZ is 0 there, and what H holds there must not
+// reach dW (0 times NaN).
+#include <initializer_list>
+
+#include "fastgl_loss.h"
+#include "gated_tile.h"
+#include "update_internal.h"
+
+namespace fastgl {
+namespace {
+
+constexpr int64_t kMostClasses = (int64_t)1 << 21, kMostInputs = (int64_t)1 << 20;
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;       // of dZ, and of packed weights, at a time
+constexpr int kPieceCols = 256;                           // a piece has a multiple of them
+
+// ------------------------------------------------------------------ packing
+// Matrices [rows][cols] (rows ld_src apart) as planes of bf16 with rows of ld elements, 0 beyond cols and in rows whose label is negative.
+struct LossPackArgs {
+    const void *src[2];
+    uint16_t *out[2];
+    const int64_t *label[2];
+    int64_t rows[2], ld_src[2], end[2];      // end: elements from src to the array's end
+    int32_t cols[2], ld[2];
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(kBlock) void k_loss_pack(LossPackArgs a)
+{
+    typedef typename Chunk<BF16>::elem T;
+    const int m = blockIdx.y;
+    const T *src = static_cast<const T *>(m ? a.src[1] : a.src[0]);
+    uint16_t *out = m ? a.out[1] : a.out[0];
+    const int64_t *label = m ? a.label[1] : a.label[0];
+    const int64_t rows = m ? a.rows[1] : a.rows[0], ld_src = m ? a.ld_src[1] : a.ld_src[0], end = m ? a.end[1] : a.end[0];
+    const int32_t cols = m ? a.cols[1] : a.cols[0], ld = m ? a.ld[1] : a.ld[0], chunks = ld / kChunk;
+    const int64_t n = rows * chunks;
+    for (int64_t u = (int64_t)blockIdx.x * kBlock + threadIdx.x; u < n; u += (int64_t)gridDim.x * kBlock) {
+        const int64_t row = u / chunks;
+        const int col = (int)(u - row * chunks) * kChunk, left = cols - col;
+        const int64_t at = row * ld_src + col;
+        Chunk<BF16> c;
+        float v[8];
+        c.load(src + at, left > 0 && at + kChunk <= end ? kChunk : left);
+        const bool on = !label || label[row] >= 0;
+        c.get(v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = on && j < left ? v[j] : 0.f;
+        uint16_t *to = out + row * ld + col;
+        Chunk<true>::store(to, v, 8);
+        if constexpr (!BF16) {
+#pragma unroll
+            for (int p = 1; p < 3; ++p) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] -= (float)(__bf16)v[j];
+                Chunk<true>::store(to + p * rows * ld, v, 8);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ joining
+// A row's maxima and sums from all column tiles, 2^lg rows and as many threads a row as are left.
+__global__ __launch_bounds__(kBlock) void k_loss_join(const float *stats, int64_t slots, const float *picked, const int64_t *label, int64_t M, int64_t N,
+                                                      int lg, float *loss, float *lse)
+{
+    constexpr float kLog2e = 1.44269504089f, kLn2 = 0.69314718056f;
+    __shared__ float most[kBlock], sums[kBlock];
+    const int parts = kBlock >> lg, part = threadIdx.x >> lg, r = threadIdx.x & ((1 << lg) - 1);
+    const int64_t row = ((int64_t)blockIdx.x << lg) + r;
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    const f2 *p = reinterpret_cast<const f2 *>(stats) + (row < M ? row : M - 1);
+    float m = -INFINITY, s = 0.f;
+#pragma unroll 4
+    for (int64_t t = part; t < slots; t += parts) {
+        const f2 x = p[t * M];
+        const float next = fmaxf(m, x[0]), base = next == -INFINITY ? 0.f : next;
+        s = s * __builtin_amdgcn_exp2f((m - base) * kLog2e) + x[1] * __builtin_amdgcn_exp2f((x[0] - base) * kLog2e);
+        m = next;
+    }
+    most[threadIdx.x] = m;
+    sums[threadIdx.x] = s;
+    __syncthreads();
+    if (part != 0 || row >= M) return;
+    for (int q = 1; q < parts; ++q) m = fmaxf(m, most[(q << lg) + r]);
+    const float base = m == -INFINITY ? 0.f : m;
+    s = 0.f;
+    for (int q = 0; q < parts; ++q) s += sums[(q << lg) + r] * __builtin_amdgcn_exp2f((most[(q << lg) + r] - base) * kLog2e);
+    const float all = m == -INFINITY && s == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(s) * kLn2;
+    if (lse) lse[row] = all;
+    const int64_t y = label[row];
+    loss[row] = y < 0 ? 0.f : y >= N ? NAN : all - picked[row];
+}
+
+// ------------------------------------------------------------------ sums of slabs, column sums
+struct LossSumArgs {
+    const float *part;               // slab s at part + s * R * C, or NULL
+    void *out;                       // rows ldo apart
+    int64_t R, C, ldo;
+    int32_t slabs;
+    int32_t blocks;                  // workgroups of the slabs, before those of the columns
+    const float *db_part;            // [db_rows][db_cols], or NULL
+    float *db;
+    int32_t db_rows, db_cols;
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(kBlock) void k_loss_sum(LossSumArgs a)
+{
+    if ((int)blockIdx.x < a.blocks) {
+        const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x, n = a.R * a.C;
+        if (i >= n) return;
+        double v = 0.0;
+#pragma unroll 8
+        for (int s = 0; s < a.slabs; ++s) v += (double)a.part[(int64_t)s * n + i];
+        const int64_t row = i / a.C, to = row * a.ldo + (i - row * a.C);
+        if constexpr (BF16) static_cast<uint16_t *>(a.out)[to] = __builtin_bit_cast(uint16_t, (__bf16)(float)v);
+        else static_cast<float *>(a.out)[to] = (float)v;
+        return;
+    }
+    __shared__ double sums[kBlock / 8][9];                             // eight columns, 32 threads a column
+    const int c = threadIdx.x & 7, r = threadIdx.x >> 3;
+    const int64_t col = ((int64_t)blockIdx.x - a.blocks) * 8 + c;
+    double v = 0.0;
+    if (col < a.db_cols) {
+#pragma unroll 8
+        for (int i = r; i < a.db_rows; i += kBlock / 8) v += (double)a.db_part[(int64_t)i * a.db_cols + col];
+    }
+    sums[r][c] = v;
+    __syncthreads();
+    if (r == 0 && col < a.db_cols) {
+        v = 0.0;
+        for (int i = 0; i < kBlock / 8; ++i) v += sums[i][c];
+        a.db[col] = (float)v;
+    }
+}
+
+// ------------------------------------------------------------------ host side
+bool misaligned_to(const void *p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
+
+struct Shape {
+    bool bf16, backward, pack_h, pack_w;
+    int planes;
+    int64_t M, K, N, ldk, pairs;
+    Shape(fastgl_dtype dtype, int64_t M_, int64_t K_, int64_t N_, bool aligned, bool backward_)
+        : bf16(dtype == FASTGL_BF16), backward(backward_), pack_h(backward_ || !bf16 || !aligned || K_ % 8), pack_w(!bf16 || !aligned || N_ % 8),
+          planes(bf16 ? 1 : 3), M(M_), K(K_), N(N_), ldk((int64_t)align_up((size_t)K_, 8)), pairs(bf16 ? 1 : 6)
+    {
+    }
+    int64_t rows() const { return (int64_t)align_up((size_t)M, 256); }
+    // Classes of a piece: dZ and packed weights stay below kPieceBytes, the pieces are of one size.
+    int64_t piece() const
+    {
+        int64_t most = N;
+        if (backward) most = kPieceBytes / (2 * planes * rows());
+        if (pack_w && K > 0 && kPieceBytes / (2 * planes * K) < most) most = kPieceBytes / (2 * planes * K);
+        most = most < 2 * kPieceCols ? kPieceCols : most / kPieceCols * kPieceCols;
+        if (most >= N || !(backward || pack_w)) return (int64_t)align_up((size_t)N, kPieceCols);
+        return (int64_t)align_up((size_t)ceil_div(N, ceil_div(N, most)), kPieceCols);
+    }
+    int64_t pieces() const { return ceil_div(N, piece()); }
+    int64_t widest() const { return piece() < N ? piece() : N; }          // columns that exist of the largest piece
+    // dZ in blocks of 32 columns, [block][row][32], a block 2304 bytes more than a multiple of 4096 (the gated update's layout and reasons);
+    // rows lie whole where eight blocks pass 32-bit offsets.
+    bool blocks() const { return M <= (int64_t)1 << 21; }
+    int64_t z_block() const { return blocks() ? (int64_t)(align_up((size_t)rows() * 64, 4096) + 2304) / 2 : 32; }
+    int64_t z_ld() const { return blocks() ? 32 : piece(); }
+    int64_t z_plane() const { return blocks() ? piece() / 32 * z_block() : rows() * piece(); }
+    Cut scores_cut() const { return cut_of(kForward, M, widest(), K, pairs, true, true); }
+    Cut rows_cut() const { return cut_of(kRows, M, K, widest(), pairs); }
+    Cut weights_cut() const { return cut_of(kWeights, K, widest(), M, pairs, true); }
+    static int64_t tile_rows(const Cut &c) { return c.size == kLarge ? 256 : 128; }
+    static int64_t wave_cols(const Cut &c) { return c.size == kSmall ? 64 : 128; }
+    int64_t slots() const                                                  // of statistics: column tiles and wavefronts of all pieces
+    {
+        const int64_t per = ceil_div(widest(), wave_cols(scores_cut()));
+        return per * pieces();
+    }
+    int64_t db_rows() const { return ceil_div(M, tile_rows(scores_cut())) * (scores_cut().size == kLarge ? 4 : 2); }
+    bool parts_h() const { return pieces() > 1 || rows_cut().slabs > 1; }
+};
+
+struct Scratch {
+    size_t used = 0;
+    char *base;
+    uint16_t *h, *w, *dz;
+    float *stats, *picked, *db, *part_h, *part_w;
+    template <class T>
+    T *take(size_t n)
+    {
+        char *p = base ? base + used : nullptr;
+        used += align_up(n * sizeof(T), 256);
+        return reinterpret_cast<T *>(p);
+    }
+    Scratch(const Shape &s, char *at) : base(at)
+    {
+        h = w = dz = nullptr;
+        stats = picked = db = part_h = part_w = nullptr;
+        if (s.pack_h) h = take<uint16_t>((size_t)(s.planes * s.M * s.ldk));
+        if (s.pack_w) w = take<uint16_t>((size_t)(s.planes * s.K * s.piece()));
+        if (!s.backward) {
+            stats = take<float>((size_t)(2 * s.slots() * s.M));
+            picked = take<float>((size_t)s.M);
+            return;
+        }
+        dz = take<uint16_t>((size_t)(s.planes * s.z_plane()));
+        db = take<float>((size_t)(s.db_rows() * s.widest()));
+        if (s.parts_h()) part_h = take<float>((size_t)(s.rows_cut().slabs * s.M * s.K));
+        const Cut c = s.weights_cut();
+        if (c.slabs > 1) part_w = take<float>((size_t)(c.slabs * s.K * s.widest()));
+    }
+};
+
+fastgl_status check(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N)
+{
+    if (dtype != FASTGL_F32 && dtype != FASTGL_BF16) {
+        set_error("bad dtype %d", (int)dtype);
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (M < 0 || K < 0 || N < 0 || (M > 0 && N == 0)) {
+        set_error("negative size, or rows without classes (M=%lld K=%lld N=%lld)", (long long)M, (long long)K, (long long)N);
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (M > kMaxIndex || K > kMostInputs || N > kMostClasses) {
+        set_error("M must stay below 2^31-1-1024, K at 2^20 and N at 2^21 or below");
+        return FASTGL_ERR_UNSUPPORTED;
+    }
+    return FASTGL_OK;
+}
+
+fastgl_status check_workspace(const void *ws, size_t bytes, size_t need)
+{
+    if (need == 0) return FASTGL_OK;
+    if (!ws || misaligned_to(ws, 256)) {
+        set_error("workspace must be a 256-byte aligned device buffer");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    if (bytes < need) {
+        set_error("workspace too small: %zu < %zu bytes", bytes, need);
+        return FASTGL_ERR_WORKSPACE;
+    }
+    return FASTGL_OK;
+}
+
+size_t workspace(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, bool aligned, bool backward)
+{
+    if (check(dtype, M, K, N) != FASTGL_OK || M == 0) return 0;
+    const size_t whole = Scratch(Shape(dtype, M, K, N, true, backward), nullptr).used;
+    if (aligned) return whole;
+    const size_t any = Scratch(Shape(dtype, M, K, N, false, backward), nullptr).used;
+    return any > whole ? any : whole;
+}
+
+// What of H and of classes n0 .. n0 + n of W a call needs packed, in one launch.
+fastgl_status pack(const Shape &d, const Scratch &o, const void *H, const void *W, const int64_t *label, int64_t n0, int64_t n, bool h, bool w, hipStream_t s)
+{
+    const int64_t el = d.bf16 ? 2 : 4;
+    LossPackArgs a = {};
+    int m = 0;
+    int64_t most = 0;
+    auto add = [&](const void *src, uint16_t *out, const int64_t *on, int64_t rows, int64_t cols, int64_t ld_src, int64_t end, int64_t ld) {
+        if (rows == 0 || cols == 0) return;
+        a.src[m] = src;
+        a.out[m] = out;
+        a.label[m] = on;
+        a.rows[m] = rows; a.ld_src[m] = ld_src; a.end[m] = end;
+        a.cols[m] = (int32_t)cols; a.ld[m++] = (int32_t)ld;
+        if (rows * (ld / kChunk) > most) most = rows * (ld / kChunk);
+    };
+    if (h) add(H, o.h, d.backward ? label : nullptr, d.M, d.K, d.K, d.M * d.K, d.ldk);
+    if (w) add(static_cast<const char *>(W) + n0 * el, o.w, nullptr, d.K, n, d.N, d.K * d.N - n0, (int64_t)align_up((size_t)n, 8));
+    if (m == 0) return FASTGL_OK;
+    const int64_t blocks = ceil_div(most, kBlock);
+    const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384), (unsigned)m);
+    if (d.bf16) hipLaunchKernelGGL(k_loss_pack<true>, grid, dim3(kBlock), 0, s, a);
+    else hipLaunchKernelGGL(k_loss_pack<false>, grid, dim3(kBlock), 0, s, a);
+    FASTGL_LAUNCH_CHECK("fastgl_loss (pack)");
+    return FASTGL_OK;
+}
+
+// One product.  PART: sums of slabs.
+template <int MODE, bool PART>
+fastgl_status launch(const LossTileArgs &args, const Cut &cut, bool bf16, hipStream_t s, const char *what)
+{
+    typename TileArgsOf<MODE>::type g = args;
+    const int64_t tr = ceil_div(g.R, Shape::tile_rows(cut)), tc = ceil_div(g.C, cut.size == kSmall ? 128 : 256), total = tr * tc * cut.slabs;
+    if (total > 0x7FFFFFFFLL || 4 * tc > 0x7FFFFFFFLL) {
+        set_error("%s: too many tiles (%lld)", what, (long long)total);
+        return FASTGL_ERR_UNSUPPORTED;
+    }
+    g.tiles_r = (int32_t)tr;
+    g.tiles_c = (int32_t)tc;
+    g.slabs = (int32_t)cut.slabs;
+    auto sized = [&](auto size) {
+        constexpr int S = decltype(size)::value;
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(Tile<MODE, S>::THREADS), 0, s, g); };
+        if constexpr (PART || MODE == kScores) go(k_gated_tile<MODE, S, float, 0, PART, false>);
+        else if (bf16) go(k_gated_tile<MODE, S, uint16_t, 0, false, false>);
+        else go(k_gated_tile<MODE, S, float, 0, false, false>);
+    };
+    if (cut.size == kLarge) sized(std::integral_constant<int, kLarge>());
+    else if (cut.size == kMiddle) sized(std::integral_constant<int, kMiddle>());
+    else sized(std::integral_constant<int, kSmall>());
+    FASTGL_LAUNCH_CHECK(what);
+    return FASTGL_OK;
+}
+
+fastgl_status launch_sum(LossSumArgs a, bool bf16, hipStream_t s, const char *what)
+{
+    a.blocks = (int32_t)(a.part ? ceil_div(a.R * a.C, kBlock) : 0);
+    const dim3 grid((unsigned)(a.blocks + (a.db_part ? ceil_div((int64_t)a.db_cols, 8) : 0)));
+    if (bf16) hipLaunchKernelGGL(k_loss_sum<true>, grid, dim3(kBlock), 0, s, a);
+    else hipLaunchKernelGGL(k_loss_sum<false>, grid, dim3(kBlock), 0, s, a);
+    FASTGL_LAUNCH_CHECK(what);
+    return FASTGL_OK;
+}
+
+// The scores' product of classes n0 .. n0 + n.
+LossTileArgs scores_of(const Shape &d, const Scratch &o, const void *H, const void *W, const float *b, const int64_t *label, int64_t n0, int64_t n)
+{
+    LossTileArgs g = {};
+    g.a[0] = d.pack_h ? o.h : (const uint16_t *)H;
+    g.b[0] = d.pack_w ? o.w : (const uint16_t *)W;
+    g.lda = d.ldk;
+    g.ldb = d.pack_w ? (int64_t)align_up((size_t)n, 8) : d.N;
+    g.shift = d.pack_w ? 0 : n0;
+    g.a_plane = d.M * d.ldk; g.b_plane = d.K * g.ldb;
+    g.R = d.M; g.C = n; g.Kc = d.K;
+    g.pairs = (int32_t)d.pairs; g.groups = 1;
+    if (!d.bf16) {
+        g.planes_a = kSixA;
+        g.planes_b = kSixB;
+    }
+    g.bias[0] = b ? b + n0 : nullptr;
+    g.label = label;
+    g.first = n0; g.classes = d.N;
+    return g;
+}
+
+bool starts_whole(std::initializer_list<const void *> ps)
+{
+    for (const void *p : ps)
+        if (misaligned_to(p, 16)) return false;
+    return true;
+}
+
+}  // namespace
+}  // namespace fastgl
+
+using namespace fastgl;
+
+extern "C" {
+
+size_t fastgl_loss_fwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned)
+{
+    return workspace(dtype, M, K, N, aligned != 0, false);
+}
+
+size_t fastgl_loss_bwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned)
+{
+    return workspace(dtype, M, K, N, aligned != 0, true);
+}
+
+fastgl_status fastgl_loss_fwd(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label, int64_t M,
+                              int64_t K, int64_t N, float *loss, float *lse, void *ws, size_t ws_bytes, void *stream)
+{
+    fastgl_status st = check(dtype, M, K, N);
+    if (st != FASTGL_OK) return st;
+    if (M == 0) return FASTGL_OK;
+    if (!label || !loss || (K > 0 && (!H || !W))) {
+        set_error("H, W, label or loss is NULL");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    const uintptr_t el = dtype == FASTGL_BF16 ? 2 : 4;
+    if (misaligned_to(H, el) || misaligned_to(W, el) || misaligned_to(b, 4) || misaligned_to(label, 8) || misaligned_to(loss, 4) || misaligned_to(lse, 4)) {
+        set_error("buffers must be aligned to their element size");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    const Shape d(dtype, M, K, N, starts_whole({H, W}), false);
+    if ((st = check_workspace(ws, ws_bytes, Scratch(d, nullptr).used)) != FASTGL_OK) return st;
+    const Scratch o(d, (char *)ws);
+    hipStream_t s = (hipStream_t)stream;
+    const Cut cut = d.scores_cut();
+    int64_t slots = 0;
+    for (int64_t n0 = 0; n0 < N; n0 += d.piece()) {
+        const int64_t n = N - n0 < d.piece() ? N - n0 : d.piece();
+        if ((st = pack(d, o, H, W, label, n0, n, d.pack_h && n0 == 0, d.pack_w, s)) != FASTGL_OK) return st;
+        LossTileArgs g = scores_of(d, o, H, W, b, label, n0, n);
+        g.stats = o.stats + 2 * slots * M;
+        g.picked = o.picked;
+        if ((st = launch<kScores, false>(g, cut, d.bf16, s, "fastgl_loss_fwd")) != FASTGL_OK) return st;
+        slots += ceil_div(n, Shape::wave_cols(cut));
+    }
+    int lg = 0;
+    while (lg < 5 && ((int64_t)1 << lg) < M) ++lg;
+    hipLaunchKernelGGL(k_loss_join, dim3((unsigned)ceil_div(M, (int64_t)1 << lg)), dim3(kBlock), 0, s, (const float *)o.stats, slots, (const float *)o.picked,
+                       label, M, N, lg, loss, lse);
+    FASTGL_LAUNCH_CHECK("fastgl_loss_fwd (rows)");
+    return FASTGL_OK;
+}
+
+fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label,
+                              const float *lse, const float *dloss, int64_t M, int64_t K, int64_t N, void *dH, void *dW, float *db,
+                              void *ws, size_t ws_bytes, void *stream)
+{
+    fastgl_status st = check(dtype, M, K, N);
+    if (st != FASTGL_OK) return st;
+    const bool want_h = dH && M > 0 && K > 0, want_w = dW && K > 0 && N > 0, want_b = db && N > 0;
+    if (!want_h && !want_w && !want_b) return FASTGL_OK;
+    if (M > 0 && (!label || !lse || !dloss || (K > 0 && (!H || !W)))) {
+        set_error("H, W, label, lse or dloss is NULL");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    const uintptr_t el = dtype == FASTGL_BF16 ? 2 : 4;
+    if (misaligned_to(H, el) || misaligned_to(W, el) || misaligned_to(b, 4) || misaligned_to(label, 8) || misaligned_to(lse, 4) ||
+        misaligned_to(dloss, 4) || misaligned_to(dH, el) || misaligned_to(dW, el) || misaligned_to(db, 4)) {
+        set_error("buffers must be aligned to their element size");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    hipStream_t s = (hipStream_t)stream;
+    if (M == 0) {                                     // sums without terms
+        if (want_w && (st = launch_no_terms(dtype == FASTGL_BF16, dW, nullptr, K, N, false, s, "fastgl_loss_bwd (dW, M = 0)")) != FASTGL_OK) return st;
+        if (want_b) return launch_no_terms(false, db, nullptr, 1, N, false, s, "fastgl_loss_bwd (db, M = 0)");
+        return FASTGL_OK;
+    }
+    const Shape d(dtype, M, K, N, starts_whole({H, W}), true);
+    if ((st = check_workspace(ws, ws_bytes, Scratch(d, nullptr).used)) != FASTGL_OK) return st;
+    const Scratch o(d, (char *)ws);
+    const Cut scores = d.scores_cut(), rows = d.rows_cut(), weights = d.weights_cut();
+    for (int64_t n0 = 0; n0 < N; n0 += d.piece()) {
+        const int64_t n = N - n0 < d.piece() ? N - n0 : d.piece();
+        if ((st = pack(d, o, H, W, label, n0, n, n0 == 0, d.pack_w, s)) != FASTGL_OK) return st;
+        LossTileArgs z = scores_of(d, o, H, W, b, label, n0, n);
+        z.lse = lse;
+        z.dloss = dloss;
+        z.dz = o.dz; z.dz_plane = d.z_plane(); z.dz_ld = d.z_ld(); z.dz_block = d.z_block();
+        z.db = want_b ? o.db : nullptr;
+        if ((st = launch<kGradient, false>(z, scores, d.bf16, s, "fastgl_loss_bwd (dZ)")) != FASTGL_OK) return st;
+        LossSumArgs sum = {};                         // the sums at the end of the piece
+        if (want_b) {
+            sum.db_part = o.db;
+            sum.db = db + n0;
+            sum.db_rows = (int32_t)d.db_rows(); sum.db_cols = (int32_t)n;
+        }
+        if (want_h) {
+            LossTileArgs g = {};
+            g.a[0] = o.dz;
+            g.b[0] = d.pack_w ? o.w : (const uint16_t *)W + n0;
+            g.a_plane = d.z_plane(); g.lda = d.z_ld();
+            g.a_blocks = d.blocks() ? d.z_block() : 0;
+            g.ldb = z.ldb; g.b_plane = z.b_plane;
+            g.R = M; g.C = K; g.Kc = n;
+            g.pairs = z.pairs; g.groups = 1;
+            g.planes_a = z.planes_a; g.planes_b = z.planes_b;
+            g.out[0] = dH;
+            g.part = o.part_h;
+            g.add = n0 > 0;
+            st = d.parts_h() ? launch<kRowsAdd, true>(g, rows, d.bf16, s, "fastgl_loss_bwd (dH)") : launch<kRows, false>(g, rows, d.bf16, s, "fastgl_loss_bwd (dH)");
+            if (st != FASTGL_OK) return st;
+        }
+        if (want_w) {
+            LossTileArgs g = {};
+            g.a[0] = o.h;
+            g.b[0] = o.dz;
+            g.a_plane = M * d.ldk; g.lda = d.ldk;
+            g.b_plane = d.z_plane(); g.ldb = d.z_ld();
+            g.b_blocks = d.blocks() ? d.z_block() : 0;
+            g.R = K; g.C = n; g.Kc = M;
+            g.pairs = z.pairs; g.groups = 1;
+            g.planes_a = z.planes_a; g.planes_b = z.planes_b;
+            g.out[0] = static_cast<char *>(dW) + n0 * (int64_t)el;
+            g.ldo = N;
+            g.part = o.part_w;
+            st = weights.slabs > 1 ? launch<kWeightsOne, true>(g, weights, d.bf16, s, "fastgl_loss_bwd (dW)")
+                                   : launch<kWeightsOne, false>(g, weights, d.bf16, s, "fastgl_loss_bwd (dW)");
+            if (st != FASTGL_OK) return st;
+            if (weights.slabs > 1) {
+                sum.part = o.part_w;
+                sum.out = g.out[0];
+                sum.R = K; sum.C = n; sum.ldo = N;
+                sum.slabs = (int32_t)weights.slabs;
+            }
+        }
+        if ((sum.part || sum.db_part) && (st = launch_sum(sum, d.bf16, s, "fastgl_loss_bwd (sums)")) != FASTGL_OK) return st;
+    }
+    if (!want_h || !d.parts_h()) return FASTGL_OK;
+    LossSumArgs sum = {};
+    sum.part = o.part_h;
+    sum.out = dH;
+    sum.R = M; sum.C = K; sum.ldo = K;
+    sum.slabs = (int32_t)rows.slabs;
+    return launch_sum(sum, d.bf16, s, "fastgl_loss_bwd (dH, sums)");
+}
+
+}  // extern "C"

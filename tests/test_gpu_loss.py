@@ -1,0 +1,239 @@
+"""A classifier's loss on the GPU against its plain 64-bit form (tests/loss_ref.py)."""
+import pytest
+import torch
+
+import rows_ref
+from loss_ref import HALF, Loss
+from paper_2409_14939_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DTYPES = rows_ref.DTYPES
+SENTINEL = -776.0
+# rows, inputs, classes: one of everything; multiples of 8, 32 and tiles, and beyond them; classes of one and of several tiles
+SHAPES = [(1, 1, 1), (1, 256, 47), (2, 5, 9), (3, 64, 64), (7, 100, 47), (17, 130, 200), (33, 7, 5), (64, 48, 128), (65, 72, 129), (100, 63, 65), (129, 200, 48),
+          (255, 256, 256), (257, 100, 257), (300, 602, 172), (513, 48, 700), (1000, 256, 1003), (2100, 520, 264), (40, 33, 5000), (1, 64, 20_000), (5000, 16, 47),
+          (3000, 8, 2)]
+
+
+def inputs(M, K, N, dtype, seed=0, bias=True, size=1.0):
+    g = torch.Generator().manual_seed(seed)
+    make = lambda *s: torch.randn(*s, generator=g)
+    t = DTYPES[dtype]
+    H, W = (size * make(M, K)).to(t), (2.0 * make(K, N) / max(K, 1) ** 0.5).to(t)
+    label = torch.randint(0, N, (M,), generator=g)
+    if M > 2:
+        label[torch.rand(M, generator=g) < 0.2] = -1
+    return H, W, 0.5 * make(N) if bias else None, label, (0.5 + torch.rand(M, generator=g)) / M
+
+
+def cuda(*xs):
+    return [None if x is None else x.cuda() for x in xs]
+
+
+def within(got, want, bound, t, what):
+    got, want = got.double().cpu(), want.double()
+    assert got.shape == want.shape, what
+    same = (got == want) | (got.isnan() & want.isnan())
+    off = torch.where(same, 0.0, (got - want).abs())
+    bad = ~((off <= bound + HALF[t] * (want.abs() + bound)) | same)
+    assert not bool(bad.any()), (what, int(bad.sum()), off[bad][:4], bound[bad][:4], want[bad][:4], got[bad][:4])
+
+
+def check(H, W, b, label, dloss, shift=0):
+    ref = Loss(H, W, b, label).backward(dloss)
+    t, (M, K), N = H.dtype, H.shape, W.shape[1]
+    bufs = [rows_ref.guarded(s, x, SENTINEL, shift) for s, x in (((M,), torch.float32), ((M,), torch.float32), ((M, K), t), ((K, N), t), ((N,), torch.float32))]
+    loss, lse, dH, dW, db = (x for _, x in bufs)
+    H, W = (rows_ref.shifted(x, shift) for x in (H, W))         # starts that are multiples of 16 bytes and not
+    b, label, dloss = cuda(b, label, dloss)
+    B.fastgl_loss_fwd(H, W, b, label, loss=loss, lse=lse)
+    B.fastgl_loss_bwd(H, W, b, label, lse, dloss, dH=dH, dW=dW, db=db)
+    torch.cuda.synchronize()
+    within(loss, ref.loss, ref.off_loss, torch.float32, "loss")
+    within(lse, ref.lse, ref.off_lse, torch.float32, "lse")
+    within(dH, ref.dH, ref.off_dH, t, "dH")
+    within(dW, ref.dW, ref.off_dW, t, "dW")
+    within(db, ref.db, ref.off_db, torch.float32, "db")
+    assert all(rows_ref.bands_intact(buf, inner, SENTINEL) for buf, inner in bufs)
+    return loss, lse, dH, dW, db
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", SHAPES)
+def test_sizes(M, K, N, dtype):
+    check(*inputs(M, K, N, dtype, seed=M))
+    check(*inputs(M, K, N, dtype, seed=N, bias=False), shift=1)
+
+
+@pytest.mark.parametrize("dtype,M,K,N", [("bf16", 40_000, 16, 8000), ("bf16", 40_000, 9, 7001), ("f32", 40_000, 8, 3000), ("f32", 300, 60_000, 1300),
+                                         ("bf16", 520, 200_000, 300 + 1)])
+def test_pieces_of_the_classes(dtype, M, K, N):
+    """dZ, or packed weights, of more than one piece; the reference on the GPU."""
+    H, W, b, label, dloss = cuda(*inputs(M, K, N, dtype))
+    size = B.fastgl_loss_bwd_workspace_bytes(dtype, M, K, N, True)
+    planes = 1 if dtype == "bf16" else 3
+    assert size < 2 * planes * (M * N + K * N + M * K) + 4 * M * K
+    ref = Loss(H, W, b, label).backward(dloss)
+    loss, lse = B.fastgl_loss_fwd(H, W, b, label)
+    dH, dW, db = B.fastgl_loss_bwd(H, W, b, label, lse, dloss)
+    for got, want, off, t, what in ((loss, ref.loss, ref.off_loss, torch.float32, "loss"), (lse, ref.lse, ref.off_lse, torch.float32, "lse"),
+                                    (dH, ref.dH, ref.off_dH, H.dtype, "dH"), (dW, ref.dW, ref.off_dW, H.dtype, "dW"), (db, ref.db, ref.off_db, torch.float32, "db")):
+        within(got, want.cpu(), off.cpu(), t, what)
+    only = B.fastgl_loss_bwd(H, W, b, label, lse, dloss, want=("dH",))
+    assert torch.equal(only[0], dH) and only[1] is None and only[2] is None
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(70, 40, 47), (300, 64, 600)])
+def test_rows_without_a_label(M, K, N, dtype):
+    """What such rows and their dloss hold reaches nothing, NaN and infinities included; a batch without any label has gradients of 0."""
+    H, W, b, label, dloss = inputs(M, K, N, dtype)
+    label[::3] = -1
+    label[1::6] = -100
+    out = label < 0
+    clean = check(H, W, b, label, dloss)
+    H[out], dloss[out] = float("nan"), float("inf")
+    H[0, 1] = -float("inf")
+    h, w, bb, y, g = cuda(H, W, b, label, dloss)
+    loss, lse = B.fastgl_loss_fwd(h, w, bb, y)
+    got = (loss, *B.fastgl_loss_bwd(h, w, bb, y, lse, g))
+    for a, b_ in zip((clean[0], *clean[2:]), got):
+        assert torch.equal(a, b_)
+    assert not bool(loss.cpu()[out].any()) and not bool(got[1].cpu()[out].any())
+    none = torch.full_like(y, -1)
+    loss, lse = B.fastgl_loss_fwd(h, w, bb, none)
+    assert not any(bool(x.any()) for x in (loss, *B.fastgl_loss_bwd(h, w, bb, none, lse, g)))
+
+
+@pytest.mark.parametrize("N", [47, 300])
+def test_labels_that_are_no_class(N):
+    H, W, b, label, dloss = cuda(*inputs(90, 24, N, "f32"))
+    label[5], label[77] = N, 2 ** 40
+    bad = torch.zeros(90, dtype=torch.bool, device="cuda")
+    bad[[5, 77]] = True
+    loss, lse = B.fastgl_loss_fwd(H, W, b, label)
+    dH, dW, db = B.fastgl_loss_bwd(H, W, b, label, lse, dloss)
+    assert torch.equal(loss.isnan(), bad) and torch.equal(dH.isnan().any(1), bad) and bool(torch.isfinite(lse).all())
+    assert bool(dW.isnan().all()) and bool(db.isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [47, 300])
+def test_classes_that_are_ruled_out_and_scores_that_are_not_finite(N, dtype):
+    H, W, b, label, dloss = inputs(80, 32, N, dtype)
+    b[::4] = -float("inf")
+    label = torch.where(label % 4 == 0, label + 1, label)                  # of classes that remain
+    label[label >= N] = 1
+    _, _, dH, dW, db = check(H, W, b, label, dloss)
+    assert not bool(db[::4].any()) and not bool(dW[:, ::4].any())
+    H[7] = float("nan")
+    label[7] = 1
+    h, w, bb, y, g = cuda(H, W, b, label, dloss)
+    loss, lse = B.fastgl_loss_fwd(h, w, bb, y)
+    got = B.fastgl_loss_bwd(h, w, bb, y, lse, g)[0]
+    others = torch.arange(80, device="cuda") != 7
+    assert bool(loss[7].isnan()) and bool(got[7].isnan().all()) and bool(torch.isfinite(loss[others]).all()) and torch.equal(got[others], dH[others])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e-3, 30.0, 500.0])
+def test_sizes_of_scores(size, dtype):
+    for M, K, N in ((50, 40, 47), (200, 64, 700)):
+        check(*inputs(M, K, N, dtype, size=size))
+
+
+def test_empty_calls():
+    for dtype in ("f32", "bf16"):
+        t = DTYPES[dtype]
+        H, W = torch.zeros(0, 5, dtype=t, device="cuda"), torch.ones(5, 7, dtype=t, device="cuda")
+        y, b, g = torch.zeros(0, dtype=torch.int64, device="cuda"), torch.zeros(7, device="cuda"), torch.zeros(0, device="cuda")
+        loss, lse = B.fastgl_loss_fwd(H, W, b, y)
+        dH, dW, db = B.fastgl_loss_bwd(H, W, b, y, lse, g, dW=torch.full_like(W, 3.0), db=torch.full_like(b, 3.0))
+        assert loss.shape == (0,) and dH.shape == (0, 5) and not bool(dW.any()) and not bool(db.any())
+        # nothing to contract: the scores are the bias
+        H, W, y, g = torch.zeros(3, 0, dtype=t, device="cuda"), torch.zeros(0, 4, dtype=t, device="cuda"), torch.tensor([0, 3, -1]).cuda(), torch.ones(3, device="cuda")
+        b = torch.tensor([0.0, 1.0, 2.0, 3.0]).cuda()
+        loss, lse = B.fastgl_loss_fwd(H, W, b, y)
+        want = torch.logsumexp(b, 0)
+        torch.testing.assert_close(loss, torch.stack((want, want - 3, 0 * want)), rtol=1e-6, atol=1e-6)
+        dH, dW, db = B.fastgl_loss_bwd(H, W, b, y, lse, g)
+        p = torch.softmax(b, 0)
+        torch.testing.assert_close(db, 2 * p - torch.tensor([1.0, 0, 0, 1]).cuda(), rtol=1e-6, atol=1e-6)
+        assert dH.shape == (3, 0) and dW.shape == (0, 4)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(65, 40, 47), (300, 64, 600)])
+def test_parts_of_the_gradient_and_again(M, K, N, dtype):
+    H, W, b, label, dloss = cuda(*inputs(M, K, N, dtype))
+    loss, lse = B.fastgl_loss_fwd(H, W, b, label)
+    assert torch.equal(B.fastgl_loss_fwd(H, W, b, label, want_lse=False)[0], loss)
+    whole = B.fastgl_loss_bwd(H, W, b, label, lse, dloss)
+    for i, name in enumerate(("dH", "dW", "db")):
+        got = B.fastgl_loss_bwd(H, W, b, label, lse, dloss, want=(name,))
+        assert [x is not None for x in got] == [j == i for j in range(3)] and torch.equal(got[i], whole[i])
+
+
+@pytest.mark.parametrize("M,K,N", [(40, 12, 19), (150, 30, 300)])
+def test_gradient_against_differences(M, K, N):
+    """Along the gradient itself: the change of the kernels' own weighted loss, in float32."""
+    H, W, b, label, dloss = cuda(*inputs(M, K, N, "f32"))
+    _, lse = B.fastgl_loss_fwd(H, W, b, label)
+    grads = B.fastgl_loss_bwd(H, W, b, label, lse, dloss)
+    for name, x, grad in (("H", H, grads[0]), ("W", W, grads[1]), ("b", b, grads[2])):
+        keep, way = x.clone(), grad.double() / grad.double().norm()
+        values = []
+        for sign in (1, -1):
+            x.copy_(keep.double() + sign * 0.02 * way)
+            values.append((B.fastgl_loss_fwd(H, W, b, label)[0].double() * dloss.double()).sum().item())
+        x.copy_(keep)
+        # the third order of a central difference of 0.02 in all, and the float32 noise of a loss of a few units over it
+        assert abs((values[0] - values[1]) / 0.04 - grad.double().norm().item()) < 2e-3 * grad.double().norm().item() + 3e-5, name
+
+
+def test_a_captured_step_replayed_with_other_inputs():
+    for dtype, M, K, N in (("bf16", 500, 72, 47), ("f32", 300, 40, 900)):
+        first, second = (cuda(*inputs(M, K, N, dtype, seed=s)) for s in (1, 2))
+        ws = torch.empty(max(B.fastgl_loss_bwd_workspace_bytes(dtype, M, K, N), B.fastgl_loss_fwd_workspace_bytes(dtype, M, K, N)), dtype=torch.uint8,
+                         device="cuda")
+
+        def step(H, W, b, label, dloss, **kw):
+            loss, lse = B.fastgl_loss_fwd(H, W, b, label, **kw)
+            return [loss, lse, *B.fastgl_loss_bwd(H, W, b, label, lse, dloss, **kw)]
+        eager = [step(*first), step(*second)]
+        held = [x.clone() for x in first]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            step(*held, workspace=ws)
+            side.synchronize()
+            with torch.cuda.graph(graph, stream=side):
+                got = step(*held, workspace=ws)
+        torch.cuda.current_stream().wait_stream(side)
+        for n in (0, 1, 0, 1):
+            for to, x in zip(held, (first, second)[n]):
+                to.copy_(x)
+            for t in got:
+                t.zero_()
+            ws.random_(0, 255)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, eager[n])), (dtype, n)
+
+
+def test_what_the_binding_refuses():
+    H, W, b, label, dloss = cuda(*inputs(20, 8, 5, "f32"))
+    _, lse = B.fastgl_loss_fwd(H, W, b, label)
+    for kind, args in ((TypeError, (H.double(), W, b, label)), (TypeError, (H, W.bfloat16(), b, label)), (TypeError, (H, W, b.double(), label)),
+                       (TypeError, (H, W, b, label.int())), (TypeError, (H, W.T.contiguous().T, b, label)), (TypeError, (H.cpu(), W, b, label)),
+                       (ValueError, (H, W[:-1], b, label)), (ValueError, (H, W, b[:-1], label)), (ValueError, (H, W, b, label[:-1])),
+                       (ValueError, (H[0], W, b, label))):
+        with pytest.raises(kind):
+            B.fastgl_loss_fwd(*args)
+    for kw in (dict(lse=lse[:-1]), dict(dloss=dloss[:-1]), dict(dH=H[:-1]), dict(dW=W[:-1]), dict(db=b[:-1])):
+        with pytest.raises(ValueError):
+            B.fastgl_loss_bwd(*(H, W, b, label), **{**dict(lse=lse, dloss=dloss), **kw})
+    with pytest.raises(B.FastglError, match="without classes"):
+        B.fastgl_loss_fwd(H, W[:, :0].contiguous(), None, label)
