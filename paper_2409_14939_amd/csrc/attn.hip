@@ -5,7 +5,7 @@
 //             k_attn_dkv (rows of the transposed block: dK, dV; ds of every edge where dbias is wanted) -> [k_attn_join]
 //             k_attn_dbias -> k_attn_dbias_sum
 //
-// A group of lanes has one row and one head, 16 bytes of the head a lane whatever its width and alignment: the last lane's piece
+// A group of lanes has one row and one head, one or two pieces of 16 bytes of the head a lane whatever its width and alignment: the last piece
 // ends with the head, and what it has in common with the one before counts once in a dot product (it is 0 in the row's own operand) and is
 // the same in both lanes' sums.  A group walks its row's edges some at a time: the dot products are joined across its lanes, the running
 // maximum is raised once for all of them, and the sums stay in registers.
@@ -21,32 +21,12 @@ namespace fastgl {
 namespace {
 
 constexpr float kLog2e = 1.44269504089f, kLn2 = 0.69314718056f;
-constexpr int kAttnUnroll = 4;            // edges a group has under way
+constexpr int kSegment = 16;              // steps that a group takes where a neighbour has more
 constexpr int kBiasBlocks = 1024;         // workgroups of k_attn_dbias
+constexpr int kJoin = 1024;               // threads of a workgroup that joins chunks
 constexpr int kBiasTile = 64;             // buckets of one of its passes
 
 // ------------------------------------------------------------------ lanes and pieces
-template <bool BF16, bool WHOLE>
-struct Piece;
-
-template <>
-struct Piece<false, true> {
-    typedef float elem;
-    static constexpr int N = 4;
-    Words<4>::x4 w;
-    __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const Words<4>::x4 *>(p); }
-    __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i]); }
-    __device__ __forceinline__ void keep(bool on)
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = on ? w[i] : 0u;
-    }
-    __device__ static __forceinline__ void store(float *p, const float (&v)[4])
-    {
-        *reinterpret_cast<Words<4>::x4 *>(p) = Words<4>::x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-    }
-};
-
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -54,45 +34,84 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
-template <>
-struct Piece<true, true> {
-    typedef uint16_t elem;
-    static constexpr int N = 8;
-    Words<2>::x4 w;
-    __device__ __forceinline__ void load(const uint16_t *p) { w = *reinterpret_cast<const Words<2>::x4 *>(p); }
-    __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16); }
+// What a lane holds of a head: PC pieces of 16 bytes, `lanes` pieces apart; PC 0: one element, for heads narrower than 16 bytes.
+template <bool BF16, int PC>
+struct Piece {
+    typedef typename std::conditional<BF16, uint16_t, float>::type elem;
+    typedef typename Words<BF16 ? 2 : 4>::x4 word;
+    static constexpr int ES = sizeof(elem), CE = 16 / ES, PIECES = PC, N = PC * CE;
+    word w[PC];
+    __device__ __forceinline__ void load(const char *p, int c) { w[c] = *reinterpret_cast<const word *>(p); }
+    __device__ __forceinline__ float get(int i) const
+    {
+        const uint32_t x = w[i / CE][i % CE * ES / 4];
+        if constexpr (BF16) return __uint_as_float(i & 1 ? x & 0xFFFF0000u : x << 16);
+        else return __uint_as_float(x);
+    }
     __device__ __forceinline__ void keep(bool on)
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = on ? w[i] : 0u;
+        for (int c = 0; c < PC; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[c][i] = on ? w[c][i] : 0u;
     }
-    __device__ static __forceinline__ void store(uint16_t *p, const float (&v)[8])
+    // Without the first `skip` elements of piece c.
+    __device__ __forceinline__ void cut(int c, int skip)
     {
-        *reinterpret_cast<Words<2>::x4 *>(p) = Words<2>::x4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (BF16) w[c][i] &= 2 * i >= skip ? 0xFFFFFFFFu : 2 * i + 1 >= skip ? 0xFFFF0000u : 0u;
+            else w[c][i] = i >= skip ? w[c][i] : 0u;
+        }
+    }
+    // The sum of products in fp32: of bf16 two at a time, exact.
+    __device__ __forceinline__ float dot(const Piece &o) const
+    {
+        float d = 0.f;
+#pragma unroll
+        for (int c = 0; c < PC; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (BF16) {
+                    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+                    const uint32_t x = w[c][i], y = o.w[c][i];
+                    d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), __builtin_bit_cast(bf16x2, y), d, false);
+                } else
+                    d = fmaf(__uint_as_float(w[c][i]), __uint_as_float(o.w[c][i]), d);
+            }
+        return d;
+    }
+    __device__ static __forceinline__ void store(char *p, int c, const float (&v)[N])
+    {
+        word o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (BF16) o[i] = pack2(v[c * CE + 2 * i], v[c * CE + 2 * i + 1]);
+            else o[i] = __float_as_uint(v[c * CE + i]);
+        }
+        *reinterpret_cast<word *>(p) = o;
     }
 };
 
-// Heads narrower than 16 bytes: an element a lane.
-template <>
-struct Piece<false, false> {
-    typedef float elem;
-    static constexpr int N = 1;
-    float w;
-    __device__ __forceinline__ void load(const float *p) { w = *p; }
-    __device__ __forceinline__ float get(int) const { return w; }
-    __device__ __forceinline__ void keep(bool on) { w = on ? w : 0.f; }
-    __device__ static __forceinline__ void store(float *p, const float (&v)[1]) { *p = v[0]; }
-};
-
-template <>
-struct Piece<true, false> {
-    typedef uint16_t elem;
-    static constexpr int N = 1;
-    uint32_t w;
-    __device__ __forceinline__ void load(const uint16_t *p) { w = *p; }
-    __device__ __forceinline__ float get(int) const { return __uint_as_float(w << 16); }
-    __device__ __forceinline__ void keep(bool on) { w = on ? w : 0u; }
-    __device__ static __forceinline__ void store(uint16_t *p, const float (&v)[1]) { *p = __builtin_bit_cast(uint16_t, (__bf16)v[0]); }
+template <bool BF16>
+struct Piece<BF16, 0> {
+    typedef typename std::conditional<BF16, uint16_t, float>::type elem;
+    static constexpr int ES = sizeof(elem), CE = 1, PIECES = 1, N = 1;
+    float x;
+    __device__ __forceinline__ void load(const char *p, int)
+    {
+        if constexpr (BF16) x = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(p) << 16);
+        else x = *reinterpret_cast<const float *>(p);
+    }
+    __device__ __forceinline__ float get(int) const { return x; }
+    __device__ __forceinline__ void keep(bool on) { x = on ? x : 0.f; }
+    __device__ __forceinline__ void cut(int, int skip) { x = skip > 0 ? 0.f : x; }
+    __device__ __forceinline__ float dot(const Piece &o) const { return x * o.x; }
+    __device__ static __forceinline__ void store(char *p, int, const float (&v)[1])
+    {
+        if constexpr (BF16) *reinterpret_cast<uint16_t *>(p) = __builtin_bit_cast(uint16_t, (__bf16)v[0]);
+        else *reinterpret_cast<float *>(p) = v[0];
+    }
 };
 
 // exp(x) of a difference of scores, x <= 0: 2^(x log2 e).  Relative error 2^-23 (1 + |x|).
@@ -118,20 +137,25 @@ __device__ __forceinline__ float over_lanes(float v)
     return v;
 }
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 struct AttnArgs {
     const int32_t *ptr, *col;      // rows of the block, or of its transpose
-    const int32_t *eid;            // transposed: the edge's number in edge order; NULL: the position is the number
-    const int32_t *bucket;         // or NULL
+    const int32_t *bucket;         // by position in col, or NULL
     const float *bias;             // or NULL
     const void *Q, *K, *V, *dO;
     int64_t ldq, ldk, ldv, lddo;
-    typedef float f4 __attribute__((ext_vector_type(4)));
-    f4 *stats;                     // [num_dst][heads]: maximum, 1 / sum, sum p dp of a row
+    f32x4 *stats;                  // [num_dst][heads]: maximum, 1 / sum, sum p dp of a row
     void *O, *dQ, *dK, *dV;        // or NULL
     int64_t ldo, lddq, lddk, lddv;
     float *lse;                    // [rows][heads], or NULL
     float *ds;                     // [position][heads], or NULL
-    int64_t units;                 // rows x heads (transposed: x key heads)
+    const int32_t *bucket_from, *eid;      // dQ: the transposed block's buckets are brought into its order on the way: bucket_to[i] =
+    int32_t *bucket_to;                    // bucket_from[eid[i]] for so many edges
+    int64_t edges;
+    int64_t units;                 // rows (dealt: to a multiple of 512) x heads (transposed: x key heads)
+    int64_t rows;
+    int32_t dealt;                 // rows are taken 64 apart
     uint64_t heads_inv;            // ceil(2^64 / heads of a unit), 0 for one
     uint32_t shared_inv;           // ceil(2^32 / shared), 0 for one: exact for 2^20 query heads of edges at most 4096 of which share
     uint32_t buckets;              // edges of this bucket and above are left out
@@ -139,89 +163,82 @@ struct AttnArgs {
     float scale;
     int32_t long_thr;              // rows of more edges are taken in chunks
     const int32_t *long_rows, *chunk_ptr, *n_long, *n_chunks;
+    int32_t chunk_waves;           // wavefronts that take chunks
     float *part, *part_more;       // sums of chunks: [chunk][unit head][width], and what else a pass has
-    int32_t chunk_blocks;          // workgroups that take chunks, before those of the rows
     int64_t part_stride;           // between the two arrays of `part` that a backward pass has
-};
-
-// Where a lane is: its group's place in the workgroup and its piece of a head.
-template <class P, int LG, bool WHOLE>
-struct Where {
-    int l, g, off, skip;
-    bool active;
-    __device__ __forceinline__ Where(int width)
-    {
-        l = threadIdx.x & ((1 << LG) - 1);
-        g = threadIdx.x >> LG;
-        const int at = l * P::N, last = width - P::N;
-        off = at < last ? at : last;
-        skip = at - off;                              // elements that the lane before has too; all of them beyond the head
-        active = at < width;
-    }
-    // This row's own operand, times `by`; 0 where another lane has it.
-    __device__ __forceinline__ void own(const typename P::elem *p, float by, float (&v)[P::N]) const
-    {
-        P x;
-        x.load(p + off);
-#pragma unroll
-        for (int i = 0; i < P::N; ++i) v[i] = i >= skip ? x.get(i) * by : 0.f;
-    }
 };
 
 __device__ __forceinline__ uint64_t over(uint64_t n, uint64_t inv) { return inv ? __umul64hi(n, inv) : n; }
 __device__ __forceinline__ uint32_t over(uint32_t n, uint32_t inv) { return inv ? __umulhi(n, inv) : n; }
 
-// The chunk's row and its edges.
-struct ChunkOf {
-    int row, beg, end;
-    __device__ __forceinline__ ChunkOf(const AttnArgs &a, int chunk, int n_long)
+// Where a lane is: its group's place in the wavefront and its pieces of a head.  A row's place in an array is a 32-bit offset where the
+// array is NEAR: fewer instructions, which is what bounds the walks (63 against 81 of 128-byte heads of bf16 an edge and lane).
+template <class P, int LG, bool NEAR>
+struct Where {
+    int l, g, off[P::PIECES], skip[P::PIECES];        // off: bytes
+    bool active[P::PIECES];
+    __device__ __forceinline__ Where(int width)
     {
-        int lo = 0, hi = n_long;                      // chunk_ptr[lo] <= chunk < chunk_ptr[hi]
-        while (hi - lo > 1) {
-            const int mid = lo + ((hi - lo) >> 1);
-            if (a.chunk_ptr[mid] <= chunk) lo = mid; else hi = mid;
+        const int lane = threadIdx.x & (kWave - 1);
+        l = lane & ((1 << LG) - 1);
+        g = lane >> LG;
+#pragma unroll
+        for (int c = 0; c < P::PIECES; ++c) {
+            const int at = (l + (c << LG)) * P::CE, last = width - P::CE, from = at < last ? at : last;
+            off[c] = from * P::ES;
+            skip[c] = at - from;                      // elements that the piece before has too; all of them beyond the head
+            active[c] = at < width;
         }
-        row = a.long_rows[lo];
-        beg = a.ptr[row] + (chunk - a.chunk_ptr[lo]) * kLongChunk;
-        const int last = a.ptr[row + 1];
-        end = beg + kLongChunk < last ? beg + kLongChunk : last;
+    }
+    __device__ __forceinline__ void load(P &x, const void *base, int64_t row, int64_t ld, int col) const
+    {
+#pragma unroll
+        for (int c = 0; c < P::PIECES; ++c) {
+            if constexpr (NEAR) x.load(static_cast<const char *>(base) + ((uint32_t)row * (uint32_t)(ld * P::ES) + (uint32_t)(col * P::ES + off[c])), c);
+            else x.load(static_cast<const char *>(base) + (row * ld + col) * P::ES + off[c], c);
+        }
+    }
+    // A row's own operand without what another piece has too.
+    __device__ __forceinline__ void cut(P &x) const
+    {
+#pragma unroll
+        for (int c = 0; c < P::PIECES; ++c) x.cut(c, skip[c]);
+    }
+    __device__ __forceinline__ void store(void *base, int64_t row, int64_t ld, int col, const float (&v)[P::N]) const
+    {
+#pragma unroll
+        for (int c = 0; c < P::PIECES; ++c)
+            if (active[c]) P::store(static_cast<char *>(base) + (row * ld + col) * P::ES + off[c], c, v);
+    }
+    __device__ __forceinline__ void store_sums(float *base, int64_t at, const float (&v)[P::N]) const       // of a chunk
+    {
+#pragma unroll
+        for (int c = 0; c < P::PIECES; ++c)
+            if (active[c]) {
+#pragma unroll
+                for (int i = 0; i < P::CE; ++i) base[at + off[c] / P::ES + i] = v[c * P::CE + i];
+            }
     }
 };
 
-// body(row, unit head, beg, end, chunk or -1) for the units of this launch: a group takes one row, or chunks of long rows in turn.
-template <int LG, class BODY>
-__device__ __forceinline__ void for_units(const AttnArgs &a, int g, BODY body)
-{
-    constexpr int GROUPS = kBlock >> LG;
-    if ((int)blockIdx.x < a.chunk_blocks) {
-        const int n_long = *a.n_long;
-        const int64_t total = (int64_t)*a.n_chunks * a.unit_heads;
-        for (int64_t unit = (int64_t)blockIdx.x * GROUPS + g; unit < total; unit += (int64_t)a.chunk_blocks * GROUPS) {
-            const int chunk = (int)over((uint64_t)unit, a.heads_inv), h = (int)(unit - (int64_t)chunk * a.unit_heads);
-            const ChunkOf c(a, chunk, n_long);
-            body(c.row, h, c.beg, c.end, (int64_t)chunk);
-        }
-        return;
-    }
-    const int64_t unit = (int64_t)(blockIdx.x - a.chunk_blocks) * GROUPS + g;
-    if (unit >= a.units) return;
-    const int64_t row = (int64_t)over((uint64_t)unit, a.heads_inv);
-    const int h = (int)(unit - row * a.unit_heads);
-    const int beg = a.ptr[row], end = a.ptr[row + 1];
-    if (end - beg > a.long_thr) return;
-    body(row, h, beg, end, (int64_t)-1);
-}
-
-// Columns (and buckets) of the next edges, the last of them again beyond the end.
+// The next edges of a row: columns and buckets, the last of them again beyond the end.  Transposed, an edge counts once for each query
+// head that shares the key head: step i is head i % shared of edge i / shared.
+template <bool T, int U>
 struct Ahead {
-    int col[kAttnUnroll], bucket[kAttnUnroll];
-    __device__ __forceinline__ void load(const AttnArgs &a, int e, int end)
+    int col[U], bucket[U], pos[T ? U : 1], head[T ? U : 1];
+    __device__ __forceinline__ void load(const AttnArgs &a, int beg, int i, int steps)
     {
 #pragma unroll
-        for (int j = 0; j < kAttnUnroll; ++j) {
-            const int at = e + j < end ? e + j : end - 1;
-            col[j] = a.col[at];
-            bucket[j] = a.bucket ? a.bucket[at] : 0;
+        for (int j = 0; j < U; ++j) {
+            int at = i + j < steps ? i + j : steps - 1;
+            if constexpr (T) {
+                const int e = (int)over((uint32_t)at, a.shared_inv);
+                head[j] = at - e * a.shared;
+                pos[j] = beg + e;
+                at = e;
+            }
+            col[j] = a.col[beg + at];
+            bucket[j] = a.bucket ? a.bucket[beg + at] : 0;
         }
     }
 };
@@ -234,264 +251,521 @@ __device__ __forceinline__ float bias_of(const AttnArgs &a, int bucket, int h)
     return in ? b : -INFINITY;
 }
 
-// ------------------------------------------------------------------ forward
-template <bool BF16, int LG, bool WHOLE>
-__global__ __launch_bounds__(kBlock) void k_attn_fwd(AttnArgs a)
+// ------------------------------------------------------------------ the walk
+// ROW has the operands and sums of one row and head (or of a part of its edges), the pass's arithmetic and where its results go.
+//
+// A group takes one row and head, a unit.  Where a unit of the wavefront has more than kSegment steps, all its units' steps are cut into segments of
+// so many, which the groups take in turn, so that nobody waits long for a neighbour's row: segments of one unit lie side by side, their sums are
+// joined across the groups and then with what earlier turns left in LDS.  Chunks of long rows, which the first wavefronts take after their own rows,
+// are units too, as many at a time as give every group a segment.
+//
+// Rows of sources are dealt to the wavefronts 64 apart: those that are neighbours of many often have numbers that lie together.
+template <class ROW>
+__device__ __forceinline__ void walk_units(const AttnArgs &a)
 {
-    typedef Piece<BF16, WHOLE> P;
-    typedef typename P::elem T;
-    constexpr int N = P::N, U = kAttnUnroll;
-    const Where<P, LG, WHOLE> w(a.width);
-    for_units<LG>(a, w.g, [&](int64_t row, int h, int beg, int end, int64_t chunk) __attribute__((always_inline)) {
-        const int hk = (int)over((uint32_t)h, a.shared_inv);
-        const T *K = static_cast<const T *>(a.K) + hk * a.width + w.off, *V = static_cast<const T *>(a.V) + hk * a.width + w.off;
-        float q[N], acc[N], m = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) acc[i] = 0.f;
-        Ahead next;
-        if (beg < end) {
-            next.load(a, beg, end);
-            w.own(static_cast<const T *>(a.Q) + row * a.ldq + h * a.width, a.scale, q);
+    constexpr int LG = ROW::LG, G = kWave >> LG, L = 1 << LG;
+    constexpr bool T = ROW::T;
+    constexpr int U = ROW::UNROLL;
+    __shared__ float kept[kBlock / kWave][ROW::VALUES][kWave];
+    ROW r(a);
+    const int lane = threadIdx.x & (kWave - 1), gw = r.w.g, mult = T ? a.shared : 1;
+    const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t wave = (int64_t)blockIdx.x * (kBlock / kWave) + in_block;
+    float (&slots)[ROW::VALUES][kWave] = kept[in_block];
+    // Steps i .. steps of a row, U at a time; the last U / 2 in one of half the size.
+    auto walk = [&](int row, int h, int beg, int i, int steps) __attribute__((always_inline)) {
+        Ahead<T, U> next;
+        if (i < steps) {
+            next.load(a, beg, i, steps);
+            r.own(row, h);
         }
-        for (int e = beg; e < end; e += U) {
-            P k[U], v[U];
-            float s[U];
-#pragma unroll
-            for (int j = 0; j < U; ++j) k[j].load(K + next.col[j] * a.ldk);
-#pragma unroll
-            for (int j = 0; j < U; ++j) v[j].load(V + next.col[j] * a.ldv);
-#pragma unroll
-            for (int j = 0; j < U; ++j) s[j] = e + j < end ? bias_of(a, next.bucket[j], h) : -INFINITY;
-            if (e + U < end) next.load(a, e + U, end);
-            float most = m;
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                float d = 0.f;
-#pragma unroll
-                for (int i = 0; i < N; ++i) d = fmaf(q[i], k[j].get(i), d);
-                d = over_lanes<LG>(d);
-                s[j] = s[j] == -INFINITY ? s[j] : d + s[j];
-                most = fmaxf(most, s[j]);
+        r.start(h);
+        for (; i + U / 2 < steps; i += U) r.template step<U>(next, beg, i, steps);
+        if constexpr (U > 1)
+            if (i < steps) r.template step<U / 2>(next, beg, i, steps);
+    };
+    const int64_t chunks = a.long_rows && wave < a.chunk_waves ? (int64_t)*a.n_chunks * a.unit_heads : 0;
+    constexpr int AT_ONCE = G * kSegment / kLongChunk > 0 ? G * kSegment / kLongChunk : 1;       // chunks
+    for (int64_t at = -1; at < chunks; at = at < 0 ? wave * AT_ONCE : at + (int64_t)a.chunk_waves * AT_ONCE) {
+        int row = 0, h = 0, beg = 0, steps = 0;
+        int64_t chunk = -1;
+        bool on;
+        if (at < 0) {
+            const int64_t unit = wave * G + gw;
+            int64_t to = (int64_t)over((uint64_t)unit, a.heads_inv);
+            h = (int)(unit - to * a.unit_heads);
+            if (T && a.dealt) to = (to & ~(int64_t)511) | ((to & 7) << 6) | ((to >> 3) & 63);
+            on = unit < a.units && to < a.rows;
+            if (on) {
+                row = (int)to;
+                beg = a.ptr[row];
+                const int len = a.ptr[row + 1] - beg;
+                on = len <= a.long_thr;
+                steps = on ? len * mult : 0;
             }
-            const float base = most == -INFINITY ? 0.f : most, old = exp_of(m - base);
-            m = most;
-            sum *= old;
-#pragma unroll
-            for (int i = 0; i < N; ++i) acc[i] *= old;
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const float p = exp_of(s[j] - base);
-                sum += p;
-                v[j].keep(p != 0.f);
-#pragma unroll
-                for (int i = 0; i < N; ++i) acc[i] = fmaf(p, v[j].get(i), acc[i]);
+        } else {
+            chunk = at + gw;
+            on = gw < AT_ONCE && chunk < chunks;
+            if (on) {
+                const int c = (int)over((uint64_t)chunk, a.heads_inv);
+                h = (int)(chunk - (int64_t)c * a.unit_heads);
+                int lo = 0, hi = *a.n_long;           // chunk_ptr[lo] <= c < chunk_ptr[hi]
+                while (hi - lo > 1) {
+                    const int mid = lo + ((hi - lo) >> 1);
+                    if (a.chunk_ptr[mid] <= c) lo = mid; else hi = mid;
+                }
+                row = a.long_rows[lo];
+                beg = a.ptr[row] + (c - a.chunk_ptr[lo]) * kLongChunk;
+                const int last = a.ptr[row + 1];
+                steps = ((beg + kLongChunk < last ? beg + kLongChunk : last) - beg) * mult;
             }
         }
-        if (chunk >= 0) {
-            const int64_t at = chunk * a.unit_heads + h;
-            if (w.active) {
+        const int segments = (steps + kSegment - 1) / kSegment;
+        int upto = segments, total = 1;               // of this group and those before, and of all
+        const bool cut = __any(segments > 1);
+        auto fence = []() __attribute__((always_inline)) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");          // a wavefront's LDS accesses are carried out in order
+            __builtin_amdgcn_wave_barrier();
+        };
+        if (cut) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) a.part[at * a.width + w.off + i] = acc[i];
+            for (int d = L; d < kWave; d <<= 1) {
+                const int before = __shfl_up(upto, d, kWave);
+                upto += lane >= d ? before : 0;
             }
-            if (w.l == 0) {
-                a.part_more[2 * at] = m;
-                a.part_more[2 * at + 1] = sum;
-            }
-            return;
+            total = __builtin_amdgcn_readlane(upto, kWave - 1);
+            r.start(h);
+            r.leave(slots, lane);
+            fence();
         }
+        for (int first = 0; first < total; first += G) {
+            int its_row = row, its_h = h, its_beg = beg, i = 0, its_end = steps, of = gw;
+            const int segment = first + gw;
+            if (cut) {
+                of = 0;                               // the group whose unit it belongs to: the first with upto > segment
+#pragma unroll
+                for (int d = G / 2; d > 0; d >>= 1) of += __shfl(upto, (of + d - 1) * L, kWave) <= segment ? d : 0;
+                const int from = of * L;
+                its_row = __shfl(row, from, kWave);
+                its_h = __shfl(h, from, kWave);
+                its_beg = __shfl(beg, from, kWave);
+                its_end = __shfl(steps, from, kWave);
+                i = (segment - __shfl(upto - segments, from, kWave)) * kSegment;
+                if (i + kSegment < its_end) its_end = i + kSegment;
+                if (segment >= total) i = its_end = 0;
+            }
+            walk(its_row, its_h, its_beg, i, its_end);
+            if (cut) {
+                const bool mine = segment < total;
+                const int id = mine ? of : -1;
+#pragma unroll
+                for (int d = L; d < kWave; d <<= 1) {
+                    const int other = __shfl_down(id, d, kWave);
+                    r.join(d, lane + d < kWave && other == id && mine);
+                }
+                const int before = __shfl_up(id, L, kWave);
+                if (mine && (gw == 0 || before != id)) r.add(slots, of * L + r.w.l);
+                fence();
+            }
+        }
+        if (cut) {
+            r.start(h);
+            r.add_from(slots, lane);
+            fence();
+        }
+        if (!on) continue;
+        if (chunk >= 0) r.store_chunk(chunk);
+        else r.store(row, h);
+    }
+}
+
+// ------------------------------------------------------------------ forward
+template <bool BF16, int PC, int LG_, bool NEAR>
+struct ForwardRow {
+    typedef Piece<BF16, PC> P;
+    static constexpr int LG = LG_, N = P::N, UNROLL = 2;
+    static constexpr bool T = false;
+    const AttnArgs &a;
+    const Where<P, LG, NEAR> w;
+    P q;                           // this row's own operand
+    int head, col;                 // col: of the key head
+    float acc[N], m, sum;
+    __device__ __forceinline__ ForwardRow(const AttnArgs &args) : a(args), w(args.width) {}
+    __device__ __forceinline__ void own(int64_t row, int h) { w.load(q, a.Q, row, a.ldq, h * a.width); }
+    __device__ __forceinline__ void start(int h)
+    {
+        head = h;
+        col = (int)over((uint32_t)h, a.shared_inv) * a.width;
+        w.cut(q);
+        m = -INFINITY;
+        sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < N; ++x) acc[x] = 0.f;
+    }
+    template <int U>
+    __device__ __forceinline__ void step(Ahead<T, UNROLL> &next, int beg, int i, int steps)
+    {
+        P k[U], v[U];
+        float s[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) w.load(k[j], a.K, next.col[j], a.ldk, col);
+#pragma unroll
+        for (int j = 0; j < U; ++j) w.load(v[j], a.V, next.col[j], a.ldv, col);
+#pragma unroll
+        for (int j = 0; j < U; ++j) s[j] = i + j < steps ? bias_of(a, next.bucket[j], head) : -INFINITY;
+        if (i + U < steps) next.load(a, beg, i + U, steps);
+        float most = m;
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const float d = over_lanes<LG>(q.dot(k[j]));
+            s[j] = s[j] == -INFINITY ? s[j] : fmaf(d, a.scale, s[j]);
+            most = fmaxf(most, s[j]);
+        }
+        const float base = most == -INFINITY ? 0.f : most, old = exp_of(m - base);
+        m = most;
+        sum *= old;
+#pragma unroll
+        for (int x = 0; x < N; ++x) acc[x] *= old;
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const float p = exp_of(s[j] - base);
+            sum += p;
+            v[j].keep(p != 0.f);
+#pragma unroll
+            for (int x = 0; x < N; ++x) acc[x] = fmaf(p, v[j].get(x), acc[x]);
+        }
+    }
+    // What another part of the row left: its maximum, sum and sums of rows.
+    __device__ __forceinline__ void merge(float m2, float sum2, const float (&acc2)[N])
+    {
+        const float most = fmaxf(m, m2), base = most == -INFINITY ? 0.f : most, by = exp_of(m - base), by2 = exp_of(m2 - base);
+        m = most;
+        sum = sum * by + sum2 * by2;
+#pragma unroll
+        for (int x = 0; x < N; ++x) acc[x] = acc[x] * by + acc2[x] * by2;
+    }
+    __device__ __forceinline__ void join(int d, bool on)
+    {
+        const float m2 = __shfl_down(m, d, kWave), sum2 = __shfl_down(sum, d, kWave);
+        float acc2[N];
+#pragma unroll
+        for (int x = 0; x < N; ++x) acc2[x] = __shfl_down(acc[x], d, kWave);
+        if (on) merge(m2, sum2, acc2);
+    }
+    static constexpr int VALUES = N + 2;
+    __device__ __forceinline__ void leave(float (&slots)[VALUES][kWave], int at) const
+    {
+        slots[0][at] = m;
+        slots[1][at] = sum;
+#pragma unroll
+        for (int x = 0; x < N; ++x) slots[2 + x][at] = acc[x];
+    }
+    __device__ __forceinline__ void add_from(float (&slots)[VALUES][kWave], int at)
+    {
+        float acc2[N];
+#pragma unroll
+        for (int x = 0; x < N; ++x) acc2[x] = slots[2 + x][at];
+        merge(slots[0][at], slots[1][at], acc2);
+    }
+    __device__ __forceinline__ void add(float (&slots)[VALUES][kWave], int at)
+    {
+        add_from(slots, at);
+        leave(slots, at);
+    }
+    __device__ __forceinline__ void store_chunk(int64_t at)
+    {
+        w.store_sums(a.part, at * a.width, acc);
+        if (w.l == 0) {
+            a.part_more[2 * at] = m;
+            a.part_more[2 * at + 1] = sum;
+        }
+    }
+    __device__ __forceinline__ void store(int64_t row, int h)
+    {
         const float by = sum == 0.f ? 0.f : 1.f / sum;
+        float o[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) acc[i] *= by;
-        if (w.active) P::store(static_cast<T *>(a.O) + row * a.ldo + h * a.width + w.off, acc);
+        for (int x = 0; x < N; ++x) o[x] = acc[x] * by;
+        w.store(a.O, row, a.ldo, h * a.width, o);
         if (a.lse && w.l == 0) a.lse[row * a.heads + h] = sum == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(sum) * kLn2;
-    });
+    }
+};
+
+template <bool BF16, int PC, int LG, bool NEAR>
+__global__ __launch_bounds__(kBlock, 4) void k_attn_fwd(AttnArgs a)
+{
+    walk_units<ForwardRow<BF16, PC, LG, NEAR>>(a);
 }
 
 // ------------------------------------------------------------------ dQ
 // sum p dp comes with the sums of p dp K and p K in one walk: dQ = scale (sum p dp K - (sum p dp) sum p K), all of them of e^(s - maximum)
 // first and divided by its sum at the end.
-template <bool BF16, int LG, bool WHOLE>
-__global__ __launch_bounds__(kBlock) void k_attn_dq(AttnArgs a)
+template <bool BF16, int PC, int LG_, bool NEAR>
+struct QueryRow {
+    typedef Piece<BF16, PC> P;
+    static constexpr int LG = LG_, N = P::N, UNROLL = 2;
+    static constexpr bool T = false;
+    const AttnArgs &a;
+    const Where<P, LG, NEAR> w;
+    P q, g;                        // this row's own operands
+    int head, col;
+    float pk[N], pdk[N], m, sum, delta;
+    __device__ __forceinline__ QueryRow(const AttnArgs &args) : a(args), w(args.width) {}
+    __device__ __forceinline__ void own(int64_t row, int h)
+    {
+        w.load(q, a.Q, row, a.ldq, h * a.width);
+        w.load(g, a.dO, row, a.lddo, h * a.width);
+    }
+    __device__ __forceinline__ void start(int h)
+    {
+        head = h;
+        col = (int)over((uint32_t)h, a.shared_inv) * a.width;
+        w.cut(q);
+        w.cut(g);
+        m = -INFINITY;
+        sum = delta = 0.f;
+#pragma unroll
+        for (int x = 0; x < N; ++x) pk[x] = pdk[x] = 0.f;
+    }
+    template <int U>
+    __device__ __forceinline__ void step(Ahead<T, UNROLL> &next, int beg, int i, int steps)
+    {
+        P k[U], v[U];
+        float s[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) w.load(k[j], a.K, next.col[j], a.ldk, col);
+#pragma unroll
+        for (int j = 0; j < U; ++j) w.load(v[j], a.V, next.col[j], a.ldv, col);
+#pragma unroll
+        for (int j = 0; j < U; ++j) s[j] = i + j < steps ? bias_of(a, next.bucket[j], head) : -INFINITY;
+        if (i + U < steps) next.load(a, beg, i + U, steps);
+        float most = m, dp[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const float d = over_lanes<LG>(q.dot(k[j]));
+            dp[j] = over_lanes<LG>(g.dot(v[j]));
+            s[j] = s[j] == -INFINITY ? s[j] : fmaf(d, a.scale, s[j]);
+            most = fmaxf(most, s[j]);
+        }
+        const float base = most == -INFINITY ? 0.f : most, old = exp_of(m - base);
+        m = most;
+        sum *= old;
+        delta *= old;
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            pk[x] *= old;
+            pdk[x] *= old;
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const float p = exp_of(s[j] - base), pd = p == 0.f ? 0.f : p * dp[j];
+            sum += p;
+            delta += pd;
+            k[j].keep(p != 0.f);
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                pk[x] = fmaf(p, k[j].get(x), pk[x]);
+                pdk[x] = fmaf(pd, k[j].get(x), pdk[x]);
+            }
+        }
+    }
+    __device__ __forceinline__ void merge(const float (&v)[2 * N + 3])
+    {
+        const float most = fmaxf(m, v[0]), base = most == -INFINITY ? 0.f : most, by = exp_of(m - base), by2 = exp_of(v[0] - base);
+        m = most;
+        sum = sum * by + v[1] * by2;
+        delta = delta * by + v[2] * by2;
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            pk[x] = pk[x] * by + v[3 + x] * by2;
+            pdk[x] = pdk[x] * by + v[3 + N + x] * by2;
+        }
+    }
+    __device__ __forceinline__ void join(int d, bool on)
+    {
+        float v[2 * N + 3];
+        v[0] = __shfl_down(m, d, kWave);
+        v[1] = __shfl_down(sum, d, kWave);
+        v[2] = __shfl_down(delta, d, kWave);
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            v[3 + x] = __shfl_down(pk[x], d, kWave);
+            v[3 + N + x] = __shfl_down(pdk[x], d, kWave);
+        }
+        if (on) merge(v);
+    }
+    static constexpr int VALUES = 2 * N + 3;
+    __device__ __forceinline__ void leave(float (&slots)[VALUES][kWave], int at) const
+    {
+        slots[0][at] = m;
+        slots[1][at] = sum;
+        slots[2][at] = delta;
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            slots[3 + x][at] = pk[x];
+            slots[3 + N + x][at] = pdk[x];
+        }
+    }
+    __device__ __forceinline__ void add_from(float (&slots)[VALUES][kWave], int at)
+    {
+        float v[2 * N + 3];
+#pragma unroll
+        for (int x = 0; x < VALUES; ++x) v[x] = slots[x][at];
+        merge(v);
+    }
+    __device__ __forceinline__ void add(float (&slots)[VALUES][kWave], int at)
+    {
+        add_from(slots, at);
+        leave(slots, at);
+    }
+    __device__ __forceinline__ void store_chunk(int64_t at)
+    {
+        w.store_sums(a.part, at * a.width, pdk);
+        w.store_sums(a.part + a.part_stride, at * a.width, pk);
+        if (w.l == 0) reinterpret_cast<f32x4 *>(a.part_more)[at] = f32x4{m, sum, delta, 0.f};
+    }
+    __device__ __forceinline__ void store(int64_t r, int h)
+    {
+        const float by = sum == 0.f ? 0.f : 1.f / sum, d = delta * by;
+        float o[N];
+#pragma unroll
+        for (int x = 0; x < N; ++x) o[x] = a.scale * by * fmaf(-d, pk[x], pdk[x]);
+        if (a.dQ) w.store(a.dQ, r, a.lddq, h * a.width, o);
+        if (w.l == 0) a.stats[r * a.heads + h] = f32x4{m, by, d, 0.f};
+    }
+};
+
+template <bool BF16, int PC, int LG, bool NEAR>
+__global__ __launch_bounds__(kBlock, BF16 ? 3 : 4) void k_attn_dq(AttnArgs a)
 {
-    typedef Piece<BF16, WHOLE> P;
-    typedef typename P::elem T;
-    constexpr int N = P::N, U = kAttnUnroll;
-    const Where<P, LG, WHOLE> w(a.width);
-    for_units<LG>(a, w.g, [&](int64_t row, int h, int beg, int end, int64_t chunk) __attribute__((always_inline)) {
-        const int hk = (int)over((uint32_t)h, a.shared_inv);
-        const T *K = static_cast<const T *>(a.K) + hk * a.width + w.off, *V = static_cast<const T *>(a.V) + hk * a.width + w.off;
-        float q[N], g[N], pk[N], pdk[N], m = -INFINITY, sum = 0.f, delta = 0.f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) pk[i] = pdk[i] = 0.f;
-        Ahead next;
-        if (beg < end) {
-            next.load(a, beg, end);
-            w.own(static_cast<const T *>(a.Q) + row * a.ldq + h * a.width, a.scale, q);
-            w.own(static_cast<const T *>(a.dO) + row * a.lddo + h * a.width, 1.f, g);
-        }
-        for (int e = beg; e < end; e += U) {
-            P k[U], v[U];
-            float s[U];
-#pragma unroll
-            for (int j = 0; j < U; ++j) k[j].load(K + next.col[j] * a.ldk);
-#pragma unroll
-            for (int j = 0; j < U; ++j) v[j].load(V + next.col[j] * a.ldv);
-#pragma unroll
-            for (int j = 0; j < U; ++j) s[j] = e + j < end ? bias_of(a, next.bucket[j], h) : -INFINITY;
-            if (e + U < end) next.load(a, e + U, end);
-            float most = m, dp[U];
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                float d = 0.f;
-                dp[j] = 0.f;
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    d = fmaf(q[i], k[j].get(i), d);
-                    dp[j] = fmaf(g[i], v[j].get(i), dp[j]);
-                }
-                d = over_lanes<LG>(d);
-                dp[j] = over_lanes<LG>(dp[j]);
-                s[j] = s[j] == -INFINITY ? s[j] : d + s[j];
-                most = fmaxf(most, s[j]);
-            }
-            const float base = most == -INFINITY ? 0.f : most, old = exp_of(m - base);
-            m = most;
-            sum *= old;
-            delta *= old;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                pk[i] *= old;
-                pdk[i] *= old;
-            }
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const float p = exp_of(s[j] - base), pd = p == 0.f ? 0.f : p * dp[j];
-                sum += p;
-                delta += pd;
-                k[j].keep(p != 0.f);
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    pk[i] = fmaf(p, k[j].get(i), pk[i]);
-                    pdk[i] = fmaf(pd, k[j].get(i), pdk[i]);
-                }
-            }
-        }
-        if (chunk >= 0) {
-            const int64_t at = chunk * a.unit_heads + h;
-            if (w.active) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    a.part[at * a.width + w.off + i] = pdk[i];
-                    a.part[a.part_stride + at * a.width + w.off + i] = pk[i];
-                }
-            }
-            if (w.l == 0) reinterpret_cast<AttnArgs::f4 *>(a.part_more)[at] = AttnArgs::f4{m, sum, delta, 0.f};
-            return;
-        }
-        const float by = sum == 0.f ? 0.f : 1.f / sum;
-        delta *= by;
-#pragma unroll
-        for (int i = 0; i < N; ++i) pdk[i] = a.scale * by * fmaf(-delta, pk[i], pdk[i]);
-        if (a.dQ && w.active) P::store(static_cast<T *>(a.dQ) + row * a.lddq + h * a.width + w.off, pdk);
-        if (w.l == 0) a.stats[row * a.heads + h] = AttnArgs::f4{m, by, delta, 0.f};
-    });
+    if (a.bucket_to)
+        for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < a.edges; i += (int64_t)gridDim.x * kBlock) a.bucket_to[i] = a.bucket_from[a.eid[i]];
+    walk_units<QueryRow<BF16, PC, LG, NEAR>>(a);
 }
 
 // ------------------------------------------------------------------ dK, dV
-// Rows are sources; a group has one of the key heads and walks the edges of its row once for each query head that shares it.
-template <bool BF16, int LG, bool WHOLE>
-__global__ __launch_bounds__(kBlock) void k_attn_dkv(AttnArgs a)
+// Rows are sources; a unit has one of the key heads, and its row's edges once for each query head that shares it.
+template <bool BF16, int PC, int LG_, bool NEAR, int U_>
+struct KeyRow {
+    typedef Piece<BF16, PC> P;
+    static constexpr int LG = LG_, N = P::N, UNROLL = U_;
+    static constexpr bool T = true;
+    const AttnArgs &a;
+    const Where<P, LG, NEAR> w;
+    P k, v;                        // this row's own operands
+    int head;                      // the first of the query heads
+    float dk[N], dv[N];
+    __device__ __forceinline__ KeyRow(const AttnArgs &args) : a(args), w(args.width) {}
+    __device__ __forceinline__ void own(int64_t row, int hk)
+    {
+        w.load(k, a.K, row, a.ldk, hk * a.width);
+        w.load(v, a.V, row, a.ldv, hk * a.width);
+    }
+    __device__ __forceinline__ void start(int hk)
+    {
+        head = hk * a.shared;
+        w.cut(k);
+        w.cut(v);
+#pragma unroll
+        for (int x = 0; x < N; ++x) dk[x] = dv[x] = 0.f;
+    }
+    template <int U>
+    __device__ __forceinline__ void step(Ahead<T, UNROLL> &next, int beg, int i, int steps)
+    {
+        P q[U], g[U];
+        float s[U];
+        f32x4 stats[U];
+        int pos[U], its[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int h = head + next.head[j];
+            w.load(q[j], a.Q, next.col[j], a.ldq, h * a.width);
+            w.load(g[j], a.dO, next.col[j], a.lddo, h * a.width);
+            stats[j] = a.stats[(int64_t)next.col[j] * a.heads + h];
+            s[j] = i + j < steps ? bias_of(a, next.bucket[j], h) : -INFINITY;
+            pos[j] = next.pos[j];
+            its[j] = h;
+        }
+        const int last = steps - i;
+        if (i + U < steps) next.load(a, beg, i + U, steps);
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const float d = over_lanes<LG>(k.dot(q[j])), dp = over_lanes<LG>(v.dot(g[j]));
+            const float z = s[j] == -INFINITY ? s[j] : fmaf(d, a.scale, s[j]), p = z == -INFINITY ? 0.f : exp_of(z - stats[j][0]) * stats[j][1];
+            const float ds = p == 0.f ? 0.f : p * (dp - stats[j][2]);
+            if (a.ds && w.l == 0 && j < last) a.ds[(int64_t)pos[j] * a.heads + its[j]] = ds;
+            q[j].keep(p != 0.f);
+            g[j].keep(p != 0.f);
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                dk[x] = fmaf(ds, q[j].get(x), dk[x]);
+                dv[x] = fmaf(p, g[j].get(x), dv[x]);
+            }
+        }
+    }
+    __device__ __forceinline__ void join(int d, bool on)
+    {
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            const float k2 = __shfl_down(dk[x], d, kWave), v2 = __shfl_down(dv[x], d, kWave);
+            dk[x] += on ? k2 : 0.f;
+            dv[x] += on ? v2 : 0.f;
+        }
+    }
+    static constexpr int VALUES = 2 * N;
+    __device__ __forceinline__ void leave(float (&slots)[VALUES][kWave], int at) const
+    {
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            slots[x][at] = dk[x];
+            slots[N + x][at] = dv[x];
+        }
+    }
+    __device__ __forceinline__ void add_from(float (&slots)[VALUES][kWave], int at)
+    {
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            dk[x] += slots[x][at];
+            dv[x] += slots[N + x][at];
+        }
+    }
+    __device__ __forceinline__ void add(float (&slots)[VALUES][kWave], int at)
+    {
+        add_from(slots, at);
+        leave(slots, at);
+    }
+    __device__ __forceinline__ void store_chunk(int64_t at)
+    {
+        w.store_sums(a.part, at * a.width, dk);
+        w.store_sums(a.part + a.part_stride, at * a.width, dv);
+    }
+    __device__ __forceinline__ void store(int64_t r, int hk)
+    {
+        float o[N];
+#pragma unroll
+        for (int x = 0; x < N; ++x) o[x] = dk[x] * a.scale;
+        if (a.dK) w.store(a.dK, r, a.lddk, hk * a.width, o);
+        if (a.dV) w.store(a.dV, r, a.lddv, hk * a.width, dv);
+    }
+};
+
+template <bool BF16, int PC, int LG, bool NEAR, int U>
+__global__ __launch_bounds__(kBlock, U == 1 ? 4 : 3) void k_attn_dkv(AttnArgs a)
 {
-    typedef Piece<BF16, WHOLE> P;
-    typedef typename P::elem T;
-    constexpr int N = P::N, U = kAttnUnroll;
-    const Where<P, LG, WHOLE> w(a.width);
-    for_units<LG>(a, w.g, [&](int64_t row, int hk, int beg, int end, int64_t chunk) __attribute__((always_inline)) {
-        const T *Q = static_cast<const T *>(a.Q) + w.off, *G = static_cast<const T *>(a.dO) + w.off;
-        float k[N], v[N], dk[N], dv[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) dk[i] = dv[i] = 0.f;
-        if (beg < end) {
-            w.own(static_cast<const T *>(a.K) + row * a.ldk + hk * a.width, a.scale, k);
-            w.own(static_cast<const T *>(a.V) + row * a.ldv + hk * a.width, 1.f, v);
-        }
-        const uint32_t steps = (uint32_t)(end - beg) * (uint32_t)a.shared;       // rows of a transposed block are chunked: 2^8 x 2^12 at most
-        for (uint32_t at = 0; at < steps; at += U) {
-            P q[U], g[U];
-            float s[U];
-            AttnArgs::f4 stats[U];
-            int pos[U], head[U];
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const uint32_t i = at + j < steps ? at + j : steps - 1, e = over(i, a.shared_inv);
-                pos[j] = beg + (int)e;
-                head[j] = hk * a.shared + (int)(i - e * (uint32_t)a.shared);
-            }
-            int u[U], b[U];
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                u[j] = a.col[pos[j]];
-                b[j] = a.bucket ? a.bucket[a.eid[pos[j]]] : 0;
-            }
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                q[j].load(Q + u[j] * a.ldq + head[j] * a.width);
-                g[j].load(G + u[j] * a.lddo + head[j] * a.width);
-                stats[j] = a.stats[(int64_t)u[j] * a.heads + head[j]];
-                s[j] = at + j < steps ? bias_of(a, b[j], head[j]) : -INFINITY;
-            }
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                float d = 0.f, dp = 0.f;
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    d = fmaf(k[i], q[j].get(i), d);
-                    dp = fmaf(v[i], g[j].get(i), dp);
-                }
-                d = over_lanes<LG>(d);
-                dp = over_lanes<LG>(dp);
-                const float z = s[j] == -INFINITY ? s[j] : d + s[j], p = z == -INFINITY ? 0.f : exp_of(z - stats[j][0]) * stats[j][1];
-                const float ds = p == 0.f ? 0.f : p * (dp - stats[j][2]);
-                if (a.ds && w.l == 0 && at + j < steps) a.ds[(int64_t)pos[j] * a.heads + head[j]] = ds;
-                q[j].keep(p != 0.f);
-                g[j].keep(p != 0.f);
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    dk[i] = fmaf(ds, q[j].get(i), dk[i]);
-                    dv[i] = fmaf(p, g[j].get(i), dv[i]);
-                }
-            }
-        }
-        if (chunk >= 0) {
-            const int64_t to = chunk * a.unit_heads + hk;
-            if (w.active) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    a.part[to * a.width + w.off + i] = dk[i];
-                    a.part[a.part_stride + to * a.width + w.off + i] = dv[i];
-                }
-            }
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) dk[i] *= a.scale;
-        if (!w.active) return;
-        if (a.dK) P::store(static_cast<T *>(a.dK) + row * a.lddk + hk * a.width + w.off, dk);
-        if (a.dV) P::store(static_cast<T *>(a.dV) + row * a.lddv + hk * a.width + w.off, dv);
-    });
+    walk_units<KeyRow<BF16, PC, LG, NEAR, U>>(a);
 }
 
 // ------------------------------------------------------------------ chunks of long rows
 // A workgroup has one long row and 2^lg of its columns at a time, and as many parts of its chunks as threads are left; the parts are joined in
 // order.  KIND 0: O and lse, 1: dQ and the row's numbers, 2: dK and dV.
 template <bool BF16, int KIND>
-__global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a, int lg)
+__global__ __launch_bounds__(kJoin) void k_attn_join(AttnArgs a, int lg)
 {
-    typedef typename Piece<BF16, true>::elem T;
+    typedef typename std::conditional<BF16, uint16_t, float>::type T;
     constexpr int MORE = KIND == 1 ? 4 : 2, NS = KIND == 0 ? 2 : KIND == 1 ? 4 : 2;       // sums: columns' (one or two), the row's
-    const int cols = a.unit_heads * a.width, tiles = (cols + (1 << lg) - 1) >> lg, parts = kBlock >> lg;
+    const int cols = a.unit_heads * a.width, tiles = (cols + (1 << lg) - 1) >> lg, parts = kJoin >> lg;
     const int c = threadIdx.x & ((1 << lg) - 1), part = threadIdx.x >> lg;
-    __shared__ float sums[NS][kBlock], most[kBlock];
+    __shared__ float sums[NS][kJoin], most[kJoin];
     const int64_t total = (int64_t)*a.n_long * tiles;
     for (int64_t unit = blockIdx.x; unit < total; unit += gridDim.x) {
         const int li = (int)(unit / tiles), col = ((int)(unit - (int64_t)li * tiles) << lg) + c;
@@ -504,6 +778,7 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a, int lg)
 #pragma unroll
         for (int i = 0; i < NS; ++i) v[i] = 0.f;
         if (KIND != 2)
+#pragma unroll 4
             for (int k = lo; k < hi; ++k) m = fmaxf(m, more[MORE * ((int64_t)k * a.unit_heads + h)]);
         const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll 4
@@ -555,7 +830,7 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a, int lg)
             } else {
                 const float delta = v[3] * by;
                 put(a.dQ, a.lddq, a.scale * by * fmaf(-delta, v[2], v[0]));
-                if (col == h * a.width) a.stats[row * a.heads + h] = AttnArgs::f4{m, by, delta, 0.f};
+                if (col == h * a.width) a.stats[row * a.heads + h] = f32x4{m, by, delta, 0.f};
             }
         }
     }
@@ -566,7 +841,7 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a, int lg)
 // meet; then table by table.  Buckets are taken kBiasTile at a time, heads 2^lg at a time.
 struct BiasArgs {
     const float *ds;               // [position][heads]
-    const int32_t *eid, *bucket;
+    const int32_t *bucket;         // [position]
     float *part;                   // [workgroup][buckets][heads]
     int64_t positions;
     int32_t heads, buckets, lg;
@@ -574,23 +849,38 @@ struct BiasArgs {
 
 __global__ __launch_bounds__(kBlock) void k_attn_dbias(BiasArgs a)
 {
-    __shared__ float table[kBiasTile * kBlock];       // [bucket][edge under way][head]
+    extern __shared__ float table[];                  // [bucket][edge under way][head]
     const int hs = 1 << a.lg, slots = kBlock >> a.lg, head0 = (int)blockIdx.z * hs, first = (int)blockIdx.y * kBiasTile;
+    const int tile = a.buckets - first < kBiasTile ? a.buckets - first : kBiasTile;
     const int h = head0 + (threadIdx.x & (hs - 1)), slot = threadIdx.x >> a.lg;
-    for (int i = 0; i < kBiasTile; ++i) table[i * kBlock + threadIdx.x] = 0.f;
-    __syncthreads();
+    for (int i = 0; i < tile; ++i) table[i * kBlock + threadIdx.x] = 0.f;
     const int64_t per = (a.positions + gridDim.x - 1) / gridDim.x, beg = per * blockIdx.x, last = beg + per < a.positions ? beg + per : a.positions;
-#pragma unroll 4
-    for (int64_t t = beg + slot; t < last; t += slots) {
-        const uint32_t b = (uint32_t)(a.bucket[a.eid[t]] - first);
-        if (b < (uint32_t)kBiasTile && h < a.heads) table[b * kBlock + threadIdx.x] += a.ds[t * a.heads + h];
+    if (h < a.heads) {                                // a thread's column is its own: no barrier before the tables are read
+        int64_t t = beg + slot;
+        constexpr int U = 8;
+        for (; t + (U - 1) * slots < last; t += U * slots) {
+            int b[U];
+            float x[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                b[j] = a.bucket[t + j * slots] - first;
+                x[j] = a.ds[(t + j * slots) * a.heads + h];
+            }
+#pragma unroll
+            for (int j = 0; j < U; ++j)
+                if ((uint32_t)b[j] < (uint32_t)tile) table[b[j] * kBlock + threadIdx.x] += x[j];
+        }
+        for (; t < last; t += slots) {
+            const int b = a.bucket[t] - first;
+            if ((uint32_t)b < (uint32_t)tile) table[b * kBlock + threadIdx.x] += a.ds[t * a.heads + h];
+        }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < kBiasTile * hs; i += kBlock) {
+    for (int i = threadIdx.x; i < tile * hs; i += kBlock) {
         const int b = i >> a.lg, c = i & (hs - 1);
         float v = 0.f;
         for (int r = 0; r < slots; ++r) v += table[b * kBlock + (r << a.lg) + c];
-        if (first + b < a.buckets && head0 + c < a.heads) a.part[((int64_t)blockIdx.x * a.buckets + first + b) * a.heads + head0 + c] = v;
+        if (head0 + c < a.heads) a.part[((int64_t)blockIdx.x * a.buckets + first + b) * a.heads + head0 + c] = v;
     }
 }
 
@@ -698,6 +988,7 @@ struct Scratch {
     size_t used = 0;
     char *base;
     float *part, *part_more, *stats, *ds, *bias;
+    int32_t *bucket;
     char *plan;
     int64_t part_stride;
     float *take(int64_t n)
@@ -709,6 +1000,7 @@ struct Scratch {
     Scratch(const fastgl_attn_desc &d, bool backward, bool own_plan, char *at) : base(at)
     {
         part = part_more = stats = ds = bias = nullptr;
+        bucket = nullptr;
         plan = nullptr;
         const int64_t chunks = d.num_edges > kLongThreshold ? cap_chunks(d.num_edges) : 0;
         part_stride = chunks * d.heads * d.width;
@@ -716,6 +1008,7 @@ struct Scratch {
         part_more = take(chunks * d.heads * (backward ? 4 : 2));
         if (backward) {
             stats = take(d.num_dst * d.heads * 4);
+            if (d.bucket) bucket = reinterpret_cast<int32_t *>(take(d.num_edges));
             if (d.bias) {
                 ds = take(d.num_edges * d.heads);
                 bias = take(bias_blocks(d) * d.num_buckets * d.heads);
@@ -735,28 +1028,33 @@ struct Scratch {
     }
 };
 
+// Lanes of a head: two pieces each, so that what is done once an edge and lane counts less; one piece where there is no more.
+// near: whether offsets into all arrays of rows are below 2^32.
 template <class F>
-fastgl_status by_shape(fastgl_dtype dtype, int64_t width, F f)
+fastgl_status by_shape(fastgl_dtype dtype, int64_t width, bool near, F f)
 {
     const bool bf16 = dtype == FASTGL_BF16;
-    const int n = bf16 ? 8 : 4;
+    const int64_t n = bf16 ? 8 : 4, pieces = ceil_div(width, n);
     typedef std::true_type Yes;
     typedef std::false_type No;
-    if (width < n) return bf16 ? f(Yes(), std::integral_constant<int, 3>(), No()) : f(No(), std::integral_constant<int, 2>(), No());
-    const int64_t pieces = ceil_div(width, n);
-    auto lanes = [&](auto b) {
-        if (pieces <= 1) return f(b, std::integral_constant<int, 0>(), Yes());
-        if (pieces <= 2) return f(b, std::integral_constant<int, 1>(), Yes());
-        if (pieces <= 4) return f(b, std::integral_constant<int, 2>(), Yes());
-        if (pieces <= 8) return f(b, std::integral_constant<int, 3>(), Yes());
-        if (pieces <= 16) return f(b, std::integral_constant<int, 4>(), Yes());
-        if constexpr (decltype(b)::value) return f(b, std::integral_constant<int, 5>(), Yes());
+    typedef std::integral_constant<int, 0> I0;
+    typedef std::integral_constant<int, 1> I1;
+    typedef std::integral_constant<int, 2> I2;
+    if (width < n) return bf16 ? f(Yes(), I0(), std::integral_constant<int, 3>(), No()) : f(No(), I0(), I2(), No());
+    auto lanes = [&](auto b, auto near_) {
+        if (pieces <= 1) return f(b, I1(), I0(), near_);
+        if (pieces <= 2) return f(b, I2(), I0(), near_);
+        if (pieces <= 4) return f(b, I2(), I1(), near_);
+        if (pieces <= 8) return f(b, I2(), I2(), near_);
+        if (pieces <= 16) return f(b, I2(), std::integral_constant<int, 3>(), near_);
+        if constexpr (decltype(b)::value) return f(b, I2(), std::integral_constant<int, 4>(), near_);
         else {
-            if (pieces <= 32) return f(b, std::integral_constant<int, 5>(), Yes());
-            return f(b, std::integral_constant<int, 6>(), Yes());
+            if (pieces <= 32) return f(b, I2(), std::integral_constant<int, 4>(), near_);
+            return f(b, I2(), std::integral_constant<int, 5>(), near_);
         }
     };
-    return bf16 ? lanes(Yes()) : lanes(No());
+    if (near) return bf16 ? lanes(Yes(), Yes()) : lanes(No(), Yes());
+    return bf16 ? lanes(Yes(), No()) : lanes(No(), No());
 }
 
 enum Pass { kPassFwd = 0, kPassDq = 1, kPassDkv = 2 };
@@ -769,7 +1067,9 @@ fastgl_status launch_walk(AttnArgs a, const fastgl_attn_desc &d, const fastgl_pl
     constexpr bool T = PASS == kPassDkv;
     const int64_t rows = T ? d.num_src : d.num_dst;
     a.unit_heads = (int32_t)(T ? d.kv_heads : d.heads);
-    a.units = rows * a.unit_heads;
+    a.rows = rows;
+    a.dealt = T && rows >= 512;
+    a.units = (a.dealt ? (int64_t)align_up((size_t)rows, 512) : rows) * a.unit_heads;
     a.heads_inv = a.unit_heads > 1 ? UINT64_MAX / (uint64_t)a.unit_heads + 1 : 0;
     const bool chunked = d.num_edges > kLongThreshold && (T || !(pl->parts & FASTGL_PLAN_SHORT_DST_ROWS));
     a.long_thr = chunked ? kLongThreshold : INT32_MAX;
@@ -780,22 +1080,21 @@ fastgl_status launch_walk(AttnArgs a, const fastgl_attn_desc &d, const fastgl_pl
         a.n_chunks = pl->counters + (T ? 3 : 1);
     }
     if (a.units == 0) return FASTGL_OK;
-    const fastgl_status st = by_shape(d.dtype, d.width, [&](auto bf16, auto lg, auto whole) {
-        constexpr bool B = decltype(bf16)::value, W = decltype(whole)::value;
-        constexpr int LG = decltype(lg)::value;
-        const int64_t groups = kBlock >> LG;
-        if (chunked) {
-            const int64_t n = ceil_div(cap_chunks(d.num_edges) * a.unit_heads, groups);
-            a.chunk_blocks = (int32_t)(n < 1024 ? n : 1024);
-        }
-        const int64_t blocks = ceil_div(a.units, groups) + a.chunk_blocks;
+    const int64_t el = d.dtype == FASTGL_BF16 ? 2 : 4, far = (int64_t)UINT32_MAX / el;
+    const bool near = d.num_dst * d.ldq <= far && d.num_src * d.ldk <= far && d.num_src * d.ldv <= far && d.num_dst * a.lddo <= far;
+    const fastgl_status st = by_shape(d.dtype, d.width, near, [&](auto bf16, auto pc, auto lg, auto near_) {
+        constexpr bool B = decltype(bf16)::value, NEAR = decltype(near_)::value;
+        constexpr int PC = decltype(pc)::value, LG = decltype(lg)::value;
+        const int64_t blocks = ceil_div(a.units, (int64_t)(kBlock >> LG));
         if (blocks > INT32_MAX) {
             set_error("%s: too many rows and heads", names[PASS]);
             return FASTGL_ERR_UNSUPPORTED;
         }
-        if constexpr (PASS == kPassFwd) hipLaunchKernelGGL((k_attn_fwd<B, LG, W>), dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
-        else if constexpr (PASS == kPassDq) hipLaunchKernelGGL((k_attn_dq<B, LG, W>), dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
-        else hipLaunchKernelGGL((k_attn_dkv<B, LG, W>), dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
+        a.chunk_waves = (int32_t)((blocks < 2048 ? blocks : 2048) * (kBlock / kWave));
+        if constexpr (PASS == kPassFwd) hipLaunchKernelGGL((k_attn_fwd<B, PC, LG, NEAR>), dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
+        else if constexpr (PASS == kPassDq) hipLaunchKernelGGL((k_attn_dq<B, PC, LG, NEAR>), dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
+        else if (a.shared == 1) hipLaunchKernelGGL((k_attn_dkv<B, PC, LG, NEAR, 1>), dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
+        else hipLaunchKernelGGL((k_attn_dkv<B, PC, LG, NEAR, 2>), dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
         FASTGL_LAUNCH_CHECK(names[PASS]);
         return FASTGL_OK;
     });
@@ -805,8 +1104,8 @@ fastgl_status launch_walk(AttnArgs a, const fastgl_attn_desc &d, const fastgl_pl
     while (lg < 8 && (1 << lg) < cols) ++lg;
     const int64_t units = cap_long_rows(d.num_edges) * ceil_div(cols, (int64_t)1 << lg);
     const dim3 grid((unsigned)(units < 1024 ? units : 1024));
-    if (d.dtype == FASTGL_BF16) hipLaunchKernelGGL((k_attn_join<true, PASS>), grid, dim3(kBlock), 0, s, a, lg);
-    else hipLaunchKernelGGL((k_attn_join<false, PASS>), grid, dim3(kBlock), 0, s, a, lg);
+    if (d.dtype == FASTGL_BF16) hipLaunchKernelGGL((k_attn_join<true, PASS>), grid, dim3(kJoin), 0, s, a, lg);
+    else hipLaunchKernelGGL((k_attn_join<false, PASS>), grid, dim3(kJoin), 0, s, a, lg);
     FASTGL_LAUNCH_CHECK("fastgl_attn (long rows)");
     return FASTGL_OK;
 }
@@ -822,7 +1121,7 @@ AttnArgs args_of(const fastgl_attn_desc &d, const Scratch &o)
     a.heads = (int32_t)d.heads; a.shared = (int32_t)(d.heads / d.kv_heads); a.width = (int32_t)d.width;
     a.shared_inv = a.shared > 1 ? (uint32_t)(0xFFFFFFFFu / (uint32_t)a.shared + 1) : 0;
     a.scale = d.scale;
-    a.stats = reinterpret_cast<AttnArgs::f4 *>(o.stats);
+    a.stats = reinterpret_cast<f32x4 *>(o.stats);
     a.part = o.part; a.part_more = o.part_more; a.part_stride = o.part_stride;
     return a;
 }
@@ -925,10 +1224,16 @@ fastgl_status fastgl_attn_bwd(const fastgl_attn_desc *desc, const void *dO, int6
     AttnArgs a = args_of(d, o);
     a.dO = dO; a.lddo = lddo;
     a.dQ = dQ; a.lddq = lddq;
+    if (d.bucket && (dK || dV || dbias)) {
+        a.bucket_from = d.bucket; a.eid = plan->perm;
+        a.bucket_to = o.bucket;
+        a.edges = d.num_edges;
+    }
     if ((st = launch_walk<kPassDq>(a, d, plan, s)) != FASTGL_OK) return st;
     if (!dK && !dV && !dbias) return FASTGL_OK;
     AttnArgs b = args_of(d, o);
-    b.ptr = plan->indptr_T; b.col = plan->indices_T; b.eid = plan->perm;
+    b.ptr = plan->indptr_T; b.col = plan->indices_T;
+    b.bucket = o.bucket;
     b.dO = dO; b.lddo = lddo;
     b.dK = dK; b.lddk = lddk;
     b.dV = dV; b.lddv = lddv;
@@ -937,14 +1242,15 @@ fastgl_status fastgl_attn_bwd(const fastgl_attn_desc *desc, const void *dO, int6
     if (!dbias) return FASTGL_OK;
     BiasArgs c = {};
     c.ds = o.ds;
-    c.eid = plan->perm; c.bucket = d.bucket;
+    c.bucket = o.bucket;
     c.part = o.bias;
     c.positions = d.num_edges;
     c.heads = (int32_t)d.heads; c.buckets = (int32_t)d.num_buckets;
     while (c.lg < 5 && (1 << c.lg) < d.heads) ++c.lg;
     const int64_t blocks = Scratch::bias_blocks(d), table = d.num_buckets * d.heads;
     const dim3 grid((unsigned)blocks, (unsigned)ceil_div(d.num_buckets, kBiasTile), (unsigned)ceil_div(d.heads, (int64_t)1 << c.lg));
-    hipLaunchKernelGGL(k_attn_dbias, grid, dim3(kBlock), 0, s, c);
+    const size_t lds = sizeof(float) * kBlock * (size_t)(d.num_buckets < kBiasTile ? d.num_buckets : kBiasTile);
+    hipLaunchKernelGGL(k_attn_dbias, grid, dim3(kBlock), lds, s, c);
     FASTGL_LAUNCH_CHECK("fastgl_attn_bwd (dbias)");
     hipLaunchKernelGGL(k_attn_dbias_sum, dim3((unsigned)ceil_div(table, 8)), dim3(kBlock), 0, s, (const float *)o.bias, (int)blocks, table, dbias);
     FASTGL_LAUNCH_CHECK("fastgl_attn_bwd (dbias, sums)");
