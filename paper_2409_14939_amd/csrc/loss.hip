@@ -4,6 +4,8 @@
 //   backward  for a piece of the classes at a time: [W packed] -> scores again, of which dZ remains (as the matrix cores take it, with column sums)
 //             -> dH += dZ W^T -> dW = H^T dZ -> k_loss_sum
 //
+// Small calls go another way, through k_loss_block: a workgroup has 32 rows and 64 classes, the scores in LDS, and all of a pass that these take part in.
+//
 // The rows of H are packed once for all pieces of a backward pass, 0 where there is no label: dZ is 0 there, and what H holds there must not
 // reach dW (0 times NaN).
 #include <initializer_list>
@@ -140,6 +142,291 @@ __global__ __launch_bounds__(kBlock) void k_loss_sum(LossSumArgs a)
     }
 }
 
+// ------------------------------------------------------------------ small calls
+// 32 rows and 64 classes a workgroup, with fp32 matrix instructions from rows and weights as they lie in memory: nothing is packed, dZ stays
+// in LDS and is not rounded.
+//   scores  the wavefronts take eight inputs each in turn; their sums are joined in LDS, where the tile then has its statistics or dZ
+//   dH      32 inputs a wavefront at a time: sums over the tile's classes, one for each strip of classes, joined afterwards
+//   dW      the same over the tile's rows
+struct LossBlockArgs {
+    const void *H, *W;
+    const float *b;
+    const int64_t *label;
+    const float *lse_in, *dloss;
+    int64_t M, N;
+    int32_t K;
+    float *loss, *lse;             // forward, one strip
+    float *stats, *picked;         // forward, several
+    void *dH, *dW;                 // or NULL
+    float *db;
+    float *part_h, *part_w, *part_b;       // [strip][M][K], [tile][K][N], [tile][N]; NULL: results go where they belong
+};
+
+constexpr int kBlockRows = 32, kBlockCols = 64, kPad = 68;
+
+// Elements by 32-bit offsets: arrays of small calls have fewer than 2^27 elements.
+template <bool BF16>
+__device__ __forceinline__ float element(const void *p, uint32_t i)
+{
+    if constexpr (BF16) return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(static_cast<const char *>(p) + 2 * i) << 16);
+    else return *reinterpret_cast<const float *>(static_cast<const char *>(p) + 4 * i);
+}
+
+// Four elements from i on, at any alignment to an element.
+template <bool BF16>
+__device__ __forceinline__ void four(const void *p, uint32_t i, float (&v)[4])
+{
+    if constexpr (BF16) {
+        const Words<2>::x2 q = *reinterpret_cast<const Words<2>::x2 *>(static_cast<const char *>(p) + 2 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(j & 1 ? q[j >> 1] & 0xFFFF0000u : q[j >> 1] << 16);
+    } else {
+        const Words<4>::x4 q = *reinterpret_cast<const Words<4>::x4 *>(static_cast<const char *>(p) + 4 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(q[j]);
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void put_result(void *out, float *part, uint32_t at, float x)
+{
+    if (part) *reinterpret_cast<float *>(reinterpret_cast<char *>(part) + 4 * at) = x;
+    else if constexpr (BF16) *reinterpret_cast<uint16_t *>(static_cast<char *>(out) + 2 * at) = __builtin_bit_cast(uint16_t, (__bf16)x);
+    else *reinterpret_cast<float *>(static_cast<char *>(out) + 4 * at) = x;
+}
+
+template <bool BF16, bool BACKWARD>
+__global__ __launch_bounds__(kBlock) void k_loss_block(LossBlockArgs a)
+{
+    constexpr float kLog2e = 1.44269504089f, kLn2 = 0.69314718056f;
+    constexpr int WAVES = kBlock / kWave;
+    __shared__ float z[WAVES][kBlockRows][kPad];
+    __shared__ float on[kBlockRows];
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r = lane & 31, h = lane >> 5;
+    const int strip = blockIdx.x, tile = blockIdx.y;
+    const int64_t col0 = (int64_t)strip * kBlockCols;
+    const int left = (int)(a.N - col0 < kBlockCols ? a.N - col0 : kBlockCols);
+    const uint32_t N = (uint32_t)a.N, K = (uint32_t)a.K;
+    uint32_t col[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) col[q] = (uint32_t)col0 + (32 * q + r < left ? 32 * q + r : left - 1);        // columns that do not exist are not used
+    float *part_h = a.part_h ? a.part_h + (int64_t)strip * a.M * a.K : nullptr, *part_w = a.part_w ? a.part_w + (int64_t)tile * a.K * a.N : nullptr;
+    const int64_t row0 = (int64_t)tile * kBlockRows;
+    const int rows = (int)(a.M - row0 < kBlockRows ? a.M - row0 : kBlockRows);
+    // ---- scores
+    f32x16 acc[2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[0][e] = acc[1][e] = 0.f;
+    const uint32_t first = (uint32_t)row0 * K, my_row = first + (uint32_t)(r < rows ? r : rows - 1) * K;
+    const int whole = a.K & ~7;
+#pragma unroll 2
+    for (int k = wave * 8; k < whole; k += WAVES * 8) {
+        float x[4], w[2][4];
+        four<BF16>(a.H, my_row + k + 4 * h, x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) w[q][j] = element<BF16>(a.W, (uint32_t)(k + 4 * h + j) * N + col[q]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) acc[q] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], w[q][j], acc[q], 0, 0, 0);
+    }
+    if (whole < a.K && wave == (whole / 8) % WAVES) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int k = whole + 4 * h + j;
+            const bool in = k < a.K;
+            const float x = in ? element<BF16>(a.H, my_row + k) : 0.f;
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                acc[q] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, in ? element<BF16>(a.W, (uint32_t)k * N + col[q]) : 0.f, acc[q], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[wave][8 * (e >> 2) + 4 * h + (e & 3)][32 * q + r] = acc[q][e];
+    __syncthreads();
+    // ---- statistics or dZ: eight threads a row, eight columns each
+    {
+        const int row = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 8;
+        const int64_t label = row < rows ? a.label[row0 + row] : -1;
+        const int mine = label >= col0 && label < col0 + left ? (int)(label - col0) - c0 : -1;       // of the label among these columns
+        float v[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) s += z[i][row][c0 + c];
+            if (a.b && c0 + c < left) s += a.b[col0 + c0 + c];
+            v[c] = c0 + c < left ? s : -INFINITY;
+        }
+        if constexpr (!BACKWARD) {
+            float most = -INFINITY, sum = 0.f, at = 0.f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) most = fmaxf(most, v[c]);
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, kWave));
+            const float base = most == -INFINITY ? 0.f : most;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                sum += __builtin_amdgcn_exp2f((v[c] - base) * kLog2e);
+                at = c == mine ? v[c] : at;
+            }
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) {
+                sum += __shfl_xor(sum, d, kWave);
+                at += __shfl_xor(at, d, kWave);
+            }
+            if (row < rows && c0 == 0) {
+                if (a.stats) {
+                    a.stats[2 * (strip * a.M + row0 + row)] = most;
+                    a.stats[2 * (strip * a.M + row0 + row) + 1] = sum;
+                    if (label >= col0 && label < col0 + left) a.picked[row0 + row] = at;
+                } else {
+                    const float all = most == -INFINITY && sum == 0.f ? -INFINITY : most + __builtin_amdgcn_logf(sum) * kLn2;
+                    if (a.lse) a.lse[row0 + row] = all;
+                    a.loss[row0 + row] = label < 0 ? 0.f : label >= a.N ? NAN : all - at;
+                }
+            }
+        } else {
+            const float lse = label >= 0 ? a.lse_in[row0 + row] : 0.f;
+            const float scale = label >= a.N ? NAN : label >= 0 ? a.dloss[row0 + row] : 0.f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const float p = __builtin_amdgcn_exp2f((v[c] - lse) * kLog2e), x = c == mine ? p - 1.f : p;
+                z[0][row][c0 + c] = label >= 0 && c0 + c < left ? x * scale : 0.f;
+            }
+            if (c0 == 0) on[row] = label >= 0 ? 1.f : 0.f;
+        }
+    }
+    if constexpr (BACKWARD) {
+        __syncthreads();
+        float db = 0.f;
+        if (a.db && threadIdx.x < kBlockCols) {
+#pragma unroll 8
+            for (int i = 0; i < kBlockRows; ++i) db += z[0][i][threadIdx.x];
+        }
+        // ---- dH
+        if (a.dH)
+            for (int k0 = wave * 32; k0 < a.K; k0 += WAVES * 32) {
+                const int k = k0 + r;
+                const uint32_t w0 = (uint32_t)(k < a.K ? k : a.K - 1) * N + (uint32_t)col0;
+                f32x16 out;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) out[e] = 0.f;
+                auto eight = [&](int c, const float (&w)[4]) __attribute__((always_inline)) {
+                    const float *x = &z[0][r][8 * c + 4 * h];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) out = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], w[j], out, 0, 0, 0);
+                };
+                if (left == kBlockCols) {
+                    float w[8][4];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) four<BF16>(a.W, w0 + 8 * c + 4 * h, w[c]);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) eight(c, w[c]);
+                } else
+                    for (int c = 0; 8 * c < left; ++c) {
+                        float w[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[j] = 8 * c + 4 * h + j < left ? element<BF16>(a.W, w0 + 8 * c + 4 * h + j) : 0.f;
+                        eight(c, w);
+                    }
+                if (k < a.K) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int row = 8 * (e >> 2) + 4 * h + (e & 3);
+                        if (row < rows) put_result<BF16>(a.dH, part_h, first + (uint32_t)row * K + (uint32_t)k, out[e]);
+                    }
+                }
+            }
+        // ---- dW
+        auto block = [&](int k0, f32x16 (&out)[2]) __attribute__((always_inline)) {
+            const int k = k0 + r < a.K ? k0 + r : a.K - 1;
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int row = 8 * (i >> 2) + 4 * h + (i & 3);
+                x[i] = element<BF16>(a.H, first + (uint32_t)(row < rows ? row : rows - 1) * K + (uint32_t)k);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int row = 8 * (i >> 2) + 4 * h + (i & 3);
+                const float v = on[row] != 0.f ? x[i] : 0.f;                   // rows without a label: whatever they hold
+#pragma unroll
+                for (int q = 0; q < 2; ++q) out[q] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, z[0][row][32 * q + r], out[q], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);    // one block's rows in registers at a time
+        };
+        auto store = [&](int k0, const f32x16 (&out)[2]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                if (32 * q + r >= left) continue;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int k = k0 + 8 * (e >> 2) + 4 * h + (e & 3);
+                    if (k < a.K) put_result<BF16>(a.dW, part_w, (uint32_t)k * N + (uint32_t)col0 + 32 * q + r, out[q][e]);
+                }
+            }
+        };
+        if (a.dW)
+            for (int k0 = wave * 32; k0 < a.K; k0 += WAVES * 32) {
+                f32x16 out[2];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) out[0][e] = out[1][e] = 0.f;
+                block(k0, out);
+                store(k0, out);
+            }
+        if (a.db && threadIdx.x < (unsigned)left) {
+            if (a.part_b) a.part_b[(int64_t)tile * a.N + col0 + threadIdx.x] = db;
+            else a.db[col0 + threadIdx.x] = db;
+        }
+    }
+}
+
+// The sums of small calls: up to three results of n elements from so many parts each, 2^lg elements a workgroup and as many threads an element
+// as are left, in fp64 and a fixed order.
+struct LossAddArgs {
+    const float *part[3];
+    void *out[3];
+    int64_t n[3], blocks[3];
+    int32_t parts[3], lg[3], bf16[3];
+};
+
+__global__ __launch_bounds__(kBlock) void k_loss_add(LossAddArgs a)
+{
+    __shared__ double sums[kBlock];
+    int64_t block = blockIdx.x;
+    int m = 0;
+    for (; m < 2 && block >= a.blocks[m]; ++m) block -= a.blocks[m];
+    const float *part = m == 0 ? a.part[0] : m == 1 ? a.part[1] : a.part[2];
+    void *out = m == 0 ? a.out[0] : m == 1 ? a.out[1] : a.out[2];
+    const int64_t n = m == 0 ? a.n[0] : m == 1 ? a.n[1] : a.n[2];
+    const int parts = m == 0 ? a.parts[0] : m == 1 ? a.parts[1] : a.parts[2], lg = m == 0 ? a.lg[0] : m == 1 ? a.lg[1] : a.lg[2];
+    const int bf16 = m == 0 ? a.bf16[0] : m == 1 ? a.bf16[1] : a.bf16[2];
+    const int c = threadIdx.x & ((1 << lg) - 1), t = threadIdx.x >> lg, threads = kBlock >> lg;
+    const int64_t i = (block << lg) + c;
+    double v = 0.0;
+    if (i < n) {
+#pragma unroll 8
+        for (int s = t; s < parts; s += threads) v += (double)part[(int64_t)s * n + i];
+    }
+    if (threads > 1) {
+        sums[threadIdx.x] = v;
+        __syncthreads();
+        for (int d = threads / 2; d > 0; d >>= 1) {
+            if (t < d) sums[threadIdx.x] += sums[threadIdx.x + (d << lg)];
+            __syncthreads();
+        }
+        v = sums[threadIdx.x];
+    }
+    if (t != 0 || i >= n) return;
+    if (bf16) static_cast<uint16_t *>(out)[i] = __builtin_bit_cast(uint16_t, (__bf16)(float)v);
+    else static_cast<float *>(out)[i] = (float)v;
+}
+
 // ------------------------------------------------------------------ host side
 bool misaligned_to(const void *p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
 
@@ -159,8 +446,8 @@ struct Shape {
         int64_t most = N;
         if (backward) most = kPieceBytes / (2 * planes * rows());
         if (pack_w && K > 0 && kPieceBytes / (2 * planes * K) < most) most = kPieceBytes / (2 * planes * K);
+        if (most >= N) return (int64_t)align_up((size_t)N, kPieceCols);
         most = most < 2 * kPieceCols ? kPieceCols : most / kPieceCols * kPieceCols;
-        if (most >= N || !(backward || pack_w)) return (int64_t)align_up((size_t)N, kPieceCols);
         return (int64_t)align_up((size_t)ceil_div(N, ceil_div(N, most)), kPieceCols);
     }
     int64_t pieces() const { return ceil_div(N, piece()); }
@@ -183,6 +470,38 @@ struct Shape {
     }
     int64_t db_rows() const { return ceil_div(M, tile_rows(scores_cut())) * (scores_cut().size == kLarge ? 4 : 2); }
     bool parts_h() const { return pieces() > 1 || rows_cut().slabs > 1; }
+
+    // ---- k_loss_block
+    int64_t tiles() const { return ceil_div(M, kBlockRows); }
+    int64_t strips() const { return ceil_div(N, kBlockCols); }
+    // Whether k_loss_block is taken: a model of both ways, in us, that the sizes go into as they are padded.  A workgroup of it costs
+    // 1.4 us and 0.009 us an input in a forward pass, four at a time a compute unit; a backward pass is 6 M N K multiply-adds at 110 TFLOP/s and its
+    // sums, written and read.  The other way costs its launches, the steps of one tile where there are few, the products at what they reach, and dZ and
+    // packed rows at 4 TB/s.  us a call, k_loss_block / tiles:
+    //   f32 forward   1 row 256 -> 47 6 / 37;  8000 rows 256 -> 47 7 / 36;  70 000 rows 256 -> 47 40 / 88;  16 rows 512 -> 50 000 35 / 93;  1645 rows
+    //                 1070 -> 2113 91 / 145;  667 rows 25 -> 18 287 34 / 23;  24 241 rows 31 -> 1548 100 / 42;  16 384 rows 512 -> 1000 182 / 100
+    //   f32 backward  16 / 43;  33 / 71;  159 / 259;  92 / 185;  613 / 280;  82 / 103;  257 / 242;  1116 / 351 (in that order)
+    //   bf16 forward  7 / 21;  8 / 14;  31 / 23;  34 / 19;  81 / 38;  34 / 17;  96 / 29;  168 / 25
+    //   bf16 backward 20 / 22;  38 / 30;  165 / 79;  91 / 57;  582 / 93;  88 / 53;  277 / 79;  1034 / 94
+    bool small() const
+    {
+        if (tiles() > 65535 || K * N >= (int64_t)1 << 27 || M * K >= (int64_t)1 << 27) return false;      // its grid and offsets
+        const double groups = (double)(tiles() * strips()), k = (double)K, m = (double)M;
+        const double all = (double)align_up((size_t)M, 128) * (double)align_up((size_t)N, 128) * (double)align_up((size_t)K, 128);
+        if (!backward) {
+            const double one = 0.017 * k, many = groups / 256.0 * (1.43 + 0.0094 * k);
+            const double here = 4.5 + (strips() > 1 ? 3.2 : 0.0) + (one > many ? one : many);
+            const double there = bf16 ? 9.5 + (pack_h || pack_w ? 4.0 : 0.0) + 0.006 * k + all * 2.0 / 0.6e9 : 15.0 + 0.085 * k + all * 2.0 / 0.17e9;
+            return here < there;
+        }
+        const double sums = 4.0 * ((tiles() > 1 ? (double)tiles() * k * (double)N : 0.0) + (strips() > 1 ? (double)strips() * m * k : 0.0));
+        if (sums > 256e6) return false;
+        const double here = (10.0 + 0.035 * k + groups * (0.004 + 6.0 * kBlockRows * kBlockCols * k / 110e6) + 2.0 * sums / 4e6) * (bf16 ? 1.15 : 1.0);
+        const double z = m * (double)align_up((size_t)N, 32);
+        const double there = bf16 ? 24.0 + 0.015 * k + all * 6.0 / 0.6e9 + (10.0 * z + 8.0 * m * k) / 4e6
+                                  : 40.0 + 0.06 * k + all * 6.0 / 0.2e9 + (18.0 * z + 12.0 * m * k) / 4e6;
+        return here < there;
+    }
 };
 
 struct Scratch {
@@ -201,6 +520,18 @@ struct Scratch {
     {
         h = w = dz = nullptr;
         stats = picked = db = part_h = part_w = nullptr;
+        if (s.small()) {
+            if (!s.backward && s.strips() > 1) {
+                stats = take<float>((size_t)(2 * s.strips() * s.M));
+                picked = take<float>((size_t)s.M);
+            }
+            if (s.backward && s.strips() > 1) part_h = take<float>((size_t)(s.strips() * s.M * s.K));
+            if (s.backward && s.tiles() > 1) {
+                part_w = take<float>((size_t)(s.tiles() * s.K * s.N));
+                db = take<float>((size_t)(s.tiles() * s.N));
+            }
+            return;
+        }
         if (s.pack_h) h = take<uint16_t>((size_t)(s.planes * s.M * s.ldk));
         if (s.pack_w) w = take<uint16_t>((size_t)(s.planes * s.K * s.piece()));
         if (!s.backward) {
@@ -254,6 +585,34 @@ size_t workspace(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, bool align
     if (aligned) return whole;
     const size_t any = Scratch(Shape(dtype, M, K, N, false, backward), nullptr).used;
     return any > whole ? any : whole;
+}
+
+// A small call: one launch, and one for the sums of several strips or workgroups a strip.
+fastgl_status launch_block(const Shape &d, LossBlockArgs a, hipStream_t s, const char *what)
+{
+    a.M = d.M; a.N = d.N;
+    a.K = (int32_t)d.K;
+    const dim3 grid((unsigned)d.strips(), (unsigned)d.tiles());
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, s, a); };
+    auto typed = [&](auto bf16) {
+        constexpr bool B = decltype(bf16)::value;
+        if (d.backward) go(k_loss_block<B, true>);
+        else go(k_loss_block<B, false>);
+    };
+    if (d.bf16) typed(std::true_type());
+    else typed(std::false_type());
+    FASTGL_LAUNCH_CHECK(what);
+    return FASTGL_OK;
+}
+
+fastgl_status launch_join(const Scratch &o, int64_t slots, const int64_t *label, int64_t M, int64_t N, float *loss, float *lse, hipStream_t s)
+{
+    int lg = 0;
+    while (lg < 5 && ((int64_t)1 << lg) < M) ++lg;
+    hipLaunchKernelGGL(k_loss_join, dim3((unsigned)ceil_div(M, (int64_t)1 << lg)), dim3(kBlock), 0, s, (const float *)o.stats, slots, (const float *)o.picked,
+                       label, M, N, lg, loss, lse);
+    FASTGL_LAUNCH_CHECK("fastgl_loss_fwd (rows)");
+    return FASTGL_OK;
 }
 
 // What of H and of classes n0 .. n0 + n of W a call needs packed, in one launch.
@@ -385,6 +744,15 @@ fastgl_status fastgl_loss_fwd(fastgl_dtype dtype, const void *H, const void *W, 
     if ((st = check_workspace(ws, ws_bytes, Scratch(d, nullptr).used)) != FASTGL_OK) return st;
     const Scratch o(d, (char *)ws);
     hipStream_t s = (hipStream_t)stream;
+    if (d.small()) {
+        LossBlockArgs a = {};
+        a.H = H; a.W = W; a.b = b;
+        a.label = label;
+        a.loss = loss; a.lse = lse;
+        a.stats = o.stats; a.picked = o.picked;
+        st = launch_block(d, a, s, "fastgl_loss_fwd (small)");
+        return st != FASTGL_OK || d.strips() == 1 ? st : launch_join(o, d.strips(), label, M, N, loss, lse, s);
+    }
     const Cut cut = d.scores_cut();
     int64_t slots = 0;
     for (int64_t n0 = 0; n0 < N; n0 += d.piece()) {
@@ -396,12 +764,7 @@ fastgl_status fastgl_loss_fwd(fastgl_dtype dtype, const void *H, const void *W, 
         if ((st = launch<kScores, false>(g, cut, d.bf16, s, "fastgl_loss_fwd")) != FASTGL_OK) return st;
         slots += ceil_div(n, Shape::wave_cols(cut));
     }
-    int lg = 0;
-    while (lg < 5 && ((int64_t)1 << lg) < M) ++lg;
-    hipLaunchKernelGGL(k_loss_join, dim3((unsigned)ceil_div(M, (int64_t)1 << lg)), dim3(kBlock), 0, s, (const float *)o.stats, slots, (const float *)o.picked,
-                       label, M, N, lg, loss, lse);
-    FASTGL_LAUNCH_CHECK("fastgl_loss_fwd (rows)");
-    return FASTGL_OK;
+    return launch_join(o, slots, label, M, N, loss, lse, s);
 }
 
 fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label,
@@ -431,6 +794,37 @@ fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, 
     const Shape d(dtype, M, K, N, starts_whole({H, W}), true);
     if ((st = check_workspace(ws, ws_bytes, Scratch(d, nullptr).used)) != FASTGL_OK) return st;
     const Scratch o(d, (char *)ws);
+    if (d.small()) {
+        LossBlockArgs a = {};
+        a.H = H; a.W = W; a.b = b;
+        a.label = label;
+        a.lse_in = lse; a.dloss = dloss;
+        a.dH = want_h ? dH : nullptr; a.dW = want_w ? dW : nullptr;
+        a.db = want_b ? db : nullptr;
+        a.part_h = o.part_h; a.part_w = o.part_w; a.part_b = o.db;
+        if ((st = launch_block(d, a, s, "fastgl_loss_bwd (small)")) != FASTGL_OK) return st;
+        LossAddArgs t = {};
+        int64_t total = 0;
+        auto add = [&](int m, const float *part, void *out, int64_t n, int64_t parts, bool bf16) {
+            if (!part || !out) return;
+            t.part[m] = part;
+            t.out[m] = out;
+            t.n[m] = n;
+            t.parts[m] = (int32_t)parts;
+            t.bf16[m] = bf16;
+            t.lg[m] = 8;                              // fewer elements a workgroup where there are few of many parts
+            while (t.lg[m] > 3 && (parts >> (8 - t.lg[m])) > 8 && ceil_div(n, (int64_t)1 << t.lg[m]) < 1024) --t.lg[m];
+            t.blocks[m] = ceil_div(n, (int64_t)1 << t.lg[m]);
+            total += t.blocks[m];
+        };
+        add(0, a.part_h, a.dH, M * K, d.strips(), d.bf16);
+        add(1, a.part_w, a.dW, K * N, d.tiles(), d.bf16);
+        add(2, a.part_b, a.db, N, d.tiles(), false);
+        if (total == 0) return FASTGL_OK;
+        hipLaunchKernelGGL(k_loss_add, dim3((unsigned)total), dim3(kBlock), 0, s, t);
+        FASTGL_LAUNCH_CHECK("fastgl_loss_bwd (sums)");
+        return FASTGL_OK;
+    }
     const Cut scores = d.scores_cut(), rows = d.rows_cut(), weights = d.weights_cut();
     for (int64_t n0 = 0; n0 < N; n0 += d.piece()) {
         const int64_t n = N - n0 < d.piece() ? N - n0 : d.piece();
