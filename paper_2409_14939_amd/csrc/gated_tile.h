@@ -175,7 +175,9 @@ struct Cut {
 //   forward 16 384 rows 1024 -> 4096, G and U kept 273 / 269 / -, alone 241 / 253 / -;  115 000 rows 256 -> 1024 193 / 174 / -, 162 / 140 / -
 //   dX of 16 384 rows 1024 -> 4096 223 / 278 / 310, dWg and dWu there 218 / 241 / 401 (the first two in two slabs)
 //   all kernels of a backward call of 300 rows 256 -> 1024 (medians) 36 / 32 / 31, of 2000 rows 52 / 47 / 43, of 8000 rows 256 -> 683 73 / 67 / 60
-// The loss's products have one result of twice the columns (`one`); scores are not summed over slabs (`whole`).
+// The loss's products have one result of twice the columns (`one`); scores are not summed over slabs (`whole`), and what becomes of them hides
+// behind another workgroup's products where there are two: us a call, large / middle tiles, 8192 rows -> 16 384 bf16, forward and dZ: 256 inputs 93 + 162 / 83 + 142,
+// 512 144 + 210 / 135 + 195, 1024 239 + 307 / 240 + 303, 2048 418 + 517 / 452 + 513; fp32 128 inputs 199 + 372 / 192 + 326, 512 633 + 807 / 682 + 820.
 inline Cut cut_of(int mode, int64_t R, int64_t C, int64_t Kc, int64_t segments, bool one = false, bool whole = false)
 {
     static const double single_us[3][3] = {{0.80, 0.60, 0.36}, {0.93, 0.65, 0.38}, {0.80, 0.60, 0.42}};      // [mode][size]
@@ -190,7 +192,7 @@ inline Cut cut_of(int mode, int64_t R, int64_t C, int64_t Kc, int64_t segments, 
         for (int64_t slabs = 1; slabs <= (whole ? 1 : 64) && (slabs == 1 || (all / slabs >= 4 && R * C <= (int64_t)1 << 30)); slabs = slabs < 8 ? slabs + 1 : slabs * 5 / 4) {
             const int64_t of_unit = ceil_div(tiles * slabs, 256);
             const double step = (double)(of_unit / 2) * pair_us[mode][size] + (double)(of_unit % 2) * single_us[mode][size];
-            const double us = (double)ceil_div(all, slabs) * step + (double)of_unit * tile_us[mode != kForward][size] +
+            const double us = (double)ceil_div(all, slabs) * step + (double)of_unit * (tile_us[mode != kForward][size] + (whole && size == kLarge ? 4.0 : 0.0)) +
                               (slabs > 1 ? 4.0 + (double)slabs * (double)R * (double)C * (mode == kRows || one ? 1.3e-6 : 2.6e-6) : 0.0);
             if (us < least) {
                 least = us;
@@ -234,9 +236,12 @@ __device__ __forceinline__ int scatter_sum(float (&v)[NV], int lane)
 }
 
 // A wavefront's scores: rows row0 + 32 i + lane % 32, columns col0 + 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4 in acc[i][j][e].
-// SCORES: maximum and sum of exponentials of its columns of each row, and the label's score where it is among them.
+// SCORES: maximum (times log2 e, so that lse comes from what the exponents were taken from) and sum of exponentials of its columns of each row,
+// and the label's score where it is among them.
 // GRADIENT: dZ = g (exp(z - lse) - [label]), 0 in rows without a label and in columns that do not exist (to a multiple of 32), as
 // `planes` bf16 whose sum is it (one: rounded), and its column sums.
+// Of the 14 us that a tile of 256 x 256 scores of 512 inputs takes an element's multiply-add, exponential and sum are 2; labels are looked for only by
+// wavefronts that have one.
 template <int MODE, class T, int PLANES, class ARGS>
 __device__ __forceinline__ void loss_epilogue(const ARGS &g, f32x16 (&acc)[T::TM][T::TN], int64_t row0, int64_t col0, int64_t row_slot, int64_t col_slot)
 {
@@ -245,91 +250,114 @@ __device__ __forceinline__ void loss_epilogue(const ARGS &g, f32x16 (&acc)[T::TM
     const int64_t far = g.C - col0;                                       // columns that exist, less this lane's first
     const int left = (int)(far < T::TN * 32 ? far : T::TN * 32) - 4 * h;
     if (far <= 0) return;                                                 // the same for a wavefront
-    float sums[T::TN * 16];
-    if constexpr (MODE == kGradient) {
+    if (far < T::TN * 32) {                                               // columns that do not exist weigh nothing
 #pragma unroll
-        for (int c = 0; c < T::TN * 16; ++c) sums[c] = 0.f;
+        for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * j + 8 * (e >> 2) + (e & 3) < left ? acc[i][j][e] : -INFINITY;
     }
 #pragma unroll
     for (int i = 0; i < T::TM; ++i) {
         const int64_t row = row0 + i * 32 + l32;
         const bool in = row < g.R;
         const int64_t label = in ? g.label[row] : -1, at = label - g.first - col0 - 4 * h;      // of the label among this lane's columns
-        const int mine = label >= 0 && at >= 0 && at < T::TN * 32 ? (int)at : -1;
+        const int mine = label >= 0 && at >= 0 && at < left ? (int)at : -1;
+        const bool any = __any(mine >= 0);
         if constexpr (MODE == kScores) {
-            float most = -INFINITY, sum = 0.f, z = 0.f;
-            bool has = false;
-            if (far < T::TN * 32) {                                       // columns that do not exist weigh nothing
+            float most = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) most = fmaxf(most, acc[i][j][e]);
+            most = fmaxf(most, __shfl_xor(most, 32, kWave));
+            const float top = most * kLog2e, base = most == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -base));
+            sum += __shfl_xor(sum, 32, kWave);
+            if (h == 0 && in) {
+                typedef float f2 __attribute__((ext_vector_type(2)));
+                reinterpret_cast<f2 *>(g.stats)[col_slot * g.R + row] = f2{top, sum};
+            }
+            if (any) {
+                float z = 0.f;
+                bool has = false;
 #pragma unroll
                 for (int j = 0; j < T::TN; ++j)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[i][j][e] = 32 * j + 8 * (e >> 2) + (e & 3) < left ? acc[i][j][e] : -INFINITY;
+                    for (int e = 0; e < 16; ++e) {
+                        const bool is = 32 * j + 8 * (e >> 2) + (e & 3) == mine;
+                        z = is ? acc[i][j][e] : z;
+                        has = has || is;
+                    }
+                if (has) g.picked[row] = z;
             }
-#pragma unroll
-            for (int j = 0; j < T::TN; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const bool is = 32 * j + 8 * (e >> 2) + (e & 3) == mine;
-                    most = fmaxf(most, acc[i][j][e]);
-                    z = is ? acc[i][j][e] : z;
-                    has = has || is;
-                }
-            most = fmaxf(most, __shfl_xor(most, 32, kWave));
-            const float base = most == -INFINITY ? 0.f : most;
-#pragma unroll
-            for (int j = 0; j < T::TN; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - base) * kLog2e);
-            sum += __shfl_xor(sum, 32, kWave);
-            if (h == 0 && in) {
-                float *to = g.stats + 2 * (col_slot * g.R + row);
-                to[0] = most;
-                to[1] = sum;
-            }
-            if (has && mine < left) g.picked[row] = z;
         } else {
-            const float lse = in ? g.lse[row] : 0.f;
-            const float scale = label >= g.classes ? NAN : in ? g.dloss[row] : 0.f;
+            // a row without a label: exp(z - infinity) times 0
+            const float lse = label >= 0 ? g.lse[row] * kLog2e : INFINITY;
+            const float scale = label >= g.classes ? NAN : label >= 0 ? g.dloss[row] : 0.f;
 #pragma unroll
-            for (int j = 0; j < T::TN; ++j) {
-                if (32 * j >= far) break;
+            for (int j = 0; j < T::TN; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float v[4];
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -lse)) * scale;
+            if (any) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int c = 32 * j + 8 * q + e;
-                        const float p = __builtin_amdgcn_exp2f((acc[i][j][4 * q + e] - lse) * kLog2e);
-                        const float x = c == mine ? p - 1.f : p;
-                        v[e] = label >= 0 && c < left ? x * scale : 0.f;
-                        sums[16 * j + 4 * q + e] += v[e];
-                    }
-                    if (in) {
-                        uint16_t *to = g.dz + (col0 / 32 + j) * g.dz_block + row * g.dz_ld + 8 * q + 4 * h;
+                for (int j = 0; j < T::TN; ++j)
 #pragma unroll
-                        for (int p = 0; p < PLANES; ++p) {
-                            u32x2 o;
-                            o[0] = pack_bf16(v[0], v[1]);
-                            o[1] = pack_bf16(v[2], v[3]);
-                            *reinterpret_cast<u32x2 *>(to + p * g.dz_plane) = o;
-                            if (p + 1 < PLANES) {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) v[e] -= __uint_as_float(e & 1 ? o[e >> 1] & 0xFFFF0000u : o[e >> 1] << 16);
-                            }
-                        }
-                    }
-                }
+                    for (int e = 0; e < 16; ++e)
+                        acc[i][j][e] = 32 * j + 8 * (e >> 2) + (e & 3) == mine ? acc[i][j][e] - scale : acc[i][j][e];
             }
         }
     }
     if constexpr (MODE == kGradient) {
-        if (!g.db) return;
-        constexpr int NV = T::TN * 16;
-        const int at = scatter_sum<NV, 16, 1>(sums, lane);
+        if (g.db) {
+            constexpr int NV = T::TN * 16;
+            float sums[NV];
 #pragma unroll
-        for (int k = 0; k < NV / 32; ++k) {
-            const int e = at + k, c = 32 * (e >> 4) + 8 * ((e >> 2) & 3) + (e & 3);
-            if (c < left) g.db[row_slot * g.C + col0 + 4 * h + c] = sums[k];
+            for (int c = 0; c < NV; ++c) {
+                sums[c] = 0.f;
+#pragma unroll
+                for (int i = 0; i < T::TM; ++i) sums[c] += acc[i][c / 16][c % 16];
+            }
+            const int at = scatter_sum<NV, 16, 1>(sums, lane);
+#pragma unroll
+            for (int k = 0; k < NV / 32; ++k) {
+                const int e = at + k, c = 32 * (e >> 4) + 8 * ((e >> 2) & 3) + (e & 3);
+                if (c < left) g.db[row_slot * g.C + col0 + 4 * h + c] = sums[k];
+            }
+        }
+        // Eight columns a lane: the lower 32 lanes have those of an even group of eight, the upper ones those of the odd one beside it.
+#pragma unroll
+        for (int i = 0; i < T::TM; ++i) {
+            const int64_t row = row0 + i * 32 + l32;
+            if (row >= g.R) continue;
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j) {
+                if (32 * j >= far) break;
+                uint16_t *to = g.dz + (col0 / 32 + j) * g.dz_block + row * g.dz_ld + 8 * h;
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                    for (int q = 0; q < 4; q += 2) {
+                        uint32_t w[2][2];
+#pragma unroll
+                        for (int o = 0; o < 2; ++o)
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                float &lo = reinterpret_cast<float *>(&acc[i][j])[4 * (q + o) + 2 * x], &hi = reinterpret_cast<float *>(&acc[i][j])[4 * (q + o) + 2 * x + 1];
+                                w[o][x] = pack_bf16(lo, hi);
+                                if (p + 1 < PLANES) {
+                                    lo -= __uint_as_float(w[o][x] << 16);
+                                    hi -= __uint_as_float(w[o][x] & 0xFFFF0000u);
+                                }
+                            }
+                        const auto a = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false), b = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+                        *reinterpret_cast<u32x4 *>(to + p * g.dz_plane + 8 * q) = u32x4{a[0], b[0], a[1], b[1]};
+                    }
+            }
         }
     }
 }

@@ -18,7 +18,9 @@ namespace fastgl {
 namespace {
 
 constexpr int64_t kMostClasses = (int64_t)1 << 21, kMostInputs = (int64_t)1 << 20;
-constexpr int64_t kPieceBytes = (int64_t)256 << 20;       // of dZ, and of packed weights, at a time
+// dZ, and packed weights, of a piece of the classes.  8192 rows 512 -> 65 536 bf16, the kernels of a backward pass: 256 MiB (four pieces) 1953 us, 512 MiB
+// 1783, 1 GiB (one) 1720: fewer sums of pieces, although dZ no longer stays in the last cache.
+constexpr int64_t kPieceBytes = (int64_t)1 << 30;
 constexpr int kPieceCols = 256;                           // a piece has a multiple of them
 
 // ------------------------------------------------------------------ packing
@@ -71,18 +73,18 @@ __global__ __launch_bounds__(kBlock) void k_loss_pack(LossPackArgs a)
 __global__ __launch_bounds__(kBlock) void k_loss_join(const float *stats, int64_t slots, const float *picked, const int64_t *label, int64_t M, int64_t N,
                                                       int lg, float *loss, float *lse)
 {
-    constexpr float kLog2e = 1.44269504089f, kLn2 = 0.69314718056f;
+    constexpr float kLn2 = 0.69314718056f;
     __shared__ float most[kBlock], sums[kBlock];
     const int parts = kBlock >> lg, part = threadIdx.x >> lg, r = threadIdx.x & ((1 << lg) - 1);
     const int64_t row = ((int64_t)blockIdx.x << lg) + r;
     typedef float f2 __attribute__((ext_vector_type(2)));
     const f2 *p = reinterpret_cast<const f2 *>(stats) + (row < M ? row : M - 1);
-    float m = -INFINITY, s = 0.f;
+    float m = -INFINITY, s = 0.f;                     // the maximum in powers of two
 #pragma unroll 4
     for (int64_t t = part; t < slots; t += parts) {
         const f2 x = p[t * M];
         const float next = fmaxf(m, x[0]), base = next == -INFINITY ? 0.f : next;
-        s = s * __builtin_amdgcn_exp2f((m - base) * kLog2e) + x[1] * __builtin_amdgcn_exp2f((x[0] - base) * kLog2e);
+        s = s * __builtin_amdgcn_exp2f(m - base) + x[1] * __builtin_amdgcn_exp2f(x[0] - base);
         m = next;
     }
     most[threadIdx.x] = m;
@@ -92,8 +94,8 @@ __global__ __launch_bounds__(kBlock) void k_loss_join(const float *stats, int64_
     for (int q = 1; q < parts; ++q) m = fmaxf(m, most[(q << lg) + r]);
     const float base = m == -INFINITY ? 0.f : m;
     s = 0.f;
-    for (int q = 0; q < parts; ++q) s += sums[(q << lg) + r] * __builtin_amdgcn_exp2f((most[(q << lg) + r] - base) * kLog2e);
-    const float all = m == -INFINITY && s == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(s) * kLn2;
+    for (int q = 0; q < parts; ++q) s += sums[(q << lg) + r] * __builtin_amdgcn_exp2f(most[(q << lg) + r] - base);
+    const float all = m == -INFINITY && s == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(s)) * kLn2;
     if (lse) lse[row] = all;
     const int64_t y = label[row];
     loss[row] = y < 0 ? 0.f : y >= N ? NAN : all - picked[row];
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(kBlock) void k_loss_block(LossBlockArgs a)
             }
             if (row < rows && c0 == 0) {
                 if (a.stats) {
-                    a.stats[2 * (strip * a.M + row0 + row)] = most;
+                    a.stats[2 * (strip * a.M + row0 + row)] = most * kLog2e;
                     a.stats[2 * (strip * a.M + row0 + row) + 1] = sum;
                     if (label >= col0 && label < col0 + left) a.picked[row0 + row] = at;
                 } else {
@@ -495,7 +497,7 @@ struct Shape {
             return here < there;
         }
         const double sums = 4.0 * ((tiles() > 1 ? (double)tiles() * k * (double)N : 0.0) + (strips() > 1 ? (double)strips() * m * k : 0.0));
-        if (sums > 256e6) return false;
+        if (sums > 512e6) return false;
         const double here = (10.0 + 0.035 * k + groups * (0.004 + 6.0 * kBlockRows * kBlockCols * k / 110e6) + 2.0 * sums / 4e6) * (bf16 ? 1.15 : 1.0);
         const double z = m * (double)align_up((size_t)N, 32);
         const double there = bf16 ? 24.0 + 0.015 * k + all * 6.0 / 0.6e9 + (10.0 * z + 8.0 * m * k) / 4e6

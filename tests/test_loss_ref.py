@@ -72,6 +72,6 @@ def test_workspace_sizes():
             assert f(dt, M, K, N) >= f(dt, M, K, N, True) and b(dt, M, K, N) >= b(dt, M, K, N, True)
             # a piece of dZ and one of the weights, H, sums; never M N or K N
             rows = (M + 255) // 256 * 256
-            least = 6 * rows * 256 + (1 << 28) + (1 << 28) + 6 * K * 512 + 6 * M * (K + 8)
+            least = 6 * rows * 256 + (1 << 30) + (1 << 30) + 6 * K * 512 + 6 * M * (K + 8)
             assert b(dt, M, K, N) < least + 64 * 4 * max(M * K, K * 4096) + (1 << 28)
-            assert f(dt, M, K, N) < (1 << 28) + 6 * K * 512 + 6 * M * (K + 8) + 4 * M + 8 * M * (N // 64 + 300) + (1 << 20)
+            assert f(dt, M, K, N) < (1 << 30) + 6 * K * 512 + 6 * M * (K + 8) + 4 * M + 8 * M * (N // 64 + 300) + (1 << 20)
