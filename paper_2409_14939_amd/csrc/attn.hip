@@ -22,6 +22,7 @@ namespace {
 
 constexpr float kLog2e = 1.44269504089f, kLn2 = 0.69314718056f;
 constexpr int kSegment = 16;              // steps that a group takes where a neighbour has more
+constexpr int kSlack = 8;                 // steps more than shorter segments have that a group takes alone rather than have them cut
 constexpr int kBiasBlocks = 1024;         // workgroups of k_attn_dbias
 constexpr int kJoin = 1024;               // threads of a workgroup that joins chunks
 constexpr int kBiasTile = 64;             // buckets of one of its passes
@@ -156,6 +157,7 @@ struct AttnArgs {
     int64_t units;                 // rows (dealt: to a multiple of 512) x heads (transposed: x key heads)
     int64_t rows;
     int32_t dealt;                 // rows are taken 64 apart
+    int32_t units_a_wave;          // the groups of a wavefront or fewer
     uint64_t heads_inv;            // ceil(2^64 / heads of a unit), 0 for one
     uint32_t shared_inv;           // ceil(2^32 / shared), 0 for one: exact for 2^20 query heads of edges at most 4096 of which share
     uint32_t buckets;              // edges of this bucket and above are left out
@@ -254,9 +256,10 @@ __device__ __forceinline__ float bias_of(const AttnArgs &a, int bucket, int h)
 // ------------------------------------------------------------------ the walk
 // ROW has the operands and sums of one row and head (or of a part of its edges), the pass's arithmetic and where its results go.
 //
-// A group takes one row and head, a unit.  Where a unit of the wavefront has more than kSegment steps, all its units' steps are cut into segments of
-// so many, which the groups take in turn, so that nobody waits long for a neighbour's row: segments of one unit lie side by side, their sums are
-// joined across the groups and then with what earlier turns left in LDS.  Chunks of long rows, which the first wavefronts take after their own rows,
+// A group takes one row and head, a unit; where there are few units a wavefront has fewer of them than groups.  Where a unit of the wavefront has more
+// than kSegment steps, all its units' steps are cut into segments of so many, which the groups take in turn, so that nobody waits long for a
+// neighbour's row: segments of one unit lie side by side, their sums are joined across the groups and then with what earlier turns left in LDS.  Where
+// there are few units segments are as short as gives every group one.  Chunks of long rows, which the first wavefronts take after their own rows,
 // are units too, as many at a time as give every group a segment.
 //
 // Rows of sources are dealt to the wavefronts 64 apart: those that are neighbours of many often have numbers that lie together.
@@ -291,11 +294,11 @@ __device__ __forceinline__ void walk_units(const AttnArgs &a)
         int64_t chunk = -1;
         bool on;
         if (at < 0) {
-            const int64_t unit = wave * G + gw;
+            const int64_t unit = wave * a.units_a_wave + gw;
             int64_t to = (int64_t)over((uint64_t)unit, a.heads_inv);
             h = (int)(unit - to * a.unit_heads);
             if (T && a.dealt) to = (to & ~(int64_t)511) | ((to & 7) << 6) | ((to >> 3) & 63);
-            on = unit < a.units && to < a.rows;
+            on = gw < a.units_a_wave && unit < a.units && to < a.rows;
             if (on) {
                 row = (int)to;
                 beg = a.ptr[row];
@@ -320,9 +323,18 @@ __device__ __forceinline__ void walk_units(const AttnArgs &a)
                 steps = ((beg + kLongChunk < last ? beg + kLongChunk : last) - beg) * mult;
             }
         }
-        const int segments = (steps + kSegment - 1) / kSegment;
+        int size = kSegment, slack = 0;               // steps of a segment
+        if (a.units_a_wave < G) {
+            int sum = steps;
+#pragma unroll
+            for (int d = L; d < kWave; d <<= 1) sum += __shfl_xor(sum, d, kWave);
+            const int fair = (sum + G * U - 1) / (G * U) * U;
+            size = fair < U ? U : fair < kSegment ? fair : kSegment;
+            slack = kSlack;
+        }
+        const int segments = (steps + size - 1) / size;
         int upto = segments, total = 1;               // of this group and those before, and of all
-        const bool cut = __any(segments > 1);
+        const bool cut = __any(steps > size + slack);
         auto fence = []() __attribute__((always_inline)) {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");          // a wavefront's LDS accesses are carried out in order
             __builtin_amdgcn_wave_barrier();
@@ -350,8 +362,8 @@ __device__ __forceinline__ void walk_units(const AttnArgs &a)
                 its_h = __shfl(h, from, kWave);
                 its_beg = __shfl(beg, from, kWave);
                 its_end = __shfl(steps, from, kWave);
-                i = (segment - __shfl(upto - segments, from, kWave)) * kSegment;
-                if (i + kSegment < its_end) its_end = i + kSegment;
+                i = (segment - __shfl(upto - segments, from, kWave)) * size;
+                if (i + size < its_end) its_end = i + size;
                 if (segment >= total) i = its_end = 0;
             }
             walk(its_row, its_h, its_beg, i, its_end);
@@ -383,7 +395,7 @@ __device__ __forceinline__ void walk_units(const AttnArgs &a)
 template <bool BF16, int PC, int LG_, bool NEAR>
 struct ForwardRow {
     typedef Piece<BF16, PC> P;
-    static constexpr int LG = LG_, N = P::N, UNROLL = 2;
+    static constexpr int LG = LG_, N = P::N, UNROLL = LG >= 4 ? 4 : 2;
     static constexpr bool T = false;
     const AttnArgs &a;
     const Where<P, LG, NEAR> w;
@@ -492,7 +504,7 @@ struct ForwardRow {
 };
 
 template <bool BF16, int PC, int LG, bool NEAR>
-__global__ __launch_bounds__(kBlock, 4) void k_attn_fwd(AttnArgs a)
+__global__ __launch_bounds__(kBlock, LG >= 4 ? 3 : 4) void k_attn_fwd(AttnArgs a)
 {
     walk_units<ForwardRow<BF16, PC, LG, NEAR>>(a);
 }
@@ -503,7 +515,7 @@ __global__ __launch_bounds__(kBlock, 4) void k_attn_fwd(AttnArgs a)
 template <bool BF16, int PC, int LG_, bool NEAR>
 struct QueryRow {
     typedef Piece<BF16, PC> P;
-    static constexpr int LG = LG_, N = P::N, UNROLL = 2;
+    static constexpr int LG = LG_, N = P::N, UNROLL = LG >= 4 ? 4 : 2;
     static constexpr bool T = false;
     const AttnArgs &a;
     const Where<P, LG, NEAR> w;
@@ -636,7 +648,7 @@ struct QueryRow {
 };
 
 template <bool BF16, int PC, int LG, bool NEAR>
-__global__ __launch_bounds__(kBlock, BF16 ? 3 : 4) void k_attn_dq(AttnArgs a)
+__global__ __launch_bounds__(kBlock, LG >= 4 ? 2 : BF16 ? 3 : 4) void k_attn_dq(AttnArgs a)
 {
     if (a.bucket_to)
         for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < a.edges; i += (int64_t)gridDim.x * kBlock) a.bucket_to[i] = a.bucket_from[a.eid[i]];
@@ -1085,7 +1097,12 @@ fastgl_status launch_walk(AttnArgs a, const fastgl_attn_desc &d, const fastgl_pl
     const fastgl_status st = by_shape(d.dtype, d.width, near, [&](auto bf16, auto pc, auto lg, auto near_) {
         constexpr bool B = decltype(bf16)::value, NEAR = decltype(near_)::value;
         constexpr int PC = decltype(pc)::value, LG = decltype(lg)::value;
-        const int64_t blocks = ceil_div(a.units, (int64_t)(kBlock >> LG));
+        // Fewer units a wavefront where there are few: so many that four wavefronts a compute unit have some, sixteen for rows of sources and wide heads
+        // (few groups a wavefront).  us, units to all groups / so: 105 rows of 15 heads, 93 sources, dK and dV 59 / 9;  597 rows of up to 350 edges, heads
+        // of 160 fp32 columns, forward 87 / 46;  16 843 rows of 16, 2 heads of 12 columns, dQ 10.4 / 10.4, with sixteen 17.
+        const int64_t groups = kWave >> LG, few = ceil_div(a.units, T || LG >= 4 ? 4096 : 1024);
+        a.units_a_wave = (int32_t)(few <= groups / 2 ? few : groups);
+        const int64_t blocks = ceil_div(a.units, (int64_t)a.units_a_wave * (kBlock / kWave));
         if (blocks > INT32_MAX) {
             set_error("%s: too many rows and heads", names[PASS]);
             return FASTGL_ERR_UNSUPPORTED;
