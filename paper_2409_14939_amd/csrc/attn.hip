@@ -823,7 +823,10 @@ __global__ __launch_bounds__(kJoin) void k_attn_join(AttnArgs a, int lg)
         for (int r = 0; r < parts; ++r) {
             const float by = KIND == 2 ? 1.f : exp_of(most[(r << lg) + c] - all);
 #pragma unroll
-            for (int i = 0; i < NS; ++i) v[i] += by == 0.f ? 0.f : by * sums[i][(r << lg) + c];
+            for (int i = 0; i < NS; ++i) {            // a sum of NaN (its scores leave no maximum) stays: every result is divided by it
+                const bool none = by == 0.f && (KIND == 2 || i != 1);
+                v[i] += none ? 0.f : by * sums[i][(r << lg) + c];
+            }
         }
         auto put = [&](void *out, int64_t ld, float x) {
             if (!out) return;

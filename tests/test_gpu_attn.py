@@ -188,6 +188,29 @@ def test_rows_that_are_not_finite_change_no_other():
         assert torch.equal(a[[0, 2]], b[[0, 2]]) and bool(b[1].isnan().all())
 
 
+def test_long_rows_that_are_not_finite():
+    """A row of several chunks: NaN in all its scores, in those of one chunk alone (scores of NaN leave no maximum), and in one of them."""
+    ptr = np.array([0, 5, 905, 908], np.int32)
+    blk = bg.Block(ptr, np.arange(908, dtype=np.int32), 3, 908)
+    for dtype in ("f32", "bf16"):
+        clean = Case(blk, 2, 1, 20, dtype, None).on_gpu()
+        O, lse = clean.forward()
+        dQ, dK, dV, _ = clean.gradients()
+        for what in ("query", "chunk", "edge"):
+            c = Case(blk, 2, 1, 20, dtype, None)
+            if what == "query":
+                c.Q[1] = float("nan")
+            else:
+                c.KV[5 + 128:5 + 256 if what == "chunk" else 5 + 129] = float("nan")
+            c.on_gpu()
+            O2, lse2 = c.forward()
+            dQ2, dK2, dV2, _ = c.gradients()
+            for a, b in ((O, O2), (lse, lse2), (dQ, dQ2)):
+                assert torch.equal(a[[0, 2]], b[[0, 2]]) and bool(b[1].isnan().all()), what
+            for a, b in ((dK, dK2), (dV, dV2)):
+                assert torch.equal(a[:5], b[:5]) and torch.equal(a[905:], b[905:]) and bool(b[5:905].isnan().all()), what
+
+
 @pytest.mark.parametrize("size,scale", [(8.0, 1.0), (1.0, -0.3), (30.0, 0.1), (1e-3, 1.0), (1.0, 0.0)])
 def test_sizes_of_scores(size, scale):
     """Scores of several hundred, of either sign of the scale, and all the same."""
