@@ -170,6 +170,9 @@ struct AttnArgs {
     int64_t part_stride;           // between the two arrays of `part` that a backward pass has
 };
 
+// Launches of more than 2^32 threads have two dimensions.
+__device__ __forceinline__ int64_t block_of() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 __device__ __forceinline__ uint64_t over(uint64_t n, uint64_t inv) { return inv ? __umul64hi(n, inv) : n; }
 __device__ __forceinline__ uint32_t over(uint32_t n, uint32_t inv) { return inv ? __umulhi(n, inv) : n; }
 
@@ -273,7 +276,7 @@ __device__ __forceinline__ void walk_units(const AttnArgs &a)
     ROW r(a);
     const int lane = threadIdx.x & (kWave - 1), gw = r.w.g, mult = T ? a.shared : 1;
     const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t wave = (int64_t)blockIdx.x * (kBlock / kWave) + in_block;
+    const int64_t wave = block_of() * (kBlock / kWave) + in_block;
     float (&slots)[ROW::VALUES][kWave] = kept[in_block];
     // Steps i .. steps of a row, U at a time; the last U / 2 in one of half the size.
     auto walk = [&](int row, int h, int beg, int i, int steps) __attribute__((always_inline)) {
@@ -651,7 +654,7 @@ template <bool BF16, int PC, int LG, bool NEAR>
 __global__ __launch_bounds__(kBlock, LG >= 4 ? 2 : BF16 ? 3 : 4) void k_attn_dq(AttnArgs a)
 {
     if (a.bucket_to)
-        for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < a.edges; i += (int64_t)gridDim.x * kBlock) a.bucket_to[i] = a.bucket_from[a.eid[i]];
+        for (int64_t i = block_of() * kBlock + threadIdx.x; i < a.edges; i += (int64_t)gridDim.x * gridDim.y * kBlock) a.bucket_to[i] = a.bucket_from[a.eid[i]];
     walk_units<QueryRow<BF16, PC, LG, NEAR>>(a);
 }
 
@@ -904,7 +907,7 @@ __global__ __launch_bounds__(kBlock) void k_attn_dbias_sum(const float *part, in
 {
     __shared__ double sums[kBlock / 8][9];
     const int c = threadIdx.x & 7, r = threadIdx.x >> 3;
-    const int64_t at = (int64_t)blockIdx.x * 8 + c;
+    const int64_t at = block_of() * 8 + c;
     double v = 0.0;
     if (at < n) {
 #pragma unroll 4
@@ -1072,6 +1075,12 @@ fastgl_status by_shape(fastgl_dtype dtype, int64_t width, bool near, F f)
     return bf16 ? lanes(Yes(), No()) : lanes(No(), No());
 }
 
+dim3 grid_of(int64_t blocks)                          // blocks beyond the last have nothing
+{
+    const int64_t x = (int64_t)1 << 20;
+    return blocks <= x ? dim3((unsigned)blocks) : dim3((unsigned)x, (unsigned)ceil_div(blocks, x));
+}
+
 enum Pass { kPassFwd = 0, kPassDq = 1, kPassDkv = 2 };
 
 // One walk and the launch that joins its chunks.
@@ -1106,15 +1115,15 @@ fastgl_status launch_walk(AttnArgs a, const fastgl_attn_desc &d, const fastgl_pl
         const int64_t groups = kWave >> LG, few = ceil_div(a.units, T || LG >= 4 ? 4096 : 1024);
         a.units_a_wave = (int32_t)(few <= groups / 2 ? few : groups);
         const int64_t blocks = ceil_div(a.units, (int64_t)a.units_a_wave * (kBlock / kWave));
-        if (blocks > INT32_MAX) {
+        if (blocks > (int64_t)65535 << 20) {
             set_error("%s: too many rows and heads", names[PASS]);
             return FASTGL_ERR_UNSUPPORTED;
         }
         a.chunk_waves = (int32_t)((blocks < 2048 ? blocks : 2048) * (kBlock / kWave));
-        if constexpr (PASS == kPassFwd) hipLaunchKernelGGL((k_attn_fwd<B, PC, LG, NEAR>), dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
-        else if constexpr (PASS == kPassDq) hipLaunchKernelGGL((k_attn_dq<B, PC, LG, NEAR>), dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
-        else if (a.shared == 1) hipLaunchKernelGGL((k_attn_dkv<B, PC, LG, NEAR, 1>), dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
-        else hipLaunchKernelGGL((k_attn_dkv<B, PC, LG, NEAR, 2>), dim3((unsigned)blocks), dim3(kBlock), 0, s, a);
+        if constexpr (PASS == kPassFwd) hipLaunchKernelGGL((k_attn_fwd<B, PC, LG, NEAR>), grid_of(blocks), dim3(kBlock), 0, s, a);
+        else if constexpr (PASS == kPassDq) hipLaunchKernelGGL((k_attn_dq<B, PC, LG, NEAR>), grid_of(blocks), dim3(kBlock), 0, s, a);
+        else if (a.shared == 1) hipLaunchKernelGGL((k_attn_dkv<B, PC, LG, NEAR, 1>), grid_of(blocks), dim3(kBlock), 0, s, a);
+        else hipLaunchKernelGGL((k_attn_dkv<B, PC, LG, NEAR, 2>), grid_of(blocks), dim3(kBlock), 0, s, a);
         FASTGL_LAUNCH_CHECK(names[PASS]);
         return FASTGL_OK;
     });
@@ -1272,7 +1281,7 @@ fastgl_status fastgl_attn_bwd(const fastgl_attn_desc *desc, const void *dO, int6
     const size_t lds = sizeof(float) * kBlock * (size_t)(d.num_buckets < kBiasTile ? d.num_buckets : kBiasTile);
     hipLaunchKernelGGL(k_attn_dbias, grid, dim3(kBlock), lds, s, c);
     FASTGL_LAUNCH_CHECK("fastgl_attn_bwd (dbias)");
-    hipLaunchKernelGGL(k_attn_dbias_sum, dim3((unsigned)ceil_div(table, 8)), dim3(kBlock), 0, s, (const float *)o.bias, (int)blocks, table, dbias);
+    hipLaunchKernelGGL(k_attn_dbias_sum, grid_of(ceil_div(table, 8)), dim3(kBlock), 0, s, (const float *)o.bias, (int)blocks, table, dbias);
     FASTGL_LAUNCH_CHECK("fastgl_attn_bwd (dbias, sums)");
     return FASTGL_OK;
 }

@@ -117,14 +117,15 @@ template <bool BF16>
 __global__ __launch_bounds__(kBlock) void k_loss_sum(LossSumArgs a)
 {
     if ((int)blockIdx.x < a.blocks) {
-        const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x, n = a.R * a.C;
-        if (i >= n) return;
-        double v = 0.0;
+        const int64_t n = a.R * a.C;
+        for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += (int64_t)a.blocks * kBlock) {
+            double v = 0.0;
 #pragma unroll 8
-        for (int s = 0; s < a.slabs; ++s) v += (double)a.part[(int64_t)s * n + i];
-        const int64_t row = i / a.C, to = row * a.ldo + (i - row * a.C);
-        if constexpr (BF16) static_cast<uint16_t *>(a.out)[to] = __builtin_bit_cast(uint16_t, (__bf16)(float)v);
-        else static_cast<float *>(a.out)[to] = (float)v;
+            for (int s = 0; s < a.slabs; ++s) v += (double)a.part[(int64_t)s * n + i];
+            const int64_t row = i / a.C, to = row * a.ldo + (i - row * a.C);
+            if constexpr (BF16) static_cast<uint16_t *>(a.out)[to] = __builtin_bit_cast(uint16_t, (__bf16)(float)v);
+            else static_cast<float *>(a.out)[to] = (float)v;
+        }
         return;
     }
     __shared__ double sums[kBlock / 8][9];                             // eight columns, 32 threads a column
@@ -610,7 +611,7 @@ fastgl_status launch_block(const Shape &d, LossBlockArgs a, hipStream_t s, const
 fastgl_status launch_join(const Scratch &o, int64_t slots, const int64_t *label, int64_t M, int64_t N, float *loss, float *lse, hipStream_t s)
 {
     int lg = 0;
-    while (lg < 5 && ((int64_t)1 << lg) < M) ++lg;
+    while ((lg < 5 && ((int64_t)1 << lg) < M) || (lg < 8 && M >> lg >= (int64_t)1 << 22)) ++lg;       // a launch has less than 2^32 threads
     hipLaunchKernelGGL(k_loss_join, dim3((unsigned)ceil_div(M, (int64_t)1 << lg)), dim3(kBlock), 0, s, (const float *)o.stats, slots, (const float *)o.picked,
                        label, M, N, lg, loss, lse);
     FASTGL_LAUNCH_CHECK("fastgl_loss_fwd (rows)");
@@ -650,7 +651,7 @@ fastgl_status launch(const LossTileArgs &args, const Cut &cut, bool bf16, hipStr
 {
     typename TileArgsOf<MODE>::type g = args;
     const int64_t tr = ceil_div(g.R, Shape::tile_rows(cut)), tc = ceil_div(g.C, cut.size == kSmall ? 128 : 256), total = tr * tc * cut.slabs;
-    if (total > 0x7FFFFFFFLL || 4 * tc > 0x7FFFFFFFLL) {
+    if (total > (int64_t)UINT32_MAX / 512 || 4 * tc > 0x7FFFFFFFLL) {
         set_error("%s: too many tiles (%lld)", what, (long long)total);
         return FASTGL_ERR_UNSUPPORTED;
     }
@@ -673,7 +674,8 @@ fastgl_status launch(const LossTileArgs &args, const Cut &cut, bool bf16, hipStr
 
 fastgl_status launch_sum(LossSumArgs a, bool bf16, hipStream_t s, const char *what)
 {
-    a.blocks = (int32_t)(a.part ? ceil_div(a.R * a.C, kBlock) : 0);
+    const int64_t blocks = a.part ? ceil_div(a.R * a.C, kBlock) : 0, most = (int64_t)1 << 20;        // a launch has less than 2^32 threads
+    a.blocks = (int32_t)(blocks < most ? blocks : most);
     const dim3 grid((unsigned)(a.blocks + (a.db_part ? ceil_div((int64_t)a.db_cols, 8) : 0)));
     if (bf16) hipLaunchKernelGGL(k_loss_sum<true>, grid, dim3(kBlock), 0, s, a);
     else hipLaunchKernelGGL(k_loss_sum<false>, grid, dim3(kBlock), 0, s, a);

@@ -64,3 +64,68 @@ def test_many_rows_and_many_classes(M, K, N, dtype):
         want, off = getattr(ref, name), getattr(ref, "off_" + name)
         bad = (got.double() - want).abs() > off + HALF[t] * (want.abs() + off)
         assert not bool(bad.any()), (name, int(bad.sum()))
+
+
+def test_attention_of_more_workgroups_than_a_launch_has_in_one_dimension():
+    """Rows of one edge: O is the neighbour's V, dV the target's dO, bit for bit."""
+    n, heads, D = (1 << 23) + 3, 5, 2
+    g = torch.Generator(device="cuda").manual_seed(4)
+    col = torch.randperm(n, generator=g, device="cuda", dtype=torch.int32)
+    ptr = torch.arange(n + 1, device="cuda", dtype=torch.int32)
+    Q, K, V, dO = (torch.randn(n, heads * D, generator=g, device="cuda").bfloat16() for _ in range(4))
+    bucket = torch.arange(n, device="cuda", dtype=torch.int32) % 3
+    how = dict(heads=heads, bucket=bucket, bias=torch.zeros(3, heads, device="cuda"))
+    O, lse = B.fastgl_attn_fwd(ptr, col, Q, K, V, **how)
+    assert torch.equal(O, V[col.long()]) and bool(torch.isfinite(lse).all())
+    dQ, dK, dV, dbias = B.fastgl_attn_bwd(ptr, col, Q, K, V, dO, **how)
+    assert torch.equal(dV[col.long()], dO) and float(dQ.abs().max()) < 2.0 ** -14
+
+
+def test_a_bias_of_very_many_buckets_and_heads():
+    """A row of one edge (its gradient is 0) and one of two, whose gradients are in the table's last rows."""
+    heads, buckets = 4096, 65536
+    g = torch.Generator(device="cuda").manual_seed(5)
+    ptr = torch.tensor([0, 1, 3], device="cuda", dtype=torch.int32)
+    col = torch.tensor([0, 1, 2], device="cuda", dtype=torch.int32)
+    Q, K, V, dO = (torch.randn(r, heads, generator=g, device="cuda") for r in (2, 3, 3, 2))
+    bucket = torch.tensor([7, buckets - 1, buckets - 2], device="cuda", dtype=torch.int32)
+    bias = torch.zeros(buckets, heads, device="cuda")
+    dbias = B.fastgl_attn_bwd(ptr, col, Q, K, V, dO, heads=heads, bucket=bucket, bias=bias)[3]
+    s = (Q[1] * K[1:]).double()
+    p = torch.softmax(s, 0)
+    dp = (dO[1] * V[1:]).double()
+    ds = p * (dp - (p * dp).sum(0))
+    # scores below 32, |dp| below 32: a weight is off by 2^-23 (2 + |s|) and dp's difference by 2^-22 of it
+    torch.testing.assert_close(dbias[-2:].flip(0).double(), ds, rtol=0, atol=2.0 ** -23 * 40 * 64)
+    assert not bool(dbias[:-2].any())
+
+
+def test_the_loss_of_half_a_billion_rows():
+    M, N = (1 << 29) + 5, 2
+    g = torch.Generator(device="cuda").manual_seed(6)
+    H = torch.randn(M, 1, generator=g, device="cuda", dtype=torch.bfloat16)
+    W, b = torch.randn(1, N, generator=g, device="cuda").bfloat16(), torch.zeros(N, device="cuda")
+    label = torch.randint(-1, N, (M,), generator=g, device="cuda")
+    loss, lse = B.fastgl_loss_fwd(H, W, b, label)
+    for at in (0, M // 2, M - 100_000):
+        part = slice(at, at + 100_000)
+        ref = Loss(H[part], W, b, label[part])
+        for got, name in ((loss[part], "loss"), (lse[part], "lse")):
+            want, off = getattr(ref, name), getattr(ref, "off_" + name)
+            assert not bool(((got.double() - want).abs() > off + 2.0 ** -24 * (want.abs() + off)).any()), (name, at)
+
+
+def test_row_gradients_of_four_billion_elements():
+    """dH of 2^32 elements from two pieces of the classes, whose sums are joined."""
+    M, K, N = (1 << 25) + 3, 128, 300
+    g = torch.Generator(device="cuda").manual_seed(7)
+    H = torch.randn(M, K, generator=g, device="cuda", dtype=torch.bfloat16)
+    W, b = (torch.randn(K, N, generator=g, device="cuda") / 8).bfloat16(), torch.zeros(N, device="cuda")
+    label, dloss = torch.randint(-1, N, (M,), generator=g, device="cuda"), torch.randn(M, generator=g, device="cuda")
+    _, lse = B.fastgl_loss_fwd(H, W, b, label)
+    dH = B.fastgl_loss_bwd(H, W, b, label, lse, dloss, want=("dH",))[0]
+    for at in (0, M // 2, M - 5000):
+        part = slice(at, at + 5000)
+        ref = Loss(H[part], W, b, label[part]).backward(dloss[part])
+        off = ref.off_dH
+        assert not bool(((dH[part].double() - ref.dH).abs() > off + 2.0 ** -8 * (ref.dH.abs() + off)).any()), at
