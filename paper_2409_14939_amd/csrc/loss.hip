@@ -166,6 +166,7 @@ struct LossBlockArgs {
 };
 
 constexpr int kBlockRows = 32, kBlockCols = 64, kPad = 68;
+constexpr int kAddThreads = 1024, kAddLg = 10;
 
 // Elements by 32-bit offsets: arrays of small calls have fewer than 2^27 elements.
 template <bool BF16>
@@ -198,11 +199,11 @@ __device__ __forceinline__ void put_result(void *out, float *part, uint32_t at, 
     else *reinterpret_cast<float *>(static_cast<char *>(out) + 4 * at) = x;
 }
 
-template <bool BF16, bool BACKWARD>
-__global__ __launch_bounds__(kBlock) void k_loss_block(LossBlockArgs a)
+template <bool BF16, bool BACKWARD, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_loss_block(LossBlockArgs a)
 {
     constexpr float kLog2e = 1.44269504089f, kLn2 = 0.69314718056f;
-    constexpr int WAVES = kBlock / kWave;
+    constexpr int WAVES = THREADS / kWave, PER = THREADS / kBlockRows, CE = kBlockCols / PER;      // threads a row, columns of each
     __shared__ float z[WAVES][kBlockRows][kPad];
     __shared__ float on[kBlockRows];
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r = lane & 31, h = lane >> 5;
@@ -251,14 +252,14 @@ __global__ __launch_bounds__(kBlock) void k_loss_block(LossBlockArgs a)
 #pragma unroll
         for (int e = 0; e < 16; ++e) z[wave][8 * (e >> 2) + 4 * h + (e & 3)][32 * q + r] = acc[q][e];
     __syncthreads();
-    // ---- statistics or dZ: eight threads a row, eight columns each
+    // ---- statistics or dZ: some columns of a row each thread
     {
-        const int row = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 8;
+        const int row = threadIdx.x / PER, c0 = threadIdx.x % PER * CE;
         const int64_t label = row < rows ? a.label[row0 + row] : -1;
         const int mine = label >= col0 && label < col0 + left ? (int)(label - col0) - c0 : -1;       // of the label among these columns
-        float v[8];
+        float v[CE];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
+        for (int c = 0; c < CE; ++c) {
             float s = 0.f;
 #pragma unroll
             for (int i = 0; i < WAVES; ++i) s += z[i][row][c0 + c];
@@ -268,17 +269,17 @@ __global__ __launch_bounds__(kBlock) void k_loss_block(LossBlockArgs a)
         if constexpr (!BACKWARD) {
             float most = -INFINITY, sum = 0.f, at = 0.f;
 #pragma unroll
-            for (int c = 0; c < 8; ++c) most = fmaxf(most, v[c]);
+            for (int c = 0; c < CE; ++c) most = fmaxf(most, v[c]);
 #pragma unroll
-            for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, kWave));
+            for (int d = 1; d < PER; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, kWave));
             const float base = most == -INFINITY ? 0.f : most;
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
+            for (int c = 0; c < CE; ++c) {
                 sum += __builtin_amdgcn_exp2f((v[c] - base) * kLog2e);
                 at = c == mine ? v[c] : at;
             }
 #pragma unroll
-            for (int d = 1; d < 8; d <<= 1) {
+            for (int d = 1; d < PER; d <<= 1) {
                 sum += __shfl_xor(sum, d, kWave);
                 at += __shfl_xor(at, d, kWave);
             }
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(kBlock) void k_loss_block(LossBlockArgs a)
             const float lse = label >= 0 ? a.lse_in[row0 + row] : 0.f;
             const float scale = label >= a.N ? NAN : label >= 0 ? a.dloss[row0 + row] : 0.f;
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
+            for (int c = 0; c < CE; ++c) {
                 const float p = __builtin_amdgcn_exp2f((v[c] - lse) * kLog2e), x = c == mine ? p - 1.f : p;
                 z[0][row][c0 + c] = label >= 0 && c0 + c < left ? x * scale : 0.f;
             }
@@ -398,9 +399,9 @@ struct LossAddArgs {
     int32_t parts[3], lg[3], bf16[3];
 };
 
-__global__ __launch_bounds__(kBlock) void k_loss_add(LossAddArgs a)
+__global__ __launch_bounds__(kAddThreads) void k_loss_add(LossAddArgs a)
 {
-    __shared__ double sums[kBlock];
+    __shared__ double sums[kAddThreads];
     int64_t block = blockIdx.x;
     int m = 0;
     for (; m < 2 && block >= a.blocks[m]; ++m) block -= a.blocks[m];
@@ -409,7 +410,7 @@ __global__ __launch_bounds__(kBlock) void k_loss_add(LossAddArgs a)
     const int64_t n = m == 0 ? a.n[0] : m == 1 ? a.n[1] : a.n[2];
     const int parts = m == 0 ? a.parts[0] : m == 1 ? a.parts[1] : a.parts[2], lg = m == 0 ? a.lg[0] : m == 1 ? a.lg[1] : a.lg[2];
     const int bf16 = m == 0 ? a.bf16[0] : m == 1 ? a.bf16[1] : a.bf16[2];
-    const int c = threadIdx.x & ((1 << lg) - 1), t = threadIdx.x >> lg, threads = kBlock >> lg;
+    const int c = threadIdx.x & ((1 << lg) - 1), t = threadIdx.x >> lg, threads = kAddThreads >> lg;
     const int64_t i = (block << lg) + c;
     double v = 0.0;
     if (i < n) {
@@ -477,31 +478,41 @@ struct Shape {
     // ---- k_loss_block
     int64_t tiles() const { return ceil_div(M, kBlockRows); }
     int64_t strips() const { return ceil_div(N, kBlockCols); }
-    // Whether k_loss_block is taken: a model of both ways, in us, that the sizes go into as they are padded.  A workgroup of it costs
-    // 1.4 us and 0.009 us an input in a forward pass, four at a time a compute unit; a backward pass is 6 M N K multiply-adds at 110 TFLOP/s and its
-    // sums, written and read.  The other way costs its launches, the steps of one tile where there are few, the products at what they reach, and dZ and
-    // packed rows at 4 TB/s.  us a call, k_loss_block / tiles:
-    //   f32 forward   1 row 256 -> 47 6 / 37;  8000 rows 256 -> 47 7 / 36;  70 000 rows 256 -> 47 40 / 88;  16 rows 512 -> 50 000 35 / 93;  1645 rows
-    //                 1070 -> 2113 91 / 145;  667 rows 25 -> 18 287 34 / 23;  24 241 rows 31 -> 1548 100 / 42;  16 384 rows 512 -> 1000 182 / 100
-    //   f32 backward  16 / 43;  33 / 71;  159 / 259;  92 / 185;  613 / 280;  82 / 103;  257 / 242;  1116 / 351 (in that order)
-    //   bf16 forward  7 / 21;  8 / 14;  31 / 23;  34 / 19;  81 / 38;  34 / 17;  96 / 29;  168 / 25
-    //   bf16 backward 20 / 22;  38 / 30;  165 / 79;  91 / 57;  582 / 93;  88 / 53;  277 / 79;  1034 / 94
+    // Whether every workgroup has a compute unit to itself: twice the wavefronts then, which share what one waits for.  us a backward pass, f32, 256
+    // threads / 512: 1 row 256 -> 47 15.8 / 12.6;  8000 rows 256 -> 47 27.6 / 24.7;  300 rows 500 -> 464 35.5 / 31.1;  with more workgroups 4000 rows
+    // 64 -> 1000 48 / 60.
+    bool one_each() const { return tiles() * strips() <= 256; }
+    // Whether k_loss_block is taken: a model of both ways, in us, that the sizes go into as they are padded.  In a forward pass a workgroup of it costs
+    // 1.4 us and 0.009 us an input, four at a time a compute unit.  A backward pass is one workgroup's chain, or 6 M N K multiply-adds at 110 TFLOP/s, and
+    // the launch of its sums, written and read.  The other way costs its launches, the steps of one tile where there are few, the products at what they
+    // reach, and dZ and packed rows at 4 (bf16: 5) TB/s.  us a call, k_loss_block / tiles:
+    //                                 f32 forward   f32 backward  bf16 forward  bf16 backward
+    //       1 row  256 ->     47       6.5 / 36      12.8 / 42      6.4 / 20      14.9 / 20.6
+    //    8000 rows 256 ->     47       7.0 / 35        25 / 71      6.9 / 13      26.6 / 29.8
+    //    8000 rows 512 ->     47      10.5 / 64        38 / 92      9.2 / 17      43.7 / 40.6
+    //  70 000 rows 256 ->     47        41 / 88       112 / 255    31.5 / 22       118 / 79
+    //      16 rows 512 -> 50 000        35 / 92        81 / 182      34 / 18        80 / 54
+    //    1645 rows 1070 ->  2113        90 / 145      614 / 277      82 / 38       584 / 93
+    //     667 rows  25 -> 18 287        34 / 21        85 / 92       34 / 16        91 / 53
+    //  24 241 rows  31 ->   1548       101 / 39       260 / 220      97 / 26       280 / 75      (f32 backward taken the slower way)
+    //  16 384 rows 512 ->   1000       183 / 100     1130 / 341     169 / 24      1047 / 90
     bool small() const
     {
         if (tiles() > 65535 || K * N >= (int64_t)1 << 27 || M * K >= (int64_t)1 << 27) return false;      // its grid and offsets
         const double groups = (double)(tiles() * strips()), k = (double)K, m = (double)M;
         const double all = (double)align_up((size_t)M, 128) * (double)align_up((size_t)N, 128) * (double)align_up((size_t)K, 128);
         if (!backward) {
-            const double one = 0.017 * k, many = groups / 256.0 * (1.43 + 0.0094 * k);
+            const double one = 0.015 * k, many = groups / 256.0 * (1.43 + 0.0094 * k);
             const double here = 4.5 + (strips() > 1 ? 3.2 : 0.0) + (one > many ? one : many);
             const double there = bf16 ? 9.5 + (pack_h || pack_w ? 4.0 : 0.0) + 0.006 * k + all * 2.0 / 0.6e9 : 15.0 + 0.085 * k + all * 2.0 / 0.17e9;
             return here < there;
         }
         const double sums = 4.0 * ((tiles() > 1 ? (double)tiles() * k * (double)N : 0.0) + (strips() > 1 ? (double)strips() * m * k : 0.0));
         if (sums > 512e6) return false;
-        const double here = (10.0 + 0.035 * k + groups * (0.004 + 6.0 * kBlockRows * kBlockCols * k / 110e6) + 2.0 * sums / 4e6) * (bf16 ? 1.15 : 1.0);
+        const double here = ((one_each() ? 4.0 + 0.034 * k : 10.0 + 0.035 * k + groups * (0.004 + 6.0 * kBlockRows * kBlockCols * k / 110e6)) +
+                             (sums > 0.0 ? 4.5 + 2.0 * sums / (one_each() ? 4e6 : 5e6) : 0.0)) * (!bf16 ? 1.0 : one_each() ? 1.15 : 1.08);
         const double z = m * (double)align_up((size_t)N, 32);
-        const double there = bf16 ? 24.0 + 0.015 * k + all * 6.0 / 0.6e9 + (10.0 * z + 8.0 * m * k) / 4e6
+        const double there = bf16 ? 23.0 + 0.015 * k + all * 6.0 / 0.6e9 + (10.0 * z + 8.0 * m * k) / 5e6
                                   : 40.0 + 0.06 * k + all * 6.0 / 0.2e9 + (18.0 * z + 12.0 * m * k) / 4e6;
         return here < there;
     }
@@ -596,14 +607,18 @@ fastgl_status launch_block(const Shape &d, LossBlockArgs a, hipStream_t s, const
     a.M = d.M; a.N = d.N;
     a.K = (int32_t)d.K;
     const dim3 grid((unsigned)d.strips(), (unsigned)d.tiles());
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, s, a); };
-    auto typed = [&](auto bf16) {
+    auto typed = [&](auto bf16, auto threads) {
         constexpr bool B = decltype(bf16)::value;
-        if (d.backward) go(k_loss_block<B, true>);
-        else go(k_loss_block<B, false>);
+        constexpr int T = decltype(threads)::value;
+        if (d.backward) hipLaunchKernelGGL((k_loss_block<B, true, T>), grid, dim3(T), 0, s, a);
+        else hipLaunchKernelGGL((k_loss_block<B, false, T>), grid, dim3(T), 0, s, a);
     };
-    if (d.bf16) typed(std::true_type());
-    else typed(std::false_type());
+    auto sized = [&](auto bf16) {
+        if (d.one_each()) typed(bf16, std::integral_constant<int, 512>());
+        else typed(bf16, std::integral_constant<int, 256>());
+    };
+    if (d.bf16) sized(std::true_type());
+    else sized(std::false_type());
     FASTGL_LAUNCH_CHECK(what);
     return FASTGL_OK;
 }
@@ -816,8 +831,10 @@ fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, 
             t.n[m] = n;
             t.parts[m] = (int32_t)parts;
             t.bf16[m] = bf16;
-            t.lg[m] = 8;                              // fewer elements a workgroup where there are few of many parts
-            while (t.lg[m] > 3 && (parts >> (8 - t.lg[m])) > 8 && ceil_div(n, (int64_t)1 << t.lg[m]) < 1024) --t.lg[m];
+            // Fewer elements a workgroup where there are few of many parts, 128 bytes of a part at least.  250 parts of 12 032 elements: 256 threads
+            // and 32 bytes of a part a workgroup 10.6 us, 1024 and 128 bytes 5.2.
+            t.lg[m] = kAddLg;
+            while (t.lg[m] > 5 && (parts >> (kAddLg - t.lg[m])) > 8 && ceil_div(n, (int64_t)1 << t.lg[m]) < 1024) --t.lg[m];
             t.blocks[m] = ceil_div(n, (int64_t)1 << t.lg[m]);
             total += t.blocks[m];
         };
@@ -825,7 +842,7 @@ fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, 
         add(1, a.part_w, a.dW, K * N, d.tiles(), d.bf16);
         add(2, a.part_b, a.db, N, d.tiles(), false);
         if (total == 0) return FASTGL_OK;
-        hipLaunchKernelGGL(k_loss_add, dim3((unsigned)total), dim3(kBlock), 0, s, t);
+        hipLaunchKernelGGL(k_loss_add, dim3((unsigned)total), dim3(kAddThreads), 0, s, t);
         FASTGL_LAUNCH_CHECK("fastgl_loss_bwd (sums)");
         return FASTGL_OK;
     }
