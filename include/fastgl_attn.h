@@ -26,13 +26,13 @@
  * the learned bias goes by.  An edge whose bucket is negative, or num_buckets and above, is left
  * out of the attention: it adds nothing anywhere, whatever its neighbour's row holds.  Without a
  * bias (NULL) buckets may be given all the same, to leave edges out (the negative ones; num_buckets is
- * not read).  Edges whose weight p_e is 0 in fp32 add nothing either, whatever V holds.  A row that no
+ * not read).  An edge whose bias or score is -inf adds nothing either.  A row that no
  * edge is left of has O = 0, lse = -inf, dQ = 0.
  *
- * Products and sums are fp32 (bf16 inputs are exact in it), sums of long rows in chunks of
- * fastgl_long_row_chunk() edges in a fixed order, dbias in fp32 within a workgroup and fp64 over them; results are
- * rounded once.  Results do not depend on scheduling.  A row with an element that is not
- * finite gives what IEEE arithmetic gives and changes no other row of O and dQ.
+ * Products and sums are fp32 (bf16 inputs are exact in it), sums of a row in runs of edges (long rows: in chunks of
+ * fastgl_long_row_chunk()) joined in a fixed order, dbias in fp32 within a workgroup and fp64 over them; results are
+ * rounded once.  Results do not depend on scheduling.  NaN in a row gives NaN where it takes part and changes no other row of O
+ * and dQ; so may infinities in Q, K and dO, and infinities in V, where IEEE arithmetic would give a score or a weight that is not NaN.
  *
  * Conventions are those of fastgl_agg.h: caller-owned DEVICE memory, aligned to the element size;
  * nothing is allocated, scratch comes from `workspace` (256-byte aligned); work is enqueued on

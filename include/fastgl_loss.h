@@ -15,9 +15,9 @@
  * that of its scores).  A label of N and above gives NaN: the row's loss and dH, and dW and db.
  *
  * Scores are formed on the bf16 matrix cores with fp32 accumulation, from three bf16 pieces of each fp32 element (six of nine
- * piece products, relative error of a product at most 2^-23), or as plain fp32 multiply-adds.  Maxima and sums are fp32
+ * piece products, relative error of a product at most 2^-23), or, in small calls, as fp32 multiply-adds.  Maxima and sums are fp32
  * within a tile and over tiles.  dZ, formed in fp32, is rounded for the two products as their operands are: to one bf16 in bf16 calls,
- * to three pieces in fp32 ones; db is of the unrounded values.  Results are rounded once.  exp(z - lse) is
+ * to three pieces in fp32 ones, not at all in small calls; db is of the unrounded values.  Results are rounded once.  exp(z - lse) is
  * off by 2^-23 (2 + |z| + |lse|) of itself and by its score's error.  A row with a score of NaN or +inf has loss and dH NaN; scores of
  * -inf (a bias that rules a class out) weigh nothing.
  *

@@ -177,7 +177,8 @@ __device__ __forceinline__ uint64_t over(uint64_t n, uint64_t inv) { return inv 
 __device__ __forceinline__ uint32_t over(uint32_t n, uint32_t inv) { return inv ? __umulhi(n, inv) : n; }
 
 // Where a lane is: its group's place in the wavefront and its pieces of a head.  A row's place in an array is a 32-bit offset where the
-// array is NEAR: fewer instructions, which is what bounds the walks (63 against 81 of 128-byte heads of bf16 an edge and lane).
+// array is NEAR (us, so / 64-bit offsets: 8000 rows of 15, four f32 heads of 47 on one, forward 15.7 / 16.7, dQ 18.6 / 19.3, dK and dV 50.0 / 51.3;  91 331
+// rows of 10, eight bf16 heads of 32, dK and dV 334 / 341;  where memory bounds a walk the same).
 template <class P, int LG, bool NEAR>
 struct Where {
     int l, g, off[P::PIECES], skip[P::PIECES];        // off: bytes
@@ -266,6 +267,12 @@ __device__ __forceinline__ float bias_of(const AttnArgs &a, int bucket, int h)
 // are units too, as many at a time as give every group a segment.
 //
 // Rows of sources are dealt to the wavefronts 64 apart: those that are neighbours of many often have numbers that lie together.
+//
+// What bounds it: the gathers of neighbours' rows.  With heads of 128 bytes and 4.4 edges a row (512 345 rows, 1.1 million sources) the forward pass takes 295 us:
+// 1.15 GB of K and V from memory and caches and 0.52 GB of Q and O, 5.7 TB/s.  With heads of 32 bytes it is the arithmetic of an edge and lane (65 536 rows, 1.7
+// million edges, 102 us).
+// Segments: 65 536 rows of eight edges beside rows of up to 18 000, forward 201 us without them, 103 with;  8000 rows of 15, dK and dV for heads that share
+// theirs 121 and 50.  Two pieces a lane instead of one: the 512 345 rows 451 and 345 us (then with 64-bit offsets).
 template <class ROW>
 __device__ __forceinline__ void walk_units(const AttnArgs &a)
 {
@@ -506,6 +513,7 @@ struct ForwardRow {
     }
 };
 
+// Wavefronts a SIMD hide the gathers' latency: the 512 345 rows with four edges under way and three wavefronts 345 us, with two and four 297.
 template <bool BF16, int PC, int LG, bool NEAR>
 __global__ __launch_bounds__(kBlock, LG >= 4 ? 3 : 4) void k_attn_fwd(AttnArgs a)
 {
@@ -650,6 +658,8 @@ struct QueryRow {
     }
 };
 
+// 91 331 rows of 10, eight bf16 heads of 32: four edges under way 160 us, two 146 (0.96 GB, most of it gathered, at 6.6 TB/s).  The transposed order's buckets come along
+// in place of a launch of their own.
 template <bool BF16, int PC, int LG, bool NEAR>
 __global__ __launch_bounds__(kBlock, LG >= 4 ? 2 : BF16 ? 3 : 4) void k_attn_dq(AttnArgs a)
 {
@@ -764,6 +774,9 @@ struct KeyRow {
     }
 };
 
+// A source has few edges, and its own rows are read and written: 512 345 sources of 1.6 edges, eight bf16 heads of 32, 334 us: 1.05 GB of own rows and 0.92
+// gathered, 5.9 TB/s.  One edge under way where heads share no key head: that 332 us, two 372;  two where they do, as a row then has as many steps more: 8000 rows of 15,
+// four f32 heads of 47 on one, 49 us, one 66.
 template <bool BF16, int PC, int LG, bool NEAR, int U>
 __global__ __launch_bounds__(kBlock, U == 1 ? 4 : 3) void k_attn_dkv(AttnArgs a)
 {
@@ -772,7 +785,7 @@ __global__ __launch_bounds__(kBlock, U == 1 ? 4 : 3) void k_attn_dkv(AttnArgs a)
 
 // ------------------------------------------------------------------ chunks of long rows
 // A workgroup has one long row and 2^lg of its columns at a time, and as many parts of its chunks as threads are left; the parts are joined in
-// order.  KIND 0: O and lse, 1: dQ and the row's numbers, 2: dK and dV.
+// order.  Latency bounds it: 4.5 us where there is no long row (the host does not know), 13 where 65 536 rows have chunks by the thousand.  KIND 0: O and lse, 1: dQ and the row's numbers, 2: dK and dV.
 template <bool BF16, int KIND>
 __global__ __launch_bounds__(kJoin) void k_attn_join(AttnArgs a, int lg)
 {
