@@ -504,10 +504,11 @@ def fastgl_gated_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G: tor
 
 
 def fastgl_attn_workspace_bytes(num_dst: int, num_src: int, num_edges: int, heads: int, width: int, dtype: str,
-                                kv_heads: Optional[int] = None, num_buckets: int = 0, backward: bool = False) -> int:
-    """num_buckets: of the bias, 0 without one."""
+                                kv_heads: Optional[int] = None, num_buckets: int = 0, backward: bool = False,
+                                bucket: bool = False) -> int:
+    """num_buckets: of the bias, 0 without one; bucket: buckets are given without a bias."""
     d = AttnDesc(num_dst=num_dst, num_src=num_src, num_edges=num_edges, heads=heads, kv_heads=kv_heads or heads, width=width,
-                 dtype=DTYPES[dtype], num_buckets=num_buckets, bucket=num_buckets and 4, bias=num_buckets and 4)
+                 dtype=DTYPES[dtype], num_buckets=num_buckets, bucket=4 if bucket or num_buckets else 0, bias=num_buckets and 4)
     return int(lib().fastgl_attn_workspace_bytes(ctypes.byref(d), int(backward)))
 
 
