@@ -313,41 +313,46 @@ __global__ __launch_bounds__(THREADS) void k_loss_block(LossBlockArgs a)
             for (int i = 0; i < kBlockRows; ++i) db += z[0][i][threadIdx.x];
         }
         // ---- dH
-        if (a.dH)
-            for (int k0 = wave * 32; k0 < a.K; k0 += WAVES * 32) {
-                const int k = k0 + r;
-                const uint32_t w0 = (uint32_t)(k < a.K ? k : a.K - 1) * N + (uint32_t)col0;
-                f32x16 out;
+        auto rows_of = [&](int k0) __attribute__((always_inline)) {
+            const int k = k0 + r;
+            const uint32_t w0 = (uint32_t)(k < a.K ? k : a.K - 1) * N + (uint32_t)col0;
+            f32x16 out;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) out[e] = 0.f;
-                auto eight = [&](int c, const float (&w)[4]) __attribute__((always_inline)) {
-                    const float *x = &z[0][r][8 * c + 4 * h];
+            for (int e = 0; e < 16; ++e) out[e] = 0.f;
+            auto eight = [&](int c, const float (&w)[4]) __attribute__((always_inline)) {
+                const float *x = &z[0][r][8 * c + 4 * h];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) out = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], w[j], out, 0, 0, 0);
-                };
-                if (left == kBlockCols) {
-                    float w[8][4];
+                for (int j = 0; j < 4; ++j) out = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], w[j], out, 0, 0, 0);
+            };
+            if (left == kBlockCols) {
+                float w[8][4];
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) four<BF16>(a.W, w0 + 8 * c + 4 * h, w[c]);
+                for (int c = 0; c < 8; ++c) four<BF16>(a.W, w0 + 8 * c + 4 * h, w[c]);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) eight(c, w[c]);
-                } else
-                    for (int c = 0; 8 * c < left; ++c) {
-                        float w[4];
+                for (int c = 0; c < 8; ++c) eight(c, w[c]);
+            } else
+                for (int c = 0; 8 * c < left; ++c) {
+                    float w[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) w[j] = 8 * c + 4 * h + j < left ? element<BF16>(a.W, w0 + 8 * c + 4 * h + j) : 0.f;
-                        eight(c, w);
-                    }
-                if (k < a.K) {
+                    for (int j = 0; j < 4; ++j) w[j] = 8 * c + 4 * h + j < left ? element<BF16>(a.W, w0 + 8 * c + 4 * h + j) : 0.f;
+                    eight(c, w);
+                }
+            if (k < a.K) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int row = 8 * (e >> 2) + 4 * h + (e & 3);
-                        if (row < rows) put_result<BF16>(a.dH, part_h, first + (uint32_t)row * K + (uint32_t)k, out[e]);
-                    }
+                for (int e = 0; e < 16; ++e) {
+                    const int row = 8 * (e >> 2) + 4 * h + (e & 3);
+                    if (row < rows) put_result<BF16>(a.dH, part_h, first + (uint32_t)row * K + (uint32_t)k, out[e]);
                 }
             }
-        // ---- dW
-        auto block = [&](int k0, f32x16 (&out)[2]) __attribute__((always_inline)) {
+        };
+        // ---- dW, of NQ times 32 classes from q0 on
+        auto weights_of = [&](int k0, int q0, auto nq) __attribute__((always_inline)) {
+            constexpr int NQ = decltype(nq)::value;
+            f32x16 out[NQ];
+#pragma unroll
+            for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) out[q][e] = 0.f;
             const int k = k0 + r < a.K ? k0 + r : a.K - 1;
             float x[16];
 #pragma unroll
@@ -360,28 +365,33 @@ __global__ __launch_bounds__(THREADS) void k_loss_block(LossBlockArgs a)
                 const int row = 8 * (i >> 2) + 4 * h + (i & 3);
                 const float v = on[row] != 0.f ? x[i] : 0.f;                   // rows without a label: whatever they hold
 #pragma unroll
-                for (int q = 0; q < 2; ++q) out[q] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, z[0][row][32 * q + r], out[q], 0, 0, 0);
+                for (int q = 0; q < NQ; ++q) out[q] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, z[0][row][32 * (q0 + q) + r], out[q], 0, 0, 0);
             }
             __builtin_amdgcn_sched_barrier(0);    // one block's rows in registers at a time
-        };
-        auto store = [&](int k0, const f32x16 (&out)[2]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                if (32 * q + r >= left) continue;
+            for (int q = 0; q < NQ; ++q) {
+                if (32 * (q0 + q) + r >= left) continue;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int k = k0 + 8 * (e >> 2) + 4 * h + (e & 3);
-                    if (k < a.K) put_result<BF16>(a.dW, part_w, (uint32_t)k * N + (uint32_t)col0 + 32 * q + r, out[q][e]);
+                    const int to = k0 + 8 * (e >> 2) + 4 * h + (e & 3);
+                    if (to < a.K) put_result<BF16>(a.dW, part_w, (uint32_t)to * N + (uint32_t)col0 + 32 * (q0 + q) + r, out[q][e]);
                 }
             }
         };
-        if (a.dW)
-            for (int k0 = wave * 32; k0 < a.K; k0 += WAVES * 32) {
-                f32x16 out[2];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) out[0][e] = out[1][e] = 0.f;
-                block(k0, out);
-                store(k0, out);
+        // Blocks of 32 inputs are dealt to the wavefronts; where there are fewer of them, dH and each half of the classes of dW by themselves.  us, all of a block to
+        // one wavefront / so: 15 507 rows 11 -> 10 080, f32, 819 / 654;  24 241 rows 31 -> 1548 259 / 221;  8000 rows 16 -> 7 11.8 / 10.3.
+        const int blocks = (a.K + 31) / 32;
+        if (blocks >= WAVES) {
+            if (a.dH)
+                for (int k = wave; k < blocks; k += WAVES) rows_of(32 * k);
+            if (a.dW)
+                for (int k = wave; k < blocks; k += WAVES) weights_of(32 * k, 0, std::integral_constant<int, 2>());
+        } else
+            for (int job = wave; job < 3 * blocks; job += WAVES) {
+                if (job < blocks) {
+                    if (a.dH) rows_of(32 * job);
+                } else if (a.dW)
+                    weights_of(32 * ((job - blocks) >> 1), (job - blocks) & 1, std::integral_constant<int, 1>());
             }
         if (a.db && threadIdx.x < (unsigned)left) {
             if (a.part_b) a.part_b[(int64_t)tile * a.N + col0 + threadIdx.x] = db;
@@ -493,8 +503,8 @@ struct Shape {
     //  70 000 rows 256 ->     47        41 / 88       112 / 255    31.5 / 22       118 / 79
     //      16 rows 512 -> 50 000        35 / 92        81 / 182      34 / 18        80 / 54
     //    1645 rows 1070 ->  2113        90 / 145      614 / 277      82 / 38       584 / 93
-    //     667 rows  25 -> 18 287        34 / 21        85 / 92       34 / 16        91 / 53
-    //  24 241 rows  31 ->   1548       101 / 39       260 / 220      97 / 26       280 / 75      (f32 backward taken the slower way)
+    //     667 rows  25 -> 18 287        34 / 21        73 / 92       34 / 16        91 / 53
+    //  24 241 rows  31 ->   1548       101 / 39       221 / 220      95 / 26       225 / 75
     //  16 384 rows 512 ->   1000       183 / 100     1130 / 341     169 / 24      1047 / 90
     bool small() const
     {
