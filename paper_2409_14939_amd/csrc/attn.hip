@@ -23,6 +23,7 @@ namespace {
 constexpr float kLog2e = 1.44269504089f, kLn2 = 0.69314718056f;
 constexpr int kSegment = 16;              // steps that a group takes where a neighbour has more
 constexpr int kSlack = 8;                 // steps more than shorter segments have that a group takes alone rather than have them cut
+constexpr int kTransposedSteps = 6;       // of a group, on average, that a wavefront of the transposed pass takes units for
 constexpr int kBiasBlocks = 1024;         // workgroups of k_attn_dbias
 constexpr int kJoin = 1024;               // threads of a workgroup that joins chunks
 constexpr int kBiasTile = 64;             // buckets of one of its passes
@@ -1127,6 +1128,13 @@ fastgl_status launch_walk(AttnArgs a, const fastgl_attn_desc &d, const fastgl_pl
         // of 160 fp32 columns, forward 87 / 46;  16 843 rows of 16, 2 heads of 12 columns, dQ 10.4 / 10.4, with sixteen 17.
         const int64_t groups = kWave >> LG, few = ceil_div(a.units, T || LG >= 4 ? 4096 : 1024);
         a.units_a_wave = (int32_t)(few <= groups / 2 ? few : groups);
+        // Rows of sources with many steps: as few as have kTransposedSteps a group on average, so that the neighbours of many do not meet in one wavefront.
+        // us, dK and dV: 2350 sources of 28 edges, 32 heads of one f32 column, eight to a key head 146 / 76 (8: 76, 16: 110);  45 157 sources of 4, 40 heads of 12 on
+        // five 357 / 238 (8: 248, 16: 282);  19 239 of 5, 18 of 19 on six 137 / 115.  Rows of targets, of alike lengths, lose by it: 30 / 49.
+        if (T && d.num_edges > 0) {
+            const int64_t so = ceil_div(groups * kTransposedSteps * rows, d.num_edges * a.shared);
+            if (so < a.units_a_wave) a.units_a_wave = (int32_t)so;
+        }
         const int64_t blocks = ceil_div(a.units, (int64_t)a.units_a_wave * (kBlock / kWave));
         if (blocks > (int64_t)65535 << 20) {
             set_error("%s: too many rows and heads", names[PASS]);
