@@ -16,8 +16,9 @@
  *
  * Scores are formed on the bf16 matrix cores with fp32 accumulation, from three bf16 pieces of each fp32 element (six of nine
  * piece products, relative error of a product at most 2^-23), or, in small calls, as fp32 multiply-adds.  Maxima and sums are fp32
- * within a tile and over tiles.  dZ, formed in fp32, is rounded for the two products as their operands are: to one bf16 in bf16 calls,
- * to three pieces in fp32 ones, not at all in small calls; db is of the unrounded values.  Results are rounded once.  exp(z - lse) is
+ * within a tile and over tiles.  dZ, formed in fp32, goes into the two products within 2^-17 of itself in bf16 calls (two bf16 pieces) and within
+ * 2^-24 in fp32 ones (three), or as it is (small calls).  fastgl_loss_bwd_coarse rounds it to one bf16 in bf16 calls, at every size: dH and dW are
+ * up to sqrt 2 times as far off, for half the products; fp32 calls are as with fastgl_loss_bwd.  db is of the unrounded values.  Results are rounded once.  exp(z - lse) is
  * off by 2^-23 (2 + |z| + |lse|) of itself and by its score's error.  A row with a score of NaN or +inf has loss and dH NaN; scores of
  * -inf (a bias that rules a class out) weigh nothing.
  *
@@ -39,6 +40,7 @@ extern "C" {
  * taken in pieces, so that the backward pass's dZ stays below 1 GiB (256 classes at least). */
 size_t fastgl_loss_fwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned);
 size_t fastgl_loss_bwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned);
+size_t fastgl_loss_bwd_coarse_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned);
 
 /* Forward pass.  b may be NULL; lse, which the backward pass reads, may be NULL. */
 fastgl_status fastgl_loss_fwd(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label, int64_t M,
@@ -48,6 +50,11 @@ fastgl_status fastgl_loss_fwd(fastgl_dtype dtype, const void *H, const void *W, 
 fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label,
                               const float *lse, const float *dloss, int64_t M, int64_t K, int64_t N, void *dH, void *dW, float *db,
                               void *workspace, size_t workspace_bytes, void *stream);
+
+/* The same with dZ rounded to one bf16 for the products of bf16 calls. */
+fastgl_status fastgl_loss_bwd_coarse(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label,
+                                     const float *lse, const float *dloss, int64_t M, int64_t K, int64_t N, void *dH, void *dW, float *db,
+                                     void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

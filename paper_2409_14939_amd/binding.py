@@ -41,6 +41,7 @@ EXPORTS = [
     "fastgl_gated_bwd_workspace_bytes", "fastgl_gated_bwd_fine", "fastgl_gated_bwd_fine_workspace_bytes",
     "fastgl_attn_fwd", "fastgl_attn_bwd", "fastgl_attn_workspace_bytes",
     "fastgl_loss_fwd", "fastgl_loss_bwd", "fastgl_loss_fwd_workspace_bytes", "fastgl_loss_bwd_workspace_bytes",
+    "fastgl_loss_bwd_coarse", "fastgl_loss_bwd_coarse_workspace_bytes",
 ]
 MAX_REORDER_BATCHES = 64
 ACTS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
@@ -149,11 +150,12 @@ def lib() -> ctypes.CDLL:
         L.fastgl_attn_workspace_bytes.restype = sz
         L.fastgl_attn_fwd.argtypes = [desc, p, i64, p, p, p, sz, p]
         L.fastgl_attn_bwd.argtypes = [desc, p, i64, p, i64, p, i64, p, i64, p, p, p, sz, p]
-        for f in (L.fastgl_loss_fwd_workspace_bytes, L.fastgl_loss_bwd_workspace_bytes):
+        for f in (L.fastgl_loss_fwd_workspace_bytes, L.fastgl_loss_bwd_workspace_bytes, L.fastgl_loss_bwd_coarse_workspace_bytes):
             f.argtypes = [i32, i64, i64, i64, i32]
             f.restype = sz
         L.fastgl_loss_fwd.argtypes = [i32, p, p, p, p, i64, i64, i64, p, p, p, sz, p]
-        L.fastgl_loss_bwd.argtypes = [i32, p, p, p, p, p, p, i64, i64, i64, p, p, p, p, sz, p]
+        for f in (L.fastgl_loss_bwd, L.fastgl_loss_bwd_coarse):
+            f.argtypes = [i32, p, p, p, p, p, p, i64, i64, i64, p, p, p, p, sz, p]
         L.fastgl_idmap_table_slots.argtypes = [i64]
         L.fastgl_idmap_table_slots.restype = i64
         L.fastgl_idmap_workspace_bytes.argtypes = [i64, i64]
@@ -539,8 +541,9 @@ def fastgl_loss_fwd_workspace_bytes(dtype: str, M: int, K: int, N: int, aligned:
     return int(lib().fastgl_loss_fwd_workspace_bytes(DTYPES[dtype], M, K, N, int(aligned)))
 
 
-def fastgl_loss_bwd_workspace_bytes(dtype: str, M: int, K: int, N: int, aligned: bool = False) -> int:
-    return int(lib().fastgl_loss_bwd_workspace_bytes(DTYPES[dtype], M, K, N, int(aligned)))
+def fastgl_loss_bwd_workspace_bytes(dtype: str, M: int, K: int, N: int, aligned: bool = False, coarse: bool = False) -> int:
+    size = lib().fastgl_loss_bwd_coarse_workspace_bytes if coarse else lib().fastgl_loss_bwd_workspace_bytes
+    return int(size(DTYPES[dtype], M, K, N, int(aligned)))
 
 
 def fastgl_loss_fwd(H: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor], label: torch.Tensor, want_lse: bool = True,
@@ -554,7 +557,8 @@ def fastgl_loss_fwd(H: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor],
 def fastgl_loss_bwd(H: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor], label: torch.Tensor, lse: torch.Tensor,
                     dloss: torch.Tensor, want=("dH", "dW", "db"), dH: Optional[torch.Tensor] = None,
                     dW: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None,
-                    workspace: Optional[torch.Tensor] = None):
+                    workspace: Optional[torch.Tensor] = None, coarse: bool = False):
     """(dH, dW, db) for the gradient dloss [M] of loss (1 / rows for a mean); parts not named in `want` (and not passed in)
-    are None.  dH and dW are of H's dtype, db float32."""
-    return _native().loss_bwd(H, W, b, label, lse, dloss, *(n in want for n in ("dH", "dW", "db")), dH, dW, db, workspace)
+    are None.  dH and dW are of H's dtype, db float32.  bfloat16 calls keep the scores' gradient to 2^-17 for the products; coarse=True rounds
+    it to one bfloat16, for half the products."""
+    return _native().loss_bwd(H, W, b, label, lse, dloss, *(n in want for n in ("dH", "dW", "db")), dH, dW, db, workspace, coarse)

@@ -361,7 +361,7 @@ __device__ __forceinline__ void loss_epilogue(const ARGS &g, f32x16 (&acc)[T::TM
     }
 }
 
-// PART: sums of a slab instead of results.  ONCE: whole lines of results go past the caches.
+// PART: sums of a slab instead of results.  ONCE: whole lines of results go past the caches.  ACT: of GRADIENT the planes of dZ.
 template <int MODE, int SIZE, class OUT, int ACT, bool PART, bool ONCE>
 __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(typename TileArgsOf<MODE>::type g)
 {
@@ -691,7 +691,7 @@ __global__ __launch_bounds__((Tile<MODE, SIZE>::THREADS), 2) void k_gated_tile(t
             store_block(NB(), out, col0 + (wn * ONE + n) * 32, [&](int i, int b, int e) { return value(i, n + b, e); });
     };
     if constexpr (MODE == kScores || MODE == kGradient) {
-        loss_epilogue<MODE, T, sizeof(OUT) == 4 ? 3 : 1>(g, acc, r_base, col0 + wn * T::TN * 32, (row0 / T::BM) * T::WM + wm, (col0 / T::BC) * T::WN + wn);
+        loss_epilogue<MODE, T, ACT>(g, acc, r_base, col0 + wn * T::TN * 32, (row0 / T::BM) * T::WM + wm, (col0 / T::BC) * T::WN + wn);
     } else if constexpr (PART) {
 #pragma unroll
         for (int q = 0; q < T::RESULTS; ++q)

@@ -984,7 +984,7 @@ PyObject *loss_fwd(PyObject *const *a)
     return tuple({loss.t, lse.t});
 }
 
-// (H, W, b, label, lse, dloss, want_dH, want_dW, want_db, dH, dW, db, workspace) -> (dH, dW, db)
+// (H, W, b, label, lse, dloss, want_dH, want_dW, want_db, dH, dW, db, workspace, coarse) -> (dH, dW, db)
 PyObject *loss_bwd(PyObject *const *a)
 {
     const Loss c(a);
@@ -994,10 +994,13 @@ PyObject *loss_bwd(PyObject *const *a)
     if (truth(a[6]) || !none(a[9])) dH = out_of(a[9], type, {c.M, c.K}, c.H, "dH");
     if (truth(a[7]) || !none(a[10])) dW = out_of(a[10], type, {c.K, c.N}, c.H, "dW");
     if (truth(a[8]) || !none(a[11])) db = out_of(a[11], at::kFloat, {c.N}, c.H, "db");
-    const Scratch ws(a[12], c.H, [&] { return fastgl_loss_bwd_workspace_bytes(c.dt, c.M, c.K, c.N, c.aligned()); });
+    const bool coarse = truth(a[13]);
+    const Scratch ws(a[12], c.H, [&] {
+        return coarse ? fastgl_loss_bwd_coarse_workspace_bytes(c.dt, c.M, c.K, c.N, c.aligned()) : fastgl_loss_bwd_workspace_bytes(c.dt, c.M, c.K, c.N, c.aligned());
+    });
     run([&](void *s) {
-        return fastgl_loss_bwd(c.dt, c.H.data_ptr(), c.W.data_ptr(), c.b, (const int64_t *)c.label.data_ptr(), lse, dloss, c.M, c.K, c.N, dH.p(),
-                               dW.p(), (float *)db.p(), ws.p(), ws.n(), s);
+        return (coarse ? fastgl_loss_bwd_coarse : fastgl_loss_bwd)(c.dt, c.H.data_ptr(), c.W.data_ptr(), c.b, (const int64_t *)c.label.data_ptr(), lse, dloss,
+                                                                   c.M, c.K, c.N, dH.p(), dW.p(), (float *)db.p(), ws.p(), ws.n(), s);
     });
     return tuple({dH.t, dW.t, db.t});
 }
@@ -1017,7 +1020,7 @@ PyMethodDef g_methods[] = {
     FN(update_fwd, 5), FN(layer_fwd, 14), FN(update_bwd, 12), FN(idmap, 7), FN(match, 7), FN(assemble_rows, 5),
     FN(overlap_counts, 3), FN(edge_weight_grad, 9), FN(edge_softmax_fwd, 4), FN(edge_softmax_bwd, 5),
     FN(edge_score_fwd, 6), FN(edge_score_bwd, 11), FN(norm_fwd, 13), FN(norm_bwd, 14), FN(dropout, 5),
-    FN(gather_rows_e4m3, 5), FN(gated_fwd, 11), FN(gated_bwd, 19), FN(attn_fwd, 15), FN(attn_bwd, 21), FN(loss_fwd, 8), FN(loss_bwd, 13), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
+    FN(gather_rows_e4m3, 5), FN(gated_fwd, 11), FN(gated_bwd, 19), FN(attn_fwd, 15), FN(attn_bwd, 21), FN(loss_fwd, 8), FN(loss_bwd, 14), FN(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
 #undef FN
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host", "Native marshalling of the C ABI's calls.", -1, g_methods,

@@ -1,10 +1,14 @@
 // Softmax cross entropy of class scores that are not kept (fastgl_loss.h has the formulas): what is around the products of gated_tile.h.
 //
 //   forward   [operands packed] -> scores by tiles, of which maximum and sum of exponentials of some columns of each row remain -> k_loss_join
-//   backward  for a piece of the classes at a time: [W packed] -> scores again, of which dZ remains (as the matrix cores take it, with column sums)
+//   backward  for a piece of the classes at a time: [W packed] -> scores again, of which dZ remains (as the matrix cores take it: fp32 calls in three bf16
+//             pieces, bf16 calls in two, or rounded to one for a caller who asks for that; with column sums)
 //             -> dH += dZ W^T -> dW = H^T dZ -> k_loss_sum
 //
 // Small calls go another way, through k_loss_block: a workgroup has 32 rows and 64 classes, the scores in LDS, and all of a pass that these take part in.
+//
+// dZ of a bf16 call in two pieces, rounded to one (us, backward): 8192 rows 512 -> 65 536 2940, 1780; 16 384 rows 512 -> 1000 128, 89.  Rounded, dH and dW are
+// 2.4e-3 of themselves off instead of 1.7e-3, which is their own rounding.
 //
 // The rows of H are packed once for all pieces of a backward pass, 0 where there is no label: dZ is 0 there, and what H holds there must not
 // reach dW (0 times NaN).
@@ -18,7 +22,7 @@ namespace fastgl {
 namespace {
 
 constexpr int64_t kMostClasses = (int64_t)1 << 21, kMostInputs = (int64_t)1 << 20;
-// dZ, and packed weights, of a piece of the classes.  8192 rows 512 -> 65 536 bf16, the kernels of a backward pass: 256 MiB (four pieces) 1953 us, 512 MiB
+// dZ, and packed weights, of a piece of the classes.  8192 rows 512 -> 65 536 bf16, dZ rounded, the kernels of a backward pass: 256 MiB (four pieces) 1953 us, 512 MiB
 // 1783, 1 GiB (one) 1720: fewer sums of pieces, although dZ no longer stays in the last cache.
 constexpr int64_t kPieceBytes = (int64_t)1 << 30;
 constexpr int kPieceCols = 256;                           // a piece has a multiple of them
@@ -151,6 +155,7 @@ __global__ __launch_bounds__(kBlock) void k_loss_sum(LossSumArgs a)
 //   scores  the wavefronts take eight inputs each in turn; their sums are joined in LDS, where the tile then has its statistics or dZ
 //   dH      32 inputs a wavefront at a time: sums over the tile's classes, one for each strip of classes, joined afterwards
 //   dW      the same over the tile's rows
+// COARSE: dH and dW are of dZ rounded to one bf16, as the caller asked for.
 struct LossBlockArgs {
     const void *H, *W;
     const float *b;
@@ -199,7 +204,7 @@ __device__ __forceinline__ void put_result(void *out, float *part, uint32_t at, 
     else *reinterpret_cast<float *>(static_cast<char *>(out) + 4 * at) = x;
 }
 
-template <bool BF16, bool BACKWARD, int THREADS>
+template <bool BF16, bool BACKWARD, int THREADS, bool COARSE>
 __global__ __launch_bounds__(THREADS) void k_loss_block(LossBlockArgs a)
 {
     constexpr float kLog2e = 1.44269504089f, kLn2 = 0.69314718056f;
@@ -312,6 +317,7 @@ __global__ __launch_bounds__(THREADS) void k_loss_block(LossBlockArgs a)
 #pragma unroll 8
             for (int i = 0; i < kBlockRows; ++i) db += z[0][i][threadIdx.x];
         }
+        auto dz = [&](int row, int c) __attribute__((always_inline)) { return COARSE ? (float)(__bf16)z[0][row][c] : z[0][row][c]; };
         // ---- dH
         auto rows_of = [&](int k0) __attribute__((always_inline)) {
             const int k = k0 + r;
@@ -320,9 +326,8 @@ __global__ __launch_bounds__(THREADS) void k_loss_block(LossBlockArgs a)
 #pragma unroll
             for (int e = 0; e < 16; ++e) out[e] = 0.f;
             auto eight = [&](int c, const float (&w)[4]) __attribute__((always_inline)) {
-                const float *x = &z[0][r][8 * c + 4 * h];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) out = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], w[j], out, 0, 0, 0);
+                for (int j = 0; j < 4; ++j) out = __builtin_amdgcn_mfma_f32_32x32x2f32(dz(r, 8 * c + 4 * h + j), w[j], out, 0, 0, 0);
             };
             if (left == kBlockCols) {
                 float w[8][4];
@@ -365,7 +370,7 @@ __global__ __launch_bounds__(THREADS) void k_loss_block(LossBlockArgs a)
                 const int row = 8 * (i >> 2) + 4 * h + (i & 3);
                 const float v = on[row] != 0.f ? x[i] : 0.f;                   // rows without a label: whatever they hold
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) out[q] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, z[0][row][32 * (q0 + q) + r], out[q], 0, 0, 0);
+                for (int q = 0; q < NQ; ++q) out[q] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, dz(row, 32 * (q0 + q) + r), out[q], 0, 0, 0);
             }
             __builtin_amdgcn_sched_barrier(0);    // one block's rows in registers at a time
 #pragma unroll
@@ -446,11 +451,12 @@ bool misaligned_to(const void *p, uintptr_t bytes) { return ((uintptr_t)p & (byt
 
 struct Shape {
     bool bf16, backward, pack_h, pack_w;
-    int planes;
-    int64_t M, K, N, ldk, pairs;
-    Shape(fastgl_dtype dtype, int64_t M_, int64_t K_, int64_t N_, bool aligned, bool backward_)
+    int planes, z_planes;          // of H and W, of dZ
+    int64_t M, K, N, ldk, pairs, z_pairs;
+    Shape(fastgl_dtype dtype, int64_t M_, int64_t K_, int64_t N_, bool aligned, bool backward_, bool coarse)
         : bf16(dtype == FASTGL_BF16), backward(backward_), pack_h(backward_ || !bf16 || !aligned || K_ % 8), pack_w(!bf16 || !aligned || N_ % 8),
-          planes(bf16 ? 1 : 3), M(M_), K(K_), N(N_), ldk((int64_t)align_up((size_t)K_, 8)), pairs(bf16 ? 1 : 6)
+          planes(bf16 ? 1 : 3), z_planes(!bf16 ? 3 : coarse ? 1 : 2), M(M_), K(K_), N(N_), ldk((int64_t)align_up((size_t)K_, 8)), pairs(bf16 ? 1 : 6),
+          z_pairs(bf16 ? z_planes : 6)
     {
     }
     int64_t rows() const { return (int64_t)align_up((size_t)M, 256); }
@@ -458,7 +464,7 @@ struct Shape {
     int64_t piece() const
     {
         int64_t most = N;
-        if (backward) most = kPieceBytes / (2 * planes * rows());
+        if (backward) most = kPieceBytes / (2 * z_planes * rows());
         if (pack_w && K > 0 && kPieceBytes / (2 * planes * K) < most) most = kPieceBytes / (2 * planes * K);
         if (most >= N) return (int64_t)align_up((size_t)N, kPieceCols);
         most = most < 2 * kPieceCols ? kPieceCols : most / kPieceCols * kPieceCols;
@@ -473,8 +479,8 @@ struct Shape {
     int64_t z_ld() const { return blocks() ? 32 : piece(); }
     int64_t z_plane() const { return blocks() ? piece() / 32 * z_block() : rows() * piece(); }
     Cut scores_cut() const { return cut_of(kForward, M, widest(), K, pairs, true, true); }
-    Cut rows_cut() const { return cut_of(kRows, M, K, widest(), pairs); }
-    Cut weights_cut() const { return cut_of(kWeights, K, widest(), M, pairs, true); }
+    Cut rows_cut() const { return cut_of(kRows, M, K, widest(), z_pairs); }
+    Cut weights_cut() const { return cut_of(kWeights, K, widest(), M, z_pairs, true); }
     static int64_t tile_rows(const Cut &c) { return c.size == kLarge ? 256 : 128; }
     static int64_t wave_cols(const Cut &c) { return c.size == kSmall ? 64 : 128; }
     int64_t slots() const                                                  // of statistics: column tiles and wavefronts of all pieces
@@ -495,17 +501,19 @@ struct Shape {
     // Whether k_loss_block is taken: a model of both ways, in us, that the sizes go into as they are padded.  In a forward pass a workgroup of it costs
     // 1.4 us and 0.009 us an input, four at a time a compute unit.  A backward pass is one workgroup's chain, or 6 M N K multiply-adds at 110 TFLOP/s, and
     // the launch of its sums, written and read.  The other way costs its launches, the steps of one tile where there are few, the products at what they
-    // reach, and dZ and packed rows at 4 (bf16: 5) TB/s.  us a call, k_loss_block / tiles:
+    // reach, and dZ and packed rows at 4 (bf16: 5) TB/s.  us a call, k_loss_block / tiles (bf16 backward: dZ in two pieces; rounded 24 241 rows 229 / 76):
     //                                 f32 forward   f32 backward  bf16 forward  bf16 backward
-    //       1 row  256 ->     47       6.5 / 36      12.8 / 42      6.4 / 20      14.9 / 20.6
-    //    8000 rows 256 ->     47       7.0 / 35        25 / 71      6.9 / 13      26.6 / 29.8
-    //    8000 rows 512 ->     47      10.5 / 64        38 / 92      9.2 / 17      43.7 / 40.6
-    //  70 000 rows 256 ->     47        41 / 88       112 / 255    31.5 / 22       118 / 79
-    //      16 rows 512 -> 50 000        35 / 92        81 / 182      34 / 18        80 / 54
-    //    1645 rows 1070 ->  2113        90 / 145      614 / 277      82 / 38       584 / 93
-    //     667 rows  25 -> 18 287        34 / 21        73 / 92       34 / 16        91 / 53
-    //  24 241 rows  31 ->   1548       101 / 39       221 / 220      95 / 26       225 / 75
-    //  16 384 rows 512 ->   1000       183 / 100     1130 / 341     169 / 24      1047 / 90
+    //       1 row  256 ->     47       6.5 / 36      12.8 / 42      6.4 / 20      14.8 / 21.4
+    //    8000 rows 256 ->     47       7.0 / 35        25 / 71      6.9 / 13      26.4 / 36.3
+    //    8000 rows 512 ->     47      10.5 / 64        38 / 92      9.2 / 17      43.3 / 46.1
+    //  70 000 rows 256 ->     47        41 / 88       112 / 255    31.5 / 22       118 / 103
+    //      16 rows 512 -> 50 000        35 / 92        81 / 182      34 / 18        81 / 65
+    //     512 rows 256 ->   1000                                                  29.5 / 37.1
+    //  20 000 rows 128 ->     60                                                  34.0 / 43.8
+    //    1645 rows 1070 ->  2113        90 / 145      614 / 277      82 / 38       584 / 105
+    //     667 rows  25 -> 18 287        34 / 21        73 / 92       34 / 16        75 / 55
+    //  24 241 rows  31 ->   1548       101 / 39       221 / 220      95 / 26       226 / 115
+    //  16 384 rows 512 ->   1000       183 / 100     1130 / 341     169 / 24      1047 / 128
     bool small() const
     {
         if (tiles() > 65535 || K * N >= (int64_t)1 << 27 || M * K >= (int64_t)1 << 27) return false;      // its grid and offsets
@@ -522,8 +530,9 @@ struct Shape {
         const double here = ((one_each() ? 4.0 + 0.034 * k : 10.0 + 0.035 * k + groups * (0.004 + 6.0 * kBlockRows * kBlockCols * k / 110e6)) +
                              (sums > 0.0 ? 4.5 + 2.0 * sums / (one_each() ? 4e6 : 5e6) : 0.0)) * (!bf16 ? 1.0 : one_each() ? 1.15 : 1.08);
         const double z = m * (double)align_up((size_t)N, 32);
-        const double there = bf16 ? 23.0 + 0.015 * k + all * 6.0 / 0.6e9 + (10.0 * z + 8.0 * m * k) / 5e6
-                                  : 40.0 + 0.06 * k + all * 6.0 / 0.2e9 + (18.0 * z + 12.0 * m * k) / 4e6;
+        const double there = z_planes == 1   ? 23.0 + 0.015 * k + all * 6.0 / 0.6e9 + (10.0 * z + 8.0 * m * k) / 5e6
+                             : z_planes == 2 ? 27.5 + 0.024 * k + all * 10.0 / 0.8e9 + (10.0 * z + 8.0 * m * k) / 5e6
+                                             : 40.0 + 0.06 * k + all * 6.0 / 0.2e9 + (18.0 * z + 12.0 * m * k) / 4e6;
         return here < there;
     }
 };
@@ -563,7 +572,7 @@ struct Scratch {
             picked = take<float>((size_t)s.M);
             return;
         }
-        dz = take<uint16_t>((size_t)(s.planes * s.z_plane()));
+        dz = take<uint16_t>((size_t)(s.z_planes * s.z_plane()));
         db = take<float>((size_t)(s.db_rows() * s.widest()));
         if (s.parts_h()) part_h = take<float>((size_t)(s.rows_cut().slabs * s.M * s.K));
         const Cut c = s.weights_cut();
@@ -602,12 +611,12 @@ fastgl_status check_workspace(const void *ws, size_t bytes, size_t need)
     return FASTGL_OK;
 }
 
-size_t workspace(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, bool aligned, bool backward)
+size_t workspace(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, bool aligned, bool backward, bool coarse = false)
 {
     if (check(dtype, M, K, N) != FASTGL_OK || M == 0) return 0;
-    const size_t whole = Scratch(Shape(dtype, M, K, N, true, backward), nullptr).used;
+    const size_t whole = Scratch(Shape(dtype, M, K, N, true, backward, coarse), nullptr).used;
     if (aligned) return whole;
-    const size_t any = Scratch(Shape(dtype, M, K, N, false, backward), nullptr).used;
+    const size_t any = Scratch(Shape(dtype, M, K, N, false, backward, coarse), nullptr).used;
     return any > whole ? any : whole;
 }
 
@@ -620,8 +629,9 @@ fastgl_status launch_block(const Shape &d, LossBlockArgs a, hipStream_t s, const
     auto typed = [&](auto bf16, auto threads) {
         constexpr bool B = decltype(bf16)::value;
         constexpr int T = decltype(threads)::value;
-        if (d.backward) hipLaunchKernelGGL((k_loss_block<B, true, T>), grid, dim3(T), 0, s, a);
-        else hipLaunchKernelGGL((k_loss_block<B, false, T>), grid, dim3(T), 0, s, a);
+        if (!d.backward) hipLaunchKernelGGL((k_loss_block<B, false, T, false>), grid, dim3(T), 0, s, a);
+        else if (B && d.z_planes == 1) hipLaunchKernelGGL((k_loss_block<B, true, T, B>), grid, dim3(T), 0, s, a);
+        else hipLaunchKernelGGL((k_loss_block<B, true, T, false>), grid, dim3(T), 0, s, a);
     };
     auto sized = [&](auto bf16) {
         if (d.one_each()) typed(bf16, std::integral_constant<int, 512>());
@@ -670,8 +680,8 @@ fastgl_status pack(const Shape &d, const Scratch &o, const void *H, const void *
     return FASTGL_OK;
 }
 
-// One product.  PART: sums of slabs.
-template <int MODE, bool PART>
+// One product.  PART: sums of slabs.  PLANES: of dZ.
+template <int MODE, bool PART, int PLANES = 0>
 fastgl_status launch(const LossTileArgs &args, const Cut &cut, bool bf16, hipStream_t s, const char *what)
 {
     typename TileArgsOf<MODE>::type g = args;
@@ -686,7 +696,7 @@ fastgl_status launch(const LossTileArgs &args, const Cut &cut, bool bf16, hipStr
     auto sized = [&](auto size) {
         constexpr int S = decltype(size)::value;
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(Tile<MODE, S>::THREADS), 0, s, g); };
-        if constexpr (PART || MODE == kScores) go(k_gated_tile<MODE, S, float, 0, PART, false>);
+        if constexpr (PART || MODE == kScores || MODE == kGradient) go(k_gated_tile<MODE, S, float, PLANES, PART, false>);
         else if (bf16) go(k_gated_tile<MODE, S, uint16_t, 0, false, false>);
         else go(k_gated_tile<MODE, S, float, 0, false, false>);
     };
@@ -737,68 +747,8 @@ bool starts_whole(std::initializer_list<const void *> ps)
     return true;
 }
 
-}  // namespace
-}  // namespace fastgl
-
-using namespace fastgl;
-
-extern "C" {
-
-size_t fastgl_loss_fwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned)
-{
-    return workspace(dtype, M, K, N, aligned != 0, false);
-}
-
-size_t fastgl_loss_bwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned)
-{
-    return workspace(dtype, M, K, N, aligned != 0, true);
-}
-
-fastgl_status fastgl_loss_fwd(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label, int64_t M,
-                              int64_t K, int64_t N, float *loss, float *lse, void *ws, size_t ws_bytes, void *stream)
-{
-    fastgl_status st = check(dtype, M, K, N);
-    if (st != FASTGL_OK) return st;
-    if (M == 0) return FASTGL_OK;
-    if (!label || !loss || (K > 0 && (!H || !W))) {
-        set_error("H, W, label or loss is NULL");
-        return FASTGL_ERR_INVALID_ARG;
-    }
-    const uintptr_t el = dtype == FASTGL_BF16 ? 2 : 4;
-    if (misaligned_to(H, el) || misaligned_to(W, el) || misaligned_to(b, 4) || misaligned_to(label, 8) || misaligned_to(loss, 4) || misaligned_to(lse, 4)) {
-        set_error("buffers must be aligned to their element size");
-        return FASTGL_ERR_INVALID_ARG;
-    }
-    const Shape d(dtype, M, K, N, starts_whole({H, W}), false);
-    if ((st = check_workspace(ws, ws_bytes, Scratch(d, nullptr).used)) != FASTGL_OK) return st;
-    const Scratch o(d, (char *)ws);
-    hipStream_t s = (hipStream_t)stream;
-    if (d.small()) {
-        LossBlockArgs a = {};
-        a.H = H; a.W = W; a.b = b;
-        a.label = label;
-        a.loss = loss; a.lse = lse;
-        a.stats = o.stats; a.picked = o.picked;
-        st = launch_block(d, a, s, "fastgl_loss_fwd (small)");
-        return st != FASTGL_OK || d.strips() == 1 ? st : launch_join(o, d.strips(), label, M, N, loss, lse, s);
-    }
-    const Cut cut = d.scores_cut();
-    int64_t slots = 0;
-    for (int64_t n0 = 0; n0 < N; n0 += d.piece()) {
-        const int64_t n = N - n0 < d.piece() ? N - n0 : d.piece();
-        if ((st = pack(d, o, H, W, label, n0, n, d.pack_h && n0 == 0, d.pack_w, s)) != FASTGL_OK) return st;
-        LossTileArgs g = scores_of(d, o, H, W, b, label, n0, n);
-        g.stats = o.stats + 2 * slots * M;
-        g.picked = o.picked;
-        if ((st = launch<kScores, false>(g, cut, d.bf16, s, "fastgl_loss_fwd")) != FASTGL_OK) return st;
-        slots += ceil_div(n, Shape::wave_cols(cut));
-    }
-    return launch_join(o, slots, label, M, N, loss, lse, s);
-}
-
-fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label,
-                              const float *lse, const float *dloss, int64_t M, int64_t K, int64_t N, void *dH, void *dW, float *db,
-                              void *ws, size_t ws_bytes, void *stream)
+fastgl_status loss_bwd(bool coarse, fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label, const float *lse,
+                       const float *dloss, int64_t M, int64_t K, int64_t N, void *dH, void *dW, float *db, void *ws, size_t ws_bytes, void *stream)
 {
     fastgl_status st = check(dtype, M, K, N);
     if (st != FASTGL_OK) return st;
@@ -820,7 +770,7 @@ fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, 
         if (want_b) return launch_no_terms(false, db, nullptr, 1, N, false, s, "fastgl_loss_bwd (db, M = 0)");
         return FASTGL_OK;
     }
-    const Shape d(dtype, M, K, N, starts_whole({H, W}), true);
+    const Shape d(dtype, M, K, N, starts_whole({H, W}), true, coarse);
     if ((st = check_workspace(ws, ws_bytes, Scratch(d, nullptr).used)) != FASTGL_OK) return st;
     const Scratch o(d, (char *)ws);
     if (d.small()) {
@@ -865,7 +815,10 @@ fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, 
         z.dloss = dloss;
         z.dz = o.dz; z.dz_plane = d.z_plane(); z.dz_ld = d.z_ld(); z.dz_block = d.z_block();
         z.db = want_b ? o.db : nullptr;
-        if ((st = launch<kGradient, false>(z, scores, d.bf16, s, "fastgl_loss_bwd (dZ)")) != FASTGL_OK) return st;
+        st = !d.bf16            ? launch<kGradient, false, 3>(z, scores, d.bf16, s, "fastgl_loss_bwd (dZ)")
+             : d.z_planes == 2 ? launch<kGradient, false, 2>(z, scores, d.bf16, s, "fastgl_loss_bwd (dZ)")
+                               : launch<kGradient, false, 1>(z, scores, d.bf16, s, "fastgl_loss_bwd (dZ)");
+        if (st != FASTGL_OK) return st;
         LossSumArgs sum = {};                         // the sums at the end of the piece
         if (want_b) {
             sum.db_part = o.db;
@@ -880,8 +833,9 @@ fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, 
             g.a_blocks = d.blocks() ? d.z_block() : 0;
             g.ldb = z.ldb; g.b_plane = z.b_plane;
             g.R = M; g.C = K; g.Kc = n;
-            g.pairs = z.pairs; g.groups = 1;
-            g.planes_a = z.planes_a; g.planes_b = z.planes_b;
+            g.pairs = (int32_t)d.z_pairs; g.groups = 1;
+            g.planes_a = !d.bf16 ? kSixA : d.z_planes == 2 ? kTwo : 0;
+            g.planes_b = !d.bf16 ? kSixB : 0;
             g.out[0] = dH;
             g.part = o.part_h;
             g.add = n0 > 0;
@@ -896,8 +850,9 @@ fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, 
             g.b_plane = d.z_plane(); g.ldb = d.z_ld();
             g.b_blocks = d.blocks() ? d.z_block() : 0;
             g.R = K; g.C = n; g.Kc = M;
-            g.pairs = z.pairs; g.groups = 1;
-            g.planes_a = z.planes_a; g.planes_b = z.planes_b;
+            g.pairs = (int32_t)d.z_pairs; g.groups = 1;
+            g.planes_a = !d.bf16 ? kSixA : 0;
+            g.planes_b = !d.bf16 ? kSixB : d.z_planes == 2 ? kTwo : 0;
             g.out[0] = static_cast<char *>(dW) + n0 * (int64_t)el;
             g.ldo = N;
             g.part = o.part_w;
@@ -920,6 +875,84 @@ fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, 
     sum.R = M; sum.C = K; sum.ldo = K;
     sum.slabs = (int32_t)rows.slabs;
     return launch_sum(sum, d.bf16, s, "fastgl_loss_bwd (dH, sums)");
+}
+
+}  // namespace
+}  // namespace fastgl
+
+using namespace fastgl;
+
+extern "C" {
+
+size_t fastgl_loss_fwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned)
+{
+    return workspace(dtype, M, K, N, aligned != 0, false);
+}
+
+size_t fastgl_loss_bwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned)
+{
+    return workspace(dtype, M, K, N, aligned != 0, true);
+}
+
+size_t fastgl_loss_bwd_coarse_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned)
+{
+    return workspace(dtype, M, K, N, aligned != 0, true, true);
+}
+
+fastgl_status fastgl_loss_fwd(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label, int64_t M,
+                              int64_t K, int64_t N, float *loss, float *lse, void *ws, size_t ws_bytes, void *stream)
+{
+    fastgl_status st = check(dtype, M, K, N);
+    if (st != FASTGL_OK) return st;
+    if (M == 0) return FASTGL_OK;
+    if (!label || !loss || (K > 0 && (!H || !W))) {
+        set_error("H, W, label or loss is NULL");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    const uintptr_t el = dtype == FASTGL_BF16 ? 2 : 4;
+    if (misaligned_to(H, el) || misaligned_to(W, el) || misaligned_to(b, 4) || misaligned_to(label, 8) || misaligned_to(loss, 4) || misaligned_to(lse, 4)) {
+        set_error("buffers must be aligned to their element size");
+        return FASTGL_ERR_INVALID_ARG;
+    }
+    const Shape d(dtype, M, K, N, starts_whole({H, W}), false, false);
+    if ((st = check_workspace(ws, ws_bytes, Scratch(d, nullptr).used)) != FASTGL_OK) return st;
+    const Scratch o(d, (char *)ws);
+    hipStream_t s = (hipStream_t)stream;
+    if (d.small()) {
+        LossBlockArgs a = {};
+        a.H = H; a.W = W; a.b = b;
+        a.label = label;
+        a.loss = loss; a.lse = lse;
+        a.stats = o.stats; a.picked = o.picked;
+        st = launch_block(d, a, s, "fastgl_loss_fwd (small)");
+        return st != FASTGL_OK || d.strips() == 1 ? st : launch_join(o, d.strips(), label, M, N, loss, lse, s);
+    }
+    const Cut cut = d.scores_cut();
+    int64_t slots = 0;
+    for (int64_t n0 = 0; n0 < N; n0 += d.piece()) {
+        const int64_t n = N - n0 < d.piece() ? N - n0 : d.piece();
+        if ((st = pack(d, o, H, W, label, n0, n, d.pack_h && n0 == 0, d.pack_w, s)) != FASTGL_OK) return st;
+        LossTileArgs g = scores_of(d, o, H, W, b, label, n0, n);
+        g.stats = o.stats + 2 * slots * M;
+        g.picked = o.picked;
+        if ((st = launch<kScores, false>(g, cut, d.bf16, s, "fastgl_loss_fwd")) != FASTGL_OK) return st;
+        slots += ceil_div(n, Shape::wave_cols(cut));
+    }
+    return launch_join(o, slots, label, M, N, loss, lse, s);
+}
+
+fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label,
+                              const float *lse, const float *dloss, int64_t M, int64_t K, int64_t N, void *dH, void *dW, float *db,
+                              void *ws, size_t ws_bytes, void *stream)
+{
+    return loss_bwd(false, dtype, H, W, b, label, lse, dloss, M, K, N, dH, dW, db, ws, ws_bytes, stream);
+}
+
+fastgl_status fastgl_loss_bwd_coarse(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label,
+                                     const float *lse, const float *dloss, int64_t M, int64_t K, int64_t N, void *dH, void *dW, float *db,
+                                     void *ws, size_t ws_bytes, void *stream)
+{
+    return loss_bwd(true, dtype, H, W, b, label, lse, dloss, M, K, N, dH, dW, db, ws, ws_bytes, stream);
 }
 
 }  // extern "C"
