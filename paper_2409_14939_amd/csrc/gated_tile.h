@@ -235,9 +235,13 @@ __device__ __forceinline__ int scatter_sum(float (&v)[NV], int lane)
     }
 }
 
+// Whether log2 e times a finite score is no float.
+__device__ __forceinline__ bool beyond_log2e(float z) { return fabsf(z) > 2.3586e38f && fabsf(z) < INFINITY; }
+
 // A wavefront's scores: rows row0 + 32 i + lane % 32, columns col0 + 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4 in acc[i][j][e].
-// SCORES: maximum (times log2 e, so that lse comes from what the exponents were taken from) and sum of exponentials of its columns of each row,
-// and the label's score where it is among them.
+// SCORES: maximum and sum of exponentials (of what the maximum leaves) of its columns of each row, and the label's score where it is among them.  The
+// exponents are taken from the rounded product of the maximum and log2 e, which costs one operation a score; what its rounding left is a factor of the
+// sum.  Where that product is no float (scores of the type's lowest value rule a class out as well as -inf does) the maximum is subtracted first.
 // GRADIENT: dZ = g (exp(z - lse) - [label]), 0 in rows without a label and in columns that do not exist (to a multiple of 32), as
 // `planes` bf16 whose sum is it (one: rounded), and its column sums.
 // Labels are looked for only by wavefronts that have one.
@@ -271,15 +275,23 @@ __device__ __forceinline__ void loss_epilogue(const ARGS &g, f32x16 (&acc)[T::TM
 #pragma unroll
                 for (int e = 0; e < 16; ++e) most = fmaxf(most, acc[i][j][e]);
             most = fmaxf(most, __shfl_xor(most, 32, kWave));
-            const float top = most * kLog2e, base = most == -INFINITY ? 0.f : top;
+            const float base = most == -INFINITY ? 0.f : most * kLog2e;
+            if (beyond_log2e(most)) {
 #pragma unroll
-            for (int j = 0; j < T::TN; ++j)
+                for (int j = 0; j < T::TN; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -base));
+                    for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - most) * kLog2e);
+            } else {
+#pragma unroll
+                for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -base));
+                if (most != -INFINITY) sum *= __builtin_amdgcn_exp2f(-fmaf(most, kLog2e, -base));
+            }
             sum += __shfl_xor(sum, 32, kWave);
             if (h == 0 && in) {
                 typedef float f2 __attribute__((ext_vector_type(2)));
-                reinterpret_cast<f2 *>(g.stats)[col_slot * g.R + row] = f2{top, sum};
+                reinterpret_cast<f2 *>(g.stats)[col_slot * g.R + row] = f2{most, sum};
             }
             if (any) {
                 float z = 0.f;
@@ -296,12 +308,19 @@ __device__ __forceinline__ void loss_epilogue(const ARGS &g, f32x16 (&acc)[T::TM
             }
         } else {
             // a row without a label: exp(z - infinity) times 0
-            const float lse = label >= 0 ? g.lse[row] * kLog2e : INFINITY;
+            const float lse = label >= 0 ? g.lse[row] : INFINITY, base = lse * kLog2e;
             const float scale = label >= g.classes ? NAN : label >= 0 ? g.dloss[row] : 0.f;
+            if (beyond_log2e(lse)) {
 #pragma unroll
-            for (int j = 0; j < T::TN; ++j)
+                for (int j = 0; j < T::TN; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[i][j][e] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -lse)) * scale;
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] = __builtin_amdgcn_exp2f((acc[i][j][e] - lse) * kLog2e) * scale;
+            } else {
+#pragma unroll
+                for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], kLog2e, -base)) * scale;
+            }
             if (any) {
 #pragma unroll
                 for (int j = 0; j < T::TN; ++j)

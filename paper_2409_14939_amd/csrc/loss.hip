@@ -77,18 +77,18 @@ __global__ __launch_bounds__(kBlock) void k_loss_pack(LossPackArgs a)
 __global__ __launch_bounds__(kBlock) void k_loss_join(const float *stats, int64_t slots, const float *picked, const int64_t *label, int64_t M, int64_t N,
                                                       int lg, float *loss, float *lse)
 {
-    constexpr float kLn2 = 0.69314718056f;
+    constexpr float kLog2e = 1.44269504089f, kLn2 = 0.69314718056f;
     __shared__ float most[kBlock], sums[kBlock];
     const int parts = kBlock >> lg, part = threadIdx.x >> lg, r = threadIdx.x & ((1 << lg) - 1);
     const int64_t row = ((int64_t)blockIdx.x << lg) + r;
     typedef float f2 __attribute__((ext_vector_type(2)));
     const f2 *p = reinterpret_cast<const f2 *>(stats) + (row < M ? row : M - 1);
-    float m = -INFINITY, s = 0.f;                     // the maximum in powers of two
+    float m = -INFINITY, s = 0.f;
 #pragma unroll 4
     for (int64_t t = part; t < slots; t += parts) {
         const f2 x = p[t * M];
         const float next = fmaxf(m, x[0]), base = next == -INFINITY ? 0.f : next;
-        s = s * __builtin_amdgcn_exp2f(m - base) + x[1] * __builtin_amdgcn_exp2f(x[0] - base);
+        s = s * __builtin_amdgcn_exp2f((m - base) * kLog2e) + x[1] * __builtin_amdgcn_exp2f((x[0] - base) * kLog2e);
         m = next;
     }
     most[threadIdx.x] = m;
@@ -98,8 +98,8 @@ __global__ __launch_bounds__(kBlock) void k_loss_join(const float *stats, int64_
     for (int q = 1; q < parts; ++q) m = fmaxf(m, most[(q << lg) + r]);
     const float base = m == -INFINITY ? 0.f : m;
     s = 0.f;
-    for (int q = 0; q < parts; ++q) s += sums[(q << lg) + r] * __builtin_amdgcn_exp2f(most[(q << lg) + r] - base);
-    const float all = m == -INFINITY && s == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(s)) * kLn2;
+    for (int q = 0; q < parts; ++q) s += sums[(q << lg) + r] * __builtin_amdgcn_exp2f((most[(q << lg) + r] - base) * kLog2e);
+    const float all = m == -INFINITY && s == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(s) * kLn2;
     if (lse) lse[row] = all;
     const int64_t y = label[row];
     loss[row] = y < 0 ? 0.f : y >= N ? NAN : all - picked[row];
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(THREADS) void k_loss_block(LossBlockArgs a)
             }
             if (row < rows && c0 == 0) {
                 if (a.stats) {
-                    a.stats[2 * (strip * a.M + row0 + row)] = most * kLog2e;
+                    a.stats[2 * (strip * a.M + row0 + row)] = most;
                     a.stats[2 * (strip * a.M + row0 + row) + 1] = sum;
                     if (label >= col0 && label < col0 + left) a.picked[row0 + row] = at;
                 } else {
