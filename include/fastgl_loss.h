@@ -20,7 +20,8 @@
  * 2^-24 in fp32 ones (three), or as it is (small calls).  fastgl_loss_bwd_coarse rounds it to one bf16 in bf16 calls, at every size: dH and dW are
  * up to sqrt 2 times as far off, for half the products; fp32 calls are as with fastgl_loss_bwd.  db is of the unrounded values.  Results are rounded once.  exp(z - lse) is
  * off by 2^-23 (2 + |z| + |lse|) of itself and by its score's error.  A row with a score of NaN or +inf has loss and dH NaN; scores of
- * -inf and of the type's lowest value (a bias that rules a class out) weigh nothing where another class remains.
+ * -inf and of the type's lowest value (a bias that rules a class out) weigh nothing where another class remains.  The pieces of an infinite
+ * fp32 element of H or W are not finite either: its scores are NaN (in small calls what IEEE arithmetic gives).
  *
  * Conventions are those of fastgl_agg.h: caller-owned DEVICE memory aligned to the element size; nothing is
  * allocated, scratch comes from `workspace` (256-byte aligned); work is enqueued on `stream` without synchronising the host;

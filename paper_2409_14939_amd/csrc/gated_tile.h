@@ -307,10 +307,14 @@ __device__ __forceinline__ void loss_epilogue(const ARGS &g, f32x16 (&acc)[T::TM
                 if (has) g.picked[row] = z;
             }
         } else {
-            // a row without a label: exp(z - infinity) times 0
-            const float lse = label >= 0 ? g.lse[row] : INFINITY, base = lse * kLog2e;
+            const float lse = label >= 0 ? g.lse[row] : 0.f, base = lse * kLog2e;
             const float scale = label >= g.classes ? NAN : label >= 0 ? g.dloss[row] : 0.f;
-            if (beyond_log2e(lse)) {
+            if (label < 0) {                                              // whatever the scores are: a NaN of the weights or the bias times 0
+#pragma unroll
+                for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+            } else if (beyond_log2e(lse)) {
 #pragma unroll
                 for (int j = 0; j < T::TN; ++j)
 #pragma unroll

@@ -6,7 +6,7 @@ from paper_2409_14939_amd import binding as B
 
 pytestmark = pytest.mark.gpu
 LOWEST = torch.finfo(torch.float32).min
-SIZES = [(7, 5, 47), (80, 8, 700), (4000, 8, 3000)]            # one strip of classes, several, tiles
+SIZES = [(7, 5, 47), (80, 8, 700), (4000, 8, 3000), (2000, 200, 2500)]            # one strip of classes, several; tiles forward, and both ways
 
 
 def inputs(M, K, N, dtype):
