@@ -38,7 +38,7 @@ extern "C" {
 #endif
 
 /* Bytes of workspace of a call.  `aligned`: whether H and W start at multiples of 16 bytes; 0 is the bound for both.  The classes are
- * taken in pieces, so that the backward pass's dZ stays below 1 GiB (256 classes at least). */
+ * taken in pieces, so that the forward pass's statistics, the backward pass's dZ and packed weights stay below 1 GiB each (256 classes at least). */
 size_t fastgl_loss_fwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned);
 size_t fastgl_loss_bwd_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned);
 size_t fastgl_loss_bwd_coarse_workspace_bytes(fastgl_dtype dtype, int64_t M, int64_t K, int64_t N, int aligned);

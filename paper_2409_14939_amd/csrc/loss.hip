@@ -1,7 +1,8 @@
 // Softmax cross entropy of class scores that are not kept (fastgl_loss.h has the formulas): what is around the products of gated_tile.h.
 //
-//   forward   [operands packed] -> scores by tiles, of which maximum and sum of exponentials of some columns of each row remain -> k_loss_join
-//   backward  for a piece of the classes at a time: [W packed] -> scores again, of which dZ remains (as the matrix cores take it: fp32 calls in three bf16
+//   forward   for a piece of the classes at a time: [operands packed] -> scores by tiles, of which maximum and sum of exponentials of some columns of
+//             each row remain -> k_loss_join
+//   backward  the same: [W packed] -> scores again, of which dZ remains (as the matrix cores take it: fp32 calls in three bf16
 //             pieces, bf16 calls in two, or rounded to one for a caller who asks for that; with column sums)
 //             -> dH += dZ W^T -> dW = H^T dZ -> k_loss_sum
 //
@@ -73,9 +74,10 @@ __global__ __launch_bounds__(kBlock) void k_loss_pack(LossPackArgs a)
 }
 
 // ------------------------------------------------------------------ joining
-// A row's maxima and sums from all column tiles, 2^lg rows and as many threads a row as are left.
-__global__ __launch_bounds__(kBlock) void k_loss_join(const float *stats, int64_t slots, const float *picked, const int64_t *label, int64_t M, int64_t N,
-                                                      int lg, float *loss, float *lse)
+// A row's maxima and sums from all column tiles of a piece of the classes and what the pieces before left (before, or NULL), 2^lg rows and as many
+// threads a row as are left; after: not the last piece, the row's pair goes there.
+__global__ __launch_bounds__(kBlock) void k_loss_join(const float *stats, int64_t slots, const float *before, float *after, const float *picked,
+                                                      const int64_t *label, int64_t M, int64_t N, int lg, float *loss, float *lse)
 {
     constexpr float kLog2e = 1.44269504089f, kLn2 = 0.69314718056f;
     __shared__ float most[kBlock], sums[kBlock];
@@ -84,6 +86,11 @@ __global__ __launch_bounds__(kBlock) void k_loss_join(const float *stats, int64_
     typedef float f2 __attribute__((ext_vector_type(2)));
     const f2 *p = reinterpret_cast<const f2 *>(stats) + (row < M ? row : M - 1);
     float m = -INFINITY, s = 0.f;
+    if (before && part == 0 && row < M) {
+        const f2 x = reinterpret_cast<const f2 *>(before)[row];
+        m = x[0];
+        s = x[1];
+    }
 #pragma unroll 4
     for (int64_t t = part; t < slots; t += parts) {
         const f2 x = p[t * M];
@@ -99,6 +106,10 @@ __global__ __launch_bounds__(kBlock) void k_loss_join(const float *stats, int64_
     const float base = m == -INFINITY ? 0.f : m;
     s = 0.f;
     for (int q = 0; q < parts; ++q) s += sums[(q << lg) + r] * __builtin_amdgcn_exp2f((most[(q << lg) + r] - base) * kLog2e);
+    if (after) {
+        reinterpret_cast<f2 *>(after)[row] = f2{m, s};
+        return;
+    }
     const float all = m == -INFINITY && s == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(s) * kLn2;
     if (lse) lse[row] = all;
     const int64_t y = label[row];
@@ -460,11 +471,11 @@ struct Shape {
     {
     }
     int64_t rows() const { return (int64_t)align_up((size_t)M, 256); }
-    // Classes of a piece: dZ and packed weights stay below kPieceBytes, the pieces are of one size.
+    // Classes of a piece: dZ, a forward pass's statistics (8 bytes for 64 classes of a row at most) and packed weights stay below kPieceBytes, the
+    // pieces are of one size.
     int64_t piece() const
     {
-        int64_t most = N;
-        if (backward) most = kPieceBytes / (2 * z_planes * rows());
+        int64_t most = backward ? kPieceBytes / (2 * z_planes * rows()) : kPieceBytes / 8 * 64 / M;
         if (pack_w && K > 0 && kPieceBytes / (2 * planes * K) < most) most = kPieceBytes / (2 * planes * K);
         if (most >= N) return (int64_t)align_up((size_t)N, kPieceCols);
         most = most < 2 * kPieceCols ? kPieceCols : most / kPieceCols * kPieceCols;
@@ -483,11 +494,7 @@ struct Shape {
     Cut weights_cut() const { return cut_of(kWeights, K, widest(), M, z_pairs, true); }
     static int64_t tile_rows(const Cut &c) { return c.size == kLarge ? 256 : 128; }
     static int64_t wave_cols(const Cut &c) { return c.size == kSmall ? 64 : 128; }
-    int64_t slots() const                                                  // of statistics: column tiles and wavefronts of all pieces
-    {
-        const int64_t per = ceil_div(widest(), wave_cols(scores_cut()));
-        return per * pieces();
-    }
+    int64_t slots() const { return ceil_div(widest(), wave_cols(scores_cut())); }      // of statistics: column tiles and wavefronts of a piece
     int64_t db_rows() const { return ceil_div(M, tile_rows(scores_cut())) * (scores_cut().size == kLarge ? 4 : 2); }
     bool parts_h() const { return pieces() > 1 || rows_cut().slabs > 1; }
 
@@ -541,7 +548,7 @@ struct Scratch {
     size_t used = 0;
     char *base;
     uint16_t *h, *w, *dz;
-    float *stats, *picked, *db, *part_h, *part_w;
+    float *stats, *picked, *joined, *db, *part_h, *part_w;
     template <class T>
     T *take(size_t n)
     {
@@ -552,7 +559,7 @@ struct Scratch {
     Scratch(const Shape &s, char *at) : base(at)
     {
         h = w = dz = nullptr;
-        stats = picked = db = part_h = part_w = nullptr;
+        stats = picked = joined = db = part_h = part_w = nullptr;
         if (s.small()) {
             if (!s.backward && s.strips() > 1) {
                 stats = take<float>((size_t)(2 * s.strips() * s.M));
@@ -570,6 +577,7 @@ struct Scratch {
         if (!s.backward) {
             stats = take<float>((size_t)(2 * s.slots() * s.M));
             picked = take<float>((size_t)s.M);
+            if (s.pieces() > 1) joined = take<float>((size_t)(2 * s.M));
             return;
         }
         dz = take<uint16_t>((size_t)(s.z_planes * s.z_plane()));
@@ -643,12 +651,12 @@ fastgl_status launch_block(const Shape &d, LossBlockArgs a, hipStream_t s, const
     return FASTGL_OK;
 }
 
-fastgl_status launch_join(const Scratch &o, int64_t slots, const int64_t *label, int64_t M, int64_t N, float *loss, float *lse, hipStream_t s)
+fastgl_status launch_join(const Scratch &o, int64_t slots, bool first, bool last, const int64_t *label, int64_t M, int64_t N, float *loss, float *lse, hipStream_t s)
 {
     int lg = 0;
     while ((lg < 5 && ((int64_t)1 << lg) < M) || (lg < 8 && M >> lg >= (int64_t)1 << 22)) ++lg;       // a launch has less than 2^32 threads
-    hipLaunchKernelGGL(k_loss_join, dim3((unsigned)ceil_div(M, (int64_t)1 << lg)), dim3(kBlock), 0, s, (const float *)o.stats, slots, (const float *)o.picked,
-                       label, M, N, lg, loss, lse);
+    hipLaunchKernelGGL(k_loss_join, dim3((unsigned)ceil_div(M, (int64_t)1 << lg)), dim3(kBlock), 0, s, (const float *)o.stats, slots,
+                       first ? nullptr : (const float *)o.joined, last ? nullptr : o.joined, (const float *)o.picked, label, M, N, lg, loss, lse);
     FASTGL_LAUNCH_CHECK("fastgl_loss_fwd (rows)");
     return FASTGL_OK;
 }
@@ -925,20 +933,19 @@ fastgl_status fastgl_loss_fwd(fastgl_dtype dtype, const void *H, const void *W, 
         a.loss = loss; a.lse = lse;
         a.stats = o.stats; a.picked = o.picked;
         st = launch_block(d, a, s, "fastgl_loss_fwd (small)");
-        return st != FASTGL_OK || d.strips() == 1 ? st : launch_join(o, d.strips(), label, M, N, loss, lse, s);
+        return st != FASTGL_OK || d.strips() == 1 ? st : launch_join(o, d.strips(), true, true, label, M, N, loss, lse, s);
     }
     const Cut cut = d.scores_cut();
-    int64_t slots = 0;
     for (int64_t n0 = 0; n0 < N; n0 += d.piece()) {
         const int64_t n = N - n0 < d.piece() ? N - n0 : d.piece();
         if ((st = pack(d, o, H, W, label, n0, n, d.pack_h && n0 == 0, d.pack_w, s)) != FASTGL_OK) return st;
         LossTileArgs g = scores_of(d, o, H, W, b, label, n0, n);
-        g.stats = o.stats + 2 * slots * M;
+        g.stats = o.stats;
         g.picked = o.picked;
         if ((st = launch<kScores, false>(g, cut, d.bf16, s, "fastgl_loss_fwd")) != FASTGL_OK) return st;
-        slots += ceil_div(n, Shape::wave_cols(cut));
+        if ((st = launch_join(o, ceil_div(n, Shape::wave_cols(cut)), n0 == 0, n0 + n == N, label, M, N, loss, lse, s)) != FASTGL_OK) return st;
     }
-    return launch_join(o, slots, label, M, N, loss, lse, s);
+    return FASTGL_OK;
 }
 
 fastgl_status fastgl_loss_bwd(fastgl_dtype dtype, const void *H, const void *W, const float *b, const int64_t *label,

@@ -1,0 +1,48 @@
+"""The loss's forward pass with the classes in several pieces, and launches of very many tiles: some rows against the 64-bit form."""
+import pytest
+import torch
+
+from loss_ref import Loss
+from paper_2409_14939_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def check_rows(H, W, b, label, loss, lse, rows):
+    ref = Loss(H[rows], W, b, label[rows])
+    for got, name in ((loss[rows], "loss"), (lse[rows], "lse")):
+        want, off = getattr(ref, name), getattr(ref, "off_" + name)
+        same = (got.double() == want)
+        assert bool((off < 1e-2 * want[torch.isfinite(want)].abs().max()).all())
+        assert bool((same | ((got.double() - want).abs() <= off + 2.0 ** -24 * (want.abs() + off))).all()), name
+
+
+# more than one piece of statistics from 2^33 rows x classes on; classes that are no multiple of 8 are packed, piece by piece
+@pytest.mark.parametrize("dtype,M,K,N", [("bf16", 300_000, 16, 40_000), ("bf16", 300_001, 9, 40_001), ("f32", 250_000, 8, 40_000), ("bf16", 1 << 22, 8, 65_536)])
+def test_statistics_of_several_pieces(dtype, M, K, N):
+    g = torch.Generator(device="cuda").manual_seed(4)
+    make = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    t = torch.float32 if dtype == "f32" else torch.bfloat16
+    H, W, b = make(M, K).to(t), (2.0 * make(K, N) / K ** 0.5).to(t), 0.5 * make(N)
+    label = torch.randint(-1, N, (M,), generator=g, device="cuda")
+    need = B.fastgl_loss_fwd_workspace_bytes(dtype, M, K, N, True)
+    assert need < (3 << 30) and M * N > 1 << 33
+    ws = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    loss, lse = B.fastgl_loss_fwd(H, W, b, label, workspace=ws[:need])
+    assert bool((ws[need:] == 0xA5).all())
+    rows = torch.cat((torch.arange(60), torch.arange(M // 2, M // 2 + 60), torch.arange(M - 60, M))).cuda()
+    check_rows(H, W, b, label, loss, lse, rows)
+    assert bool(torch.isfinite(loss).all()) and not bool(loss[label < 0].any())
+    ws[:need] = 0xFF
+    again = B.fastgl_loss_fwd(H, W, b, label, workspace=ws[:need])
+    assert torch.equal(again[0], loss) and torch.equal(again[1], lse)
+    # classes that are ruled out: all of the first piece, all of the last, all of them
+    label[label >= 0] = N // 2
+    b[:N // 2 - 100] = -float("inf")
+    loss, lse = B.fastgl_loss_fwd(H, W, b, label, workspace=ws[:need])
+    check_rows(H, W, b, label, loss, lse, rows)
+    b[N // 2 + 100:] = torch.finfo(torch.float32).min
+    loss, lse = B.fastgl_loss_fwd(H, W, b, label, workspace=ws[:need])
+    check_rows(H, W[:, N // 2 - 100:N // 2 + 100], b[N // 2 - 100:N // 2 + 100], torch.where(label < 0, -1, 100), loss, lse, rows)
+    b[:] = -float("inf")
+    assert bool((B.fastgl_loss_fwd(H, W, b, label)[1] == -float("inf")).all())

@@ -18,3 +18,16 @@ def test_coarse_calls_are_checked_alike():
         assert size("bf16", M, K, N) > 2 * 2 * M * N and size("bf16", M, K, N, coarse=True) > 2 * M * N      # two pieces of dZ, one
         assert size("f32", M, K, N, coarse=True) == size("f32", M, K, N)
     assert coarse(M=4096, K=128, N=4096, wsb=size("bf16", 4096, 128, 4096, True, coarse=True) - 1) == WORKSPACE
+
+
+def test_no_workspace_grows_with_rows_times_classes():
+    """H and W packed, a piece of statistics (8 bytes for 64 classes of a row at most) or of dZ, sums of rows; over the whole range of sizes."""
+    for dt in ("f32", "bf16"):
+        for M in (1, 300, 8192, 32_768, 10 ** 6, 2 ** 20, 2 ** 22, 2 ** 26, 2 ** 31 - 1 - 1024):
+            for N in (1, 47, 65_536, 10 ** 6, 2 ** 21):
+                for K in (0, 1, 256, 512):
+                    if M * K > 2 ** 38:
+                        continue
+                    for aligned in (False, True):
+                        size = B.fastgl_loss_fwd_workspace_bytes(dt, M, K, N, aligned)
+                        assert size <= 6 * M * (K + 8) + max(1 << 30, 6 * K * 512) + max(1 << 30, 8 * M * 4) + 12 * M + 4096, (dt, M, K, N, size)
