@@ -694,7 +694,7 @@ fastgl_status launch(const LossTileArgs &args, const Cut &cut, bool bf16, hipStr
 {
     typename TileArgsOf<MODE>::type g = args;
     const int64_t tr = ceil_div(g.R, Shape::tile_rows(cut)), tc = ceil_div(g.C, cut.size == kSmall ? 128 : 256), total = tr * tc * cut.slabs;
-    if (total > (int64_t)UINT32_MAX / 512 || 4 * tc > 0x7FFFFFFFLL) {
+    if (total > (int64_t)UINT32_MAX / (cut.size == kLarge ? Tile<MODE, kLarge>::THREADS : Tile<MODE, kSmall>::THREADS) || 4 * tc > 0x7FFFFFFFLL) {
         set_error("%s: too many tiles (%lld)", what, (long long)total);
         return FASTGL_ERR_UNSUPPORTED;
     }

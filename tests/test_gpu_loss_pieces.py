@@ -46,3 +46,21 @@ def test_statistics_of_several_pieces(dtype, M, K, N):
     check_rows(H, W[:, N // 2 - 100:N // 2 + 100], b[N // 2 - 100:N // 2 + 100], torch.where(label < 0, -1, 100), loss, lse, rows)
     b[:] = -float("inf")
     assert bool((B.fastgl_loss_fwd(H, W, b, label)[1] == -float("inf")).all())
+
+
+def test_more_rows_than_tiles_of_512_threads_have():
+    """A launch has less than 2^32 threads: 2^30 rows are 2^23 tiles of 256."""
+    M, N = (1 << 30) + 5, 2
+    H = torch.zeros(M, 1, device="cuda", dtype=torch.bfloat16)
+    label = torch.full((M,), -1, device="cuda", dtype=torch.int64)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    parts = [slice(at, at + 1000) for at in (0, M // 2, M - 1000)]
+    for part in parts:
+        H[part] = torch.randn(1000, 1, generator=g, device="cuda").bfloat16()
+        label[part] = torch.randint(-1, N, (1000,), generator=g, device="cuda")
+    W, b = torch.randn(1, N, generator=g, device="cuda").bfloat16(), torch.randn(N, generator=g, device="cuda")
+    loss, lse = B.fastgl_loss_fwd(H, W, b, label)
+    rows = torch.cat([torch.arange(p.start, p.stop) for p in parts]).cuda()
+    check_rows(H, W, b, label, loss, lse, rows)
+    between = slice(1000, M // 2)
+    assert bool((lse[between] == lse[1000]).all()) and not bool(loss[between].any())
