@@ -69,8 +69,8 @@ size_t fastgl_attn_workspace_bytes(const fastgl_attn_desc *desc, int backward);
 
 /* Forward pass.  lse may be NULL.  plan: NULL, or a plan of exactly this block with
  * FASTGL_PLAN_FWD; it is read for rows of more than fastgl_long_row_threshold() edges, and a block of so few edges needs
- * none.  With NULL the bookkeeping is rebuilt inside `workspace`.  With FASTGL_PLAN_SHORT_DST_ROWS every row is walked by one
- * group of lanes. */
+ * none.  With NULL the bookkeeping is rebuilt inside `workspace`.  With FASTGL_PLAN_SHORT_DST_ROWS every row of a block
+ * of at most 2^24 edges is walked by one wavefront. */
 fastgl_status fastgl_attn_fwd(const fastgl_attn_desc *desc, void *O, int64_t ldo, float *lse, const fastgl_plan *plan,
                               void *workspace, size_t workspace_bytes, void *stream);
 

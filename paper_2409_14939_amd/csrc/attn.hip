@@ -25,6 +25,7 @@ constexpr int kSegment = 16;              // steps that a group takes where a ne
 constexpr int kSlack = 8;                 // steps more than shorter segments have that a group takes alone rather than have them cut
 constexpr int kTransposedSteps = 6;       // of a group, on average, that a wavefront of the transposed pass takes units for
 constexpr int kBiasBlocks = 1024;         // workgroups of k_attn_dbias
+constexpr int64_t kHintEdges = (int64_t)1 << 24;      // blocks of more have their long rows looked for whatever the plan's hint says
 constexpr int kJoin = 1024;               // threads of a workgroup that joins chunks
 constexpr int kBiasTile = 64;             // buckets of one of its passes
 
@@ -1109,7 +1110,8 @@ fastgl_status launch_walk(AttnArgs a, const fastgl_attn_desc &d, const fastgl_pl
     a.dealt = T && rows >= 512;
     a.units = (a.dealt ? (int64_t)align_up((size_t)rows, 512) : rows) * a.unit_heads;
     a.heads_inv = a.unit_heads > 1 ? UINT64_MAX / (uint64_t)a.unit_heads + 1 : 0;
-    const bool chunked = d.num_edges > kLongThreshold && (T || !(pl->parts & FASTGL_PLAN_SHORT_DST_ROWS));
+    // The hint may be wrong: a wavefront's units together then have up to 64 num_edges steps, which are counted in 32 bits.
+    const bool chunked = d.num_edges > kLongThreshold && (T || !(pl->parts & FASTGL_PLAN_SHORT_DST_ROWS) || d.num_edges > kHintEdges);
     a.long_thr = chunked ? kLongThreshold : INT32_MAX;
     if (chunked) {
         a.long_rows = T ? pl->long_src : pl->long_dst;
