@@ -524,7 +524,9 @@ __global__ __launch_bounds__(kBlock, LG >= 4 ? 3 : 4) void k_attn_fwd(AttnArgs a
 
 // ------------------------------------------------------------------ dQ
 // sum p dp comes with the sums of p dp K and p K in one walk: dQ = scale (sum p dp K - (sum p dp) sum p K), all of them of e^(s - maximum)
-// first and divided by its sum at the end.
+// first and divided by its sum at the end.  dp is taken less that of the first edge that takes part (of a group's part of the row; joined parts are
+// brought to one of them), which changes no result but its error: with |dp - delta|, not with |dp|, where V or K have a mean, and nothing at all in a
+// row of one edge.
 template <bool BF16, int PC, int LG_, bool NEAR>
 struct QueryRow {
     typedef Piece<BF16, PC> P;
@@ -534,7 +536,7 @@ struct QueryRow {
     const Where<P, LG, NEAR> w;
     P q, g;                        // this row's own operands
     int head, col;
-    float pk[N], pdk[N], m, sum, delta;
+    float pk[N], pdk[N], m, sum, delta, ref;      // pdk and delta: of dp - ref
     __device__ __forceinline__ QueryRow(const AttnArgs &args) : a(args), w(args.width) {}
     __device__ __forceinline__ void own(int64_t row, int h)
     {
@@ -548,7 +550,7 @@ struct QueryRow {
         w.cut(q);
         w.cut(g);
         m = -INFINITY;
-        sum = delta = 0.f;
+        sum = delta = ref = 0.f;
 #pragma unroll
         for (int x = 0; x < N; ++x) pk[x] = pdk[x] = 0.f;
     }
@@ -573,6 +575,9 @@ struct QueryRow {
             most = fmaxf(most, s[j]);
         }
         const float base = most == -INFINITY ? 0.f : most, old = exp_of(m - base);
+        const bool none = m == -INFINITY;             // nothing has taken part yet
+#pragma unroll
+        for (int j = U - 1; j >= 0; --j) ref = none && s[j] > -INFINITY && fabsf(dp[j]) < INFINITY ? dp[j] : ref;
         m = most;
         sum *= old;
         delta *= old;
@@ -583,7 +588,7 @@ struct QueryRow {
         }
 #pragma unroll
         for (int j = 0; j < U; ++j) {
-            const float p = exp_of(s[j] - base), pd = p == 0.f ? 0.f : p * dp[j];
+            const float p = exp_of(s[j] - base), pd = p == 0.f ? 0.f : p * (dp[j] - ref);
             sum += p;
             delta += pd;
             k[j].keep(p != 0.f);
@@ -594,46 +599,50 @@ struct QueryRow {
             }
         }
     }
-    __device__ __forceinline__ void merge(const float (&v)[2 * N + 3])
+    __device__ __forceinline__ void merge(const float (&v)[2 * N + 4])
     {
         const float most = fmaxf(m, v[0]), base = most == -INFINITY ? 0.f : most, by = exp_of(m - base), by2 = exp_of(v[0] - base);
+        ref = m == -INFINITY ? v[3] : ref;
+        const float more = v[3] - ref;                // 0 - ref where the other part has nothing: of sums that are 0
         m = most;
+        delta = delta * by + fmaf(more, v[1], v[2]) * by2;
         sum = sum * by + v[1] * by2;
-        delta = delta * by + v[2] * by2;
 #pragma unroll
         for (int x = 0; x < N; ++x) {
-            pk[x] = pk[x] * by + v[3 + x] * by2;
-            pdk[x] = pdk[x] * by + v[3 + N + x] * by2;
+            pk[x] = pk[x] * by + v[4 + x] * by2;
+            pdk[x] = pdk[x] * by + fmaf(more, v[4 + x], v[4 + N + x]) * by2;
         }
     }
     __device__ __forceinline__ void join(int d, bool on)
     {
-        float v[2 * N + 3];
+        float v[2 * N + 4];
         v[0] = __shfl_down(m, d, kWave);
         v[1] = __shfl_down(sum, d, kWave);
         v[2] = __shfl_down(delta, d, kWave);
+        v[3] = __shfl_down(ref, d, kWave);
 #pragma unroll
         for (int x = 0; x < N; ++x) {
-            v[3 + x] = __shfl_down(pk[x], d, kWave);
-            v[3 + N + x] = __shfl_down(pdk[x], d, kWave);
+            v[4 + x] = __shfl_down(pk[x], d, kWave);
+            v[4 + N + x] = __shfl_down(pdk[x], d, kWave);
         }
         if (on) merge(v);
     }
-    static constexpr int VALUES = 2 * N + 3;
+    static constexpr int VALUES = 2 * N + 4;
     __device__ __forceinline__ void leave(float (&slots)[VALUES][kWave], int at) const
     {
         slots[0][at] = m;
         slots[1][at] = sum;
         slots[2][at] = delta;
+        slots[3][at] = ref;
 #pragma unroll
         for (int x = 0; x < N; ++x) {
-            slots[3 + x][at] = pk[x];
-            slots[3 + N + x][at] = pdk[x];
+            slots[4 + x][at] = pk[x];
+            slots[4 + N + x][at] = pdk[x];
         }
     }
     __device__ __forceinline__ void add_from(float (&slots)[VALUES][kWave], int at)
     {
-        float v[2 * N + 3];
+        float v[2 * N + 4];
 #pragma unroll
         for (int x = 0; x < VALUES; ++x) v[x] = slots[x][at];
         merge(v);
@@ -647,7 +656,7 @@ struct QueryRow {
     {
         w.store_sums(a.part, at * a.width, pdk);
         w.store_sums(a.part + a.part_stride, at * a.width, pk);
-        if (w.l == 0) reinterpret_cast<f32x4 *>(a.part_more)[at] = f32x4{m, sum, delta, 0.f};
+        if (w.l == 0) reinterpret_cast<f32x4 *>(a.part_more)[at] = f32x4{m, sum, delta, ref};
     }
     __device__ __forceinline__ void store(int64_t r, int h)
     {
@@ -656,7 +665,7 @@ struct QueryRow {
 #pragma unroll
         for (int x = 0; x < N; ++x) o[x] = a.scale * by * fmaf(-d, pk[x], pdk[x]);
         if (a.dQ) w.store(a.dQ, r, a.lddq, h * a.width, o);
-        if (w.l == 0) a.stats[r * a.heads + h] = f32x4{m, by, d, 0.f};
+        if (w.l == 0) a.stats[r * a.heads + h] = f32x4{m, by, ref + d, 0.f};
     }
 };
 
@@ -795,7 +804,7 @@ __global__ __launch_bounds__(kJoin) void k_attn_join(AttnArgs a, int lg)
     constexpr int MORE = KIND == 1 ? 4 : 2, NS = KIND == 0 ? 2 : KIND == 1 ? 4 : 2;       // sums: columns' (one or two), the row's
     const int cols = a.unit_heads * a.width, tiles = (cols + (1 << lg) - 1) >> lg, parts = kJoin >> lg;
     const int c = threadIdx.x & ((1 << lg) - 1), part = threadIdx.x >> lg;
-    __shared__ float sums[NS][kJoin], most[kJoin];
+    __shared__ float sums[NS][kJoin], most[kJoin], refs[KIND == 1 ? kJoin : 1];
     const int64_t total = (int64_t)*a.n_long * tiles;
     for (int64_t unit = blockIdx.x; unit < total; unit += gridDim.x) {
         const int li = (int)(unit / tiles), col = ((int)(unit - (int64_t)li * tiles) << lg) + c;
@@ -804,12 +813,17 @@ __global__ __launch_bounds__(kJoin) void k_attn_join(AttnArgs a, int lg)
         const int lo = first + part * per, hi = lo + per < first + n ? lo + per : first + n;
         const int h = col < cols ? col / a.width : 0;
         const float *p = a.part + (col < cols ? col : 0), *more = a.part_more;
-        float v[NS], m = -INFINITY;
+        float v[NS], m = -INFINITY, ref = 0.f;        // ref: of a chunk that something takes part in, see dQ's walk
 #pragma unroll
         for (int i = 0; i < NS; ++i) v[i] = 0.f;
         if (KIND != 2)
 #pragma unroll 4
-            for (int k = lo; k < hi; ++k) m = fmaxf(m, more[MORE * ((int64_t)k * a.unit_heads + h)]);
+            for (int k = lo; k < hi; ++k) {
+                const int64_t at = MORE * ((int64_t)k * a.unit_heads + h);
+                const float its = more[at];
+                if constexpr (KIND == 1) ref = m == -INFINITY ? more[at + 3] : ref;
+                m = fmaxf(m, its);
+            }
         const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll 4
         for (int k = lo; k < hi; ++k) {
@@ -819,11 +833,14 @@ __global__ __launch_bounds__(kJoin) void k_attn_join(AttnArgs a, int lg)
                 v[1] += p[a.part_stride + to];
             } else {
                 const float by = exp_of(more[at] - base);
-                v[0] += by == 0.f ? 0.f : by * p[to];
                 v[1] += by * more[at + 1];
-                if constexpr (KIND == 1) {
-                    v[2] += by == 0.f ? 0.f : by * p[a.part_stride + to];
-                    v[3] += by == 0.f ? 0.f : by * more[at + 2];
+                if constexpr (KIND == 0) {
+                    v[0] += by == 0.f ? 0.f : by * p[to];
+                } else {
+                    const float x = more[at + 3] - ref, pk = p[a.part_stride + to];
+                    v[0] += by == 0.f ? 0.f : by * fmaf(x, pk, p[to]);
+                    v[2] += by == 0.f ? 0.f : by * pk;
+                    v[3] += by == 0.f ? 0.f : by * fmaf(x, more[at + 1], more[at + 2]);
                 }
             }
         }
@@ -831,19 +848,26 @@ __global__ __launch_bounds__(kJoin) void k_attn_join(AttnArgs a, int lg)
 #pragma unroll
         for (int i = 0; i < NS; ++i) sums[i][threadIdx.x] = v[i];
         if (KIND != 2) most[threadIdx.x] = m;
+        if (KIND == 1) refs[threadIdx.x] = ref;
         __syncthreads();
         if (part != 0 || col >= cols) continue;       // the barriers of the next row are reached by all
         if (KIND != 2)
-            for (int r = 1; r < parts; ++r) m = fmaxf(m, most[(r << lg) + c]);
+            for (int r = 1; r < parts; ++r) {
+                if constexpr (KIND == 1) ref = m == -INFINITY ? refs[(r << lg) + c] : ref;
+                m = fmaxf(m, most[(r << lg) + c]);
+            }
         const float all = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int i = 0; i < NS; ++i) v[i] = 0.f;
         for (int r = 0; r < parts; ++r) {
             const float by = KIND == 2 ? 1.f : exp_of(most[(r << lg) + c] - all);
+            const float x = KIND == 1 ? refs[KIND == 1 ? (r << lg) + c : 0] - ref : 0.f;
 #pragma unroll
             for (int i = 0; i < NS; ++i) {            // a sum of NaN (its scores leave no maximum) stays: every result is divided by it
                 const bool none = by == 0.f && (KIND == 2 || i != 1);
-                v[i] += none ? 0.f : by * sums[i][(r << lg) + c];
+                float its = sums[i][(r << lg) + c];
+                if (KIND == 1 && (i == 0 || i == 3)) its = fmaf(x, sums[i == 0 ? 2 : 1][(r << lg) + c], its);
+                v[i] += none ? 0.f : by * its;
             }
         }
         auto put = [&](void *out, int64_t ld, float x) {
@@ -863,7 +887,7 @@ __global__ __launch_bounds__(kJoin) void k_attn_join(AttnArgs a, int lg)
             } else {
                 const float delta = v[3] * by;
                 put(a.dQ, a.lddq, a.scale * by * fmaf(-delta, v[2], v[0]));
-                if (col == h * a.width) a.stats[row * a.heads + h] = f32x4{m, by, delta, 0.f};
+                if (col == h * a.width) a.stats[row * a.heads + h] = f32x4{m, by, ref + delta, 0.f};
             }
         }
     }
