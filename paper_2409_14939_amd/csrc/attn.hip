@@ -121,10 +121,11 @@ struct Piece<BF16, 0> {
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // x + x of the lane across: the first four exchanges stay within sixteen lanes and need no LDS.  After them both lanes of a pair
-// hold the same sum, so that mirrored lanes are as good as those across.
+// hold the same sum, so that mirrored lanes are as good as those across: a product of one element a lane is rounded before it is added.
 template <int CTRL>
 __device__ __forceinline__ float plus_dpp(float v)
 {
+#pragma clang fp contract(off)
     return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
 }
 

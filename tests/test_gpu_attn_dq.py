@@ -32,7 +32,7 @@ def test_a_row_of_one_edge_has_no_gradient(heads, kv, D, dtype):
         O, lse = B.fastgl_attn_fwd(dev_i32(ptr), col.cuda(), Q, K, V, heads, kv, bucket=bucket.cuda(), bias=bias)
         dQ, dK, dV, dbias = B.fastgl_attn_bwd(dev_i32(ptr), col.cuda(), Q, K, V, dO, heads, kv, bucket=bucket.cuda(), bias=bias)
         assert bool(torch.isfinite(lse).all()) and bool(O.any()) and bool(dV.any())
-        assert not bool(dQ.any())
+        assert not bool(dQ.any()) and not bool(dK.any()) and not bool(dbias.any())
 
 
 @pytest.mark.parametrize("heads,kv,D", [(1, 1, 3), (4, 2, 8), (3, 3, 20), (2, 1, 64)])
