@@ -26,7 +26,7 @@ constexpr int64_t kMostClasses = (int64_t)1 << 21, kMostInputs = (int64_t)1 << 2
 // dZ, and packed weights, of a piece of the classes.  8192 rows 512 -> 65 536 bf16, dZ rounded, the kernels of a backward pass: 256 MiB (four pieces) 1953 us, 512 MiB
 // 1783, 1 GiB (one) 1720: fewer sums of pieces, although dZ no longer stays in the last cache.
 constexpr int64_t kPieceBytes = (int64_t)1 << 30;
-constexpr int kPieceCols = 256;                           // a piece has a multiple of them
+constexpr int kPieceCols = 256;                           // one of several pieces has a multiple of them
 
 // ------------------------------------------------------------------ packing
 // Matrices [rows][cols] (rows ld_src apart) as planes of bf16 with rows of ld elements, 0 beyond cols and in rows whose label is negative.
@@ -477,7 +477,7 @@ struct Shape {
     {
         int64_t most = backward ? kPieceBytes / (2 * z_planes * rows()) : kPieceBytes / 8 * 64 / M;
         if (pack_w && K > 0 && kPieceBytes / (2 * planes * K) < most) most = kPieceBytes / (2 * planes * K);
-        if (most >= N) return (int64_t)align_up((size_t)N, kPieceCols);
+        if (most >= N) return (int64_t)align_up((size_t)N, 32);            // the columns of dZ that are written and read
         most = most < 2 * kPieceCols ? kPieceCols : most / kPieceCols * kPieceCols;
         return (int64_t)align_up((size_t)ceil_div(N, ceil_div(N, most)), kPieceCols);
     }

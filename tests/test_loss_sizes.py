@@ -31,3 +31,15 @@ def test_no_workspace_grows_with_rows_times_classes():
                     for aligned in (False, True):
                         size = B.fastgl_loss_fwd_workspace_bytes(dt, M, K, N, aligned)
                         assert size <= 6 * M * (K + 8) + max(1 << 30, 6 * K * 512) + max(1 << 30, 8 * M * 4) + 12 * M + 4096, (dt, M, K, N, size)
+
+
+def test_dz_has_no_more_columns_than_it_needs():
+    """Where all classes are one piece: a multiple of 32 of them; H packed, sums of dH, dW and db beside it."""
+    for dt, planes in (("f32", 3), ("bf16", 2)):
+        for M in (70_000, 2 ** 21, 2 ** 21 + 1):
+            for K, N in ((8, 2), (8, 47), (64, 65), (300, 200)):
+                rows, cols = M + 256, (N + 31) // 32 * 32
+                if 2 * planes * rows * cols > 1 << 30:
+                    continue
+                size = B.fastgl_loss_bwd_workspace_bytes(dt, M, K, N, True)
+                assert size < 2 * planes * cols * (rows + 100) + 6 * M * (K + 8) + 6 * K * cols + 3 * 4 * M * K + 64 * 4 * K * N + M * cols // 4 + (1 << 20), (dt, M, K, N)
