@@ -62,3 +62,42 @@ def test_values_with_a_mean(heads, kv, D):
     assert not bool(bad.any()), (int(bad.sum()), (got - a.dQ).abs()[bad][:4], bound[bad][:4])
     long = a.n[:, 0] >= 4
     assert float(bound[long].median()) < 0.05 * float(a.dQ[long].abs().median())          # the check can fail
+
+
+@pytest.mark.parametrize("heads,kv,D", [(1, 1, 3), (4, 2, 8), (3, 3, 20), (2, 1, 64), (2, 2, 160)])
+def test_an_edge_of_no_weight_is_no_reference(heads, kv, D):
+    """The first edge of a row, and one inside, have values far from the others' and weights of e^-60: they are worth nothing in dQ, nor is what is subtracted for them."""
+    blk = bg.random_block(np.random.default_rng(D), 200, 300, 6.0, empty_frac=0.1, hub_rows=4, hub_deg=900)
+    g = torch.Generator().manual_seed(D)
+    n, k = heads * D, kv * D
+    col = torch.as_tensor(blk.indices).long() % 290
+    ptr = torch.as_tensor(blk.indptr).long()
+    bucket = torch.zeros(blk.num_edges, dtype=torch.int32)
+    for a, b in zip(ptr[:-1].tolist(), ptr[1:].tolist()):
+        for e in {a, (a + b) // 2} if b - a > 3 else ():
+            col[e], bucket[e] = 290 + e % 10, 1
+    bias = torch.tensor([[0.0], [-60.0]]).repeat(1, heads)
+    Q, K = torch.randn(200, n, generator=g) / 4, 2.0 + torch.randn(300, k, generator=g)
+    V = torch.randint(-8, 9, (300, k), generator=g).float()
+    V[290:] = (1 << 19) // D
+    dO = torch.randint(0, 3, (200, n), generator=g).float()
+    a = Attention(blk.indptr, col, Q, K, V, heads, kv, D ** -0.5, bucket, bias).backward(dO)
+    dQ = B.fastgl_attn_bwd(dev_i32(blk.indptr), col.int().cuda(), Q.cuda(), K.cuda(), V.cuda(), dO.cuda(), heads, kv, bucket=bucket.cuda(), bias=bias.cuda(),
+                           want=("dQ",))[0]
+    u, k1 = a.u, a.k[a.v].abs()
+    dp = (dO.double().reshape(200, heads, D)[u] * a.x[a.v]).sum(2)
+    from_mean = (dp - a.to_rows(a.p * dp)[u]).abs()
+    off_p = a.off_s + a.off_lse[u]
+    widest = torch.zeros(200, heads, D, dtype=torch.float64).scatter_reduce_(0, u[:, None, None].expand(-1, heads, D), k1, "amax")
+    # weights: as above, of what is left of dp.  Sums: a running mean of the first t edges is off the row's by at most B / (their weight), B = sum p |dp - delta|,
+    # so that an edge's terms and what it moves the mean by are at most some 4 B of K's largest element, each rounded three times
+    # The reference is a float: rounded, and from a reciprocal that is off by 2^-23, it is up to 2^-22 of itself off the mean, and so is every dp of a row that
+    # has one value alone: what is left of such terms cancels but for their own rounding (seen where all that B has is e^-60 2^19 = 5e-21).
+    B_ = (a.to_rows(a.p * from_mean) + 2.0 ** -22 * a.to_rows(a.p * dp).abs())[:, :, None]
+    weights = a.to_rows((a.p * off_p * from_mean)[:, :, None] * k1) + a.to_rows(a.p * off_p * from_mean)[:, :, None] * widest
+    bound = a.scale * (weights + 12 * U32 * (a.n + 40)[:, :, None] * B_ * widest) + 4 * U32 * a.dQ.abs()
+    got = dQ.double().cpu().reshape(a.dQ.shape)
+    bad = (got - a.dQ).abs() > bound
+    assert not bool(bad.any()), (int(bad.sum()), (got - a.dQ).abs()[bad][:4], bound[bad][:4])
+    some = (a.n[:, 0] >= 4) & (a.n[:, 0] < 100)
+    assert float(bound[some].median()) < 0.05 * float(a.dQ[some].abs().median())
