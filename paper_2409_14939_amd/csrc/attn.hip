@@ -272,8 +272,9 @@ __device__ __forceinline__ float bias_of(const AttnArgs &a, int bucket, int h)
 // Rows of sources are dealt to the wavefronts 64 apart: those that are neighbours of many often have numbers that lie together.
 //
 // What bounds it: the gathers of neighbours' rows.  With heads of 128 bytes and 4.4 edges a row (512 345 rows, 1.1 million sources) the forward pass takes 295 us:
-// 1.15 GB of K and V from memory and caches and 0.52 GB of Q and O, 5.7 TB/s.  With heads of 32 bytes it is the arithmetic of an edge and lane (65 536 rows, 1.7
-// million edges, 102 us).
+// 1.15 GB of K and V from memory and caches and 0.52 GB of Q and O, 5.7 TB/s.  With heads of 32 bytes (65 536 rows, 1.7 million edges: forward 104 us, dQ 143, dK and
+// dV 133) three quarters of the forward pass's and dQ's lines are not in L2, 0.49 and 0.61 GB at 4.7 and 4.3 TB/s, and the vector ALUs are busy for 33, 40 and 54 % of
+// the time: a step's rows are asked for after the step before, so that a wavefront waits for them once a step (two thirds of its time and more, with the four wavefronts that a SIMD has here).
 // Segments: 65 536 rows of eight edges beside rows of up to 18 000, forward 201 us without them, 103 with;  8000 rows of 15, dK and dV for heads that share
 // theirs 121 and 50.  Two pieces a lane instead of one: the 512 345 rows 451 and 345 us (then with 64-bit offsets).
 template <class ROW>
@@ -684,7 +685,7 @@ struct QueryRow {
     }
 };
 
-// 91 331 rows of 10, eight bf16 heads of 32: four edges under way 160 us, two 146 (0.96 GB, most of it gathered, at 6.6 TB/s).  The transposed order's buckets come along
+// 91 331 rows of 10, eight bf16 heads of 32: four edges under way 160 us, two 148 (0.96 GB, most of it gathered, at 6.5 TB/s).  The transposed order's buckets come along
 // in place of a launch of their own.
 template <bool BF16, int PC, int LG, bool NEAR>
 __global__ __launch_bounds__(kBlock, LG >= 4 ? 2 : BF16 ? 3 : 4) void k_attn_dq(AttnArgs a)
@@ -811,7 +812,7 @@ __global__ __launch_bounds__(kBlock, U == 1 ? 4 : 3) void k_attn_dkv(AttnArgs a)
 
 // ------------------------------------------------------------------ chunks of long rows
 // A workgroup has one long row and 2^lg of its columns at a time, and as many parts of its chunks as threads are left; the parts are joined in
-// order.  Latency bounds it: 4.5 us where there is no long row (the host does not know), 13 where 65 536 rows have chunks by the thousand.  KIND 0: O and lse, 1: dQ and the row's numbers, 2: dK and dV.
+// order.  Latency bounds it: 4.5 us where there is no long row (the host does not know), 13 to 16 where 65 536 rows have chunks by the thousand.  KIND 0: O and lse, 1: dQ and the row's numbers, 2: dK and dV.
 template <bool BF16, int KIND>
 __global__ __launch_bounds__(kJoin) void k_attn_join(AttnArgs a, int lg)
 {

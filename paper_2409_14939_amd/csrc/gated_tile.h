@@ -176,7 +176,7 @@ struct Cut {
 //   dX of 16 384 rows 1024 -> 4096 223 / 278 / 310, dWg and dWu there 218 / 241 / 401 (the first two in two slabs)
 //   all kernels of a backward call of 300 rows 256 -> 1024 (medians) 36 / 32 / 31, of 2000 rows 52 / 47 / 43, of 8000 rows 256 -> 683 73 / 67 / 60
 // The loss's products have one result of twice the columns (`one`); scores are not summed over slabs (`whole`), and what becomes of them hides
-// behind another workgroup's products where there are two: us a call, large / middle tiles, 8192 rows -> 16 384 bf16, forward and dZ: 256 inputs 93 + 162 / 83 + 142,
+// behind another workgroup's products where there are two: us a call, large / middle tiles, 8192 rows -> 16 384 bf16, forward and dZ (one piece): 256 inputs 93 + 162 / 83 + 142,
 // 512 144 + 210 / 135 + 195, 1024 239 + 307 / 240 + 303, 2048 418 + 517 / 452 + 513; fp32 128 inputs 199 + 372 / 192 + 326, 512 633 + 807 / 682 + 820.
 inline Cut cut_of(int mode, int64_t R, int64_t C, int64_t Kc, int64_t segments, bool one = false, bool whole = false)
 {

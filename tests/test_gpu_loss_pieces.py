@@ -64,3 +64,39 @@ def test_more_rows_than_tiles_of_512_threads_have():
     check_rows(H, W, b, label, loss, lse, rows)
     between = slice(1000, M // 2)
     assert bool((lse[between] == lse[1000]).all()) and not bool(loss[between].any())
+
+
+@pytest.mark.parametrize("coarse", [False, True])
+def test_a_captured_step_of_several_pieces(coarse):
+    """Statistics carried from piece to piece, dZ and dH by pieces: replays on other inputs, with a workspace that holds anything."""
+    M, K, N = 300_000, 8, 40_000
+    g = torch.Generator(device="cuda").manual_seed(5)
+    make = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    sets = [[make(M, K).bfloat16(), make(K, N).bfloat16(), make(N), torch.randint(-1, N, (M,), generator=g, device="cuda"), make(M)] for _ in range(2)]
+    need = max(B.fastgl_loss_fwd_workspace_bytes("bf16", M, K, N, True), B.fastgl_loss_bwd_workspace_bytes("bf16", M, K, N, True, coarse=coarse))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+
+    def step(H, W, b, label, dloss):
+        loss, lse = B.fastgl_loss_fwd(H, W, b, label, workspace=ws)
+        return [loss, lse, *B.fastgl_loss_bwd(H, W, b, label, lse, dloss, workspace=ws, coarse=coarse)]
+    eager = [[x.clone() for x in step(*s)] for s in sets]
+    held = [x.clone() for x in sets[0]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        step(*held)
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            got = step(*held)
+    torch.cuda.current_stream().wait_stream(side)
+    for n in (0, 1, 0):
+        for to, x in zip(held, sets[n]):
+            to.copy_(x)
+        for t in got:
+            t.zero_()
+        ws.random_(0, 255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, eager[n])), n
